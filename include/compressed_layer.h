@@ -471,6 +471,125 @@ int32_t cl_maxpool_forward(const float *d_X, float *d_Y, int32_t batch, int32_t 
 int32_t cl_lrn_forward(const float *d_X, float *d_Y, int32_t batch, int32_t C, int32_t H, int32_t W,
                        int32_t n, float alpha, float beta, float k, void *stream);
 
+/* ------------------------------------------------------------------------- *
+ * Microscaled 4-bit matrices, and layers of routed experts.
+ *
+ * A second compressed form beside the pruned, coded one: every weight kept, in 4.25 bits, in the format that the chip's matrix
+ * units multiply without decoding (OCP MXFP4).  32 consecutive elements of a row are a block: 32 codes of 4 bits - sign, and one
+ * of 0 0.5 1 1.5 2 3 4 6 - and one scale of 8 bits, 2^(byte - 127), byte 255 for NaN.
+ *   codes    row after row, CL_MX_ROW_BLOCKS(K) blocks of 16 bytes each; element 2 j of a block is the low half of its byte j,
+ *            element 2 j + 1 the high half.  The elements from K on, to whole groups of four blocks, are zeros.
+ *   scales   row after row, one byte a block
+ * codes are 16-byte aligned, scales 4-byte.
+ * ------------------------------------------------------------------------- */
+#define CL_MX_ROW_BLOCKS(K) (((K) + 127) / 128 * 4)
+/* Most elements of a row. */
+#define CL_MX_MAX_K (1 << 24)
+
+/* Element types. */
+enum { CL_F32 = 0, CL_BF16 = 1, CL_F16 = 2, CL_MX4 = 3 /* (codes and scales; inputs of products only) */ };
+
+/* A matrix in that form; a stack of experts' matrices of one shape is one after the other (rows: of one of them). */
+typedef struct {
+    const void *d_codes, *d_scales;
+    int32_t rows, K;
+} cl_mx_matrix;
+
+/* Rows that a product reads: numbers (d_X, `stride` elements from row to row), quantised on the way, or CL_MX4: codes (d_X)
+ * and scales. */
+typedef struct {
+    const void *d_X, *d_scales;
+    int32_t type;
+    int64_t stride;
+} cl_mx_input;
+
+/* Rows of numbers to that form.  The scale of a block is 2^(floor(log2(largest magnitude)) - 2), at least 2^-127, so that the
+ * largest magnitude lies between 4 and 8 of it; a value takes the nearest code, ties to the one with an even last bit,
+ * what is above 6 takes 6.  A block with a value that is not finite is NaN as a whole.  Zero rows are no error.
+ * cl_mx_dequantize gives the values that codes and scales stand for (exact in fp32 and bf16, rounded to nearest in fp16).
+ *  type      CL_F32, CL_BF16 or CL_F16    x_stride, y_stride   elements from row to row, at least K
+ * Errors: CL_EINVAL (null pointers, sizes, alignment, overlapping rows), CL_EUNSUPPORTED (K above CL_MX_MAX_K) - nothing is
+ * launched then; CL_EHIP. */
+int32_t cl_mx_quantize(const void *d_X, int32_t type, int64_t x_stride, int64_t rows, int32_t K, void *d_codes, void *d_scales, void *stream);
+int32_t cl_mx_dequantize(const void *d_codes, const void *d_scales, int64_t rows, int32_t K, void *d_Y, int32_t type, int64_t y_stride, void *stream);
+
+/* What follows a product. */
+enum {
+    CL_ACT_NONE = 0,
+    CL_ACT_RELU = 1,
+    CL_ACT_GATED = 2      /* rows 2 i and 2 i + 1 of the matrix give g and u: output i is g / (1 + exp(-g)) * u; half as many */
+                          /*   outputs as rows                                                                             */
+};
+
+/* Y = act(X W^T + v) with W in 4-bit blocks and X quantised the same way: products of codes are exact, sums are fp32, one
+ * rounding to Y's type at the end.
+ *  X         batch rows of W->K             d_bias   W->rows fp32 or NULL
+ *  d_Y       batch rows of W->rows (CL_ACT_GATED: half as many) of y_type (CL_F32, CL_BF16, CL_F16), overwritten
+ *  d_workspace  at least cl_mx_fc_workspace_bytes() (0 for X in CL_MX4), 256-byte aligned
+ * Run-to-run identical.  A batch of 0 is no error.
+ * Errors: CL_EINVAL (null pointers, sizes, alignment, workspace too small), CL_EUNSUPPORTED (CL_MX_MAX_K, a launch that does
+ * not fit a grid) - nothing is launched then; CL_EHIP. */
+int32_t cl_mx_fc_workspace_bytes(const cl_mx_matrix *W, int32_t batch, int32_t x_type, size_t *out);
+int32_t cl_mx_fc_forward(const cl_mx_matrix *W, const cl_mx_input *X, const float *d_bias_or_null, void *d_Y, int32_t y_type, int32_t batch,
+                         int32_t act, void *d_workspace, size_t workspace_bytes, void *stream);
+
+/* The choice of experts for tokens.  Per token, in fp32:
+ *   scores  softmax (CL_SCORE_SOFTMAX) or logistic function (CL_SCORE_SIGMOID) of its logits
+ *   keys    scores + bias; without a bias the logits themselves, which have the same order
+ *   groups  the experts in `groups` runs of equal length; the groups_kept with the largest group score stay: their largest
+ *           score + bias (CL_GROUP_MAX) or the sum of their two largest (CL_GROUP_TOP2)
+ *   chosen  the k experts of those groups with the largest keys, in descending order; equal keys (and groups): the lower first
+ *   weights the scores - without the bias - of the chosen, divided by their sum if renormalize, times scale
+ * A logit that is -inf, the lowest finite value of its type or NaN, and a bias that is NaN or -inf, mask an expert: its
+ * score is 0 (as a logit) and it is never chosen.  Where fewer than k experts are left, the last places have expert -1 and
+ * weight 0; so has every place of a token whose experts are all masked.  Keys that differ by less than the rounding of
+ * their fp32 arithmetic may come in either order.
+ *  d_logits  tokens rows of desc->experts, x_stride elements from row to row    d_bias  desc->experts fp32 or NULL
+ *  d_experts, d_weights   tokens x k int32 and fp32, overwritten
+ * Errors: CL_EINVAL (null pointers, sizes, groups that do not divide the experts, k above the experts of the kept groups),
+ * CL_EUNSUPPORTED (more than CL_ROUTE_MAX_EXPERTS, _GROUPS, _K) - nothing is launched then; CL_EHIP.  Zero tokens are no error. */
+#define CL_ROUTE_MAX_EXPERTS 1024
+#define CL_ROUTE_MAX_GROUPS 64
+#define CL_ROUTE_MAX_K 32
+enum { CL_SCORE_SOFTMAX = 0, CL_SCORE_SIGMOID = 1 };
+enum { CL_GROUP_MAX = 0, CL_GROUP_TOP2 = 1 };
+typedef struct {
+    int32_t experts, k;
+    int32_t score;
+    int32_t groups, groups_kept, group_score;
+    int32_t renormalize;
+    float scale;
+} cl_route_desc;
+int32_t cl_route_experts(const void *d_logits, int32_t type, int64_t x_stride, const float *d_bias_or_null, int32_t tokens,
+                         const cl_route_desc *desc, int32_t *d_experts, float *d_weights, void *stream);
+
+/* The pairs (token, j) of d_experts[tokens][k] in the order of their experts, for the products of several matrices with one
+ * choice of experts.  Starts with experts + 2 int32: where each expert's pairs begin, where the pairs without an expert
+ * (any value outside 0 .. experts - 1) begin, and the end; the rest is the library's own.  256-byte aligned. */
+int32_t cl_expert_lists_bytes(int32_t tokens, int32_t k, int32_t experts, size_t *out);
+int32_t cl_expert_lists(const int32_t *d_experts, int32_t tokens, int32_t k, int32_t experts, void *d_lists, size_t lists_bytes, void *stream);
+
+/* A call of routed experts' products. */
+typedef struct {
+    int32_t tokens, k;
+    const int32_t *d_experts;      /* tokens x k: expert of each pair; any value outside 0 .. experts - 1: none                */
+    const float *d_weights;        /* tokens x k, or NULL                                                                      */
+    const float *d_bias;           /* experts x rows fp32, or NULL                                                             */
+    const void *d_lists;           /* cl_expert_lists() of d_experts, or NULL: made on the way                                 */
+    int32_t act;                   /* CL_ACT_*                                                                                 */
+    int32_t x_per_pair;            /* X has a row for each pair (token * k + j), else for each token                           */
+} cl_mx_experts_call;
+
+/* P[t k + j] = act(X[t] W_e^T + v_e) with e = d_experts[t][j] - of `experts` matrices W of one shape, one after the other -
+ * and, with d_weights, Y[t] = sum over j of d_weights[t][j] P[t k + j], added in fp32 in the order of j.
+ *  d_Y       with d_weights tokens rows, else tokens x k rows, of W->rows (CL_ACT_GATED: half as many), overwritten; pairs
+ *            without an expert add nothing, and without d_weights their rows are zeros
+ *  d_workspace  at least cl_mx_experts_workspace_bytes() for this call, 256-byte aligned
+ * Sums, rounding, errors as cl_mx_fc_forward; run-to-run identical.  Zero tokens are no error. */
+int32_t cl_mx_experts_workspace_bytes(const cl_mx_matrix *W, int32_t experts, const cl_mx_experts_call *call, int32_t x_type, size_t *out);
+int32_t cl_mx_experts_forward(const cl_mx_matrix *W, int32_t experts, const cl_mx_input *X, const cl_mx_experts_call *call, void *d_Y,
+                              int32_t y_type, void *d_workspace, size_t workspace_bytes, void *stream);
+
 /* Measurement hook for benchmarks (not part of the paper's method).  While
  * enabled, every forward call brackets the first launch of its main kernel (the
  * first batch tile; not the small reduction kernel) with a pair of HIP events on

@@ -18,6 +18,10 @@ CL_OK, CL_EINVAL, CL_ENOMEM, CL_ECORRUPT, CL_EUNSUPPORTED, CL_EHIP = 0, -1, -2, 
 PATH_AUTO, PATH_SPARSE, PATH_MFMA_F32, PATH_MFMA_BF16, PATH_SPARSE_WIDE = 0, 1, 2, 3, 4
 CHUNK_BITS, RECORD_BITS, RECORDS_PER_CHUNK, MAX_RECORD_ENTRIES, MAX_CODE_LEN = 4096, 64, 64, 15, 12
 STATIC_SCRATCH_BYTES = 16 << 20        # CL_STATIC_SCRATCH_BYTES
+MX4 = 3                                # CL_MX4, after the element types of _element_type
+ACTIVATIONS = {"none": 0, "relu": 1, "gated": 2}
+SCORES = {"softmax": 0, "sigmoid": 1}
+GROUP_SCORES = {"max": 0, "top2": 1}
 
 EXPORTS = [
     "cl_last_error", "cl_compress_layer", "cl_layer_upload", "cl_layer_free", "cl_layer_stats",
@@ -27,6 +31,8 @@ EXPORTS = [
     "cl_compressed_fc_group_forward", "cl_conv_workspace_bytes", "cl_conv_workspace_bytes_min", "cl_conv_workspace_bytes_unsplit",
     "cl_compressed_conv_forward", "cl_plan_batches", "cl_maxpool_forward", "cl_lrn_forward",
     "cl_set_kernel_timing", "cl_last_kernel_ms",
+    "cl_mx_quantize", "cl_mx_dequantize", "cl_mx_fc_workspace_bytes", "cl_mx_fc_forward", "cl_route_experts", "cl_expert_lists_bytes",
+    "cl_expert_lists", "cl_mx_experts_workspace_bytes", "cl_mx_experts_forward",
 ]
 
 
@@ -56,6 +62,23 @@ class HostView(C.Structure):
 
 class ConvDesc(C.Structure):
     _fields_ = [(n, C.c_int32) for n in ("C", "H", "W", "R", "S", "stride", "pad", "groups", "out_channels")]
+
+
+class MxMatrix(C.Structure):
+    _fields_ = [("d_codes", C.c_void_p), ("d_scales", C.c_void_p), ("rows", C.c_int32), ("K", C.c_int32)]
+
+
+class MxInput(C.Structure):
+    _fields_ = [("d_X", C.c_void_p), ("d_scales", C.c_void_p), ("type", C.c_int32), ("stride", C.c_int64)]
+
+
+class RouteDesc(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("experts", "k", "score", "groups", "groups_kept", "group_score", "renormalize")] + [("scale", C.c_float)]
+
+
+class MxExpertsCall(C.Structure):
+    _fields_ = [("tokens", C.c_int32), ("k", C.c_int32), ("d_experts", C.c_void_p), ("d_weights", C.c_void_p), ("d_bias", C.c_void_p),
+                ("d_lists", C.c_void_p), ("act", C.c_int32), ("x_per_pair", C.c_int32)]
 
 
 class CLError(RuntimeError):
@@ -114,6 +137,15 @@ def lib():
     L.cl_lrn_forward.argtypes = [p, p] + [i32] * 5 + [C.c_float] * 3 + [p]
     L.cl_set_kernel_timing.argtypes = [i32]
     L.cl_last_kernel_ms.argtypes = [C.POINTER(C.c_float), C.POINTER(i32)]
+    L.cl_mx_quantize.argtypes = [p, i32, i64, i64, i32, p, p, p]
+    L.cl_mx_dequantize.argtypes = [p, p, i64, i32, p, i32, i64, p]
+    L.cl_mx_fc_workspace_bytes.argtypes = [C.POINTER(MxMatrix), i32, i32, C.POINTER(sz)]
+    L.cl_mx_fc_forward.argtypes = [C.POINTER(MxMatrix), C.POINTER(MxInput), p, p, i32, i32, i32, p, sz, p]
+    L.cl_route_experts.argtypes = [p, i32, i64, p, i32, C.POINTER(RouteDesc), p, p, p]
+    L.cl_expert_lists_bytes.argtypes = [i32, i32, i32, C.POINTER(sz)]
+    L.cl_expert_lists.argtypes = [p, i32, i32, i32, p, sz, p]
+    L.cl_mx_experts_workspace_bytes.argtypes = [C.POINTER(MxMatrix), i32, C.POINTER(MxExpertsCall), i32, C.POINTER(sz)]
+    L.cl_mx_experts_forward.argtypes = [C.POINTER(MxMatrix), i32, C.POINTER(MxInput), C.POINTER(MxExpertsCall), p, i32, p, sz, p]
     for name in EXPORTS:
         if name not in ("cl_last_error", "cl_layer_group_free"):
             getattr(L, name).restype = i32
@@ -501,6 +533,253 @@ def plan_batches(time_ms, batch_set, in_bytes_per_image, out_bytes_per_image, ws
         return float("inf"), None
     _check(rc)
     return ms.value, plan.tolist()
+
+
+# --------------------------------------------------------------------------- #
+# microscaled 4-bit matrices and routed experts
+# --------------------------------------------------------------------------- #
+_types = None
+
+
+def _element_type(dtype, what):
+    """CL_F32, CL_BF16 or CL_F16."""
+    global _types
+    if _types is None:
+        import torch
+        _types = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+    try:
+        return _types[dtype]
+    except KeyError:
+        raise ValueError(f"{what} must be float32, bfloat16 or float16, got {dtype}") from None
+
+
+def _rows(t, what, cols=None):
+    """A matrix whose rows are contiguous, at any distance from each other -> (element type, distance)."""
+    ty = _element_type(t.dtype, what)
+    if t.dim() != 2 or not t.is_cuda or (t.shape[1] > 1 and t.stride(1) != 1) or (cols is not None and t.shape[1] != cols):
+        raise ValueError(f"{what} must be a CUDA matrix with contiguous rows{'' if cols is None else f' of {cols}'}, "
+                         f"got {tuple(t.shape)} with strides {t.stride()}")
+    return ty, t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def _same_device(device, *tensors):
+    """The kernels run on the current device and its current stream."""
+    import torch
+    if device.index != torch.cuda.current_device():
+        raise ValueError(f"the input is on {device}, the current device is cuda:{torch.cuda.current_device()}")
+    for t in tensors:
+        if t is not None and t.device != device:
+            raise ValueError(f"a tensor is on {t.device}, the input on {device}")
+
+
+class MxTensor:
+    """A matrix - or a stack of matrices of one shape, for experts - in blocks of 32 four-bit floats under one scale:
+    codes (..., rows, blocks * 16) and scales (..., rows, blocks), uint8, blocks = mx_row_blocks(K)."""
+
+    __slots__ = ("codes", "scales", "K")
+
+    def __init__(self, codes, scales, K):
+        import torch
+        kb = mx_row_blocks(K)
+        if codes.dtype != torch.uint8 or scales.dtype != torch.uint8 or not codes.is_cuda or not codes.is_contiguous() or not scales.is_contiguous():
+            raise ValueError("codes and scales must be contiguous uint8 CUDA tensors")
+        if codes.dim() < 2 or codes.shape[-1] != kb * 16 or scales.shape != codes.shape[:-1] + (kb,) or scales.device != codes.device:
+            raise ValueError(f"rows of {K} elements have {kb * 16} bytes of codes and {kb} scales, got {tuple(codes.shape)} and {tuple(scales.shape)}")
+        self.codes, self.scales, self.K = codes, scales, K
+
+    @property
+    def shape(self):
+        return tuple(self.codes.shape[:-1]) + (self.K,)
+
+    @property
+    def device(self):
+        return self.codes.device
+
+
+def mx_row_blocks(K: int) -> int:
+    """Blocks of a row of K elements: whole groups of four."""
+    if K < 1:
+        raise ValueError("a row has at least one element")
+    return (K + 127) // 128 * 4
+
+
+def mx_quantize(X, out: MxTensor | None = None) -> MxTensor:
+    """Rows of X ((..., K), float32, bfloat16 or float16; a matrix's rows at any distance) -> MxTensor of the same shape."""
+    import torch
+    lead = X.shape[:-1]
+    if X.dim() > 2:
+        X = X.reshape(-1, X.shape[-1])
+    ty, stride = _rows(X, "X")
+    rows, K = X.shape
+    if out is None:
+        kb = mx_row_blocks(K)
+        out = MxTensor(torch.empty(lead + (kb * 16,), dtype=torch.uint8, device=X.device), torch.empty(lead + (kb,), dtype=torch.uint8, device=X.device), K)
+    elif out.shape != lead + (K,):
+        raise ValueError(f"out must hold {tuple(lead) + (K,)}, holds {out.shape}")
+    _same_device(X.device, out.codes)
+    _check(lib().cl_mx_quantize(X.data_ptr(), ty, stride, rows, K, out.codes.data_ptr(), out.scales.data_ptr(), _stream()))
+    return out
+
+
+def mx_dequantize(Q: MxTensor, dtype=None, out=None):
+    """The values Q stands for, (..., K) of dtype (float32 unless given)."""
+    import torch
+    if out is None:
+        out = torch.empty(Q.shape, dtype=dtype or torch.float32, device=Q.device)
+    elif tuple(out.shape) != Q.shape or not (out.is_contiguous() or out.dim() == 2) or (dtype is not None and out.dtype != dtype):
+        raise ValueError(f"out must be {Q.shape}{'' if dtype is None else f' of {dtype}'}, contiguous or a matrix with contiguous rows")
+    Y = out if out.dim() == 2 else out.view(-1, Q.K)
+    ty, stride = _rows(Y, "out", Q.K)
+    _same_device(Q.device, out)
+    _check(lib().cl_mx_dequantize(Q.codes.data_ptr(), Q.scales.data_ptr(), Y.shape[0], Q.K, out.data_ptr(), ty, stride, _stream()))
+    return out
+
+
+def _mx_input(X, K):
+    """-> (struct, rows, element type of an output that names none)"""
+    import torch
+    if isinstance(X, MxTensor):
+        if len(X.shape) != 2 or X.K != K:
+            raise ValueError(f"X must have rows of {K}, got {X.shape}")
+        return MxInput(X.codes.data_ptr(), X.scales.data_ptr(), MX4, 0), X.shape[0], torch.float32
+    ty, stride = _rows(X, "X", K)
+    return MxInput(X.data_ptr(), None, ty, stride), X.shape[0], X.dtype
+
+
+def _mx_output(out, shape, dtype, device):
+    """-> (tensor, element type)"""
+    import torch
+    if out is None:
+        out = torch.empty(shape, dtype=dtype, device=device)
+    elif tuple(out.shape) != shape or not out.is_contiguous() or out.dtype != dtype:
+        raise ValueError(f"out must be a contiguous {dtype} tensor of shape {shape}, got {out.dtype} {tuple(out.shape)}")
+    return out, _element_type(out.dtype, "out")
+
+
+def _workspace(workspace, need, device):
+    import torch
+    if workspace is None and need:
+        workspace = torch.empty(need, dtype=torch.uint8, device=device)
+    if workspace is None:
+        return None, None, 0
+    return workspace, _dev_ptr(workspace), workspace.numel() * workspace.element_size()
+
+
+def _act(act):
+    if act not in ACTIVATIONS:
+        raise ValueError(f"act must be one of {', '.join(ACTIVATIONS)}, got {act!r}")
+    return ACTIVATIONS[act]
+
+
+def mx_fc_workspace_bytes(W: MxTensor, batch: int, dtype=None) -> int:
+    """Scratch of mx_fc_forward for `batch` rows of dtype (None: an MxTensor, which needs none)."""
+    n = C.c_size_t(0)
+    m = MxMatrix(None, None, W.shape[0], W.K)
+    _check(lib().cl_mx_fc_workspace_bytes(C.byref(m), batch, MX4 if dtype is None else _element_type(dtype, "X"), C.byref(n)))
+    return n.value
+
+
+def mx_fc_forward(W: MxTensor, X, bias=None, relu=False, act=None, dtype=None, out=None, workspace=None):
+    """act(X W^T + bias) with W (M, K) in 4-bit blocks and X (B, K) - float32, bfloat16 or float16, quantised on the way, or an MxTensor.
+    act: "none", "relu" (the same as relu=True) or "gated" (rows 2 i and 2 i + 1 of W give gate and value of output i).  The output is of
+    dtype, X's own unless given (float32 for an MxTensor)."""
+    if len(W.shape) != 2:
+        raise ValueError(f"W must be a matrix, got {W.shape}")
+    M, K = W.shape
+    act = _act(act or ("relu" if relu else "none"))
+    xs, B, own_dtype = _mx_input(X, K)
+    _want(bias, (M,), "bias")
+    Y, y_type = _mx_output(out, (B, M // 2 if act == 2 else M), dtype or (out.dtype if out is not None else own_dtype), X.device)
+    _same_device(X.device, W.codes, bias, Y, workspace)
+    m, L, n = MxMatrix(W.codes.data_ptr(), W.scales.data_ptr(), M, K), lib(), C.c_size_t(0)
+    _check(L.cl_mx_fc_workspace_bytes(m, B, xs.type, n))
+    workspace, ws, ws_bytes = _workspace(workspace, n.value, X.device)
+    _check(L.cl_mx_fc_forward(m, xs, None if bias is None else bias.data_ptr(), Y.data_ptr(), y_type, B, act, ws, ws_bytes, _stream()))
+    return Y
+
+
+def route_experts(logits, k: int, bias=None, score="softmax", groups: int = 1, groups_kept: int | None = None, group_score="max", renormalize=True,
+                  scale: float = 1.0):
+    """logits (T, E) -> (experts (T, k) int32, weights (T, k) float32): the k experts of each token with the largest scores + bias (within the
+    groups_kept best of `groups` runs of experts), and their scores without the bias, divided by their sum if renormalize, times scale.
+    -1 and 0 where no expert is left (logits of -inf, the lowest value or NaN mask an expert)."""
+    import torch
+    ty, stride = _rows(logits, "logits")
+    T, E = logits.shape
+    _want(bias, (E,), "bias")
+    if score not in SCORES or group_score not in GROUP_SCORES:
+        raise ValueError(f"score must be one of {', '.join(SCORES)} and group_score of {', '.join(GROUP_SCORES)}, got {score!r} and {group_score!r}")
+    _same_device(logits.device, bias)
+    d = RouteDesc(E, k, SCORES[score], groups, groups if groups_kept is None else groups_kept, GROUP_SCORES[group_score], int(renormalize), scale)
+    experts = torch.empty((T, max(k, 0)), dtype=torch.int32, device=logits.device)
+    weights = torch.empty((T, max(k, 0)), dtype=torch.float32, device=logits.device)
+    _check(lib().cl_route_experts(logits.data_ptr(), ty, stride, None if bias is None else bias.data_ptr(), T, d, experts.data_ptr(), weights.data_ptr(),
+                                  _stream()))
+    return experts, weights
+
+
+def _want_experts(experts):
+    import torch
+    if experts.dtype != torch.int32 or experts.dim() != 2 or not experts.is_cuda or not experts.is_contiguous():
+        raise ValueError(f"experts must be a contiguous int32 CUDA matrix, got {experts.dtype} {tuple(experts.shape)}")
+
+
+class ExpertLists:
+    """The pairs of a choice of experts in the order of their experts (cl_expert_lists), for several products with one choice."""
+
+    __slots__ = ("buffer", "tokens", "k", "n_experts")
+
+    def __init__(self, buffer, tokens, k, n_experts):
+        self.buffer, self.tokens, self.k, self.n_experts = buffer, tokens, k, n_experts
+
+    @property
+    def offsets(self):
+        """(n_experts + 2) int32: where each expert's pairs begin, where those without one do, and the end."""
+        import torch
+        return self.buffer[:4 * (self.n_experts + 2)].view(torch.int32)
+
+
+def expert_lists(experts, n_experts: int) -> ExpertLists:
+    """experts (T, k) int32, as route_experts gives them."""
+    import torch
+    _want_experts(experts)
+    _same_device(experts.device)
+    T, k = experts.shape
+    n = C.c_size_t(0)
+    _check(lib().cl_expert_lists_bytes(T, k, n_experts, n))
+    buffer = torch.empty(n.value, dtype=torch.uint8, device=experts.device)
+    _check(lib().cl_expert_lists(experts.data_ptr(), T, k, n_experts, buffer.data_ptr(), n.value, _stream()))
+    return ExpertLists(buffer, T, k, n_experts)
+
+
+def mx_experts_forward(W: MxTensor, X, experts, weights=None, bias=None, act="none", x_per_pair=False, lists: ExpertLists | None = None, dtype=None,
+                       out=None, workspace=None):
+    """The products of rows with their experts' matrices: W (E, M, K) in 4-bit blocks, X (T, K) - or (T * k, K) with x_per_pair -, experts (T, k) int32.
+    With weights (T, k): (T, M), the weighted sum of each token's k products; without: (T * k, M), one row a pair.  bias (E, M); act as in
+    mx_fc_forward, before the sum.  Pairs with an expert outside 0 .. E - 1 give nothing (a row of zeros without weights)."""
+    if len(W.shape) != 3:
+        raise ValueError(f"W must be (experts, rows, K), got {W.shape}")
+    E, M, K = W.shape
+    _want_experts(experts)
+    T, k = experts.shape
+    act = _act(act)
+    xs, rows, own_dtype = _mx_input(X, K)
+    if rows != (T * k if x_per_pair else T):
+        raise ValueError(f"X must have {T * k if x_per_pair else T} rows, got {rows}")
+    _want(weights, (T, k), "weights")
+    _want(bias, (E, M), "bias")
+    if lists is not None and (lists.tokens, lists.k, lists.n_experts) != (T, k, E):
+        raise ValueError(f"lists of {lists.tokens} x {lists.k} of {lists.n_experts} experts, wanted {T} x {k} of {E}")
+    Y, y_type = _mx_output(out, (T if weights is not None else T * k, M // 2 if act == 2 else M),
+                           dtype or (out.dtype if out is not None else own_dtype), X.device)
+    _same_device(X.device, W.codes, experts, weights, bias, Y, workspace, None if lists is None else lists.buffer)
+    call = MxExpertsCall(T, k, experts.data_ptr(), None if weights is None else weights.data_ptr(), None if bias is None else bias.data_ptr(),
+                         None if lists is None else lists.buffer.data_ptr(), act, int(x_per_pair))
+    m, L, n = MxMatrix(W.codes.data_ptr(), W.scales.data_ptr(), M, K), lib(), C.c_size_t(0)
+    _check(L.cl_mx_experts_workspace_bytes(m, E, call, xs.type, n))
+    workspace, ws, ws_bytes = _workspace(workspace, n.value, X.device)
+    _check(L.cl_mx_experts_forward(m, E, xs, call, Y.data_ptr(), y_type, ws, ws_bytes, _stream()))
+    return Y
 
 
 def set_kernel_timing(enable: bool):

@@ -8,7 +8,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libcompressed_layer.so")
-SOURCES = ["compress.cpp", "huffman.cpp", "planner.cpp", "device.hip"]
+SOURCES = ["compress.cpp", "huffman.cpp", "planner.cpp", "device.hip", "mx/quantize.hip", "mx/route.hip", "mx/product.hip"]
 
 HIPCC_FLAGS = [
     "-O3", "-std=c++17", "-fPIC", "-shared", "--offload-arch=gfx950",
@@ -39,7 +39,7 @@ def build_library(verbose: bool = False) -> str:
     inc = ["-I", os.path.join(ROOT, "include"), "-I", CSRC]
     objs = []
     for s in SOURCES:
-        obj = os.path.join(bdir, s + ".o")
+        obj = os.path.join(bdir, s.replace("/", "_") + ".o")
         if s.endswith(".hip"):
             _run([hipcc(), *[f for f in HIPCC_FLAGS if f != "-shared"], *inc, "-c", os.path.join(CSRC, s), "-o", obj], verbose)
         else:
@@ -53,7 +53,7 @@ def library_is_stale() -> bool:
     if not os.path.exists(LIB):
         return True
     t = os.path.getmtime(LIB)
-    deps = [os.path.join(CSRC, f) for f in os.listdir(CSRC)] + [os.path.join(ROOT, "include", "compressed_layer.h")]
+    deps = [os.path.join(d, f) for d, _, fs in os.walk(CSRC) for f in fs] + [os.path.join(ROOT, "include", "compressed_layer.h")]
     return any(os.path.getmtime(d) > t for d in deps)
 
 
