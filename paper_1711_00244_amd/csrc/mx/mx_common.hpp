@@ -4,6 +4,7 @@
 #include <hip/hip_fp16.h>
 #include <hip/hip_runtime.h>
 
+#include <atomic>
 #include <climits>
 #include <cstdint>
 
@@ -87,6 +88,19 @@ template <class F> static int32_t with_type(int32_t type, F f)
 inline size_t round_up(size_t n, size_t to) { return (n + to - 1) / to * to; }
 inline bool aligned(const void *p, size_t to) { return ((uintptr_t)p & (to - 1)) == 0; }
 
+// Raises a kernel's limit of dynamic LDS, once per device (the attribute stays).  `seen` belongs to one kernel.
+struct LdsLimit { std::atomic<bool> done[64]; };
+inline int32_t allow_lds(const void *kernel, size_t bytes, LdsLimit &seen)
+{
+    int dev = 0;
+    MX_HIP_TRY(hipGetDevice(&dev));
+    const bool tracked = dev >= 0 && dev < 64;
+    if (tracked && seen.done[dev].load(std::memory_order_relaxed)) return CL_OK;
+    MX_HIP_TRY(hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes));
+    if (tracked) seen.done[dev].store(true, std::memory_order_relaxed);
+    return CL_OK;
+}
+
 // quantize.hip: rows of X (stride in elements) to codes and scales, no checks.
 int32_t launch_quantize(const void *X, int32_t type, int64_t stride, int64_t rows, int32_t K, uint8_t *codes, uint8_t *scales, hipStream_t st);
 
@@ -95,13 +109,13 @@ struct ExpertLists {
     int32_t *offsets;                // experts + 2: first pair of each expert, of the pairs without one, and the end
     int32_t *order;                  // tokens * k pairs (token * k + j), expert by expert, ascending within one
     int32_t *tile_count;             // kTileWidths: tiles of each width
-    int2 *tiles[3];                  // per width: (expert, first pair) of each tile; an expert's pairs begin a tile
+    int2 *tiles[4];                  // per width: (expert, first pair) of each tile; an expert's pairs begin a tile
     int32_t *chunk_counts;           // scratch of the launches that build it
-    int64_t max_tiles[3];
+    int64_t max_tiles[4];
     size_t bytes;
 };
-constexpr int kTileWidths = 3;
-constexpr int kTileWidth[kTileWidths] = {16, 64, 256};
+constexpr int kTileWidths = 4;
+constexpr int kTileWidth[kTileWidths] = {16, 64, 128, 256};
 constexpr int kListChunk = 1024;     // pairs that one workgroup counts
 ExpertLists expert_lists_at(void *base, int32_t tokens, int32_t k, int32_t experts);
 int32_t launch_expert_lists(const int32_t *experts_of, int32_t tokens, int32_t k, int32_t experts, const ExpertLists &L, hipStream_t st);

@@ -1,6 +1,9 @@
 // Products with microscaled 4-bit matrices on the scaled matrix instructions: one matrix for all rows of X, or one per expert
 // for the rows that were routed to it.
 #include <algorithm>
+#include <atomic>
+#include <cmath>
+#include <type_traits>
 
 #include "mx_common.hpp"
 
@@ -20,7 +23,10 @@ struct ProductArgs {
     int blocks, M, rows, experts, act;
     int out_width;                                           // elements of a row of Y
     int x_div;                                               // pair / x_div is its row of X
+    float *part;                                             // not null: sums of a share of k, [split][row of Y][pitch], to be finished
+    int splits, pitch;
     int tile0;                                               // tile of the launch's blockIdx.y of 0
+    int y_wide;                                              // rows of Y are whole aligned fours
     int skip_unrouted;                                       // the rows of Y of pairs without an expert are not read
 };
 
@@ -61,9 +67,32 @@ template <class T> __device__ __forceinline__ void store_outputs(const ProductAr
         return;
     }
     y += m;
+    T out[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-        if (m + i < a.M) y[i] = (T)(a.act == CL_ACT_RELU && v[i] < 0.0f ? 0.0f : v[i])   /* (NaN stays) */;
+    for (int i = 0; i < 4; ++i) out[i] = (T)(a.act == CL_ACT_RELU && v[i] < 0.0f ? 0.0f : v[i]);      // (NaN stays)
+    if (a.y_wide) {
+        __builtin_memcpy(__builtin_assume_aligned(y, sizeof out), out, sizeof out);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (m + i < a.M) y[i] = out[i];
+    }
+}
+
+// The same for any column: the pairs without an expert get zeros, whatever the activation would make of a bias.
+template <class T> __device__ __forceinline__ void finish_outputs(const ProductArgs &a, int expert, int64_t row, int m, f32x4 v)
+{
+    if (!a.order || expert < a.experts) return store_outputs<T>(a, expert, row, m, v);
+    const int step = a.act == CL_ACT_GATED ? 2 : 1;
+    T *y = (T *)a.Y + row * a.out_width;
+    for (int i = 0; i < 4; i += step)
+        if (m + i + step <= a.M) y[(m + i) / step] = (T)0.0f;
+}
+
+// Four sums of a share of k.  (A row of partial sums is padded to whole fours.)
+__device__ __forceinline__ void store_part(const ProductArgs &a, int split, int64_t row, int m, f32x4 v)
+{
+    if (m < a.M) *(f32x4 *)(a.part + ((int64_t)split * a.rows + row) * a.pitch + m) = v;
 }
 
 // A workgroup of eight wavefronts makes 16 outputs (blockIdx.x) of 16 NT columns (blockIdx.y).  The wavefronts share out the
@@ -121,44 +150,160 @@ template <int NT, class T> __global__ __launch_bounds__(kRowsWaves * 64) void mx
 #pragma unroll
         for (int w = 1; w < kRowsWaves; ++w) v += part[w][t][l];
         const int64_t y_row = a.order ? a.order[c.first + n] : c.first + n;
-        if (a.order && c.expert == a.experts) {              // no expert: zeros, whatever the activation makes of zero and a bias
-            T *y = (T *)a.Y + y_row * a.out_width;
-            const int step = a.act == CL_ACT_GATED ? 2 : 1, m = m0 + 4 * (l >> 4);
-            for (int i = 0; i < 4; i += step)
-                if (m + i + step <= a.M) y[(m + i) / step] = (T)0.0f;
-        } else {
-            store_outputs<T>(a, c.expert, y_row, m0 + 4 * (l >> 4), v);
+        if (a.part) store_part(a, 0, y_row, m0 + 4 * (l >> 4), v);
+        else finish_outputs<T>(a, c.expert, y_row, m0 + 4 * (l >> 4), v);
+    }
+}
+
+#include "tile_kernel.hpp"
+
+// Y[t] = sum over j of weights[t][j] act(sum over the splits of a pair's parts + bias), both in order, of the pairs that have an
+// expert.  A thread makes four consecutive outputs of one row (two, of a gated product).
+struct FinishArgs {
+    const float *part, *bias, *weights;
+    const int32_t *experts_of;                               // null: one matrix
+    void *Y;
+    int64_t split_stride;
+    int tokens, k, experts, M, pitch, splits, act, out_width;
+};
+
+template <class T> __global__ __launch_bounds__(256) void mx_finish_kernel(FinishArgs a, int quads)
+{
+    const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int64_t t = at / quads;
+    if (t >= a.tokens) return;
+    const int m = (int)(at - t * quads) * 4;
+    f32x4 sum = {0, 0, 0, 0};
+    for (int j = 0; j < a.k; ++j) {
+        const int64_t pair = t * a.k + j;
+        const int e = a.experts_of ? a.experts_of[pair] : 0;
+        if (e < 0 || e >= a.experts) continue;
+        const float *p = a.part + pair * a.pitch + m;
+        f32x4 v = *(const f32x4 *)p;
+        for (int s = 1; s < a.splits; ++s) v += *(const f32x4 *)(p + s * a.split_stride);
+        if (a.bias) {
+            const float *b = a.bias + (int64_t)e * a.M + m;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (m + i < a.M) v[i] += b[i];
+        }
+        if (a.act == CL_ACT_GATED) {
+            v[0] = v[0] / (1.0f + expf(-v[0])) * v[1];
+            v[1] = v[2] / (1.0f + expf(-v[2])) * v[3];
+        } else if (a.act == CL_ACT_RELU) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = v[i] < 0.0f ? 0.0f : v[i];
+        }
+        sum += a.weights ? v * a.weights[pair] : v;
+    }
+    const int n = a.act == CL_ACT_GATED ? 2 : 4, out = a.act == CL_ACT_GATED ? m / 2 : m;
+    T *y = (T *)a.Y + t * a.out_width + out;
+    for (int i = 0; i < n; ++i)
+        if (out + i < a.out_width) y[i] = (T)sum[i];
+}
+
+template <int BM, int BN, int WM, int WN, int D, class T> static int32_t launch_tiles(const ProductArgs &a, int64_t tiles, hipStream_t st)
+{
+    using C = Tile<BM, BN, WM, WN, D>;
+    auto kernel = mx_tile_kernel<BM, BN, WM, WN, D, T>;
+    static LdsLimit seen;
+    if (int32_t rc = allow_lds((const void *)kernel, C::kLds, seen)) return rc;
+    const int64_t row_tiles = (a.M + BM - 1) / BM;
+    if (row_tiles * tiles > INT32_MAX) return fail(CL_EUNSUPPORTED, "a launch of %lld workgroups does not fit a grid", (long long)(row_tiles * tiles));
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(row_tiles * tiles), (unsigned)a.splits), dim3(C::kThreads), C::kLds, st, a, (int)row_tiles);
+    MX_HIP_TRY(hipGetLastError());
+    return CL_OK;
+}
+
+// ------------------------------------------------------------------------- //
+// which kernel
+// ------------------------------------------------------------------------- //
+enum Form { kRows, kTile64, kTile128, kTile256x128, kTile256 };
+
+struct Choice {
+    Form form;
+    int width;                                               // columns of a tile: an index of kTileWidth
+    int splits;
+};
+
+// A form's price in microseconds, from measurements over M 1000 .. 4096, 64 .. 4096 columns, K 4096 .. 25088 (within a
+// quarter of each): a start (launch, first loads, last stores), and per step of 128 k what a workgroup takes alone on its compute
+// unit, or its share of a full one where the launch has more workgroups than the chip has compute units.
+struct Price { int bm, bn, width; float start, alone, shared; };
+constexpr Price kPrices[] = {{16, 64, 1, 3.0f, 0.0f, 0.0f}, {64, 64, 1, 3.5f, 0.15f, 0.18f}, {128, 128, 2, 4.5f, 0.50f, 0.40f}, {256, 128, 2, 6.0f, 0.74f, 0.74f},
+                             {256, 256, 3, 8.0f, 0.95f, 1.17f}};
+constexpr int kCus = 256;
+
+// rows: columns of the product in all; lists: how many runs they are cut into (experts, or 1), each of which fills its last tile
+// half on average.
+static Choice choose(int M, int blocks, int64_t rows, int64_t runs, bool part)
+{
+    const int steps = blocks / 4;
+    runs = std::min(runs, rows);
+    Choice best{kRows, 1, 1};
+    if (steps < 4) return best;                              // (the tile kernels read scales four steps at a time)
+    if (rows <= 16 * runs) return best;
+    float least = 1e30f;
+    for (int f = kTile64; f <= kTile256; ++f) {
+        const Price &p = kPrices[f];
+        const int64_t tiles = runs == 1 ? (rows + p.bn - 1) / p.bn : std::max(runs, rows / p.bn + runs / 2);
+        const int64_t wgs = tiles * ((M + p.bm - 1) / p.bm);
+        for (int splits = 1; splits <= 8 && steps / splits >= 4; splits *= 2) {
+            if (splits > 1 && (runs > 1 || wgs * splits > 2 * kCus)) break;
+            const float full = (float)(wgs * splits) / kCus;
+            const float each = full <= 1.0f ? p.alone : std::max(p.alone, p.shared * (f >= kTile256x128 ? std::ceil(full) : full));
+            float us = p.start * (f >= kTile256x128 ? std::max(1.0f, std::ceil(full)) : 1.0f) + each * (steps + splits - 1) / splits;
+            if (splits > 1 && !part) us += 3.0f;
+            if (splits > 1) us += (float)(2 * splits - 1) * rows * M * 4e-6f / 4.0f;
+            if (us < least) least = us, best = Choice{(Form)f, p.width, splits};
         }
     }
+    return best;
 }
 
-// Y[t] = sum over j of weights[t][j] P[t k + j], in the order of j, of the pairs that have an expert.
-template <class T>
-__global__ __launch_bounds__(256) void join_kernel(const float *__restrict__ P, const int32_t *__restrict__ experts_of, const float *__restrict__ weights,
-                                                   T *__restrict__ Y, int k, int experts, int width)
+// The tiles of a product: rows of X in order, or what the lists have.
+template <class T> static int32_t launch_product(ProductArgs a, const Choice &c, const ExpertLists *L, hipStream_t st)
 {
-    const int m = (int)(blockIdx.x * 256u + threadIdx.x);
-    if (m >= width) return;
-    const int64_t t = blockIdx.y + (int64_t)blockIdx.z * gridDim.y;
-    float sum = 0.0f;
-    for (int j = 0; j < k; ++j) {
-        const int e = experts_of[t * k + j];
-        if (e >= 0 && e < experts) sum += weights[t * k + j] * P[(t * k + j) * width + m];
+    int64_t tiles = ((int64_t)a.rows + kTileWidth[c.width] - 1) / kTileWidth[c.width];
+    if (L) {
+        a.tiles = L->tiles[c.width];
+        a.tile_count = L->tile_count + c.width;
+        tiles = L->max_tiles[c.width];
     }
-    Y[t * width + m] = (T)sum;
-}
-
-template <class T> static int32_t launch_product(const ProductArgs &a, int64_t tiles, hipStream_t st)
-{
-    const int64_t gx = (a.M + 15) / 16;
+    a.splits = c.splits;
+    switch (c.form) {
+    case kTile64: return launch_tiles<64, 64, 2, 2, 6, T>(a, tiles, st);
+    case kTile128: return launch_tiles<128, 128, 2, 2, 4, T>(a, tiles, st);
+    case kTile256x128: return launch_tiles<256, 128, 4, 2, 4, T>(a, tiles, st);
+    case kTile256: return launch_tiles<256, 256, 2, 4, 4, T>(a, tiles, st);
+    default: break;
+    }
     // (a grid is at most 65535 high: taller ones go in pieces)
     for (int64_t t0 = 0; t0 < tiles; t0 += 65535) {
-        ProductArgs p = a;
-        p.tile0 = (int)t0;
-        hipLaunchKernelGGL((mx_rows_kernel<4, T>), dim3((unsigned)gx, (unsigned)std::min<int64_t>(tiles - t0, 65535)), dim3(kRowsWaves * 64), 0, st, p);
+        a.tile0 = (int)t0;
+        hipLaunchKernelGGL((mx_rows_kernel<4, T>), dim3((unsigned)((a.M + 15) / 16), (unsigned)std::min<int64_t>(tiles - t0, 65535)), dim3(kRowsWaves * 64), 0, st, a);
         MX_HIP_TRY(hipGetLastError());
     }
     return CL_OK;
+}
+
+// The product, and what is left to do where it gives partial sums: rows of Y (k pairs to each) from a.part.
+static int32_t run_product(ProductArgs a, const Choice &c, const ExpertLists *L, void *Y, int32_t y_type, int32_t tokens, int32_t k, const int32_t *experts_of,
+                           const float *weights, hipStream_t st)
+{
+    a.Y = Y;
+    a.y_wide = a.out_width % 4 == 0 && aligned(Y, 4 * type_bytes(y_type));
+    if (!a.part) return with_type(y_type, [&](auto t) { return launch_product<decltype(t)>(a, c, L, st); });
+    if (int32_t rc = launch_product<float>(a, c, L, st)) return rc;
+    const FinishArgs f{a.part, a.bias, weights, experts_of, Y, (int64_t)a.rows * a.pitch, tokens, k, experts_of ? a.experts : 1, a.M, a.pitch, c.splits, a.act, a.out_width};
+    const int quads = a.pitch / 4;
+    const int64_t wgs = ((int64_t)tokens * quads + 255) / 256;
+    if (wgs > INT32_MAX) return fail(CL_EUNSUPPORTED, "a launch of %lld workgroups does not fit a grid", (long long)wgs);
+    return with_type(y_type, [&](auto t) -> int32_t {
+        hipLaunchKernelGGL(mx_finish_kernel<decltype(t)>, dim3((unsigned)wgs), dim3(256), 0, st, f, quads);
+        MX_HIP_TRY(hipGetLastError());
+        return CL_OK;
+    });
 }
 
 static int32_t check_matrix(const cl_mx_matrix *W)
@@ -228,13 +373,28 @@ static int32_t quantised_input(ProductArgs &a, const cl_mx_input *X, int64_t row
     return launch_quantize(X->d_X, X->type, X->stride, rows, K, codes, scales, st);
 }
 
-static Scratch experts_scratch(int32_t M, int32_t K, int32_t x_type, int64_t x_rows, int32_t tokens, int32_t k, int32_t experts, bool join, bool own_lists, int32_t act)
+static size_t part_bytes(int32_t M, int64_t rows, int splits) { return (size_t)splits * rows * round_up(M, 4) * 4; }
+
+static Scratch fc_scratch(const Choice &c, int32_t M, int32_t K, int32_t x_type, int32_t batch)
 {
     Scratch s;
-    scratch_input(s, x_type, x_rows, K);
-    if (join) s.pairs = s.take((size_t)tokens * k * (act == CL_ACT_GATED ? M / 2 : M) * 4);
-    if (own_lists) s.lists = s.take(expert_lists_at(nullptr, tokens, k, experts).bytes);
+    scratch_input(s, x_type, batch, K);
+    if (c.splits > 1) s.pairs = s.take(part_bytes(M, batch, c.splits));
     return s;
+}
+
+static Scratch experts_scratch(const Choice &c, int32_t M, int32_t K, int32_t x_type, int32_t experts, const cl_mx_experts_call &call)
+{
+    Scratch s;
+    scratch_input(s, x_type, (int64_t)call.tokens * (call.x_per_pair ? call.k : 1), K);
+    if (call.d_weights) s.pairs = s.take(part_bytes(M, (int64_t)call.tokens * call.k, c.splits));
+    if (!call.d_lists) s.lists = s.take(expert_lists_at(nullptr, call.tokens, call.k, experts).bytes);
+    return s;
+}
+
+static Choice choose_experts(int32_t M, int32_t K, int32_t experts, const cl_mx_experts_call &call)
+{
+    return choose(M, row_blocks(K), (int64_t)call.tokens * call.k, std::max(2, experts), call.d_weights != nullptr);
 }
 
 }  // namespace mx
@@ -248,9 +408,7 @@ extern "C" int32_t cl_mx_fc_workspace_bytes(const cl_mx_matrix *W, int32_t batch
     if (!out) return fail(CL_EINVAL, "null pointer");
     if (int32_t rc = check_forward(W, x_type, CL_F32, CL_ACT_NONE)) return rc;
     if (batch < 0) return fail(CL_EINVAL, "batch of %d", (int)batch);
-    Scratch s;
-    scratch_input(s, x_type, batch, W->K);
-    *out = s.bytes;
+    *out = fc_scratch(choose(W->rows, row_blocks(W->K), batch, 1, false), W->rows, W->K, x_type, batch).bytes;
     clear_error();
     return CL_OK;
 }
@@ -263,8 +421,8 @@ extern "C" int32_t cl_mx_fc_forward(const cl_mx_matrix *W, const cl_mx_input *X,
     if (batch < 0) return fail(CL_EINVAL, "batch of %d", (int)batch);
     if (batch == 0) return CL_OK;
     if (int32_t rc = check_pointers(W, X, d_Y, batch)) return rc;
-    Scratch s;
-    scratch_input(s, X->type, batch, W->K);
+    const Choice c = choose(W->rows, row_blocks(W->K), batch, 1, false);
+    const Scratch s = fc_scratch(c, W->rows, W->K, X->type, batch);
     if (int32_t rc = check_scratch(s, d_workspace, workspace_bytes)) return rc;
     hipStream_t st = (hipStream_t)stream;
     ProductArgs a{};
@@ -272,14 +430,14 @@ extern "C" int32_t cl_mx_fc_forward(const cl_mx_matrix *W, const cl_mx_input *X,
     a.w_codes = (const uint8_t *)W->d_codes;
     a.w_scales = (const uint8_t *)W->d_scales;
     a.bias = d_bias;
-    a.Y = d_Y;
+    a.part = c.splits > 1 ? (float *)((uint8_t *)d_workspace + s.pairs) : nullptr;
+    a.pitch = (int)round_up(W->rows, 4);
     a.blocks = row_blocks(W->K);
     a.M = W->rows;
     a.rows = batch;
     a.act = act;
     a.out_width = act == CL_ACT_GATED ? W->rows / 2 : W->rows;
-    const int32_t rc = with_type(y_type, [&](auto t) { return launch_product<decltype(t)>(a, ((int64_t)batch + 63) / 64, st); });
-    if (rc) return rc;
+    if (int32_t rc = run_product(a, c, nullptr, d_Y, y_type, batch, 1, nullptr, nullptr, st)) return rc;
     clear_error();
     return CL_OK;
 }
@@ -297,8 +455,7 @@ extern "C" int32_t cl_mx_experts_workspace_bytes(const cl_mx_matrix *W, int32_t 
     if (!out || !call) return fail(CL_EINVAL, "null pointer");
     if (int32_t rc = check_forward(W, x_type, CL_F32, call->act)) return rc;
     if (int32_t rc = check_experts(W, experts, call->tokens, call->k)) return rc;
-    const int64_t x_rows = (int64_t)call->tokens * (call->x_per_pair ? call->k : 1);
-    *out = experts_scratch(W->rows, W->K, x_type, x_rows, call->tokens, call->k, experts, call->d_weights != nullptr, call->d_lists == nullptr, call->act).bytes;
+    *out = experts_scratch(choose_experts(W->rows, W->K, experts, *call), W->rows, W->K, x_type, experts, *call).bytes;
     clear_error();
     return CL_OK;
 }
@@ -316,7 +473,8 @@ extern "C" int32_t cl_mx_experts_forward(const cl_mx_matrix *W, int32_t experts,
     if (!call->d_experts) return fail(CL_EINVAL, "null pointer");
     if (call->d_lists && !aligned(call->d_lists, 256)) return fail(CL_EINVAL, "lists must be 256-byte aligned");
     const bool join = call->d_weights != nullptr;
-    const Scratch s = experts_scratch(W->rows, W->K, X->type, x_rows, tokens, k, experts, join, call->d_lists == nullptr, call->act);
+    const Choice c = choose_experts(W->rows, W->K, experts, *call);
+    const Scratch s = experts_scratch(c, W->rows, W->K, X->type, experts, *call);
     if (int32_t rc = check_scratch(s, d_workspace, workspace_bytes)) return rc;
     hipStream_t st = (hipStream_t)stream;
     ProductArgs a{};
@@ -336,27 +494,10 @@ extern "C" int32_t cl_mx_experts_forward(const cl_mx_matrix *W, int32_t experts,
     a.x_div = call->x_per_pair ? 1 : k;
     a.order = L.order;
     a.offsets = L.offsets;
-    a.tiles = L.tiles[1];
-    a.tile_count = L.tile_count + 1;
     a.skip_unrouted = join;
-    a.Y = join ? (uint8_t *)d_workspace + s.pairs : d_Y;
-    int32_t rc = with_type(join ? (int32_t)CL_F32 : y_type, [&](auto t) { return launch_product<decltype(t)>(a, L.max_tiles[1], st); });
-    if (rc) return rc;
-    if (join) {
-        rc = with_type(y_type, [&](auto t) -> int32_t {
-            using T = decltype(t);
-            const unsigned gy = (unsigned)std::min(tokens, 32768), gz = 1;
-            for (int32_t t0 = 0; t0 < tokens; t0 += (int32_t)gy) {
-                const unsigned n = (unsigned)std::min<int64_t>(gy, tokens - t0);
-                hipLaunchKernelGGL(join_kernel<T>, dim3((unsigned)((a.out_width + 255) / 256), n, gz), dim3(256), 0, st,
-                                   (const float *)a.Y + (int64_t)t0 * k * a.out_width, call->d_experts + (int64_t)t0 * k, call->d_weights + (int64_t)t0 * k,
-                                   (T *)d_Y + (int64_t)t0 * a.out_width, k, experts, a.out_width);
-                MX_HIP_TRY(hipGetLastError());
-            }
-            return CL_OK;
-        });
-        if (rc) return rc;
-    }
+    a.part = join ? (float *)((uint8_t *)d_workspace + s.pairs) : nullptr;
+    a.pitch = (int)round_up(W->rows, 4);
+    if (int32_t rc = run_product(a, c, &L, d_Y, y_type, tokens, k, call->d_experts, call->d_weights, st)) return rc;
     clear_error();
     return CL_OK;
 }

@@ -1,0 +1,212 @@
+// The product for many columns: tiles of the output, operands through LDS.  Part of product.hip's translation unit, inside
+// namespace cl::mx.
+#pragma once
+
+// A workgroup of WM x WN wavefronts makes BM outputs (rows of W) of BN columns (rows of X), a wavefront TI x TJ pieces of
+// 16 x 16.  A step is one matrix instruction deep: 128 k, four blocks, 64 bytes and one word of scales of each row.
+//
+// LDS holds D steps.  Step t is multiplied while t + 1 lies there and t + 2 .. t + D - 1 are on their way, written by the
+// loads themselves.  Its fragments are read from LDS between the multiplies: a row's fragment two pieces before its use, the
+// columns' fragments, which a whole step uses, during the step before (a second set of registers).  Requests, reads and
+// multiplies stay in program order (scheduling barriers): in a bunch behind the step's barrier they would fill their queues
+// and the multiplies would wait behind them.
+//
+// In LDS a row's four blocks are 64 consecutive bytes, block c of row r in place c ^ (r / 4 % 4): sixteen lanes that read one
+// block of sixteen rows then touch each of the 64 banks once.
+template <int BM, int BN, int WM, int WN, int D> struct Tile {
+    static constexpr int kWaves = WM * WN, kThreads = kWaves * 64;
+    static constexpr int TI = BM / WM / 16, TJ = BN / WN / 16;
+    static constexpr int kAhead = TI <= 4 ? TI : 4;          // how many pieces before its use a row fragment is read
+    static constexpr int kRing = TI <= 4 ? 2 * TI : TI;      // row fragments in registers
+    static constexpr int slot(int f, int p) { return f % TI + (kRing > TI && ((f / TI + p) & 1) ? TI : 0); }    // of piece f, a step of parity p
+    static constexpr int kCodeLoads = (BM + BN) / 16 / kWaves;    // of a wavefront and step
+    static constexpr int kScaleLoads = (BM + BN) / 64;       // of the workgroup and four steps; wavefronts beyond that number repeat the last
+    static constexpr int kScaleShare = (kScaleLoads + kWaves - 1) / kWaves;
+    static constexpr int kBuffer = (BM + BN) * 64;
+    static constexpr int kScales = D * kBuffer;              // where the scales start: two buffers of four steps
+    static constexpr int kScaleBuffer = (BM + BN) * 16;
+    static constexpr int kLds = kScales + 2 * kScaleBuffer;
+    static_assert(BM % (WM * 16) == 0 && BN % (WN * 16) == 0 && TI >= TJ, "");
+    static_assert((BM + BN) / 16 % kWaves == 0 && BM % 64 == 0 && BN % 64 == 0, "");
+    // loads of a wavefront that may be on their way when step s (of four) begins: those asked for in the D - 3 steps before, but
+    // when the last of four begins, of those after the scales of the next four
+    static constexpr int on_their_way(int s)
+    {
+        int n = 0;
+        for (int i = 1; i <= (s == 3 && D > 5 ? 2 : D - 3); ++i) n += kCodeLoads + ((s + 8 - i) % 4 == 0 ? kScaleShare : 0);
+        return n;
+    }
+    static_assert(D >= 3 && D <= 8 && (D - 3) * kCodeLoads + kScaleShare < 16, "");       // (the count that a wait names)
+};
+
+template <int BM, int BN, int WM, int WN, int D, class T>
+__global__ __launch_bounds__(WM * WN * 64, 2) void mx_tile_kernel(ProductArgs a, int row_tiles)
+{
+    using C = Tile<BM, BN, WM, WN, D>;
+    constexpr int TI = C::TI, TJ = C::TJ;
+    extern __shared__ __align__(128) uint8_t lds[];
+    typedef __attribute__((address_space(3))) void *lds_ptr;
+    typedef const __attribute__((address_space(1))) void *global_ptr;
+    const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = (int)(threadIdx.x & 63), r = lane & 15, g = lane >> 4;
+
+    const int tile = (int)blockIdx.x;
+    const int m0 = (tile % row_tiles) * BM;
+    Columns c;
+    if (!columns_of<BN>(a, tile / row_tiles, c)) return;
+    const bool routed = !a.order || c.expert < a.experts;
+    const int split = (int)blockIdx.y, all_steps = a.blocks / 4;
+    const int t_first = (int)((int64_t)all_steps * split / a.splits), t_end = (int)((int64_t)all_steps * (split + 1) / a.splits);
+    const int steps = routed ? t_end - t_first : 0;
+
+    // where each load of a wavefront reads: rows of W beyond the last and columns beyond the last repeat the last one
+    const int64_t row_bytes = (int64_t)a.blocks * 16;
+    const int64_t w_first = routed ? (int64_t)c.expert * a.M : 0;
+    auto x_row = [&](int n) -> int64_t {
+        const int at = c.first + min(n, c.count - 1);
+        return a.order ? a.order[at] / a.x_div : at;
+    };
+    const uint8_t *code_at[C::kCodeLoads], *scale_at[C::kScaleShare];
+#pragma unroll
+    for (int i = 0; i < C::kCodeLoads; ++i) {
+        const int q = i * C::kWaves + wave, row = q * 16 + (lane >> 2), chunk = (lane & 3) ^ (lane >> 4 & 3);
+        code_at[i] = (q < BM / 16 ? a.w_codes + (w_first + min(m0 + row, a.M - 1)) * row_bytes : a.x_codes + x_row(row - BM) * row_bytes) + chunk * 16;
+    }
+    auto scale_load = [&](int i) { return min(i * C::kWaves + wave, C::kScaleLoads - 1); };
+#pragma unroll
+    for (int i = 0; i < C::kScaleShare; ++i) {
+        const int row = scale_load(i) * 64 + lane;
+        scale_at[i] = row < BM ? a.w_scales + (w_first + min(m0 + row, a.M - 1)) * a.blocks : a.x_scales + x_row(row - BM) * a.blocks;
+    }
+    // code load k of step t into its buffer
+    auto request_code = [&](int t, uint8_t *buf, int k) {
+        __builtin_amdgcn_global_load_lds((global_ptr)(code_at[k] + (int64_t)(t_first + t) * 64), (lds_ptr)(buf + (k * C::kWaves + wave) * 1024), 16, 0, 0);
+    };
+    // scale load k of steps 4 q .. 4 q + 3.  (One word a step and row would be a load of 64 cache lines each time.)  Where fewer
+    // than four steps are left in the row, its last four are loaded: shift(q) words in front of what is wanted.
+    auto request_scales = [&](int q, uint8_t *buf, int k) {
+        const int at = min(t_first + 4 * q, all_steps - 4);
+        __builtin_amdgcn_global_load_lds((global_ptr)(scale_at[k] + (int64_t)at * 4), (lds_ptr)(buf + scale_load(k) * 1024), 16, 0, 0);
+    };
+    auto shift = [&](int q) { return t_first + 4 * q - min(t_first + 4 * q, all_steps - 4); };
+
+    const int wi = (wave / WN) * TI * 16 + r, wj = BM + (wave % WN) * TJ * 16 + r;        // the lane's rows of the buffer
+    const int at_code = (g ^ (r >> 2)) * 16;
+    auto read_code = [&](const uint8_t *buf, int row) { return *(const i32x4 *)(buf + row * 64 + at_code); };
+    auto read_scale = [&](const uint8_t *buf, int row) -> int { return buf[row * 16 + g]; };
+
+    f32x4 acc[TI][TJ];
+#pragma unroll
+    for (auto &x : acc)
+#pragma unroll
+        for (auto &y : x) y = f32x4{0, 0, 0, 0};
+    i32x4 w[C::kRing], x[2][TJ];
+    int sw[C::kRing], sx[2][TJ];
+
+    constexpr int kWaitLds = 0xc07f, kWaitLoads = 0xf70;     // s_waitcnt: no LDS access left; no load left, or-ed with n < 16: n left
+    auto barrier = [&] {
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+    };
+    // Step t = 4 q + S: `now` and `next` hold its codes and those of the step after, `to` receives those of step `ask`; likewise the
+    // scales, which step 4 q asks for four steps ahead.
+    auto step = [&](auto S, const uint8_t *__restrict__ now, const uint8_t *__restrict__ next, uint8_t *__restrict__ to, const uint8_t *__restrict__ scales_now,
+                    const uint8_t *__restrict__ scales_next, uint8_t *__restrict__ scales_to, int ask, int ask_scales) {
+        constexpr int s = decltype(S)::value, p = s & 1;
+        // every wavefront's loads of step t + 1 have arrived, and all reads of the buffers that are asked for next are done
+        __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_waitcnt(kWaitLds);
+        __builtin_amdgcn_s_waitcnt(kWaitLoads | C::on_their_way(s));
+        barrier();
+#pragma unroll
+        for (int i = 0; i < TI; ++i) {
+#pragma unroll
+            for (int j = 0; j < TJ; ++j) {
+                if (j == 0) {
+                    const int f = i + C::kAhead;
+                    w[C::slot(f, p)] = read_code(f < TI ? now : next, wi + f % TI * 16);
+                    sw[C::slot(f, p)] = read_scale(f < TI ? scales_now : scales_next, wi + f % TI * 16);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                if (j == TJ / 2 && i >= TI - TJ) {
+                    const int f = i - (TI - TJ);
+                    x[1 - p][f] = read_code(next, wj + f * 16);
+                    sx[1 - p][f] = read_scale(scales_next, wj + f * 16);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                if (j == TJ - 1) {
+#pragma unroll
+                    for (int k = i; k < C::kCodeLoads; k += TI) request_code(ask, to, k);
+                    if (s == 0 && i == TI - 1) {
+#pragma unroll
+                        for (int k = 0; k < C::kScaleShare; ++k) request_scales(ask_scales, scales_to, k);
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                acc[i][j] = mfma_fp4<0>(w[C::slot(i, p)], x[p][j], acc[i][j], sw[C::slot(i, p)], sx[p][j]);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        }
+    };
+
+    if (steps > 0) {
+        auto buffer = [&](int t) { return lds + t % D * C::kBuffer; };
+        auto scales = [&](int q) { return lds + C::kScales + (q & 1) * C::kScaleBuffer; };
+        // step t of which the row has S before it in its four
+        auto at = [&](auto S, int t) {
+            constexpr int s = decltype(S)::value;
+            const int q = t / 4, qn = (t + 1) / 4;
+            step(S, buffer(t), buffer(t + 1), buffer(t + D - 1), scales(q) + (shift(q) + s) * 4, scales(qn) + (shift(qn) + (s + 1) % 4) * 4, scales(q + 1),
+                 min(t + D - 1, steps - 1), min(q + 1, (steps - 1) / 4));
+        };
+        // (requests beyond the last step repeat it, so that a wait always counts the same; nothing reads what they bring)
+#pragma unroll
+        for (int k = 0; k < C::kScaleShare; ++k) request_scales(0, scales(0), k);
+#pragma unroll
+        for (int t = 0; t < D - 1; ++t)
+#pragma unroll
+            for (int k = 0; k < C::kCodeLoads; ++k) request_code(min(t, steps - 1), buffer(t), k);
+        __builtin_amdgcn_s_waitcnt(kWaitLoads);
+        barrier();
+        const uint8_t *first = scales(0) + shift(0) * 4;
+#pragma unroll
+        for (int j = 0; j < TJ; ++j) x[0][j] = read_code(lds, wj + j * 16), sx[0][j] = read_scale(first, wj + j * 16);
+#pragma unroll
+        for (int i = 0; i < C::kAhead; ++i) w[i] = read_code(lds, wi + i * 16), sw[i] = read_scale(first, wi + i * 16);
+        int t = 0;
+        for (; t + 4 <= steps; t += 4) {
+            at(std::integral_constant<int, 0>{}, t);
+            at(std::integral_constant<int, 1>{}, t + 1);
+            at(std::integral_constant<int, 2>{}, t + 2);
+            at(std::integral_constant<int, 3>{}, t + 3);
+        }
+        if (t < steps) at(std::integral_constant<int, 0>{}, t);
+        if (t + 1 < steps) at(std::integral_constant<int, 1>{}, t + 1);
+        if (t + 2 < steps) at(std::integral_constant<int, 2>{}, t + 2);
+        __builtin_amdgcn_s_waitcnt(kWaitLds);
+        __builtin_amdgcn_s_waitcnt(kWaitLoads);
+        barrier();
+    }
+
+    // A wavefront's outputs go through LDS, sixteen columns at a time, so that what it stores of a row of Y is consecutive.
+    constexpr int kWide = TI * 16, kPitch = kWide + 4, kLanes = kWide / 4;
+    static_assert(C::kWaves * 16 * kPitch * 4 <= C::kLds, "");
+    float *mine = (float *)lds + wave * 16 * kPitch;
+#pragma unroll
+    for (int j = 0; j < TJ; ++j) {
+#pragma unroll
+        for (int i = 0; i < TI; ++i) *(f32x4 *)(mine + r * kPitch + i * 16 + 4 * g) = acc[i][j];
+        __builtin_amdgcn_wave_barrier();
+        const int first = (wave % WN) * TJ * 16 + j * 16, m = m0 + (wave / WN) * kWide + lane % kLanes * 4;
+#pragma unroll 1
+        for (int n = lane / kLanes; n < 16; n += 64 / kLanes)
+            if (first + n < c.count) {
+                const int at = c.first + first + n;
+                const f32x4 v = *(const f32x4 *)(mine + n * kPitch + lane % kLanes * 4);
+                const int64_t row = a.order ? a.order[at] : at;
+                if (a.part) store_part(a, split, row, m, v);
+                else finish_outputs<T>(a, c.expert, row, m, v);
+            }
+        __builtin_amdgcn_wave_barrier();
+    }
+}
