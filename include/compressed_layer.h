@@ -551,6 +551,8 @@ int32_t cl_mx_fc_forward(const cl_mx_matrix *W, const cl_mx_input *X, const floa
 #define CL_ROUTE_MAX_EXPERTS 1024
 #define CL_ROUTE_MAX_GROUPS 64
 #define CL_ROUTE_MAX_K 32
+/* Most pairs of token and expert of one call. */
+#define CL_EXPERTS_MAX_PAIRS (1 << 30)
 enum { CL_SCORE_SOFTMAX = 0, CL_SCORE_SIGMOID = 1 };
 enum { CL_GROUP_MAX = 0, CL_GROUP_TOP2 = 1 };
 typedef struct {

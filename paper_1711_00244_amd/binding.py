@@ -8,6 +8,7 @@ library is missing or was not built, importing a symbol from it raises.
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import os
 
 import numpy as np
@@ -538,38 +539,60 @@ def plan_batches(time_ms, batch_set, in_bytes_per_image, out_bytes_per_image, ws
 # --------------------------------------------------------------------------- #
 # microscaled 4-bit matrices and routed experts
 # --------------------------------------------------------------------------- #
-_types = None
+# (A call of these takes a few microseconds on the GPU where rows are few: what the host does for it is kept short.)
+_types: dict = {}
+_current_device = _raw_stream = None
+
+
+def _start():
+    """The library, with what the calls below use of torch at hand."""
+    global _current_device, _raw_stream
+    if not _types:
+        import torch
+        L = lib()
+        _current_device = torch.cuda.current_device
+        _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
+        _types.update({torch.float32: 0, torch.bfloat16: 1, torch.float16: 2})
+        return L
+    return _lib
 
 
 def _element_type(dtype, what):
     """CL_F32, CL_BF16 or CL_F16."""
-    global _types
-    if _types is None:
-        import torch
-        _types = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
-    try:
-        return _types[dtype]
-    except KeyError:
-        raise ValueError(f"{what} must be float32, bfloat16 or float16, got {dtype}") from None
+    ty = _types.get(dtype)
+    if ty is None:
+        raise ValueError(f"{what} must be float32, bfloat16 or float16, got {dtype}")
+    return ty
 
 
 def _rows(t, what, cols=None):
     """A matrix whose rows are contiguous, at any distance from each other -> (element type, distance)."""
     ty = _element_type(t.dtype, what)
-    if t.dim() != 2 or not t.is_cuda or (t.shape[1] > 1 and t.stride(1) != 1) or (cols is not None and t.shape[1] != cols):
-        raise ValueError(f"{what} must be a CUDA matrix with contiguous rows{'' if cols is None else f' of {cols}'}, "
-                         f"got {tuple(t.shape)} with strides {t.stride()}")
-    return ty, t.stride(0) if t.shape[0] > 1 else t.shape[1]
+    shape = t.shape
+    if len(shape) != 2 or not t.is_cuda or (cols is not None and shape[1] != cols):
+        raise ValueError(f"{what} must be a CUDA matrix{'' if cols is None else f' with rows of {cols}'}, got {tuple(shape)} on {t.device}")
+    stride, one = t.stride()
+    if one != 1 and shape[1] > 1:
+        raise ValueError(f"{what} must have contiguous rows, got strides {t.stride()}")
+    return ty, stride if shape[0] > 1 else shape[1]
 
 
-def _same_device(device, *tensors):
-    """The kernels run on the current device and its current stream."""
-    import torch
-    if device.index != torch.cuda.current_device():
-        raise ValueError(f"the input is on {device}, the current device is cuda:{torch.cuda.current_device()}")
+def _on(device, *tensors):
+    """The stream of a call, which runs on the current device: where all its tensors have to be."""
+    index = device.index
+    if index != _current_device():
+        raise ValueError(f"the input is on {device}, the current device is cuda:{_current_device()}")
     for t in tensors:
         if t is not None and t.device != device:
             raise ValueError(f"a tensor is on {t.device}, the input on {device}")
+    return _raw_stream(index)
+
+
+def mx_row_blocks(K: int) -> int:
+    """Blocks of a row of K elements: whole groups of four."""
+    if K < 1:
+        raise ValueError("a row has at least one element")
+    return (K + 127) // 128 * 4
 
 
 class MxTensor:
@@ -579,12 +602,13 @@ class MxTensor:
     __slots__ = ("codes", "scales", "K")
 
     def __init__(self, codes, scales, K):
-        import torch
         kb = mx_row_blocks(K)
+        import torch
         if codes.dtype != torch.uint8 or scales.dtype != torch.uint8 or not codes.is_cuda or not codes.is_contiguous() or not scales.is_contiguous():
             raise ValueError("codes and scales must be contiguous uint8 CUDA tensors")
-        if codes.dim() < 2 or codes.shape[-1] != kb * 16 or scales.shape != codes.shape[:-1] + (kb,) or scales.device != codes.device:
-            raise ValueError(f"rows of {K} elements have {kb * 16} bytes of codes and {kb} scales, got {tuple(codes.shape)} and {tuple(scales.shape)}")
+        shape = codes.shape
+        if len(shape) < 2 or shape[-1] != kb * 16 or scales.shape != shape[:-1] + (kb,) or scales.device != codes.device:
+            raise ValueError(f"rows of {K} elements have {kb * 16} bytes of codes and {kb} scales, got {tuple(shape)} and {tuple(scales.shape)}")
         self.codes, self.scales, self.K = codes, scales, K
 
     @property
@@ -596,105 +620,117 @@ class MxTensor:
         return self.codes.device
 
 
-def mx_row_blocks(K: int) -> int:
-    """Blocks of a row of K elements: whole groups of four."""
-    if K < 1:
-        raise ValueError("a row has at least one element")
-    return (K + 127) // 128 * 4
-
-
 def mx_quantize(X, out: MxTensor | None = None) -> MxTensor:
     """Rows of X ((..., K), float32, bfloat16 or float16; a matrix's rows at any distance) -> MxTensor of the same shape."""
     import torch
-    lead = X.shape[:-1]
-    if X.dim() > 2:
-        X = X.reshape(-1, X.shape[-1])
+    L = _start()
+    shape = X.shape
+    K, lead = shape[-1], shape[:-1]
+    if len(shape) > 2:
+        X = X.reshape(-1, K)
     ty, stride = _rows(X, "X")
-    rows, K = X.shape
     if out is None:
         kb = mx_row_blocks(K)
-        out = MxTensor(torch.empty(lead + (kb * 16,), dtype=torch.uint8, device=X.device), torch.empty(lead + (kb,), dtype=torch.uint8, device=X.device), K)
+        out = MxTensor.__new__(MxTensor)
+        out.codes = torch.empty(lead + (kb * 16,), dtype=torch.uint8, device=X.device)
+        out.scales = torch.empty(lead + (kb,), dtype=torch.uint8, device=X.device)
+        out.K = K
     elif out.shape != lead + (K,):
         raise ValueError(f"out must hold {tuple(lead) + (K,)}, holds {out.shape}")
-    _same_device(X.device, out.codes)
-    _check(lib().cl_mx_quantize(X.data_ptr(), ty, stride, rows, K, out.codes.data_ptr(), out.scales.data_ptr(), _stream()))
+    stream = _on(X.device, out.codes)
+    _check(L.cl_mx_quantize(X.data_ptr(), ty, stride, X.shape[0], K, out.codes.data_ptr(), out.scales.data_ptr(), stream))
     return out
 
 
 def mx_dequantize(Q: MxTensor, dtype=None, out=None):
     """The values Q stands for, (..., K) of dtype (float32 unless given)."""
     import torch
+    L = _start()
+    codes = Q.codes
+    shape = codes.shape[:-1] + (Q.K,)
     if out is None:
-        out = torch.empty(Q.shape, dtype=dtype or torch.float32, device=Q.device)
-    elif tuple(out.shape) != Q.shape or not (out.is_contiguous() or out.dim() == 2) or (dtype is not None and out.dtype != dtype):
-        raise ValueError(f"out must be {Q.shape}{'' if dtype is None else f' of {dtype}'}, contiguous or a matrix with contiguous rows")
-    Y = out if out.dim() == 2 else out.view(-1, Q.K)
+        out = torch.empty(shape, dtype=dtype or torch.float32, device=codes.device)
+    elif out.shape != shape or not (out.is_contiguous() or len(shape) == 2) or (dtype is not None and out.dtype != dtype):
+        raise ValueError(f"out must be {tuple(shape)}{'' if dtype is None else f' of {dtype}'}, contiguous or a matrix with contiguous rows")
+    Y = out if len(shape) == 2 else out.view(-1, Q.K)
     ty, stride = _rows(Y, "out", Q.K)
-    _same_device(Q.device, out)
-    _check(lib().cl_mx_dequantize(Q.codes.data_ptr(), Q.scales.data_ptr(), Y.shape[0], Q.K, out.data_ptr(), ty, stride, _stream()))
+    stream = _on(codes.device, out)
+    _check(L.cl_mx_dequantize(codes.data_ptr(), Q.scales.data_ptr(), Y.shape[0], Q.K, out.data_ptr(), ty, stride, stream))
     return out
 
 
 def _mx_input(X, K):
     """-> (struct, rows, element type of an output that names none)"""
-    import torch
     if isinstance(X, MxTensor):
-        if len(X.shape) != 2 or X.K != K:
+        if len(X.codes.shape) != 2 or X.K != K:
             raise ValueError(f"X must have rows of {K}, got {X.shape}")
-        return MxInput(X.codes.data_ptr(), X.scales.data_ptr(), MX4, 0), X.shape[0], torch.float32
+        import torch
+        return MxInput(X.codes.data_ptr(), X.scales.data_ptr(), MX4, 0), X.codes.shape[0], torch.float32
     ty, stride = _rows(X, "X", K)
     return MxInput(X.data_ptr(), None, ty, stride), X.shape[0], X.dtype
 
 
 def _mx_output(out, shape, dtype, device):
     """-> (tensor, element type)"""
-    import torch
     if out is None:
+        import torch
         out = torch.empty(shape, dtype=dtype, device=device)
     elif tuple(out.shape) != shape or not out.is_contiguous() or out.dtype != dtype:
         raise ValueError(f"out must be a contiguous {dtype} tensor of shape {shape}, got {out.dtype} {tuple(out.shape)}")
-    return out, _element_type(out.dtype, "out")
+    return out, _element_type(dtype, "out")
 
 
-def _workspace(workspace, need, device):
-    import torch
-    if workspace is None and need:
-        workspace = torch.empty(need, dtype=torch.uint8, device=device)
+def _mx_workspace(workspace, need, device):
+    """-> (tensor, address, bytes)"""
     if workspace is None:
-        return None, None, 0
-    return workspace, _dev_ptr(workspace), workspace.numel() * workspace.element_size()
+        if not need:
+            return None, None, 0
+        import torch
+        workspace = torch.empty(need, dtype=torch.uint8, device=device)
+    elif not workspace.is_contiguous():
+        raise ValueError("the workspace must be contiguous")
+    return workspace, workspace.data_ptr(), workspace.numel() * workspace.element_size()
 
 
 def _act(act):
-    if act not in ACTIVATIONS:
+    code = ACTIVATIONS.get(act)
+    if code is None:
         raise ValueError(f"act must be one of {', '.join(ACTIVATIONS)}, got {act!r}")
-    return ACTIVATIONS[act]
+    return code
+
+
+@functools.lru_cache(maxsize=1024)
+def _mx_fc_need(M, K, batch, x_type):
+    n = C.c_size_t(0)
+    _check(lib().cl_mx_fc_workspace_bytes(MxMatrix(None, None, M, K), batch, x_type, n))
+    return n.value
 
 
 def mx_fc_workspace_bytes(W: MxTensor, batch: int, dtype=None) -> int:
-    """Scratch of mx_fc_forward for `batch` rows of dtype (None: an MxTensor, which needs none)."""
-    n = C.c_size_t(0)
-    m = MxMatrix(None, None, W.shape[0], W.K)
-    _check(lib().cl_mx_fc_workspace_bytes(C.byref(m), batch, MX4 if dtype is None else _element_type(dtype, "X"), C.byref(n)))
-    return n.value
+    """Scratch of mx_fc_forward for `batch` rows of dtype (None: an MxTensor)."""
+    _start()
+    return _mx_fc_need(W.shape[0], W.K, batch, MX4 if dtype is None else _element_type(dtype, "X"))
 
 
 def mx_fc_forward(W: MxTensor, X, bias=None, relu=False, act=None, dtype=None, out=None, workspace=None):
     """act(X W^T + bias) with W (M, K) in 4-bit blocks and X (B, K) - float32, bfloat16 or float16, quantised on the way, or an MxTensor.
     act: "none", "relu" (the same as relu=True) or "gated" (rows 2 i and 2 i + 1 of W give gate and value of output i).  The output is of
     dtype, X's own unless given (float32 for an MxTensor)."""
-    if len(W.shape) != 2:
+    L = _start()
+    codes, K = W.codes, W.K
+    if len(codes.shape) != 2:
         raise ValueError(f"W must be a matrix, got {W.shape}")
-    M, K = W.shape
+    M = codes.shape[0]
     act = _act(act or ("relu" if relu else "none"))
     xs, B, own_dtype = _mx_input(X, K)
-    _want(bias, (M,), "bias")
-    Y, y_type = _mx_output(out, (B, M // 2 if act == 2 else M), dtype or (out.dtype if out is not None else own_dtype), X.device)
-    _same_device(X.device, W.codes, bias, Y, workspace)
-    m, L, n = MxMatrix(W.codes.data_ptr(), W.scales.data_ptr(), M, K), lib(), C.c_size_t(0)
-    _check(L.cl_mx_fc_workspace_bytes(m, B, xs.type, n))
-    workspace, ws, ws_bytes = _workspace(workspace, n.value, X.device)
-    _check(L.cl_mx_fc_forward(m, xs, None if bias is None else bias.data_ptr(), Y.data_ptr(), y_type, B, act, ws, ws_bytes, _stream()))
+    if bias is not None:
+        _want(bias, (M,), "bias")
+    device = X.device
+    Y, y_type = _mx_output(out, (B, M // 2 if act == 2 else M), dtype or (own_dtype if out is None else out.dtype), device)
+    stream = _on(device, codes, bias, Y, workspace)
+    workspace, ws, ws_bytes = _mx_workspace(workspace, _mx_fc_need(M, K, B, xs.type), device)
+    _check(L.cl_mx_fc_forward(MxMatrix(codes.data_ptr(), W.scales.data_ptr(), M, K), xs, None if bias is None else bias.data_ptr(), Y.data_ptr(), y_type, B,
+                              act, ws, ws_bytes, stream))
     return Y
 
 
@@ -704,17 +740,19 @@ def route_experts(logits, k: int, bias=None, score="softmax", groups: int = 1, g
     groups_kept best of `groups` runs of experts), and their scores without the bias, divided by their sum if renormalize, times scale.
     -1 and 0 where no expert is left (logits of -inf, the lowest value or NaN mask an expert)."""
     import torch
+    L = _start()
     ty, stride = _rows(logits, "logits")
     T, E = logits.shape
-    _want(bias, (E,), "bias")
+    if bias is not None:
+        _want(bias, (E,), "bias")
     if score not in SCORES or group_score not in GROUP_SCORES:
         raise ValueError(f"score must be one of {', '.join(SCORES)} and group_score of {', '.join(GROUP_SCORES)}, got {score!r} and {group_score!r}")
-    _same_device(logits.device, bias)
+    device = logits.device
+    stream = _on(device, bias)
     d = RouteDesc(E, k, SCORES[score], groups, groups if groups_kept is None else groups_kept, GROUP_SCORES[group_score], int(renormalize), scale)
-    experts = torch.empty((T, max(k, 0)), dtype=torch.int32, device=logits.device)
-    weights = torch.empty((T, max(k, 0)), dtype=torch.float32, device=logits.device)
-    _check(lib().cl_route_experts(logits.data_ptr(), ty, stride, None if bias is None else bias.data_ptr(), T, d, experts.data_ptr(), weights.data_ptr(),
-                                  _stream()))
+    experts = torch.empty((T, max(k, 0)), dtype=torch.int32, device=device)
+    weights = torch.empty((T, max(k, 0)), dtype=torch.float32, device=device)
+    _check(L.cl_route_experts(logits.data_ptr(), ty, stride, None if bias is None else bias.data_ptr(), T, d, experts.data_ptr(), weights.data_ptr(), stream))
     return experts, weights
 
 
@@ -742,14 +780,23 @@ class ExpertLists:
 def expert_lists(experts, n_experts: int) -> ExpertLists:
     """experts (T, k) int32, as route_experts gives them."""
     import torch
+    L = _start()
     _want_experts(experts)
-    _same_device(experts.device)
+    stream = _on(experts.device)
     T, k = experts.shape
     n = C.c_size_t(0)
-    _check(lib().cl_expert_lists_bytes(T, k, n_experts, n))
+    _check(L.cl_expert_lists_bytes(T, k, n_experts, n))
     buffer = torch.empty(n.value, dtype=torch.uint8, device=experts.device)
-    _check(lib().cl_expert_lists(experts.data_ptr(), T, k, n_experts, buffer.data_ptr(), n.value, _stream()))
+    _check(L.cl_expert_lists(experts.data_ptr(), T, k, n_experts, buffer.data_ptr(), n.value, stream))
     return ExpertLists(buffer, T, k, n_experts)
+
+
+@functools.lru_cache(maxsize=1024)
+def _mx_experts_need(M, K, E, T, k, weighted, lists, act, x_per_pair, x_type):
+    n = C.c_size_t(0)
+    call = MxExpertsCall(T, k, None, 256 if weighted else None, None, 256 if lists else None, act, x_per_pair)
+    _check(lib().cl_mx_experts_workspace_bytes(MxMatrix(None, None, M, K), E, call, x_type, n))
+    return n.value
 
 
 def mx_experts_forward(W: MxTensor, X, experts, weights=None, bias=None, act="none", x_per_pair=False, lists: ExpertLists | None = None, dtype=None,
@@ -757,28 +804,31 @@ def mx_experts_forward(W: MxTensor, X, experts, weights=None, bias=None, act="no
     """The products of rows with their experts' matrices: W (E, M, K) in 4-bit blocks, X (T, K) - or (T * k, K) with x_per_pair -, experts (T, k) int32.
     With weights (T, k): (T, M), the weighted sum of each token's k products; without: (T * k, M), one row a pair.  bias (E, M); act as in
     mx_fc_forward, before the sum.  Pairs with an expert outside 0 .. E - 1 give nothing (a row of zeros without weights)."""
-    if len(W.shape) != 3:
+    L = _start()
+    codes, K = W.codes, W.K
+    if len(codes.shape) != 3:
         raise ValueError(f"W must be (experts, rows, K), got {W.shape}")
-    E, M, K = W.shape
+    E, M, _ = codes.shape
     _want_experts(experts)
     T, k = experts.shape
     act = _act(act)
     xs, rows, own_dtype = _mx_input(X, K)
     if rows != (T * k if x_per_pair else T):
         raise ValueError(f"X must have {T * k if x_per_pair else T} rows, got {rows}")
-    _want(weights, (T, k), "weights")
-    _want(bias, (E, M), "bias")
+    if weights is not None:
+        _want(weights, (T, k), "weights")
+    if bias is not None:
+        _want(bias, (E, M), "bias")
     if lists is not None and (lists.tokens, lists.k, lists.n_experts) != (T, k, E):
         raise ValueError(f"lists of {lists.tokens} x {lists.k} of {lists.n_experts} experts, wanted {T} x {k} of {E}")
-    Y, y_type = _mx_output(out, (T if weights is not None else T * k, M // 2 if act == 2 else M),
-                           dtype or (out.dtype if out is not None else own_dtype), X.device)
-    _same_device(X.device, W.codes, experts, weights, bias, Y, workspace, None if lists is None else lists.buffer)
+    device = X.device
+    Y, y_type = _mx_output(out, (T if weights is not None else T * k, M // 2 if act == 2 else M), dtype or (own_dtype if out is None else out.dtype), device)
+    stream = _on(device, codes, experts, weights, bias, Y, workspace, None if lists is None else lists.buffer)
+    need = _mx_experts_need(M, K, E, T, k, weights is not None, lists is not None, act, int(x_per_pair), xs.type)
+    workspace, ws, ws_bytes = _mx_workspace(workspace, need, device)
     call = MxExpertsCall(T, k, experts.data_ptr(), None if weights is None else weights.data_ptr(), None if bias is None else bias.data_ptr(),
                          None if lists is None else lists.buffer.data_ptr(), act, int(x_per_pair))
-    m, L, n = MxMatrix(W.codes.data_ptr(), W.scales.data_ptr(), M, K), lib(), C.c_size_t(0)
-    _check(L.cl_mx_experts_workspace_bytes(m, E, call, xs.type, n))
-    workspace, ws, ws_bytes = _workspace(workspace, n.value, X.device)
-    _check(L.cl_mx_experts_forward(m, E, xs, call, Y.data_ptr(), y_type, ws, ws_bytes, _stream()))
+    _check(L.cl_mx_experts_forward(MxMatrix(codes.data_ptr(), W.scales.data_ptr(), M, K), E, xs, call, Y.data_ptr(), y_type, ws, ws_bytes, stream))
     return Y
 
 

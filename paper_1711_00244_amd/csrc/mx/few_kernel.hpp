@@ -1,0 +1,161 @@
+// The product for very few rows of X: one launch, which quantises X itself.  Part of product.hip's translation unit, inside
+// namespace cl::mx.
+#pragma once
+
+// A workgroup of up to sixteen wavefronts makes the sums of 16 F rows of matrices and up to kFewColumns rows of X.  It quantises
+// those into LDS - every workgroup all of them, which for so few costs less than a launch of its own - while its first weights
+// are on their way; then the wavefronts share out the runs of 16 blocks as in mx_rows_kernel, and their sums meet in LDS.
+//
+// One matrix: 16 F consecutive rows of it.  Experts: one token (blockIdx.y), `rows_each` rows of each of its k experts' matrices,
+// which are rows of one matrix instruction like any others, so that a token's weighted sum needs no second launch either.
+// (One token, 64 experts of 1024 x 4096, eight chosen: lists, quantisation, product and sum apart took 33 us in five launches.)
+constexpr int kFewColumns = 4, kFewWaves = kRowsWaves;
+constexpr size_t kFewLds = 64 << 10;
+
+struct FewArgs {
+    ProductArgs p;
+    const void *X;
+    int64_t x_stride;
+    int K, columns;
+    const int32_t *experts_of;
+    const float *weights;
+    int k, rows_each, x_per_pair;
+    int x_wide;                                              // rows of X are 16-byte aligned
+};
+
+inline size_t few_lds(int blocks, int columns) { return (size_t)columns * blocks * 17; }
+
+template <class X, class T, bool EXPERTS> __global__ __launch_bounds__(kFewWaves * 64) void mx_few_kernel(FewArgs a)
+{
+    constexpr int kFewF = EXPERTS ? 2 : 1;
+    extern __shared__ __align__(16) uint8_t lds[];
+    __shared__ f32x4 part[kFewWaves][kFewF][64];
+    __shared__ float sums[kFewF * 16];
+    const ProductArgs &p = a.p;
+    const int waves = (int)blockDim.x / 64, wave = threadIdx.x / 64, lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
+    const int64_t token = EXPERTS ? blockIdx.y : 0;
+    const int m0 = (int)blockIdx.x * (EXPERTS ? a.rows_each : 16 * kFewF);
+    uint8_t *codes = lds, *scales = lds + (size_t)a.columns * p.blocks * 16;
+
+    // the values of this thread's first unit, then the weights of the wavefront's first run, then the other units
+    const int per_row = p.blocks * 4, units = a.columns * per_row;
+    auto load = [&](int u, float *x) {
+        const int row = u / per_row, k0 = (u - row * per_row) * 8;
+        load_unit<X>((const X *)a.X + (EXPERTS ? token * (a.x_per_pair ? a.k : 1) + row : row) * a.x_stride + k0, a.K - k0, a.x_wide, x);
+    };
+    float x0[8];
+    if ((int)threadIdx.x < units) load(threadIdx.x, x0);
+
+    const uint8_t *w_codes[kFewF], *w_scales[kFewF];
+#pragma unroll
+    for (int f = 0; f < kFewF; ++f) {
+        const int q = f * 16 + r;
+        int64_t row;
+        if (EXPERTS) {
+            const int j = min(q / a.rows_each, a.k - 1), e = a.experts_of[token * a.k + j];
+            row = (int64_t)(e >= 0 && e < p.experts ? e : 0) * p.M + min(m0 + q % a.rows_each, p.M - 1);
+        } else {
+            row = min(m0 + q, p.M - 1);
+        }
+        w_codes[f] = p.w_codes + row * p.blocks * 16;
+        w_scales[f] = p.w_scales + row * p.blocks;
+    }
+    i32x4 w[kFewF][4];
+    int sw[kFewF];
+    auto load_run = [&](int b) {
+        const bool in = b < p.blocks;                        // (four blocks are in or out together)
+#pragma unroll
+        for (int f = 0; f < kFewF; ++f) {
+#pragma unroll
+            for (int s = 0; s < 4; ++s) w[f][s] = in ? ((const i32x4 *)(w_codes[f] + (int64_t)b * 16))[s] : i32x4{};
+            sw[f] = in ? *(const int *)(w_scales[f] + b) : 0;
+        }
+    };
+    int b = wave * 16 + g * 4;
+    load_run(b);
+
+    for (int u = threadIdx.x; u < units; u += (int)blockDim.x) {  // (a row has whole blocks: a quad's lanes stay together)
+        float x[8];
+        if (u == (int)threadIdx.x) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = x0[i];
+        } else {
+            load(u, x);
+        }
+        uint32_t byte;
+        ((uint32_t *)codes)[u] = quantise_unit(x, byte);
+        if ((u & 3) == 0) scales[u >> 2] = (uint8_t)byte;
+    }
+    __syncthreads();
+
+    f32x4 acc[kFewF] = {};
+    const int column = min(r, a.columns - 1);
+    const uint8_t *xc = codes + (size_t)column * p.blocks * 16, *xs = scales + (size_t)column * p.blocks;
+    for (; b - g * 4 < p.blocks; b += waves * 16) {
+        const bool in = b < p.blocks;
+        i32x4 x[4];
+#pragma unroll
+        for (int s = 0; s < 4; ++s) x[s] = in ? ((const i32x4 *)(xc + (size_t)b * 16))[s] : i32x4{};
+        const int sx = in ? *(const int *)(xs + b) : 0;
+        i32x4 now[kFewF][4];
+        int sn[kFewF];
+#pragma unroll
+        for (int f = 0; f < kFewF; ++f) {
+#pragma unroll
+            for (int s = 0; s < 4; ++s) now[f][s] = w[f][s];
+            sn[f] = sw[f];
+        }
+        if (b - g * 4 + waves * 16 < p.blocks) load_run(b + waves * 16);
+#pragma unroll
+        for (int f = 0; f < kFewF; ++f) {
+            acc[f] = mfma_fp4<0>(now[f][0], x[0], acc[f], sn[f], sx);
+            acc[f] = mfma_fp4<1>(now[f][1], x[1], acc[f], sn[f], sx);
+            acc[f] = mfma_fp4<2>(now[f][2], x[2], acc[f], sn[f], sx);
+            acc[f] = mfma_fp4<3>(now[f][3], x[3], acc[f], sn[f], sx);
+        }
+    }
+#pragma unroll
+    for (int f = 0; f < kFewF; ++f) part[wave][f][lane] = acc[f];
+    __syncthreads();
+    for (int at = threadIdx.x; at < kFewF * 64; at += (int)blockDim.x) {
+        const int f = at / 64, l = at & 63;
+        f32x4 v = part[0][f][l];
+        for (int i = 1; i < waves; ++i) v += part[i][f][l];
+        if (!EXPERTS) {
+            if ((l & 15) < a.columns) store_outputs<T>(p, 0, l & 15, m0 + f * 16 + 4 * (l >> 4), v);
+        } else {
+            // every column has the token's row, or column j the row of its j-th pair
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int q = f * 16 + 4 * (l >> 4) + i;
+                if ((l & 15) == (a.x_per_pair ? q / a.rows_each : 0)) sums[q] = v[i];
+            }
+        }
+    }
+    if (!EXPERTS) return;
+    __syncthreads();
+    // row j rows_each + i is output m0 + i of the token's j-th expert
+    const int step = p.act == CL_ACT_GATED ? 2 : 1, i = (int)threadIdx.x * step, m = m0 + i;
+    if (i >= a.rows_each || m + step > p.M) return;
+    float total = 0.0f;
+    for (int j = 0; j < a.k; ++j) {
+        const int64_t pair = token * a.k + j;
+        const int e = a.experts_of[pair];
+        const bool routed = e >= 0 && e < p.experts;
+        float v = 0.0f;
+        if (routed) {
+            v = sums[j * a.rows_each + i];
+            if (p.bias) v += p.bias[(int64_t)e * p.M + m];
+            if (p.act == CL_ACT_GATED) {
+                float u = sums[j * a.rows_each + i + 1];
+                if (p.bias) u += p.bias[(int64_t)e * p.M + m + 1];
+                v = v / (1.0f + expf(-v)) * u;
+            } else if (p.act == CL_ACT_RELU) {
+                v = v < 0.0f ? 0.0f : v;
+            }
+        }
+        if (!a.weights) ((T *)p.Y)[pair * p.out_width + m / step] = (T)v;
+        else if (routed) total = fmaf(a.weights[pair], v, total);
+    }
+    if (a.weights) ((T *)p.Y)[token * p.out_width + m / step] = (T)total;
+}

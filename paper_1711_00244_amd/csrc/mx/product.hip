@@ -95,18 +95,18 @@ __device__ __forceinline__ void store_part(const ProductArgs &a, int split, int6
     if (m < a.M) *(f32x4 *)(a.part + ((int64_t)split * a.rows + row) * a.pitch + m) = v;
 }
 
-// A workgroup of eight wavefronts makes 16 outputs (blockIdx.x) of 16 NT columns (blockIdx.y).  The wavefronts share out the
+// A workgroup of up to sixteen wavefronts makes 16 outputs (blockIdx.x) of 16 NT columns (blockIdx.y).  The wavefronts share out the
 // row's runs of 16 blocks; of a run, a lane's group has four consecutive blocks - 64 bytes and one word of scales - which
 // are its 32 k of four matrix instructions (the order of k does not matter as long as both operands have the same).
 // Their sums meet in LDS and are added in the order of the wavefronts.
-constexpr int kRowsWaves = 8;
+constexpr int kRowsWaves = 16;
 
 template <int NT, class T> __global__ __launch_bounds__(kRowsWaves * 64) void mx_rows_kernel(ProductArgs a)
 {
     __shared__ f32x4 part[kRowsWaves][NT][64];
     Columns c;
     if (!columns_of<16 * NT>(a, a.tile0 + (int)blockIdx.y, c)) return;
-    const int wave = threadIdx.x / 64, lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
+    const int waves = (int)blockDim.x / 64, wave = threadIdx.x / 64, lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
     const int m0 = (int)blockIdx.x * 16;
     f32x4 acc[NT] = {};
     if (!a.order || c.expert < a.experts) {                  // (the pairs without an expert: zeros)
@@ -120,7 +120,7 @@ template <int NT, class T> __global__ __launch_bounds__(kRowsWaves * 64) void mx
             xc[t] = a.x_codes + x_row * a.blocks * 16;
             xs[t] = a.x_scales + x_row * a.blocks;
         }
-        for (int b = wave * 16 + g * 4; b - g * 4 < a.blocks; b += kRowsWaves * 16) {
+        for (int b = wave * 16 + g * 4; b - g * 4 < a.blocks; b += waves * 16) {
             const bool in = b < a.blocks;                    // (four blocks are in or out together)
             const int bb = in ? b : 0;
             i32x4 w[4];
@@ -143,18 +143,18 @@ template <int NT, class T> __global__ __launch_bounds__(kRowsWaves * 64) void mx
 #pragma unroll
     for (int t = 0; t < NT; ++t) part[wave][t][lane] = acc[t];
     __syncthreads();
-    for (int e = threadIdx.x; e < NT * 64; e += kRowsWaves * 64) {
+    for (int e = threadIdx.x; e < NT * 64; e += (int)blockDim.x) {
         const int t = e / 64, l = e & 63, n = t * 16 + (l & 15);
         if (n >= c.count) continue;
         f32x4 v = part[0][t][l];
-#pragma unroll
-        for (int w = 1; w < kRowsWaves; ++w) v += part[w][t][l];
+        for (int w = 1; w < waves; ++w) v += part[w][t][l];
         const int64_t y_row = a.order ? a.order[c.first + n] : c.first + n;
         if (a.part) store_part(a, 0, y_row, m0 + 4 * (l >> 4), v);
         else finish_outputs<T>(a, c.expert, y_row, m0 + 4 * (l >> 4), v);
     }
 }
 
+#include "few_kernel.hpp"
 #include "tile_kernel.hpp"
 
 // Y[t] = sum over j of weights[t][j] act(sum over the splits of a pair's parts + bias), both in order, of the pairs that have an
@@ -194,7 +194,9 @@ template <class T> __global__ __launch_bounds__(256) void mx_finish_kernel(Finis
 #pragma unroll
             for (int i = 0; i < 4; ++i) v[i] = v[i] < 0.0f ? 0.0f : v[i];
         }
-        sum += a.weights ? v * a.weights[pair] : v;
+        const float weight = a.weights ? a.weights[pair] : 1.0f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sum[i] = fmaf(weight, v[i], sum[i]);
     }
     const int n = a.act == CL_ACT_GATED ? 2 : 4, out = a.act == CL_ACT_GATED ? m / 2 : m;
     T *y = (T *)a.Y + t * a.out_width + out;
@@ -209,8 +211,8 @@ template <int BM, int BN, int WM, int WN, int D, class T> static int32_t launch_
     static LdsLimit seen;
     if (int32_t rc = allow_lds((const void *)kernel, C::kLds, seen)) return rc;
     const int64_t row_tiles = (a.M + BM - 1) / BM;
-    if (row_tiles * tiles > INT32_MAX) return fail(CL_EUNSUPPORTED, "a launch of %lld workgroups does not fit a grid", (long long)(row_tiles * tiles));
-    hipLaunchKernelGGL(kernel, dim3((unsigned)(row_tiles * tiles), (unsigned)a.splits), dim3(C::kThreads), C::kLds, st, a, (int)row_tiles);
+    if (row_tiles * tiles > INT32_MAX - 8) return fail(CL_EUNSUPPORTED, "a launch of %lld workgroups does not fit a grid", (long long)(row_tiles * tiles));
+    hipLaunchKernelGGL(kernel, dim3((unsigned)round_up(row_tiles * tiles, 8), (unsigned)a.splits), dim3(C::kThreads), C::kLds, st, a, (int)row_tiles);
     MX_HIP_TRY(hipGetLastError());
     return CL_OK;
 }
@@ -218,7 +220,7 @@ template <int BM, int BN, int WM, int WN, int D, class T> static int32_t launch_
 // ------------------------------------------------------------------------- //
 // which kernel
 // ------------------------------------------------------------------------- //
-enum Form { kRows, kTile64, kTile128, kTile256x128, kTile256 };
+enum Form { kFew, kRows, kTile64, kTile128, kTile256x128, kTile256 };
 
 struct Choice {
     Form form;
@@ -230,7 +232,7 @@ struct Choice {
 // quarter of each): a start (launch, first loads, last stores), and per step of 128 k what a workgroup takes alone on its compute
 // unit, or its share of a full one where the launch has more workgroups than the chip has compute units.
 struct Price { int bm, bn, width; float start, alone, shared; };
-constexpr Price kPrices[] = {{16, 64, 1, 3.0f, 0.0f, 0.0f}, {64, 64, 1, 3.5f, 0.15f, 0.18f}, {128, 128, 2, 4.5f, 0.50f, 0.40f}, {256, 128, 2, 6.0f, 0.74f, 0.74f},
+constexpr Price kPrices[] = {{16, 4, 0, 0, 0, 0}, {16, 64, 1, 0, 0, 0}, {64, 64, 1, 3.5f, 0.15f, 0.18f}, {128, 128, 2, 4.5f, 0.50f, 0.40f}, {256, 128, 2, 6.0f, 0.74f, 0.74f},
                              {256, 256, 3, 8.0f, 0.95f, 1.17f}};
 constexpr int kCus = 256;
 
@@ -240,9 +242,9 @@ static Choice choose(int M, int blocks, int64_t rows, int64_t runs, bool part)
 {
     const int steps = blocks / 4;
     runs = std::min(runs, rows);
-    Choice best{kRows, 1, 1};
-    if (steps < 4) return best;                              // (the tile kernels read scales four steps at a time)
-    if (rows <= 16 * runs) return best;
+    const Choice narrow{kRows, 0, 1};                        // columns sixteen at a time
+    if (steps < 4 || rows <= 16 * runs) return narrow;       // (the tile kernels read scales four steps at a time)
+    Choice best = narrow;
     float least = 1e30f;
     for (int f = kTile64; f <= kTile256; ++f) {
         const Price &p = kPrices[f];
@@ -259,6 +261,14 @@ static Choice choose(int M, int blocks, int64_t rows, int64_t runs, bool part)
         }
     }
     return best;
+}
+
+// Wavefronts that share out the runs of 16 blocks of a row: as many rounds as sixteen would need, and no more than that takes.
+// (The same in both kernels that do: the same sums, bit for bit.)
+static int run_waves(int blocks)
+{
+    const int runs = (blocks + 15) / 16, rounds = (runs + kRowsWaves - 1) / kRowsWaves;
+    return (runs + rounds - 1) / rounds;
 }
 
 // The tiles of a product: rows of X in order, or what the lists have.
@@ -281,10 +291,44 @@ template <class T> static int32_t launch_product(ProductArgs a, const Choice &c,
     // (a grid is at most 65535 high: taller ones go in pieces)
     for (int64_t t0 = 0; t0 < tiles; t0 += 65535) {
         a.tile0 = (int)t0;
-        hipLaunchKernelGGL((mx_rows_kernel<4, T>), dim3((unsigned)((a.M + 15) / 16), (unsigned)std::min<int64_t>(tiles - t0, 65535)), dim3(kRowsWaves * 64), 0, st, a);
+        hipLaunchKernelGGL((mx_rows_kernel<1, T>), dim3((unsigned)((a.M + 15) / 16), (unsigned)std::min<int64_t>(tiles - t0, 65535)), dim3(run_waves(a.blocks) * 64), 0, st, a);
         MX_HIP_TRY(hipGetLastError());
     }
     return CL_OK;
+}
+
+static bool wide_rows(const ProductArgs &a, int32_t y_type) { return a.out_width % 4 == 0 && aligned(a.Y, 4 * type_bytes(y_type)); }
+
+static int wide_input(const cl_mx_input &X) { return aligned(X.d_X, 16) && X.stride * (int64_t)type_bytes(X.type) % 16 == 0; }
+
+// Whether few_kernel takes a call.  One matrix: up to four rows.  Experts: where reading a matrix once for every token that
+// is sent to it, and not once, costs less than the launches that sort the tokens by expert.
+static bool few_fc(int blocks, int batch, int32_t x_type)
+{
+    return x_type != CL_MX4 && batch <= kFewColumns && few_lds(blocks, batch) <= kFewLds;
+}
+static bool few_experts(int blocks, int M, int32_t x_type, int experts, const cl_mx_experts_call &call)
+{
+    const int64_t pairs = (int64_t)call.tokens * call.k, again = pairs - std::min<int64_t>(pairs, experts);
+    return x_type != CL_MX4 && !call.d_lists && pairs <= 1024 && call.k <= 16 && again * M * blocks * 17 <= (24 << 20) &&
+           few_lds(blocks, call.x_per_pair ? call.k : 1) <= kFewLds;
+}
+
+static int32_t launch_few(const FewArgs &a, int32_t x_type, int32_t y_type, bool experts, dim3 grid, hipStream_t st)
+{
+    const size_t lds = few_lds(a.p.blocks, a.columns);
+    return with_type(x_type, [&](auto x) -> int32_t {
+        return with_type(y_type, [&](auto y) -> int32_t {
+            using X = decltype(x);
+            using Y = decltype(y);
+            auto kernel = experts ? mx_few_kernel<X, Y, true> : mx_few_kernel<X, Y, false>;
+            static LdsLimit seen[2];
+            if (int32_t rc = allow_lds((const void *)kernel, kFewLds, seen[experts])) return rc;
+            hipLaunchKernelGGL(kernel, grid, dim3(run_waves(a.p.blocks) * 64), lds, st, a);
+            MX_HIP_TRY(hipGetLastError());
+            return CL_OK;
+        });
+    });
 }
 
 // The product, and what is left to do where it gives partial sums: rows of Y (k pairs to each) from a.part.
@@ -292,7 +336,7 @@ static int32_t run_product(ProductArgs a, const Choice &c, const ExpertLists *L,
                            const float *weights, hipStream_t st)
 {
     a.Y = Y;
-    a.y_wide = a.out_width % 4 == 0 && aligned(Y, 4 * type_bytes(y_type));
+    a.y_wide = wide_rows(a, y_type);
     if (!a.part) return with_type(y_type, [&](auto t) { return launch_product<decltype(t)>(a, c, L, st); });
     if (int32_t rc = launch_product<float>(a, c, L, st)) return rc;
     const FinishArgs f{a.part, a.bias, weights, experts_of, Y, (int64_t)a.rows * a.pitch, tokens, k, experts_of ? a.experts : 1, a.M, a.pitch, c.splits, a.act, a.out_width};
@@ -408,7 +452,7 @@ extern "C" int32_t cl_mx_fc_workspace_bytes(const cl_mx_matrix *W, int32_t batch
     if (!out) return fail(CL_EINVAL, "null pointer");
     if (int32_t rc = check_forward(W, x_type, CL_F32, CL_ACT_NONE)) return rc;
     if (batch < 0) return fail(CL_EINVAL, "batch of %d", (int)batch);
-    *out = fc_scratch(choose(W->rows, row_blocks(W->K), batch, 1, false), W->rows, W->K, x_type, batch).bytes;
+    *out = few_fc(row_blocks(W->K), batch, x_type) ? 0 : fc_scratch(choose(W->rows, row_blocks(W->K), batch, 1, false), W->rows, W->K, x_type, batch).bytes;
     clear_error();
     return CL_OK;
 }
@@ -421,22 +465,30 @@ extern "C" int32_t cl_mx_fc_forward(const cl_mx_matrix *W, const cl_mx_input *X,
     if (batch < 0) return fail(CL_EINVAL, "batch of %d", (int)batch);
     if (batch == 0) return CL_OK;
     if (int32_t rc = check_pointers(W, X, d_Y, batch)) return rc;
-    const Choice c = choose(W->rows, row_blocks(W->K), batch, 1, false);
-    const Scratch s = fc_scratch(c, W->rows, W->K, X->type, batch);
-    if (int32_t rc = check_scratch(s, d_workspace, workspace_bytes)) return rc;
     hipStream_t st = (hipStream_t)stream;
     ProductArgs a{};
-    if (int32_t rc = quantised_input(a, X, batch, W->K, s, d_workspace, st)) return rc;
     a.w_codes = (const uint8_t *)W->d_codes;
     a.w_scales = (const uint8_t *)W->d_scales;
     a.bias = d_bias;
-    a.part = c.splits > 1 ? (float *)((uint8_t *)d_workspace + s.pairs) : nullptr;
-    a.pitch = (int)round_up(W->rows, 4);
     a.blocks = row_blocks(W->K);
     a.M = W->rows;
     a.rows = batch;
     a.act = act;
     a.out_width = act == CL_ACT_GATED ? W->rows / 2 : W->rows;
+    if (few_fc(a.blocks, batch, X->type)) {
+        a.Y = d_Y;
+        a.y_wide = wide_rows(a, y_type);
+        const FewArgs f{a, X->d_X, X->stride, W->K, batch, nullptr, nullptr, 1, 0, 0, wide_input(*X)};
+        if (int32_t rc = launch_few(f, X->type, y_type, false, dim3((unsigned)((a.M + 15) / 16)), st)) return rc;
+        clear_error();
+        return CL_OK;
+    }
+    const Choice c = choose(W->rows, a.blocks, batch, 1, false);
+    const Scratch s = fc_scratch(c, W->rows, W->K, X->type, batch);
+    if (int32_t rc = check_scratch(s, d_workspace, workspace_bytes)) return rc;
+    if (int32_t rc = quantised_input(a, X, batch, W->K, s, d_workspace, st)) return rc;
+    a.part = c.splits > 1 ? (float *)((uint8_t *)d_workspace + s.pairs) : nullptr;
+    a.pitch = (int)round_up(W->rows, 4);
     if (int32_t rc = run_product(a, c, nullptr, d_Y, y_type, batch, 1, nullptr, nullptr, st)) return rc;
     clear_error();
     return CL_OK;
@@ -446,7 +498,7 @@ static int32_t check_experts(const cl_mx_matrix *W, int32_t experts, int32_t tok
 {
     if (experts < 1 || tokens < 0 || k < 1) return fail(CL_EINVAL, "%d tokens, %d of %d experts", (int)tokens, (int)k, (int)experts);
     if (experts > CL_ROUTE_MAX_EXPERTS) return fail(CL_EUNSUPPORTED, "%d experts: at most %d", (int)experts, CL_ROUTE_MAX_EXPERTS);
-    if ((int64_t)tokens * k > (int64_t)INT32_MAX - kListChunk) return fail(CL_EUNSUPPORTED, "more than 2^31 pairs of token and expert");
+    if ((int64_t)tokens * k > CL_EXPERTS_MAX_PAIRS) return fail(CL_EUNSUPPORTED, "more than 2^30 pairs of token and expert");
     return CL_OK;
 }
 
@@ -455,7 +507,7 @@ extern "C" int32_t cl_mx_experts_workspace_bytes(const cl_mx_matrix *W, int32_t 
     if (!out || !call) return fail(CL_EINVAL, "null pointer");
     if (int32_t rc = check_forward(W, x_type, CL_F32, call->act)) return rc;
     if (int32_t rc = check_experts(W, experts, call->tokens, call->k)) return rc;
-    *out = experts_scratch(choose_experts(W->rows, W->K, experts, *call), W->rows, W->K, x_type, experts, *call).bytes;
+    *out = few_experts(row_blocks(W->K), W->rows, x_type, experts, *call) ? 0 : experts_scratch(choose_experts(W->rows, W->K, experts, *call), W->rows, W->K, x_type, experts, *call).bytes;
     clear_error();
     return CL_OK;
 }
@@ -472,16 +524,8 @@ extern "C" int32_t cl_mx_experts_forward(const cl_mx_matrix *W, int32_t experts,
     if (int32_t rc = check_pointers(W, X, d_Y, x_rows)) return rc;
     if (!call->d_experts) return fail(CL_EINVAL, "null pointer");
     if (call->d_lists && !aligned(call->d_lists, 256)) return fail(CL_EINVAL, "lists must be 256-byte aligned");
-    const bool join = call->d_weights != nullptr;
-    const Choice c = choose_experts(W->rows, W->K, experts, *call);
-    const Scratch s = experts_scratch(c, W->rows, W->K, X->type, experts, *call);
-    if (int32_t rc = check_scratch(s, d_workspace, workspace_bytes)) return rc;
     hipStream_t st = (hipStream_t)stream;
     ProductArgs a{};
-    const ExpertLists L = expert_lists_at(call->d_lists ? const_cast<void *>(call->d_lists) : (uint8_t *)d_workspace + s.lists, tokens, k, experts);
-    if (!call->d_lists)
-        if (int32_t rc = launch_expert_lists(call->d_experts, tokens, k, experts, L, st)) return rc;
-    if (int32_t rc = quantised_input(a, X, x_rows, W->K, s, d_workspace, st)) return rc;
     a.w_codes = (const uint8_t *)W->d_codes;
     a.w_scales = (const uint8_t *)W->d_scales;
     a.bias = call->d_bias;
@@ -491,6 +535,22 @@ extern "C" int32_t cl_mx_experts_forward(const cl_mx_matrix *W, int32_t experts,
     a.experts = experts;
     a.act = call->act;
     a.out_width = call->act == CL_ACT_GATED ? W->rows / 2 : W->rows;
+    if (few_experts(a.blocks, a.M, X->type, experts, *call)) {
+        a.Y = d_Y;
+        const int rows_each = 32 / k / 2 * 2;                // (even: a gated product's rows come in pairs)
+        const FewArgs f{a, X->d_X, X->stride, W->K, call->x_per_pair ? k : 1, call->d_experts, call->d_weights, k, rows_each, call->x_per_pair, wide_input(*X)};
+        if (int32_t rc = launch_few(f, X->type, y_type, true, dim3((unsigned)((a.M + rows_each - 1) / rows_each), (unsigned)tokens), st)) return rc;
+        clear_error();
+        return CL_OK;
+    }
+    const bool join = call->d_weights != nullptr;
+    const Choice c = choose_experts(W->rows, W->K, experts, *call);
+    const Scratch s = experts_scratch(c, W->rows, W->K, X->type, experts, *call);
+    if (int32_t rc = check_scratch(s, d_workspace, workspace_bytes)) return rc;
+    const ExpertLists L = expert_lists_at(call->d_lists ? const_cast<void *>(call->d_lists) : (uint8_t *)d_workspace + s.lists, tokens, k, experts);
+    if (!call->d_lists)
+        if (int32_t rc = launch_expert_lists(call->d_experts, tokens, k, experts, L, st)) return rc;
+    if (int32_t rc = quantised_input(a, X, x_rows, W->K, s, d_workspace, st)) return rc;
     a.x_div = call->x_per_pair ? 1 : k;
     a.order = L.order;
     a.offsets = L.offsets;

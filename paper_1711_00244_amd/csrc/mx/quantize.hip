@@ -21,24 +21,7 @@ static Div make_div(uint32_t d)
     return Div{(uint32_t)((((1ull << s) - d) << 32) / d + 1), s > 0 ? 1u : 0u, s > 0 ? s - 1 : 0u, d};
 }
 
-// Values of a unit (eight consecutive elements of a row), four lanes to a block.
-constexpr int kUnit = 8;
-
-template <class T, bool ALIGNED> __device__ __forceinline__ void load_unit(const T *p, int left, float *x)
-{
-    if (ALIGNED && left >= kUnit) {
-        T v[kUnit];
-        __builtin_memcpy(v, __builtin_assume_aligned(p, 16), sizeof v);
-#pragma unroll
-        for (int i = 0; i < kUnit; ++i) x[i] = to_float(v[i]);
-    } else {
-#pragma unroll
-        for (int i = 0; i < kUnit; ++i) x[i] = i < left ? to_float(p[i]) : 0.0f;
-    }
-}
-
-// A unit per lane.  The maximum of a block is taken on the bits of the magnitudes (in order for finite values, Inf and NaN
-// above them), over four lanes by two exchanges within the quad.
+// A unit per lane.
 template <class T, bool ALIGNED>
 __global__ __launch_bounds__(256) void mx_quantize_kernel(const T *__restrict__ X, int64_t stride, uint32_t units, Div per_row, int K,
                                                           uint32_t *__restrict__ codes, uint8_t *__restrict__ scales)
@@ -48,22 +31,9 @@ __global__ __launch_bounds__(256) void mx_quantize_kernel(const T *__restrict__ 
     const uint32_t row = per_row.quotient(u);
     const int k0 = (int)(u - row * per_row.d) * kUnit;
     float x[kUnit];
-    load_unit<T, ALIGNED>(X + (int64_t)row * stride + k0, K - k0, x);
-    uint32_t top = 0;
-#pragma unroll
-    for (int i = 0; i < kUnit; ++i) top = max(top, __float_as_uint(x[i]) & 0x7fffffffu);
-    top = max(top, (uint32_t)__builtin_amdgcn_mov_dpp((int)top, 0xB1, 0xF, 0xF, true));      // lanes 1 0 3 2 of a quad
-    top = max(top, (uint32_t)__builtin_amdgcn_mov_dpp((int)top, 0x4E, 0xF, 0xF, true));      // lanes 2 3 0 1
-    const uint32_t byte = scale_byte(top);
-    const float inv = scale_inverse(byte);
-    uint32_t c = 0;
-    // (the instruction rounds to nearest, ties to even, and takes what is above 6 to 6; scaling beforehand is exact but for
-    // values that round to zero either way)
-    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[0] * inv, x[1] * inv, 1.0f, 0);
-    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[2] * inv, x[3] * inv, 1.0f, 1);
-    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[4] * inv, x[5] * inv, 1.0f, 2);
-    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[6] * inv, x[7] * inv, 1.0f, 3);
-    codes[u] = byte == kScaleNaN ? 0u : c;                   // (Inf * 0 is no code)
+    load_unit<T>(X + (int64_t)row * stride + k0, K - k0, ALIGNED, x);
+    uint32_t byte;
+    codes[u] = quantise_unit(x, byte);
     if ((u & 3) == 0) scales[u >> 2] = (uint8_t)byte;
 }
 

@@ -141,10 +141,14 @@ template <class T, int L, int C> static int32_t launch_route(const RouteArgs &a,
 // ------------------------------------------------------------------------- //
 // the lists: a stable counting sort of the pairs (token, j) by their expert, pairs without one last
 // ------------------------------------------------------------------------- //
+// Pairs of one workgroup: a multiple of 4096 that makes at most 256 workgroups, each of which adds the others' counts up.
+constexpr int kListThreads = 1024, kListWaves = kListThreads / 64;
+static int64_t list_chunk(int64_t pairs) { return std::max<int64_t>(1, (pairs + 4096 * 256 - 1) / (4096 * 256)) * 4096; }
+
 ExpertLists expert_lists_at(void *base, int32_t tokens, int32_t k, int32_t experts)
 {
     ExpertLists L;
-    const int64_t pairs = (int64_t)tokens * k, chunks = (pairs + kListChunk - 1) / kListChunk;
+    const int64_t pairs = (int64_t)tokens * k, chunk = list_chunk(pairs), chunks = (pairs + chunk - 1) / chunk;
     size_t at = 0;
     auto take = [&](size_t bytes) { char *p = (char *)base + at; at += round_up(bytes, 256); return p; };
     L.offsets = (int32_t *)take(((size_t)experts + 2) * 4);
@@ -154,130 +158,131 @@ ExpertLists expert_lists_at(void *base, int32_t tokens, int32_t k, int32_t exper
         L.max_tiles[w] = pairs / kTileWidth[w] + std::min<int64_t>(pairs, (int64_t)experts + 1);
         L.tiles[w] = (int2 *)take((size_t)L.max_tiles[w] * sizeof(int2));
     }
-    L.chunk_counts = (int32_t *)take((size_t)chunks * ((size_t)experts + 1) * 4);
+    L.chunk_counts = (int32_t *)take(chunks > 1 ? (size_t)chunks * ((size_t)experts + 1) * 4 : 0);
     L.bytes = at;
     return L;
 }
 
 __device__ __forceinline__ int bucket_of(int e, int experts) { return e >= 0 && e < experts ? e : experts; }
 
-__global__ __launch_bounds__(256) void lists_count_kernel(const int32_t *__restrict__ experts_of, int pairs, int experts, int32_t *counts)
+__global__ __launch_bounds__(kListThreads) void lists_count_kernel(const int32_t *__restrict__ experts_of, int pairs, int chunk, int experts, int32_t *counts)
 {
     __shared__ int32_t n[CL_ROUTE_MAX_EXPERTS + 1];
-    for (int b = threadIdx.x; b <= experts; b += 256) n[b] = 0;
+    for (int b = threadIdx.x; b <= experts; b += kListThreads) n[b] = 0;
     __syncthreads();
-    const int64_t p0 = (int64_t)blockIdx.x * kListChunk;
-    for (int i = threadIdx.x; i < kListChunk; i += 256)
-        if (p0 + i < pairs) atomicAdd(&n[bucket_of(experts_of[p0 + i], experts)], 1);
+    const int64_t p0 = (int64_t)blockIdx.x * chunk, p1 = min((int64_t)pairs, p0 + chunk);
+    for (int64_t p = p0 + threadIdx.x; p < p1; p += kListThreads) atomicAdd(&n[bucket_of(experts_of[p], experts)], 1);
     __syncthreads();
-    for (int b = threadIdx.x; b <= experts; b += 256) counts[(int64_t)blockIdx.x * (experts + 1) + b] = n[b];
+    for (int b = threadIdx.x; b <= experts; b += kListThreads) counts[(int64_t)blockIdx.x * (experts + 1) + b] = n[b];
 }
 
-// Exclusive sums of v over 1024 threads, and the total.
-__device__ __forceinline__ int exclusive_sum(int v, int *s, int &total)
+// Every workgroup finds where its own pairs of each expert go (the first: also the tiles), and puts them there.  Wavefront w has the
+// w-th sixteenth of the chunk.
+__global__ __launch_bounds__(kListThreads) void lists_place_kernel(ExpertLists L, const int32_t *__restrict__ experts_of, int pairs, int chunk, int chunks, int experts)
 {
-    const int t = threadIdx.x;
+    extern __shared__ int32_t list_lds[];
+    const int buckets = experts + 1, wave = (int)threadIdx.x / 64, lane = (int)threadIdx.x & 63;
+    int32_t *at = list_lds;                                  // [wavefront][bucket]: how many, then where the next goes
+    int32_t *starts = at + kListWaves * buckets;             // [1 + kTileWidths][bucket + 1]: first pair, first tile of each width
+    __shared__ int32_t wave_sum[kListWaves][1 + kTileWidths];
+    for (int i = threadIdx.x; i < kListWaves * buckets; i += kListThreads) at[i] = 0;
     __syncthreads();
-    s[t] = v;
+    const int64_t first = (int64_t)blockIdx.x * chunk + (int64_t)wave * (chunk / kListWaves);
+    const int64_t end = min((int64_t)pairs, first + chunk / kListWaves);
+    for (int64_t p = first + lane; p < end; p += 64) atomicAdd(&at[wave * buckets + bucket_of(experts_of[p], experts)], 1);
     __syncthreads();
-    for (int d = 1; d < 1024; d *= 2) {
-        const int o = t >= d ? s[t - d] : 0;
-        __syncthreads();
-        s[t] += o;
-        __syncthreads();
-    }
-    total = s[1023];
-    return s[t] - v;
-}
-
-// One workgroup: where each expert's pairs start, how many of them the chunks before a chunk have, and the tiles.  A thread
-// takes two buckets (experts + 1 <= 2048).
-__global__ __launch_bounds__(1024) void lists_scan_kernel(ExpertLists L, int chunks, int experts)
-{
-    __shared__ int s[1024];
+    // a thread has two buckets: all pairs of each, and those of earlier chunks
     const int b0 = 2 * (int)threadIdx.x;
-    int n[2] = {0, 0};
-    for (int i = 0; i < 2; ++i)
-        if (b0 + i <= experts)
+    int all[2] = {0, 0}, before[2] = {0, 0};
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int b = b0 + i;
+        if (b >= buckets) continue;
+        if (chunks > 1) {
             for (int c = 0; c < chunks; ++c) {
-                int32_t *p = L.chunk_counts + (int64_t)c * (experts + 1) + b0 + i;
-                const int v = *p;
-                *p = n[i];
-                n[i] += v;
+                const int n = L.chunk_counts[(int64_t)c * buckets + b];
+                all[i] += n;
+                before[i] += c < (int)blockIdx.x ? n : 0;
             }
-    int total;
-    int start[2];
-    start[0] = exclusive_sum(n[0] + n[1], s, total);
-    start[1] = start[0] + n[0];
-    for (int i = 0; i < 2; ++i)
-        if (b0 + i <= experts) L.offsets[b0 + i] = start[i];
-    if (threadIdx.x == 0) L.offsets[experts + 1] = total;
-    for (int w = 0; w < kTileWidths; ++w) {
-        const int width = kTileWidth[w];
-        const int t0 = (n[0] + width - 1) / width, t1 = (n[1] + width - 1) / width;
-        int at = exclusive_sum(t0 + t1, s, total);
-        if (threadIdx.x == 0) L.tile_count[w] = total;
-        for (int i = 0; i < 2; ++i)
-            for (int j = 0; j < (i ? t1 : t0); ++j) L.tiles[w][at++] = make_int2(b0 + i, start[i] + j * width);
-    }
-}
-
-__global__ __launch_bounds__(256) void lists_scatter_kernel(ExpertLists L, const int32_t *__restrict__ experts_of, int pairs, int experts)
-{
-    __shared__ int32_t at[4][CL_ROUTE_MAX_EXPERTS + 1];
-    const int wave = threadIdx.x / 64, lane = threadIdx.x & 63;
-    for (int b = threadIdx.x; b < 4 * (CL_ROUTE_MAX_EXPERTS + 1); b += 256) at[0][b] = 0;
-    __syncthreads();
-    // a wavefront has a quarter of the chunk, 64 pairs at a time
-    const int64_t p0 = (int64_t)blockIdx.x * kListChunk + wave * (kListChunk / 4) + lane;
-    int bucket[kListChunk / 256];
-    for (int i = 0; i < kListChunk / 256; ++i) {
-        const int64_t p = p0 + i * 64;
-        bucket[i] = p < pairs ? bucket_of(experts_of[p], experts) : -1;
-        if (bucket[i] >= 0) atomicAdd(&at[wave][bucket[i]], 1);
-    }
-    __syncthreads();
-    for (int b = threadIdx.x; b <= experts; b += 256) {
-        int sum = L.offsets[b] + L.chunk_counts[(int64_t)blockIdx.x * (experts + 1) + b];
-        for (int w = 0; w < 4; ++w) {
-            const int n = at[w][b];
-            at[w][b] = sum;
-            sum += n;
+        } else {
+            for (int w = 0; w < kListWaves; ++w) all[i] += at[w * buckets + b];
         }
     }
+    // exclusive sums over the buckets of the pairs and of the tiles of each width
+    int sum[1 + kTileWidths], mine[1 + kTileWidths];
+#pragma unroll
+    for (int v = 0; v <= kTileWidths; ++v) {
+        const int width = v ? kTileWidth[v ? v - 1 : 0] : 1;
+        mine[v] = (all[0] + width - 1) / width + (all[1] + width - 1) / width;
+        sum[v] = mine[v];
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) {
+            const int o = __shfl_up(sum[v], d);
+            sum[v] += lane >= d ? o : 0;
+        }
+        if (lane == 63) wave_sum[wave][v] = sum[v];
+    }
     __syncthreads();
-    for (int i = 0; i < kListChunk / 256; ++i) {
-        const int b = bucket[i];
+#pragma unroll
+    for (int v = 0; v <= kTileWidths; ++v) {
+        const int width = v ? kTileWidth[v ? v - 1 : 0] : 1;
+        int start = sum[v] - mine[v];
+        for (int w = 0; w < wave; ++w) start += wave_sum[w][v];
+        if (b0 <= buckets) starts[v * (buckets + 1) + b0] = start;
+        if (b0 + 1 <= buckets) starts[v * (buckets + 1) + b0 + 1] = start + (all[0] + width - 1) / width;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int b = b0 + i;
+        if (b >= buckets) continue;
+        int to = starts[b] + before[i];
+        for (int w = 0; w < kListWaves; ++w) {
+            const int n = at[w * buckets + b];
+            at[w * buckets + b] = to;
+            to += n;
+        }
+    }
+    if (blockIdx.x == 0) {
+        for (int b = threadIdx.x; b <= buckets; b += kListThreads) L.offsets[b] = starts[b];
+        if (threadIdx.x < kTileWidths) L.tile_count[threadIdx.x] = starts[(threadIdx.x + 1) * (buckets + 1) + buckets];
+        for (int b = wave; b < buckets; b += kListWaves)
+#pragma unroll
+            for (int v = 1; v <= kTileWidths; ++v) {
+                const int t0 = starts[v * (buckets + 1) + b], t1 = starts[v * (buckets + 1) + b + 1];
+                for (int t = t0 + lane; t < t1; t += 64) L.tiles[v - 1][t] = make_int2(b, starts[b] + (t - t0) * kTileWidth[v - 1]);
+            }
+    }
+    __syncthreads();
+    for (int64_t p0 = first; p0 < end; p0 += 64) {
+        const int64_t p = p0 + lane;
+        const int b = p < end ? bucket_of(experts_of[p], experts) : -1;
         // the lanes with the same expert, by its bits
         uint64_t same = __ballot(b >= 0);
         for (int bit = 0; bit < 11; ++bit) {
             const uint64_t set = __ballot(b >> bit & 1);
             same &= b >> bit & 1 ? set : ~set;
         }
-        if (b >= 0) {
-            const int rank = __popcll(same & ((1ull << lane) - 1));
-            const int to = at[wave][b] + rank;
-            L.order[to] = (int32_t)(p0 + i * 64);
-        }
+        if (b >= 0) L.order[at[wave * buckets + b] + __popcll(same & ((1ull << lane) - 1))] = (int32_t)p;
         __builtin_amdgcn_wave_barrier();
-        if (b >= 0 && (same >> lane) == 1) at[wave][b] += __popcll(same);        // the highest of them
+        if (b >= 0 && (same >> lane) == 1) at[wave * buckets + b] += __popcll(same);      // the highest of them
         __builtin_amdgcn_wave_barrier();
     }
 }
 
 int32_t launch_expert_lists(const int32_t *experts_of, int32_t tokens, int32_t k, int32_t experts, const ExpertLists &L, hipStream_t st)
 {
-    const int pairs = tokens * k, chunks = (pairs + kListChunk - 1) / kListChunk;
-    if (chunks) {
-        hipLaunchKernelGGL(lists_count_kernel, dim3((unsigned)chunks), dim3(256), 0, st, experts_of, pairs, experts, L.chunk_counts);
+    const int pairs = tokens * k, chunk = (int)list_chunk(pairs), chunks = std::max(1, (int)(((int64_t)pairs + chunk - 1) / chunk));
+    if (chunks > 1) {
+        hipLaunchKernelGGL(lists_count_kernel, dim3((unsigned)chunks), dim3(kListThreads), 0, st, experts_of, pairs, chunk, experts, L.chunk_counts);
         MX_HIP_TRY(hipGetLastError());
     }
-    hipLaunchKernelGGL(lists_scan_kernel, dim3(1), dim3(1024), 0, st, L, chunks, experts);
+    const size_t lds = ((size_t)kListWaves * (experts + 1) + (1 + kTileWidths) * ((size_t)experts + 2)) * 4;
+    static LdsLimit seen;
+    if (lds > 32768)
+        if (int32_t rc = allow_lds((const void *)lists_place_kernel, ((size_t)kListWaves * (CL_ROUTE_MAX_EXPERTS + 1) + (1 + kTileWidths) * (CL_ROUTE_MAX_EXPERTS + 2)) * 4, seen)) return rc;
+    hipLaunchKernelGGL(lists_place_kernel, dim3((unsigned)chunks), dim3(kListThreads), lds, st, L, experts_of, pairs, chunk, chunks, experts);
     MX_HIP_TRY(hipGetLastError());
-    if (chunks) {
-        hipLaunchKernelGGL(lists_scatter_kernel, dim3((unsigned)chunks), dim3(256), 0, st, L, experts_of, pairs, experts);
-        MX_HIP_TRY(hipGetLastError());
-    }
     return CL_OK;
 }
 
@@ -324,7 +329,7 @@ static int32_t check_lists(int32_t tokens, int32_t k, int32_t experts)
 {
     if (tokens < 0 || k < 1 || experts < 1) return fail(CL_EINVAL, "bad lists: %d tokens, %d of %d experts", (int)tokens, (int)k, (int)experts);
     if (experts > CL_ROUTE_MAX_EXPERTS) return fail(CL_EUNSUPPORTED, "%d experts: at most %d", (int)experts, CL_ROUTE_MAX_EXPERTS);
-    if ((int64_t)tokens * k > (int64_t)INT32_MAX - kListChunk) return fail(CL_EUNSUPPORTED, "more than 2^31 pairs of token and expert");
+    if ((int64_t)tokens * k > CL_EXPERTS_MAX_PAIRS) return fail(CL_EUNSUPPORTED, "more than 2^30 pairs of token and expert");
     return CL_OK;
 }
 

@@ -23,20 +23,19 @@ template <int BM, int BN, int WM, int WN, int D> struct Tile {
     static constexpr int kScaleLoads = (BM + BN) / 64;       // of the workgroup and four steps; wavefronts beyond that number repeat the last
     static constexpr int kScaleShare = (kScaleLoads + kWaves - 1) / kWaves;
     static constexpr int kBuffer = (BM + BN) * 64;
-    static constexpr int kScales = D * kBuffer;              // where the scales start: two buffers of four steps
+    static constexpr int kScales = D * kBuffer;              // where the scales start: three buffers of four steps
     static constexpr int kScaleBuffer = (BM + BN) * 16;
-    static constexpr int kLds = kScales + 2 * kScaleBuffer;
+    static constexpr int kLds = kScales + 3 * kScaleBuffer;
     static_assert(BM % (WM * 16) == 0 && BN % (WN * 16) == 0 && TI >= TJ, "");
     static_assert((BM + BN) / 16 % kWaves == 0 && BM % 64 == 0 && BN % 64 == 0, "");
-    // loads of a wavefront that may be on their way when step s (of four) begins: those asked for in the D - 3 steps before, but
-    // when the last of four begins, of those after the scales of the next four
+    // loads of a wavefront that may be on their way when step s (of four) begins: those asked for in the D - 3 steps before
     static constexpr int on_their_way(int s)
     {
         int n = 0;
-        for (int i = 1; i <= (s == 3 && D > 5 ? 2 : D - 3); ++i) n += kCodeLoads + ((s + 8 - i) % 4 == 0 ? kScaleShare : 0);
+        for (int i = 1; i <= D - 3; ++i) n += kCodeLoads + ((s + 8 - i) % 4 == 0 ? kScaleShare : 0);
         return n;
     }
-    static_assert(D >= 3 && D <= 8 && (D - 3) * kCodeLoads + kScaleShare < 16, "");       // (the count that a wait names)
+    static_assert(BM + BN <= kThreads && D >= 3 && D <= 7 && (D - 3) * kCodeLoads + kScaleShare < 16 && (D - 2) * kCodeLoads < 16, "");       // (the count that a wait names)
 };
 
 template <int BM, int BN, int WM, int WN, int D, class T>
@@ -49,10 +48,25 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void mx_tile_kernel(ProductArgs a,
     typedef const __attribute__((address_space(1))) void *global_ptr;
     const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = (int)(threadIdx.x & 63), r = lane & 15, g = lane >> 4;
 
-    const int tile = (int)blockIdx.x;
-    const int m0 = (tile % row_tiles) * BM;
+    int column, m0;
+    if (BM * BN >= 128 * 128 && !a.order) {
+        // Workgroups go to the eight dies in turn.  Each die takes a run of tiles, four columns of tiles at a time, so that
+        // what it has in flight shares rows of W and of X in its cache.  (4096 x 8192 x 4096: 121 us, tiles in order 125.  With
+        // smaller tiles, and with the short columns of experts, the order as it is is 2 % faster.)
+        const int columns = (a.rows + BN - 1) / BN, tiles = columns * row_tiles;
+        const int per = tiles / 8, more = tiles % 8, die = (int)blockIdx.x % 8, i = (int)blockIdx.x / 8;
+        if (i >= per + (die < more)) return;
+        const int tile = die * per + min(die, more) + i, four = tile / (4 * row_tiles), in = tile - four * (4 * row_tiles);
+        const int across = min(4, columns - 4 * four);
+        column = 4 * four + in % across;
+        m0 = in / across * BM;
+    } else {
+        column = (int)blockIdx.x / row_tiles;
+        m0 = ((int)blockIdx.x - column * row_tiles) * BM;
+        if (!a.order && column * BN >= a.rows) return;
+    }
     Columns c;
-    if (!columns_of<BN>(a, tile / row_tiles, c)) return;
+    if (!columns_of<BN>(a, column, c)) return;
     const bool routed = !a.order || c.expert < a.experts;
     const int split = (int)blockIdx.y, all_steps = a.blocks / 4;
     const int t_first = (int)((int64_t)all_steps * split / a.splits), t_end = (int)((int64_t)all_steps * (split + 1) / a.splits);
@@ -89,10 +103,24 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void mx_tile_kernel(ProductArgs a,
     };
     auto shift = [&](int q) { return t_first + 4 * q - min(t_first + 4 * q, all_steps - 4); };
 
+    const bool idle = (wave % WN) * TJ * 16 >= c.count;      // no columns: the wavefront loads, and multiplies nothing
     const int wi = (wave / WN) * TI * 16 + r, wj = BM + (wave % WN) * TJ * 16 + r;        // the lane's rows of the buffer
     const int at_code = (g ^ (r >> 2)) * 16;
     auto read_code = [&](const uint8_t *buf, int row) { return *(const i32x4 *)(buf + row * 64 + at_code); };
-    auto read_scale = [&](const uint8_t *buf, int row) -> int { return buf[row * 16 + g]; };
+    // The scales of a row's four steps, by step when they arrive, are turned in place (a thread per row) so that the word of
+    // block g has its bytes of the four steps: one read for four multiplies, which pick their byte.  (Reading a byte a
+    // step, the LDS reads of scales took a third of the time: 4096 x 4096 x 25088 240 us.)
+    auto turn_scales = [&](uint8_t *buf, int q) {
+        if (threadIdx.x >= BM + BN) return;
+        u32x4 *at = (u32x4 *)(buf + threadIdx.x * 16);
+        const u32x4 v = *at;
+        const uint32_t ab01 = __builtin_amdgcn_perm(v[1], v[0], 0x05010400), ab23 = __builtin_amdgcn_perm(v[1], v[0], 0x07030602);
+        const uint32_t cd01 = __builtin_amdgcn_perm(v[3], v[2], 0x05010400), cd23 = __builtin_amdgcn_perm(v[3], v[2], 0x07030602);
+        const int late = 8 * shift(q);
+        *at = u32x4{__builtin_amdgcn_perm(cd01, ab01, 0x05040100) >> late, __builtin_amdgcn_perm(cd01, ab01, 0x07060302) >> late,
+                    __builtin_amdgcn_perm(cd23, ab23, 0x05040100) >> late, __builtin_amdgcn_perm(cd23, ab23, 0x07060302) >> late};
+    };
+    auto read_scales = [&](const uint8_t *buf, int row) { return *(const int *)(buf + row * 16 + g * 4); };
 
     f32x4 acc[TI][TJ];
 #pragma unroll
@@ -100,7 +128,7 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void mx_tile_kernel(ProductArgs a,
 #pragma unroll
         for (auto &y : x) y = f32x4{0, 0, 0, 0};
     i32x4 w[C::kRing], x[2][TJ];
-    int sw[C::kRing], sx[2][TJ];
+    int sw[TI], sx[TJ], sx_next[TJ];
 
     constexpr int kWaitLds = 0xc07f, kWaitLoads = 0xf70;     // s_waitcnt: no LDS access left; no load left, or-ed with n < 16: n left
     auto barrier = [&] {
@@ -108,16 +136,31 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void mx_tile_kernel(ProductArgs a,
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
     };
-    // Step t = 4 q + S: `now` and `next` hold its codes and those of the step after, `to` receives those of step `ask`; likewise the
-    // scales, which step 4 q asks for four steps ahead.
-    auto step = [&](auto S, const uint8_t *__restrict__ now, const uint8_t *__restrict__ next, uint8_t *__restrict__ to, const uint8_t *__restrict__ scales_now,
-                    const uint8_t *__restrict__ scales_next, uint8_t *__restrict__ scales_to, int ask, int ask_scales) {
+    // Step t = 4 q + S: `now` and `next` hold its codes and those of the step after, `to` receives those of step `ask`.  Step 4 q
+    // asks for the scales of the eighth to eleventh step after it, step 4 q + 2 turns those of the next four, and step 4 q + 3
+    // reads them.
+    auto step = [&](auto S, const uint8_t *__restrict__ now, const uint8_t *__restrict__ next, uint8_t *__restrict__ to, uint8_t *__restrict__ scales_next,
+                    uint8_t *__restrict__ scales_to, int q, int ask, int ask_scales) __attribute__((always_inline)) {
         constexpr int s = decltype(S)::value, p = s & 1;
         // every wavefront's loads of step t + 1 have arrived, and all reads of the buffers that are asked for next are done
         __builtin_amdgcn_sched_barrier(0);
         __builtin_amdgcn_s_waitcnt(kWaitLds);
         __builtin_amdgcn_s_waitcnt(kWaitLoads | C::on_their_way(s));
         barrier();
+        if (s == 2) turn_scales(scales_next, q + 1);
+        if (idle) {
+#pragma unroll
+            for (int k = 0; k < C::kCodeLoads; ++k) request_code(ask, to, k);
+            if (s == 0) {
+#pragma unroll
+                for (int k = 0; k < C::kScaleShare; ++k) request_scales(ask_scales, scales_to, k);
+            }
+            return;
+        }
+        if (s == 0) {
+#pragma unroll
+            for (int j = 0; j < TJ; ++j) sx[j] = sx_next[j];
+        }
 #pragma unroll
         for (int i = 0; i < TI; ++i) {
 #pragma unroll
@@ -125,13 +168,12 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void mx_tile_kernel(ProductArgs a,
                 if (j == 0) {
                     const int f = i + C::kAhead;
                     w[C::slot(f, p)] = read_code(f < TI ? now : next, wi + f % TI * 16);
-                    sw[C::slot(f, p)] = read_scale(f < TI ? scales_now : scales_next, wi + f % TI * 16);
                     __builtin_amdgcn_sched_barrier(0);
                 }
                 if (j == TJ / 2 && i >= TI - TJ) {
                     const int f = i - (TI - TJ);
                     x[1 - p][f] = read_code(next, wj + f * 16);
-                    sx[1 - p][f] = read_scale(scales_next, wj + f * 16);
+                    if (s == 3) sx_next[f] = read_scales(scales_next, wj + f * 16);
                     __builtin_amdgcn_sched_barrier(0);
                 }
                 if (j == TJ - 1) {
@@ -143,7 +185,11 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void mx_tile_kernel(ProductArgs a,
                     }
                     __builtin_amdgcn_sched_barrier(0);
                 }
-                acc[i][j] = mfma_fp4<0>(w[C::slot(i, p)], x[p][j], acc[i][j], sw[C::slot(i, p)], sx[p][j]);
+                acc[i][j] = mfma_fp4<s>(w[C::slot(i, p)], x[p][j], acc[i][j], sw[i], sx[j]);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            if (s == 3) {
+                sw[i] = read_scales(scales_next, wi + i * 16);
                 __builtin_amdgcn_sched_barrier(0);
             }
         }
@@ -151,28 +197,32 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void mx_tile_kernel(ProductArgs a,
 
     if (steps > 0) {
         auto buffer = [&](int t) { return lds + t % D * C::kBuffer; };
-        auto scales = [&](int q) { return lds + C::kScales + (q & 1) * C::kScaleBuffer; };
-        // step t of which the row has S before it in its four
-        auto at = [&](auto S, int t) {
-            constexpr int s = decltype(S)::value;
-            const int q = t / 4, qn = (t + 1) / 4;
-            step(S, buffer(t), buffer(t + 1), buffer(t + D - 1), scales(q) + (shift(q) + s) * 4, scales(qn) + (shift(qn) + (s + 1) % 4) * 4, scales(q + 1),
-                 min(t + D - 1, steps - 1), min(q + 1, (steps - 1) / 4));
+        auto scales = [&](int q) { return lds + C::kScales + q % 3 * C::kScaleBuffer; };
+        const int last = steps - 1;
+        auto at = [&](auto S, int t) __attribute__((always_inline)) {
+            const int q = t / 4;
+            step(S, buffer(t), buffer(t + 1), buffer(t + D - 1), scales(q + 1), scales(q + 2), q, min(t + D - 1, last), min(q + 2, last / 4));
         };
         // (requests beyond the last step repeat it, so that a wait always counts the same; nothing reads what they bring)
 #pragma unroll
-        for (int k = 0; k < C::kScaleShare; ++k) request_scales(0, scales(0), k);
+        for (int q = 0; q < 2; ++q)
+#pragma unroll
+            for (int k = 0; k < C::kScaleShare; ++k) request_scales(min(q, last / 4), scales(q), k);
 #pragma unroll
         for (int t = 0; t < D - 1; ++t)
 #pragma unroll
-            for (int k = 0; k < C::kCodeLoads; ++k) request_code(min(t, steps - 1), buffer(t), k);
-        __builtin_amdgcn_s_waitcnt(kWaitLoads);
+            for (int k = 0; k < C::kCodeLoads; ++k) request_code(min(t, last), buffer(t), k);
+        __builtin_amdgcn_s_waitcnt(kWaitLoads | (D - 2) * C::kCodeLoads);
         barrier();
-        const uint8_t *first = scales(0) + shift(0) * 4;
+        turn_scales(scales(0), 0);
+        __builtin_amdgcn_s_waitcnt(kWaitLds);
+        barrier();
 #pragma unroll
-        for (int j = 0; j < TJ; ++j) x[0][j] = read_code(lds, wj + j * 16), sx[0][j] = read_scale(first, wj + j * 16);
+        for (int j = 0; j < TJ; ++j) x[0][j] = read_code(lds, wj + j * 16), sx_next[j] = read_scales(scales(0), wj + j * 16);
 #pragma unroll
-        for (int i = 0; i < C::kAhead; ++i) w[i] = read_code(lds, wi + i * 16), sw[i] = read_scale(first, wi + i * 16);
+        for (int i = 0; i < TI; ++i) sw[i] = read_scales(scales(0), wi + i * 16);
+#pragma unroll
+        for (int i = 0; i < C::kAhead; ++i) w[i] = read_code(lds, wi + i * 16);
         int t = 0;
         for (; t + 4 <= steps; t += 4) {
             at(std::integral_constant<int, 0>{}, t);

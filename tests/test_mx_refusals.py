@@ -28,15 +28,16 @@ def test_product():
     L = binding.lib()
     n = C.c_size_t(0)
     W, X = MxMatrix(4096, 4096, 64, 200), MxInput(4096, None, 0, 200)
-    assert L.cl_mx_fc_workspace_bytes(W, 3, 0, n) == CL_OK and n.value >= 3 * 256 // 32 * 17
-    assert L.cl_mx_fc_workspace_bytes(W, 3, 3, n) == CL_OK and n.value == 0
+    assert L.cl_mx_fc_workspace_bytes(W, 30, 0, n) == CL_OK and n.value >= 30 * 256 // 32 * 17
+    assert L.cl_mx_fc_workspace_bytes(W, 30, 3, n) == CL_OK and n.value == 0
+    assert L.cl_mx_fc_workspace_bytes(W, 3, 0, n) == CL_OK and n.value == 0            # quantised where it is multiplied
     for bad in (MxMatrix(4096, 4096, 0, 200), MxMatrix(4096, 4096, 64, 0)):
         assert L.cl_mx_fc_workspace_bytes(bad, 3, 0, n) == CL_EINVAL
     assert L.cl_mx_fc_workspace_bytes(W, -1, 0, n) == CL_EINVAL and L.cl_mx_fc_workspace_bytes(W, 1, 9, n) == CL_EINVAL
     assert L.cl_mx_fc_workspace_bytes(W, 1, 0, None) == CL_EINVAL and L.cl_mx_fc_workspace_bytes(None, 1, 0, n) == CL_EINVAL
     big = 1 << 20
 
-    def call(W=W, X=X, y=P, y_type=0, batch=3, act=0, ws=P, ws_bytes=big):
+    def call(W=W, X=X, y=P, y_type=0, batch=30, act=0, ws=P, ws_bytes=big):
         return L.cl_mx_fc_forward(W, X, None, y, y_type, batch, act, ws, ws_bytes, None)
 
     assert call(W=None) == CL_EINVAL and call(X=None) == CL_EINVAL and call(y=None) == CL_EINVAL
@@ -69,12 +70,12 @@ def test_experts():
     L = binding.lib()
     n = C.c_size_t(0)
     W, X = MxMatrix(4096, 4096, 64, 200), MxInput(4096, None, 0, 200)
-    base = dict(tokens=5, k=2, d_experts=4096, d_weights=4096, d_bias=None, d_lists=None, act=0, x_per_pair=0)
+    base = dict(tokens=5000, k=2, d_experts=4096, d_weights=4096, d_bias=None, d_lists=None, act=0, x_per_pair=0)
 
     def call(W=W, experts=8, X=X, y=P, y_type=0, ws=P, ws_bytes=1 << 24, **c):
         return L.cl_mx_experts_forward(W, experts, X, MxExpertsCall(**{**base, **c}), y, y_type, ws, ws_bytes, None)
 
-    assert L.cl_mx_experts_workspace_bytes(W, 8, MxExpertsCall(**base), 0, n) == CL_OK and n.value > 5 * 2 * 64 * 4
+    assert L.cl_mx_experts_workspace_bytes(W, 8, MxExpertsCall(**base), 0, n) == CL_OK and n.value > 5000 * 2 * 64 * 4
     assert L.cl_mx_experts_workspace_bytes(W, 8, None, 0, n) == CL_EINVAL
     assert L.cl_expert_lists_bytes(5, 2, 8, n) == CL_OK and n.value >= 4 * (10 + 10)
     assert L.cl_expert_lists_bytes(5, 0, 8, n) == CL_EINVAL and L.cl_expert_lists_bytes(5, 1, 1025, n) == CL_EUNSUPPORTED
