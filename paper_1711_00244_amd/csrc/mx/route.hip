@@ -16,6 +16,7 @@ struct RouteArgs {
     int32_t *experts_out;
     float *weights_out;
     int tokens, experts, k, groups, kept, top2, sigmoid, renormalize;
+    int wide;                                                // rows of logits are 16-byte aligned
     float scale;
 };
 
@@ -128,6 +129,229 @@ template <class T, int L, int C> __global__ __launch_bounds__(256) void route_ke
         a.experts_out[(int64_t)token * a.k + sub] = chosen;
         a.weights_out[(int64_t)token * a.k + sub] = weight * a.scale;
     }
+}
+
+// exp(x) from the hardware's 2^x: what rounding leaves of x log2(e), and log2(e) itself, goes in as a factor, so that the error stays
+// near one unit in the last place where |x| is large.
+__device__ __forceinline__ float exp_of(float x)
+{
+    const float log2e = 1.44269504f, rest = 1.92596299e-8f, ln2 = 0.693147181f;
+    const float p = x * log2e, r = fmaf(x, log2e, -p) + x * rest, e = __builtin_amdgcn_exp2f(p);
+    return fmaf(e, r * ln2, e);
+}
+
+template <int CTRL> __device__ __forceinline__ uint32_t dpp(uint32_t x) { return (uint32_t)__builtin_amdgcn_mov_dpp((int)x, CTRL, 0xF, 0xF, true); }
+template <int CTRL> __device__ __forceinline__ float dpp(float x) { return __uint_as_float(dpp<CTRL>(__float_as_uint(x))); }
+constexpr int kXor1 = 0xB1, kXor2 = 0x4E, kHalfMirror = 0x141, kMirror = 0x140, kRotate = 0x120;
+
+// f over the sixteen lanes of a row, in every lane.  (Mirrors stand in for the exchanges over 4 and 8, as what they exchange is the
+// same in all lanes of a quad and of a half.)
+template <class V, class F> __device__ __forceinline__ V over_row(V v, F f)
+{
+    v = f(v, dpp<kXor1>(v));
+    v = f(v, dpp<kXor2>(v));
+    v = f(v, dpp<kHalfMirror>(v));
+    return f(v, dpp<kMirror>(v));
+}
+
+// Numbers in the order of floats, the two zeros equal; 0 is below all of them.
+__device__ __forceinline__ uint32_t ordered(float x)
+{
+    const uint32_t u = __float_as_uint(x + 0.0f);
+    return x == -INFINITY ? 0u : u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+
+// Groups (of `lanes` lanes each) that come before this lane's: a larger score, or an equal one and lower experts.
+template <int R> __device__ __forceinline__ void groups_before(float v, int g, int row_lane, int lanes, int &before)
+{
+    if constexpr (R < 16) {
+        if (R % lanes == 0) {
+            const float o = dpp<kRotate + R>(v);
+            const int og = ((row_lane - R) & 15) / lanes;
+            before += o > v || (o == v && og < g);
+        }
+        groups_before<R + 1>(v, g, row_lane, lanes, before);
+    }
+}
+
+// The same for up to sixteen choices among up to 16 C experts: sixteen lanes - a row, within which lanes exchange registers without the LDS -
+// to a token, C experts to a lane, four tokens to a wavefront.  A lane keeps its three largest keys and looks for the next
+// three only when all are taken (8 of 256 experts in half of eight groups: one round of eight, over a wavefront's four tokens).
+// What bounds it is instructions: 16381 tokens of 256 experts, logistic scores, a bias, groups, 8 chosen, 16.5 us - of 16.8 MB,
+// which take 3.5 - where sixty-four lanes to a token, four experts each, and exchanges through LDS took 30.
+// group_lanes: lanes of a group, a power of two; 0: groups do not end with a lane (16381 tokens, 12 groups of 20 experts: 16 us, 33).
+template <class T, int C> __global__ __launch_bounds__(256) void route_rows_kernel(RouteArgs a, int group_lanes)
+{
+    __shared__ float s_score[16][16 * C];
+    __shared__ int32_t s_chosen[16][16];
+    const int sub = threadIdx.x & 15, local = threadIdx.x / 16, lane = threadIdx.x & 63;
+    const int token = (int)blockIdx.x * 16 + local;
+    const bool live = token < a.tokens;
+    const float lowest = sizeof(T) == 4 ? -3.402823466e38f : std::is_same<T, f16_t>::value ? -65504.0f : -3.38953138925e38f;
+    const T *x = (const T *)a.logits + (int64_t)(live ? token : 0) * a.stride + sub * C;
+    const int mine = live ? a.experts - sub * C : 0;         // experts of this lane, or more
+    float logit[C], score[C];
+    float top = -INFINITY;
+    if (a.wide && mine >= C) {
+        T v[C];
+        __builtin_memcpy(v, __builtin_assume_aligned(x, C * sizeof(T) < 16 ? C * sizeof(T) : 16), sizeof v);
+#pragma unroll
+        for (int j = 0; j < C; ++j) logit[j] = to_float(v[j]);
+    } else {
+#pragma unroll
+        for (int j = 0; j < C; ++j) logit[j] = j < mine ? to_float(x[j]) : -INFINITY;
+    }
+#pragma unroll
+    for (int j = 0; j < C; ++j) {
+        logit[j] = logit[j] > lowest ? logit[j] : -INFINITY;         // (NaN too)
+        top = fmaxf(top, logit[j]);
+    }
+    // (values first, choices after: a choice between a value and its computation would be a branch each)
+    if (a.sigmoid) {
+        // (below -88, where exp(-x) would leave the range: 0; the reciprocal's error is one unit in the last place)
+#pragma unroll
+        for (int j = 0; j < C; ++j) {
+            const float s = __builtin_amdgcn_rcpf(1.0f + exp_of(__builtin_amdgcn_fmed3f(-logit[j], -100.0f, 88.0f)));
+            score[j] = logit[j] < -88.0f ? 0.0f : s;
+        }
+    } else {
+        top = over_row(top, [](float p, float q) { return fmaxf(p, q); });
+        float sum = 0.0f;
+#pragma unroll
+        for (int j = 0; j < C; ++j) {
+            // (equal to the largest: 1 also where that is infinite; masked: 0 also where all are)
+            const float e = exp_of(fmaxf(logit[j] - top, -200.0f)), s = logit[j] == top ? 1.0f : e;
+            score[j] = logit[j] == -INFINITY ? 0.0f : s;
+            sum += score[j];
+        }
+        sum = over_row(sum, [](float p, float q) { return p + q; });
+        const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
+#pragma unroll
+        for (int j = 0; j < C; ++j) score[j] *= inv;
+    }
+    uint32_t key[C];
+    bool open = true;
+    if (a.bias || a.groups > 1) {
+        float biased[C];
+#pragma unroll
+        for (int j = 0; j < C; ++j) biased[j] = score[j];
+        if (a.bias) {
+            float bias[C];
+            if (mine >= C) {
+                __builtin_memcpy(bias, a.bias + sub * C, sizeof bias);
+            } else {
+#pragma unroll
+                for (int j = 0; j < C; ++j) bias[j] = a.bias[min(sub * C + j, a.experts - 1)];
+            }
+#pragma unroll
+            for (int j = 0; j < C; ++j) biased[j] += bias[j];
+        }
+        float best = -INFINITY, second = -INFINITY;
+#pragma unroll
+        for (int j = 0; j < C; ++j) {
+            biased[j] = logit[j] == -INFINITY || !(biased[j] == biased[j]) ? -INFINITY : biased[j];
+            key[j] = ordered(a.bias ? biased[j] : logit[j]);
+            second = fmaxf(second, fminf(best, biased[j]));
+            best = fmaxf(best, biased[j]);
+        }
+        if (a.groups > 1 && group_lanes > 0) {
+            auto merge = [&](float b, float s) {
+                second = fmaxf(fmaxf(second, s), fminf(best, b));
+                best = fmaxf(best, b);
+            };
+            if (group_lanes > 1) merge(dpp<kXor1>(best), dpp<kXor1>(second));
+            if (group_lanes > 2) merge(dpp<kXor2>(best), dpp<kXor2>(second));
+            if (group_lanes > 4) merge(dpp<kHalfMirror>(best), dpp<kHalfMirror>(second));
+            const float v = a.top2 && second != -INFINITY ? best + second : best;
+            int before = 0;
+            groups_before<1>(v, sub / group_lanes, sub, group_lanes, before);
+            open = before < a.kept;
+        } else if (a.groups > 1) {
+            // groups that do not end with a lane: lane g looks group g over in LDS
+            const int size = a.experts / a.groups;
+#pragma unroll
+            for (int j = 0; j < C; ++j) s_score[local][sub * C + j] = biased[j];
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            best = second = -INFINITY;
+            if (sub < a.groups)
+                for (int i = 0; i < size; ++i) {
+                    const float v = s_score[local][sub * size + i];
+                    second = fmaxf(second, fminf(best, v));
+                    best = fmaxf(best, v);
+                }
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            const float v = a.top2 && second != -INFINITY ? best + second : best;
+            int before = 0;
+            groups_before<1>(v, sub, sub, 1, before);
+            const uint32_t kept = (uint32_t)(__ballot(sub < a.groups && before < a.kept) >> (lane & 48)) & 0xffffu;
+            int g = sub * C / size, left = (g + 1) * size - sub * C;         // the group of expert j, and how many it has from there on
+#pragma unroll
+            for (int j = 0; j < C; ++j) {
+                key[j] = g < 16 && kept >> g & 1 ? key[j] : 0u;
+                if (--left == 0) ++g, left = size;
+            }
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < C; ++j) key[j] = ordered(logit[j]);
+    }
+#pragma unroll
+    for (int j = 0; j < C; ++j) s_score[local][sub * C + j] = score[j];
+    // the three largest keys of the lane that are not taken, the lower expert first where they are equal
+    uint32_t best = 0, second = 0, third = 0, taken = 0;
+    int best_at = 0, second_at = 0, third_at = 0;
+    auto look = [&] {
+        best = second = third = 0;
+#pragma unroll
+        for (int j = 0; j < C; ++j) {
+            const uint32_t k = taken >> j & 1 ? 0u : key[j];
+            const bool before_best = k > best, before_second = k > second, before_third = k > third;
+            third_at = before_second ? second_at : before_third ? j : third_at;
+            second_at = before_best ? best_at : before_second ? j : second_at;
+            best_at = before_best ? j : best_at;
+            third = max(third, min(second, k));
+            second = max(second, min(best, k));
+            best = max(best, k);
+        }
+    };
+    if (open) look();
+    for (int i = 0; i < a.k; ++i) {
+        const uint32_t most = over_row(best, [](uint32_t p, uint32_t q) { return p > q ? p : q; });
+        const uint32_t has = (uint32_t)(__ballot(best == most) >> (lane & 48)) & 0xffffu;
+        const bool winner = (has & (0u - has)) == 1u << sub;
+        if (winner) {
+            s_chosen[local][i] = most ? sub * C + best_at : -1;
+            taken |= 1u << best_at;
+            best = second;
+            best_at = second_at;
+            second = third;
+            second_at = third_at;
+            third = 0;
+            if (best == 0 && most != 0 && i + 1 < a.k) look();
+        }
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");   // (a token's lanes are one wavefront's: its LDS accesses are in order)
+    int chosen = -1;
+    float weight = 0.0f;
+    if (sub < a.k) {
+        chosen = s_chosen[local][sub];
+        weight = chosen >= 0 ? s_score[local][chosen] : 0.0f;
+    }
+    if (a.renormalize) {
+        const float sum = over_row(weight, [](float p, float q) { return p + q; });
+        weight = sum > 0.0f ? weight / sum : 0.0f;
+    }
+    if (live && sub < a.k) {
+        a.experts_out[(int64_t)token * a.k + sub] = chosen;
+        a.weights_out[(int64_t)token * a.k + sub] = weight * a.scale;
+    }
+}
+
+template <class T, int C> static int32_t launch_route_rows(const RouteArgs &a, int group_lanes, hipStream_t st)
+{
+    hipLaunchKernelGGL((route_rows_kernel<T, C>), dim3((unsigned)((a.tokens + 15) / 16)), dim3(256), 0, st, a, group_lanes);
+    MX_HIP_TRY(hipGetLastError());
+    return CL_OK;
 }
 
 template <class T, int L, int C> static int32_t launch_route(const RouteArgs &a, hipStream_t st)
@@ -311,12 +535,19 @@ extern "C" int32_t cl_route_experts(const void *d_logits, int32_t type, int64_t 
     if (!d_logits || !d_experts || !d_weights) return fail(CL_EINVAL, "null pointer");
     if (tokens > 1 && x_stride < d.experts) return fail(CL_EINVAL, "rows of %d logits overlap at a stride of %lld", (int)d.experts, (long long)x_stride);
     RouteArgs a{d_logits, x_stride, d_bias, d_experts, d_weights, tokens, d.experts, d.k, d.groups, d.groups_kept, d.group_score == CL_GROUP_TOP2,
-                d.score == CL_SCORE_SIGMOID, d.renormalize, d.scale};
+                d.score == CL_SCORE_SIGMOID, d.renormalize, aligned(d_logits, 16) && x_stride * (int64_t)type_bytes(type) % 16 == 0, d.scale};
     const int32_t rc = with_type(type, [&](auto t) -> int32_t {
         using T = decltype(t);
         hipStream_t st = (hipStream_t)stream;
-        if (d.experts <= 64 && d.k <= 16) return launch_route<T, 16, 4>(a, st);
-        if (d.experts <= 128) return launch_route<T, 32, 4>(a, st);
+        // sixteen lanes to a token while experts, choices and groups are few enough for them
+        if (d.experts <= 512 && d.k <= 16 && d.groups <= 16) {
+            const int C = d.experts <= 64 ? 4 : d.experts <= 128 ? 8 : d.experts <= 256 ? 16 : 32, size = d.experts / d.groups;
+            const int lanes = size % C == 0 && (size / C & (size / C - 1)) == 0 ? size / C : 0;
+            if (C == 4) return launch_route_rows<T, 4>(a, lanes, st);
+            if (C == 8) return launch_route_rows<T, 8>(a, lanes, st);
+            if (C == 16) return launch_route_rows<T, 16>(a, lanes, st);
+            return launch_route_rows<T, 32>(a, lanes, st);
+        }
         if (d.experts <= 256) return launch_route<T, 64, 4>(a, st);
         return launch_route<T, 64, 16>(a, st);
     });
