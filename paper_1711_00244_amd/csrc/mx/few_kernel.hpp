@@ -9,6 +9,7 @@
 // One matrix: 16 F consecutive rows of it.  Experts: one token (blockIdx.y), `rows_each` rows of each of its k experts' matrices,
 // which are rows of one matrix instruction like any others, so that a token's weighted sum needs no second launch either.
 // (One token, 64 experts of 1024 x 4096, eight chosen: lists, quantisation, product and sum apart took 33 us in five launches.)
+constexpr int kUnit = 8;                                     // values that a lane quantises at a time
 constexpr int kFewColumns = 4, kFewWaves = kRowsWaves;
 constexpr size_t kFewLds = 64 << 10;
 
@@ -37,14 +38,22 @@ template <class X, class T, bool EXPERTS> __global__ __launch_bounds__(kFewWaves
     const int m0 = (int)blockIdx.x * (EXPERTS ? a.rows_each : 16 * kFewF);
     uint8_t *codes = lds, *scales = lds + (size_t)a.columns * p.blocks * 16;
 
-    // the values of this thread's first unit, then the weights of the wavefront's first run, then the other units
-    const int per_row = p.blocks * 4, units = a.columns * per_row;
+    // the values of this thread's first two units, then the weights of the wavefront's first two runs, then the other units: what
+    // is asked for first arrives first
+    const int per_row = p.blocks * 4, units = a.columns * per_row, threads = (int)blockDim.x;
     auto load = [&](int u, float *x) {
-        const int row = u / per_row, k0 = (u - row * per_row) * 8;
-        load_unit<X>((const X *)a.X + (EXPERTS ? token * (a.x_per_pair ? a.k : 1) + row : row) * a.x_stride + k0, a.K - k0, a.x_wide, x);
+        const int row = u / per_row, k0 = (u - row * per_row) * kUnit;
+        load_unit<kUnit>((const X *)a.X + (EXPERTS ? token * (a.x_per_pair ? a.k : 1) + row : row) * a.x_stride + k0, a.K - k0, a.x_wide, x);
     };
-    float x0[8];
-    if ((int)threadIdx.x < units) load(threadIdx.x, x0);
+    auto quantise = [&](int u, const float *x) {             // (a row has whole blocks: a quad's lanes stay together)
+        uint32_t byte;
+        ((uint32_t *)codes)[u] = quantise_unit<kUnit>(x, byte);
+        if ((u & 3) == 0) scales[u >> 2] = (uint8_t)byte;
+    };
+    float x0[kUnit], x1[kUnit];
+    const int u0 = (int)threadIdx.x, u1 = u0 + threads;
+    if (u0 < units) load(u0, x0);
+    if (u1 < units) load(u1, x1);
 
     const uint8_t *w_codes[kFewF], *w_scales[kFewF];
 #pragma unroll
@@ -60,58 +69,60 @@ template <class X, class T, bool EXPERTS> __global__ __launch_bounds__(kFewWaves
         w_codes[f] = p.w_codes + row * p.blocks * 16;
         w_scales[f] = p.w_scales + row * p.blocks;
     }
-    i32x4 w[kFewF][4];
-    int sw[kFewF];
-    auto load_run = [&](int b) {
+    struct Run {
+        i32x4 w[kFewF][4];
+        int scales[kFewF];
+    };
+    auto load_run = [&](Run &run, int b) {
         const bool in = b < p.blocks;                        // (four blocks are in or out together)
 #pragma unroll
         for (int f = 0; f < kFewF; ++f) {
 #pragma unroll
-            for (int s = 0; s < 4; ++s) w[f][s] = in ? ((const i32x4 *)(w_codes[f] + (int64_t)b * 16))[s] : i32x4{};
-            sw[f] = in ? *(const int *)(w_scales[f] + b) : 0;
+            for (int s = 0; s < 4; ++s) run.w[f][s] = in ? ((const i32x4 *)(w_codes[f] + (int64_t)b * 16))[s] : i32x4{};
+            run.scales[f] = in ? *(const int *)(w_scales[f] + b) : 0;
         }
     };
-    int b = wave * 16 + g * 4;
-    load_run(b);
+    const int b0 = wave * 16 + g * 4, stride = (int)blockDim.x / 4;      // (sixteen blocks a wavefront)
+    constexpr bool kTwo = !EXPERTS;                          // (two runs of two rows' fragments do not fit the registers)
+    Run even, odd;
+    load_run(even, b0);
+    if (kTwo) load_run(odd, b0 + stride);
 
-    for (int u = threadIdx.x; u < units; u += (int)blockDim.x) {  // (a row has whole blocks: a quad's lanes stay together)
-        float x[8];
-        if (u == (int)threadIdx.x) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] = x0[i];
-        } else {
-            load(u, x);
-        }
-        uint32_t byte;
-        ((uint32_t *)codes)[u] = quantise_unit(x, byte);
-        if ((u & 3) == 0) scales[u >> 2] = (uint8_t)byte;
+    if (u0 < units) quantise(u0, x0);
+    if (u1 < units) quantise(u1, x1);
+    for (int u = u1 + threads; u < units; u += threads) {
+        load(u, x0);
+        quantise(u, x0);
     }
     __syncthreads();
 
     f32x4 acc[kFewF] = {};
     const int column = min(r, a.columns - 1);
     const uint8_t *xc = codes + (size_t)column * p.blocks * 16, *xs = scales + (size_t)column * p.blocks;
-    for (; b - g * 4 < p.blocks; b += waves * 16) {
+    auto multiply = [&](const Run &run, int b) {
         const bool in = b < p.blocks;
         i32x4 x[4];
 #pragma unroll
         for (int s = 0; s < 4; ++s) x[s] = in ? ((const i32x4 *)(xc + (size_t)b * 16))[s] : i32x4{};
         const int sx = in ? *(const int *)(xs + b) : 0;
-        i32x4 now[kFewF][4];
-        int sn[kFewF];
 #pragma unroll
         for (int f = 0; f < kFewF; ++f) {
-#pragma unroll
-            for (int s = 0; s < 4; ++s) now[f][s] = w[f][s];
-            sn[f] = sw[f];
+            acc[f] = mfma_fp4<0>(run.w[f][0], x[0], acc[f], run.scales[f], sx);
+            acc[f] = mfma_fp4<1>(run.w[f][1], x[1], acc[f], run.scales[f], sx);
+            acc[f] = mfma_fp4<2>(run.w[f][2], x[2], acc[f], run.scales[f], sx);
+            acc[f] = mfma_fp4<3>(run.w[f][3], x[3], acc[f], run.scales[f], sx);
         }
-        if (b - g * 4 + waves * 16 < p.blocks) load_run(b + waves * 16);
-#pragma unroll
-        for (int f = 0; f < kFewF; ++f) {
-            acc[f] = mfma_fp4<0>(now[f][0], x[0], acc[f], sn[f], sx);
-            acc[f] = mfma_fp4<1>(now[f][1], x[1], acc[f], sn[f], sx);
-            acc[f] = mfma_fp4<2>(now[f][2], x[2], acc[f], sn[f], sx);
-            acc[f] = mfma_fp4<3>(now[f][3], x[3], acc[f], sn[f], sx);
+    };
+    for (int b = b0; b - g * 4 < p.blocks; b += stride) {
+        multiply(even, b);
+        if (kTwo) {
+            load_run(even, b + 2 * stride);
+            b += stride;
+            if (b - g * 4 >= p.blocks) break;
+            multiply(odd, b);
+            load_run(odd, b + 2 * stride);
+        } else {
+            load_run(even, b + stride);
         }
     }
 #pragma unroll

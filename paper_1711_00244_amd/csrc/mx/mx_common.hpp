@@ -72,39 +72,42 @@ __device__ __forceinline__ float to_float(float x) { return x; }
 __device__ __forceinline__ float to_float(bf16_t x) { return (float)x; }
 __device__ __forceinline__ float to_float(f16_t x) { return (float)x; }
 
-// What a lane quantises: eight consecutive elements of a row, four lanes to a block.  `wide`: p is 16-byte aligned.
-constexpr int kUnit = 8;
-template <class T> __device__ __forceinline__ void load_unit(const T *p, int left, bool wide, float *x)
+// V consecutive elements of a row, of which `left` exist.  `wide`: p is aligned to 16 bytes, or to all V.
+template <int V, class T> __device__ __forceinline__ void load_unit(const T *p, int left, bool wide, float *x)
 {
-    if (wide && left >= kUnit) {
-        T v[kUnit];
-        __builtin_memcpy(v, __builtin_assume_aligned(p, 16), sizeof v);
+    if (wide && left >= V) {
+        T v[V];
+        __builtin_memcpy(v, __builtin_assume_aligned(p, V * sizeof(T) < 16 ? V * sizeof(T) : 16), sizeof v);
 #pragma unroll
-        for (int i = 0; i < kUnit; ++i) x[i] = to_float(v[i]);
+        for (int i = 0; i < V; ++i) x[i] = to_float(v[i]);
     } else {
 #pragma unroll
-        for (int i = 0; i < kUnit; ++i) x[i] = i < left ? to_float(p[i]) : 0.0f;
+        for (int i = 0; i < V; ++i) x[i] = i < left ? to_float(p[i]) : 0.0f;
     }
 }
 
-// The codes of a lane's eight values and the scale byte of their block, whose 32 values the four lanes of a quad have.  The
-// maximum is taken on the bits of the magnitudes (in order for finite values, Inf and NaN above them).  The instruction rounds
-// to nearest, ties to even, and takes what is above 6 to 6; the values are scaled beforehand, which is exact but for those that
-// round to zero either way.
-__device__ __forceinline__ uint32_t quantise_unit(const float *x, uint32_t &byte)
+// The codes of a lane's V values (four or eight) and the scale byte of their block, whose 32 values 32 / V neighbouring lanes have.
+// The maximum is taken on the bits of the magnitudes (in order for finite values, Inf and NaN above them).  The instruction
+// rounds to nearest, ties to even, and takes what is above 6 to 6; the values are scaled beforehand, which is exact but for
+// those that round to zero either way.
+template <int V> __device__ __forceinline__ uint32_t quantise_unit(const float *x, uint32_t &byte)
 {
+    static_assert(V == 4 || V == 8, "");
     uint32_t top = 0;
 #pragma unroll
-    for (int i = 0; i < kUnit; ++i) top = max(top, __float_as_uint(x[i]) & 0x7fffffffu);
+    for (int i = 0; i < V; ++i) top = max(top, __float_as_uint(x[i]) & 0x7fffffffu);
     top = max(top, (uint32_t)__builtin_amdgcn_mov_dpp((int)top, 0xB1, 0xF, 0xF, true));      // lanes 1 0 3 2 of a quad
     top = max(top, (uint32_t)__builtin_amdgcn_mov_dpp((int)top, 0x4E, 0xF, 0xF, true));      // lanes 2 3 0 1
+    if (V == 4) top = max(top, (uint32_t)__builtin_amdgcn_mov_dpp((int)top, 0x141, 0xF, 0xF, true));     // the other quad of eight lanes
     byte = scale_byte(top);
     const float inv = scale_inverse(byte);
     uint32_t c = 0;
     c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[0] * inv, x[1] * inv, 1.0f, 0);
     c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[2] * inv, x[3] * inv, 1.0f, 1);
-    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[4] * inv, x[5] * inv, 1.0f, 2);
-    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[6] * inv, x[7] * inv, 1.0f, 3);
+    if (V == 8) {
+        c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[4] * inv, x[5] * inv, 1.0f, 2);
+        c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[6] * inv, x[7] * inv, 1.0f, 3);
+    }
     return byte == kScaleNaN ? 0u : c;                       // (Inf * 0 is no code)
 }
 

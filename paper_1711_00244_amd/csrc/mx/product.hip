@@ -180,7 +180,14 @@ template <class T> __global__ __launch_bounds__(256) void mx_finish_kernel(Finis
         if (e < 0 || e >= a.experts) continue;
         const float *p = a.part + pair * a.pitch + m;
         f32x4 v = *(const f32x4 *)p;
-        for (int s = 1; s < a.splits; ++s) v += *(const f32x4 *)(p + s * a.split_stride);
+        if (a.splits > 1) {
+            f32x4 more[7];                                   // (all on their way together; at most eight)
+#pragma unroll
+            for (int s = 1; s < 8; ++s) more[s - 1] = *(const f32x4 *)(p + min(s, a.splits - 1) * a.split_stride);
+#pragma unroll
+            for (int s = 1; s < 8; ++s)
+                if (s < a.splits) v += more[s - 1];
+        }
         if (a.bias) {
             const float *b = a.bias + (int64_t)e * a.M + m;
 #pragma unroll
@@ -220,7 +227,7 @@ template <int BM, int BN, int WM, int WN, int D, class T> static int32_t launch_
 // ------------------------------------------------------------------------- //
 // which kernel
 // ------------------------------------------------------------------------- //
-enum Form { kFew, kRows, kTile64, kTile128, kTile256x128, kTile256 };
+enum Form { kRows, kTile64, kTile128, kTile256x128, kTile256 };
 
 struct Choice {
     Form form;
@@ -228,35 +235,35 @@ struct Choice {
     int splits;
 };
 
-// A form's price in microseconds, from measurements over M 1000 .. 4096, 64 .. 4096 columns, K 4096 .. 25088 (within a
-// quarter of each): a start (launch, first loads, last stores), and per step of 128 k what a workgroup takes alone on its compute
-// unit, or its share of a full one where the launch has more workgroups than the chip has compute units.
+// What a form takes in microseconds, from measurements over M 1000 .. 4096, 16 .. 4096 columns, K 4096 .. 25088 (within a
+// quarter of each).  Tiles: a start (launch, first loads, last stores), and per step of 128 k what a workgroup takes alone on its
+// compute unit, or its share of a full one where the launch has more workgroups than the chip has compute units.
 struct Price { int bm, bn, width; float start, alone, shared; };
-constexpr Price kPrices[] = {{16, 4, 0, 0, 0, 0}, {16, 64, 1, 0, 0, 0}, {64, 64, 1, 3.5f, 0.15f, 0.18f}, {128, 128, 2, 4.5f, 0.50f, 0.40f}, {256, 128, 2, 6.0f, 0.74f, 0.74f},
-                             {256, 256, 3, 8.0f, 0.95f, 1.17f}};
+constexpr Price kPrices[] = {{64, 64, 1, 3.5f, 0.15f, 0.18f}, {128, 128, 2, 4.5f, 0.50f, 0.40f}, {256, 128, 2, 6.0f, 0.70f, 0.70f}, {256, 256, 3, 8.0f, 0.90f, 1.05f}};
 constexpr int kCus = 256;
 
 // rows: columns of the product in all; lists: how many runs they are cut into (experts, or 1), each of which fills its last tile
-// half on average.
-static Choice choose(int M, int blocks, int64_t rows, int64_t runs, bool part)
+// half on average; part: a finishing launch follows in any case.
+static Choice choose(int M, int blocks, int64_t rows, int64_t lists, bool part)
 {
-    const int steps = blocks / 4;
-    runs = std::min(runs, rows);
-    const Choice narrow{kRows, 0, 1};                        // columns sixteen at a time
-    if (steps < 4 || rows <= 16 * runs) return narrow;       // (the tile kernels read scales four steps at a time)
-    Choice best = narrow;
-    float least = 1e30f;
+    const int steps = blocks / 4, runs = (blocks + 15) / 16;
+    lists = std::min(lists, rows);
+    auto tiles_of = [&](int bn) { return lists == 1 ? (rows + bn - 1) / bn : std::max(lists, rows / bn + lists / 2); };
+    // columns sixteen at a time: every workgroup reads all it multiplies itself
+    const float wgs = (float)((M + 15) / 16) * (float)tiles_of(16);
+    Choice best{kRows, 0, 1};
+    float least = 2.5f + std::max(1.12e-3f * wgs * runs, 1.0f + 0.9f * ((runs + kRowsWaves - 1) / kRowsWaves));
+    if (steps < 4) return best;                              // (the tile kernels read scales four steps at a time)
     for (int f = kTile64; f <= kTile256; ++f) {
-        const Price &p = kPrices[f];
-        const int64_t tiles = runs == 1 ? (rows + p.bn - 1) / p.bn : std::max(runs, rows / p.bn + runs / 2);
-        const int64_t wgs = tiles * ((M + p.bm - 1) / p.bm);
+        const Price &p = kPrices[f - kTile64];
+        const int64_t n = tiles_of(p.bn) * ((M + p.bm - 1) / p.bm);
+        const bool alone = f >= kTile256x128;                // (one workgroup to a compute unit: whole rounds)
         for (int splits = 1; splits <= 8 && steps / splits >= 4; splits *= 2) {
-            if (splits > 1 && (runs > 1 || wgs * splits > 2 * kCus)) break;
-            const float full = (float)(wgs * splits) / kCus;
-            const float each = full <= 1.0f ? p.alone : std::max(p.alone, p.shared * (f >= kTile256x128 ? std::ceil(full) : full));
-            float us = p.start * (f >= kTile256x128 ? std::max(1.0f, std::ceil(full)) : 1.0f) + each * (steps + splits - 1) / splits;
-            if (splits > 1 && !part) us += 3.0f;
-            if (splits > 1) us += (float)(2 * splits - 1) * rows * M * 4e-6f / 4.0f;
+            if (splits > 1 && (lists > 1 || n * splits > 2 * kCus)) break;
+            const float full = (float)(n * splits) / kCus, rounds = std::max(1.0f, std::ceil(full));
+            const float each = full <= 1.0f ? p.alone : std::max(p.alone, p.shared * (alone ? rounds : full));
+            float us = p.start * (alone ? rounds : 1.0f) + each * (steps + splits - 1) / splits;
+            if (splits > 1) us += (part ? 0.0f : 3.5f) + (float)(2 * splits - 1) * rows * M * 1e-6f;
             if (us < least) least = us, best = Choice{(Form)f, p.width, splits};
         }
     }

@@ -413,58 +413,86 @@ __global__ __launch_bounds__(kListThreads) void lists_place_kernel(ExpertLists L
     __syncthreads();
     const int64_t first = (int64_t)blockIdx.x * chunk + (int64_t)wave * (chunk / kListWaves);
     const int64_t end = min((int64_t)pairs, first + chunk / kListWaves);
-    for (int64_t p = first + lane; p < end; p += 64) atomicAdd(&at[wave * buckets + bucket_of(experts_of[p], experts)], 1);
+    // the buckets of four times 64 pairs from p0 on, -1 beyond the end; asked for together
+    auto buckets_of = [&](int64_t p0, int *b) {
+        int e[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) e[i] = experts_of[min(p0 + i * 64 + lane, (int64_t)pairs - 1)];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) b[i] = p0 + i * 64 + lane < end ? bucket_of(e[i], experts) : -1;
+    };
+    int b[4];
+    for (int64_t p0 = first; p0 < end; p0 += 256) {
+        buckets_of(p0, b);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (b[i] >= 0) atomicAdd(&at[wave * buckets + b[i]], 1);
+    }
     __syncthreads();
     // a thread has two buckets: all pairs of each, and those of earlier chunks
     const int b0 = 2 * (int)threadIdx.x;
     int all[2] = {0, 0}, before[2] = {0, 0};
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-        const int b = b0 + i;
-        if (b >= buckets) continue;
+        const int bucket = b0 + i;
+        if (bucket >= buckets) continue;
         if (chunks > 1) {
+#pragma unroll 8
             for (int c = 0; c < chunks; ++c) {
-                const int n = L.chunk_counts[(int64_t)c * buckets + b];
+                const int n = L.chunk_counts[(int64_t)c * buckets + bucket];
                 all[i] += n;
                 before[i] += c < (int)blockIdx.x ? n : 0;
             }
         } else {
-            for (int w = 0; w < kListWaves; ++w) all[i] += at[w * buckets + b];
+#pragma unroll
+            for (int w = 0; w < kListWaves; ++w) all[i] += at[w * buckets + bucket];
         }
     }
-    // exclusive sums over the buckets of the pairs and of the tiles of each width
-    int sum[1 + kTileWidths], mine[1 + kTileWidths];
+    // exclusive sums over the buckets of the pairs and of the tiles of each width, by the wavefronts that have buckets
+    const int scanning = buckets / 128 + 1;                  // (one more than the last bucket: the end)
+    int sum[1 + kTileWidths] = {}, mine[1 + kTileWidths] = {};
+    if (wave < scanning) {
 #pragma unroll
-    for (int v = 0; v <= kTileWidths; ++v) {
-        const int width = v ? kTileWidth[v ? v - 1 : 0] : 1;
-        mine[v] = (all[0] + width - 1) / width + (all[1] + width - 1) / width;
-        sum[v] = mine[v];
+        for (int v = 0; v <= kTileWidths; ++v) {
+            const int width = v ? kTileWidth[v ? v - 1 : 0] : 1;
+            mine[v] = sum[v] = (all[0] + width - 1) / width + (all[1] + width - 1) / width;
+        }
 #pragma unroll
         for (int d = 1; d < 64; d *= 2) {
-            const int o = __shfl_up(sum[v], d);
-            sum[v] += lane >= d ? o : 0;
+            int o[1 + kTileWidths];
+#pragma unroll
+            for (int v = 0; v <= kTileWidths; ++v) o[v] = __shfl_up(sum[v], d);
+#pragma unroll
+            for (int v = 0; v <= kTileWidths; ++v) sum[v] += lane >= d ? o[v] : 0;
         }
-        if (lane == 63) wave_sum[wave][v] = sum[v];
+        if (lane == 63) {
+#pragma unroll
+            for (int v = 0; v <= kTileWidths; ++v) wave_sum[wave][v] = sum[v];
+        }
     }
     __syncthreads();
+    if (wave < scanning) {
 #pragma unroll
-    for (int v = 0; v <= kTileWidths; ++v) {
-        const int width = v ? kTileWidth[v ? v - 1 : 0] : 1;
-        int start = sum[v] - mine[v];
-        for (int w = 0; w < wave; ++w) start += wave_sum[w][v];
-        if (b0 <= buckets) starts[v * (buckets + 1) + b0] = start;
-        if (b0 + 1 <= buckets) starts[v * (buckets + 1) + b0 + 1] = start + (all[0] + width - 1) / width;
+        for (int v = 0; v <= kTileWidths; ++v) {
+            const int width = v ? kTileWidth[v ? v - 1 : 0] : 1;
+            int start = sum[v] - mine[v];
+            for (int w = 0; w < wave; ++w) start += wave_sum[w][v];
+            if (b0 <= buckets) starts[v * (buckets + 1) + b0] = start;
+            if (b0 + 1 <= buckets) starts[v * (buckets + 1) + b0 + 1] = start + (all[0] + width - 1) / width;
+        }
     }
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-        const int b = b0 + i;
-        if (b >= buckets) continue;
-        int to = starts[b] + before[i];
+        const int bucket = b0 + i;
+        if (bucket >= buckets) continue;
+        int n[kListWaves], to = starts[bucket] + before[i];
+#pragma unroll
+        for (int w = 0; w < kListWaves; ++w) n[w] = at[w * buckets + bucket];
+#pragma unroll
         for (int w = 0; w < kListWaves; ++w) {
-            const int n = at[w * buckets + b];
-            at[w * buckets + b] = to;
-            to += n;
+            at[w * buckets + bucket] = to;
+            to += n[w];
         }
     }
     if (blockIdx.x == 0) {
@@ -478,19 +506,22 @@ __global__ __launch_bounds__(kListThreads) void lists_place_kernel(ExpertLists L
             }
     }
     __syncthreads();
-    for (int64_t p0 = first; p0 < end; p0 += 64) {
-        const int64_t p = p0 + lane;
-        const int b = p < end ? bucket_of(experts_of[p], experts) : -1;
-        // the lanes with the same expert, by its bits
-        uint64_t same = __ballot(b >= 0);
-        for (int bit = 0; bit < 11; ++bit) {
-            const uint64_t set = __ballot(b >> bit & 1);
-            same &= b >> bit & 1 ? set : ~set;
+    const int bits = 32 - __clz(experts);                    // (experts is the bucket of the pairs without one)
+    for (int64_t p0 = first; p0 < end; p0 += 256) {
+        if (p0 > first || chunk > 256 * kListWaves) buckets_of(p0, b);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            // the lanes with the same expert, by its bits
+            uint64_t same = __ballot(b[i] >= 0);
+            for (int bit = 0; bit < bits; ++bit) {
+                const uint64_t set = __ballot(b[i] >> bit & 1);
+                same &= b[i] >> bit & 1 ? set : ~set;
+            }
+            if (b[i] >= 0) L.order[at[wave * buckets + b[i]] + __popcll(same & ((1ull << lane) - 1))] = (int32_t)(p0 + i * 64 + lane);
+            __builtin_amdgcn_wave_barrier();
+            if (b[i] >= 0 && (same >> lane) == 1) at[wave * buckets + b[i]] += __popcll(same);        // the highest of them
+            __builtin_amdgcn_wave_barrier();
         }
-        if (b >= 0) L.order[at[wave * buckets + b] + __popcll(same & ((1ull << lane) - 1))] = (int32_t)p;
-        __builtin_amdgcn_wave_barrier();
-        if (b >= 0 && (same >> lane) == 1) at[wave * buckets + b] += __popcll(same);      // the highest of them
-        __builtin_amdgcn_wave_barrier();
     }
 }
 
