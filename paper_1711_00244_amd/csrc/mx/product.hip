@@ -167,6 +167,8 @@ struct FinishArgs {
     int tokens, k, experts, M, pitch, splits, act, out_width;
 };
 
+constexpr int kTogether = 4;
+
 template <class T> __global__ __launch_bounds__(256) void mx_finish_kernel(FinishArgs a, int quads)
 {
     const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
@@ -174,36 +176,49 @@ template <class T> __global__ __launch_bounds__(256) void mx_finish_kernel(Finis
     if (t >= a.tokens) return;
     const int m = (int)(at - t * quads) * 4;
     f32x4 sum = {0, 0, 0, 0};
-    for (int j = 0; j < a.k; ++j) {
-        const int64_t pair = t * a.k + j;
-        const int e = a.experts_of ? a.experts_of[pair] : 0;
-        if (e < 0 || e >= a.experts) continue;
-        const float *p = a.part + pair * a.pitch + m;
-        f32x4 v = *(const f32x4 *)p;
-        if (a.splits > 1) {
-            f32x4 more[7];                                   // (all on their way together; at most eight)
+    for (int j0 = 0; j0 < a.k; j0 += kTogether) {
+        // what kTogether pairs need, on its way together
+        int e[kTogether];
+        float weight[kTogether];
+        f32x4 v[kTogether], bias[kTogether];
+#pragma unroll
+        for (int i = 0; i < kTogether; ++i) {
+            const int64_t pair = t * a.k + min(j0 + i, a.k - 1);
+            e[i] = a.experts_of ? a.experts_of[pair] : 0;
+            weight[i] = a.weights ? a.weights[pair] : 1.0f;
+            v[i] = *(const f32x4 *)(a.part + pair * a.pitch + m);
+        }
+        if (a.splits > 1) {                                  // (at most eight; then k is 1)
+            const float *p = a.part + t * a.pitch + m;
+            f32x4 more[7];
 #pragma unroll
             for (int s = 1; s < 8; ++s) more[s - 1] = *(const f32x4 *)(p + min(s, a.splits - 1) * a.split_stride);
 #pragma unroll
             for (int s = 1; s < 8; ++s)
-                if (s < a.splits) v += more[s - 1];
+                if (s < a.splits) v[0] += more[s - 1];
         }
         if (a.bias) {
-            const float *b = a.bias + (int64_t)e * a.M + m;
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                if (m + i < a.M) v[i] += b[i];
+            for (int i = 0; i < kTogether; ++i) {
+                const float *b = a.bias + (int64_t)(e[i] >= 0 && e[i] < a.experts ? e[i] : 0) * a.M;
+#pragma unroll
+                for (int c = 0; c < 4; ++c) bias[i][c] = b[min(m + c, a.M - 1)];
+            }
         }
-        if (a.act == CL_ACT_GATED) {
-            v[0] = v[0] / (1.0f + expf(-v[0])) * v[1];
-            v[1] = v[2] / (1.0f + expf(-v[2])) * v[3];
-        } else if (a.act == CL_ACT_RELU) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] = v[i] < 0.0f ? 0.0f : v[i];
+        for (int i = 0; i < kTogether; ++i) {
+            if (j0 + i >= a.k || e[i] < 0 || e[i] >= a.experts) continue;
+            if (a.bias) v[i] += bias[i];
+            if (a.act == CL_ACT_GATED) {
+                v[i][0] = v[i][0] / (1.0f + expf(-v[i][0])) * v[i][1];
+                v[i][1] = v[i][2] / (1.0f + expf(-v[i][2])) * v[i][3];
+            } else if (a.act == CL_ACT_RELU) {
+#pragma unroll
+                for (int c = 0; c < 4; ++c) v[i][c] = v[i][c] < 0.0f ? 0.0f : v[i][c];
+            }
+#pragma unroll
+            for (int c = 0; c < 4; ++c) sum[c] = fmaf(weight[i], v[i][c], sum[c]);
         }
-        const float weight = a.weights ? a.weights[pair] : 1.0f;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) sum[i] = fmaf(weight, v[i], sum[i]);
     }
     const int n = a.act == CL_ACT_GATED ? 2 : 4, out = a.act == CL_ACT_GATED ? m / 2 : m;
     T *y = (T *)a.Y + t * a.out_width + out;
@@ -235,11 +250,13 @@ struct Choice {
     int splits;
 };
 
-// What a form takes in microseconds, from measurements over M 1000 .. 4096, 16 .. 4096 columns, K 4096 .. 25088 (within a
-// quarter of each).  Tiles: a start (launch, first loads, last stores), and per step of 128 k what a workgroup takes alone on its
-// compute unit, or its share of a full one where the launch has more workgroups than the chip has compute units.
-struct Price { int bm, bn, width; float start, alone, shared; };
-constexpr Price kPrices[] = {{64, 64, 1, 3.5f, 0.15f, 0.18f}, {128, 128, 2, 4.5f, 0.50f, 0.40f}, {256, 128, 2, 6.0f, 0.70f, 0.70f}, {256, 256, 3, 8.0f, 0.90f, 1.05f}};
+// What a form takes in microseconds, from measurements over M 358 .. 4096, 16 .. 8192 columns, K 636 .. 25088, one matrix and 5 to
+// 64 (most within a quarter).  Tiles: a start (launch, first loads, last stores), and per step of 128 k what a workgroup takes
+// alone on its compute unit, or its share of a full one where the launch has more workgroups than the chip has compute
+// units; that is more with experts, whose matrices change within a launch.
+struct Price { int bm, bn, width; float start, alone, shared, shared_experts; };
+constexpr Price kPrices[] = {{64, 64, 1, 3.5f, 0.15f, 0.18f, 0.25f}, {128, 128, 2, 4.5f, 0.50f, 0.40f, 0.45f}, {256, 128, 2, 6.0f, 0.70f, 0.70f, 0.70f},
+                             {256, 256, 3, 8.0f, 0.90f, 1.05f, 1.05f}};
 constexpr int kCus = 256;
 
 // rows: columns of the product in all; lists: how many runs they are cut into (experts, or 1), each of which fills its last tile
@@ -253,16 +270,15 @@ static Choice choose(int M, int blocks, int64_t rows, int64_t lists, bool part)
     const float wgs = (float)((M + 15) / 16) * (float)tiles_of(16);
     Choice best{kRows, 0, 1};
     float least = 2.5f + std::max(1.12e-3f * wgs * runs, 1.0f + 0.9f * ((runs + kRowsWaves - 1) / kRowsWaves));
-    if (steps < 4) return best;                              // (the tile kernels read scales four steps at a time)
     for (int f = kTile64; f <= kTile256; ++f) {
         const Price &p = kPrices[f - kTile64];
         const int64_t n = tiles_of(p.bn) * ((M + p.bm - 1) / p.bm);
-        const bool alone = f >= kTile256x128;                // (one workgroup to a compute unit: whole rounds)
-        for (int splits = 1; splits <= 8 && steps / splits >= 4; splits *= 2) {
+        const bool alone = f >= kTile256x128;                // (one workgroup to a compute unit: whole rounds; else two, which hide starts)
+        for (int splits = 1; splits <= 8 && (splits == 1 || steps / splits >= 4); splits *= 2) {
             if (splits > 1 && (lists > 1 || n * splits > 2 * kCus)) break;
             const float full = (float)(n * splits) / kCus, rounds = std::max(1.0f, std::ceil(full));
-            const float each = full <= 1.0f ? p.alone : std::max(p.alone, p.shared * (alone ? rounds : full));
-            float us = p.start * (alone ? rounds : 1.0f) + each * (steps + splits - 1) / splits;
+            const float each = full <= 1.0f ? p.alone : std::max(p.alone, (lists > 1 ? p.shared_experts : p.shared) * (alone ? rounds : full));
+            float us = p.start * (alone ? rounds : 1.0f + 0.4f * std::max(0.0f, full / 2 - 1)) + each * (steps + splits - 1) / splits;
             if (splits > 1) us += (part ? 0.0f : 3.5f) + (float)(2 * splits - 1) * rows * M * 1e-6f;
             if (us < least) least = us, best = Choice{(Form)f, p.width, splits};
         }

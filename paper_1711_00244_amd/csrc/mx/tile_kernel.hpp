@@ -48,22 +48,24 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void mx_tile_kernel(ProductArgs a,
     typedef const __attribute__((address_space(1))) void *global_ptr;
     const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = (int)(threadIdx.x & 63), r = lane & 15, g = lane >> 4;
 
+    // Workgroups go to the eight dies in turn.  Each die takes a run of tiles - with one matrix and large tiles four columns of
+    // tiles at a time - so that what it has in flight shares rows of W and of X in its cache.  (4096 x 8192 x 4096: 121 us, tiles in
+    // order 125; 15 experts of 561 x 3661, 4784 pairs, 64 x 64: 25 us, in order 31.  With one matrix and small tiles the order as
+    // it is is 2 % faster; so it is, by 8 %, with experts and the largest, few to a die, which the fuller experts' die then
+    // waits for.)
     int column, m0;
-    if (BM * BN >= 128 * 128 && !a.order) {
-        // Workgroups go to the eight dies in turn.  Each die takes a run of tiles, four columns of tiles at a time, so that
-        // what it has in flight shares rows of W and of X in its cache.  (4096 x 8192 x 4096: 121 us, tiles in order 125.  With
-        // smaller tiles, and with the short columns of experts, the order as it is is 2 % faster.)
-        const int columns = (a.rows + BN - 1) / BN, tiles = columns * row_tiles;
+    const int columns = a.order ? *a.tile_count : (a.rows + BN - 1) / BN, tiles = columns * row_tiles;
+    if (a.order ? BM * BN <= 128 * 128 : BM * BN >= 128 * 128) {
         const int per = tiles / 8, more = tiles % 8, die = (int)blockIdx.x % 8, i = (int)blockIdx.x / 8;
         if (i >= per + (die < more)) return;
-        const int tile = die * per + min(die, more) + i, four = tile / (4 * row_tiles), in = tile - four * (4 * row_tiles);
-        const int across = min(4, columns - 4 * four);
-        column = 4 * four + in % across;
+        const int tile = die * per + min(die, more) + i, band = a.order ? 1 : 4;
+        const int first = tile / (band * row_tiles) * band, in = tile - first * row_tiles, across = min(band, columns - first);
+        column = first + in % across;
         m0 = in / across * BM;
     } else {
+        if ((int)blockIdx.x >= tiles) return;
         column = (int)blockIdx.x / row_tiles;
         m0 = ((int)blockIdx.x - column * row_tiles) * BM;
-        if (!a.order && column * BN >= a.rows) return;
     }
     Columns c;
     if (!columns_of<BN>(a, column, c)) return;
@@ -89,7 +91,8 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void mx_tile_kernel(ProductArgs a,
 #pragma unroll
     for (int i = 0; i < C::kScaleShare; ++i) {
         const int row = scale_load(i) * 64 + lane;
-        scale_at[i] = row < BM ? a.w_scales + (w_first + min(m0 + row, a.M - 1)) * a.blocks : a.x_scales + x_row(row - BM) * a.blocks;
+        // (a row of fewer than four steps is read below, and what these loads bring is not used)
+        scale_at[i] = all_steps < 4 ? a.w_codes : row < BM ? a.w_scales + (w_first + min(m0 + row, a.M - 1)) * a.blocks : a.x_scales + x_row(row - BM) * a.blocks;
     }
     // code load k of step t into its buffer
     auto request_code = [&](int t, uint8_t *buf, int k) {
@@ -98,10 +101,10 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void mx_tile_kernel(ProductArgs a,
     // scale load k of steps 4 q .. 4 q + 3.  (One word a step and row would be a load of 64 cache lines each time.)  Where fewer
     // than four steps are left in the row, its last four are loaded: shift(q) words in front of what is wanted.
     auto request_scales = [&](int q, uint8_t *buf, int k) {
-        const int at = min(t_first + 4 * q, all_steps - 4);
+        const int at = max(0, min(t_first + 4 * q, all_steps - 4));
         __builtin_amdgcn_global_load_lds((global_ptr)(scale_at[k] + (int64_t)at * 4), (lds_ptr)(buf + scale_load(k) * 1024), 16, 0, 0);
     };
-    auto shift = [&](int q) { return t_first + 4 * q - min(t_first + 4 * q, all_steps - 4); };
+    auto shift = [&](int q) { return all_steps < 4 ? 0 : t_first + 4 * q - min(t_first + 4 * q, all_steps - 4); };
 
     const bool idle = (wave % WN) * TJ * 16 >= c.count;      // no columns: the wavefront loads, and multiplies nothing
     const int wi = (wave / WN) * TI * 16 + r, wj = BM + (wave % WN) * TJ * 16 + r;        // the lane's rows of the buffer
@@ -110,15 +113,27 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void mx_tile_kernel(ProductArgs a,
     // The scales of a row's four steps, by step when they arrive, are turned in place (a thread per row) so that the word of
     // block g has its bytes of the four steps: one read for four multiplies, which pick their byte.  (Reading a byte a
     // step, the LDS reads of scales took a third of the time: 4096 x 4096 x 25088 240 us.)
+    auto turned = [&](u32x4 v, int late) {
+        const uint32_t ab01 = __builtin_amdgcn_perm(v[1], v[0], 0x05010400), ab23 = __builtin_amdgcn_perm(v[1], v[0], 0x07030602);
+        const uint32_t cd01 = __builtin_amdgcn_perm(v[3], v[2], 0x05010400), cd23 = __builtin_amdgcn_perm(v[3], v[2], 0x07030602);
+        return u32x4{__builtin_amdgcn_perm(cd01, ab01, 0x05040100) >> late, __builtin_amdgcn_perm(cd01, ab01, 0x07060302) >> late,
+                     __builtin_amdgcn_perm(cd23, ab23, 0x05040100) >> late, __builtin_amdgcn_perm(cd23, ab23, 0x07060302) >> late};
+    };
     auto turn_scales = [&](uint8_t *buf, int q) {
         if (threadIdx.x >= BM + BN) return;
         u32x4 *at = (u32x4 *)(buf + threadIdx.x * 16);
-        const u32x4 v = *at;
-        const uint32_t ab01 = __builtin_amdgcn_perm(v[1], v[0], 0x05010400), ab23 = __builtin_amdgcn_perm(v[1], v[0], 0x07030602);
-        const uint32_t cd01 = __builtin_amdgcn_perm(v[3], v[2], 0x05010400), cd23 = __builtin_amdgcn_perm(v[3], v[2], 0x07030602);
-        const int late = 8 * shift(q);
-        *at = u32x4{__builtin_amdgcn_perm(cd01, ab01, 0x05040100) >> late, __builtin_amdgcn_perm(cd01, ab01, 0x07060302) >> late,
-                    __builtin_amdgcn_perm(cd23, ab23, 0x05040100) >> late, __builtin_amdgcn_perm(cd23, ab23, 0x07060302) >> late};
+        *at = turned(*at, 8 * shift(q));
+    };
+    // (apart from the above: a load into registers there would have every turn wait for all loads on their way)
+    auto short_scales = [&](uint8_t *buf) {
+        if (threadIdx.x >= BM + BN) return;
+        const int row = (int)threadIdx.x;
+        const uint8_t *from = row < BM ? a.w_scales + (w_first + min(m0 + row, a.M - 1)) * a.blocks : a.x_scales + x_row(row - BM) * a.blocks;
+        u32x4 v = {0, 0, 0, 0};
+#pragma unroll
+        for (int i = 0; i < 3; ++i)
+            if (i < all_steps) v[i] = ((const uint32_t *)from)[i];
+        *(u32x4 *)(buf + row * 16) = turned(v, 0);
     };
     auto read_scales = [&](const uint8_t *buf, int row) { return *(const int *)(buf + row * 16 + g * 4); };
 
@@ -214,7 +229,8 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void mx_tile_kernel(ProductArgs a,
             for (int k = 0; k < C::kCodeLoads; ++k) request_code(min(t, last), buffer(t), k);
         __builtin_amdgcn_s_waitcnt(kWaitLoads | (D - 2) * C::kCodeLoads);
         barrier();
-        turn_scales(scales(0), 0);
+        if (all_steps < 4) short_scales(scales(0));
+        else turn_scales(scales(0), 0);
         __builtin_amdgcn_s_waitcnt(kWaitLds);
         barrier();
 #pragma unroll
