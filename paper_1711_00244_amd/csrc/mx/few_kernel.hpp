@@ -21,7 +21,6 @@ struct FewArgs {
     const int32_t *experts_of;
     const float *weights;
     int k, rows_each, x_per_pair;
-    int x_wide;                                              // rows of X are 16-byte aligned
 };
 
 inline size_t few_lds(int blocks, int columns) { return (size_t)columns * blocks * 17; }
@@ -43,7 +42,7 @@ template <class X, class T, bool EXPERTS> __global__ __launch_bounds__(kFewWaves
     const int per_row = p.blocks * 4, units = a.columns * per_row, threads = (int)blockDim.x;
     auto load = [&](int u, float *x) {
         const int row = u / per_row, k0 = (u - row * per_row) * kUnit;
-        load_unit<kUnit>((const X *)a.X + (EXPERTS ? token * (a.x_per_pair ? a.k : 1) + row : row) * a.x_stride + k0, a.K - k0, a.x_wide, x);
+        load_unit<kUnit>((const X *)a.X + (EXPERTS ? token * (a.x_per_pair ? a.k : 1) + row : row) * a.x_stride + k0, a.K - k0, x);
     };
     auto quantise = [&](int u, const float *x) {             // (a row has whole blocks: a quad's lanes stay together)
         uint32_t byte;

@@ -72,12 +72,16 @@ __device__ __forceinline__ float to_float(float x) { return x; }
 __device__ __forceinline__ float to_float(bf16_t x) { return (float)x; }
 __device__ __forceinline__ float to_float(f16_t x) { return (float)x; }
 
-// V consecutive elements of a row, of which `left` exist.  `wide`: p is aligned to 16 bytes, or to all V.
-template <int V, class T> __device__ __forceinline__ void load_unit(const T *p, int left, bool wide, float *x)
+// N consecutive values at any element's address, with one access (gfx950 takes any alignment).
+template <int N, class T> __device__ __forceinline__ void load_values(const T *p, T *v) { __builtin_memcpy(v, p, N * sizeof(T)); }
+template <int N, class T> __device__ __forceinline__ void store_values(T *p, const T *v) { __builtin_memcpy(p, v, N * sizeof(T)); }
+
+// V consecutive elements of a row, of which `left` exist.
+template <int V, class T> __device__ __forceinline__ void load_unit(const T *p, int left, float *x)
 {
-    if (wide && left >= V) {
+    if (left >= V) {
         T v[V];
-        __builtin_memcpy(v, __builtin_assume_aligned(p, V * sizeof(T) < 16 ? V * sizeof(T) : 16), sizeof v);
+        load_values<V>(p, v);
 #pragma unroll
         for (int i = 0; i < V; ++i) x[i] = to_float(v[i]);
     } else {

@@ -26,7 +26,6 @@ struct ProductArgs {
     float *part;                                             // not null: sums of a share of k, [split][row of Y][pitch], to be finished
     int splits, pitch;
     int tile0;                                               // tile of the launch's blockIdx.y of 0
-    int y_wide;                                              // rows of Y are whole aligned fours
     int skip_unrouted;                                       // the rows of Y of pairs without an expert are not read
 };
 
@@ -52,10 +51,16 @@ template <class T> __device__ __forceinline__ void store_outputs(const ProductAr
 {
     if (m >= a.M) return;
     if (a.bias) {
-        const float *b = a.bias + (int64_t)expert * a.M + m;
+        const float *at = a.bias + (int64_t)expert * a.M + m;
+        float b[4];
+        if (m + 4 <= a.M) {
+            load_values<4>(at, b);
+        } else {
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (m + i < a.M) v[i] += b[i];
+            for (int i = 0; i < 4; ++i) b[i] = m + i < a.M ? at[i] : 0.0f;
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] += b[i];
     }
     T *y = (T *)a.Y + row * a.out_width;
     if (a.act == CL_ACT_GATED) {
@@ -70,8 +75,8 @@ template <class T> __device__ __forceinline__ void store_outputs(const ProductAr
     T out[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) out[i] = (T)(a.act == CL_ACT_RELU && v[i] < 0.0f ? 0.0f : v[i]);      // (NaN stays)
-    if (a.y_wide) {
-        __builtin_memcpy(__builtin_assume_aligned(y, sizeof out), out, sizeof out);
+    if (m + 4 <= a.M) {
+        store_values<4>(y, out);
     } else {
 #pragma unroll
         for (int i = 0; i < 4; ++i)
@@ -200,9 +205,15 @@ template <class T> __global__ __launch_bounds__(256) void mx_finish_kernel(Finis
         if (a.bias) {
 #pragma unroll
             for (int i = 0; i < kTogether; ++i) {
-                const float *b = a.bias + (int64_t)(e[i] >= 0 && e[i] < a.experts ? e[i] : 0) * a.M;
+                const float *at = a.bias + (int64_t)(e[i] >= 0 && e[i] < a.experts ? e[i] : 0) * a.M + m;
+                float b[4];
+                if (m + 4 <= a.M) {
+                    load_values<4>(at, b);
+                } else {
 #pragma unroll
-                for (int c = 0; c < 4; ++c) bias[i][c] = b[min(m + c, a.M - 1)];
+                    for (int c = 0; c < 4; ++c) b[c] = at[min(c, a.M - 1 - m)];
+                }
+                bias[i] = f32x4{b[0], b[1], b[2], b[3]};
             }
         }
 #pragma unroll
@@ -222,8 +233,13 @@ template <class T> __global__ __launch_bounds__(256) void mx_finish_kernel(Finis
     }
     const int n = a.act == CL_ACT_GATED ? 2 : 4, out = a.act == CL_ACT_GATED ? m / 2 : m;
     T *y = (T *)a.Y + t * a.out_width + out;
-    for (int i = 0; i < n; ++i)
-        if (out + i < a.out_width) y[i] = (T)sum[i];
+    if (out + 4 <= a.out_width && n == 4) {
+        const T v[4] = {(T)sum[0], (T)sum[1], (T)sum[2], (T)sum[3]};
+        store_values<4>(y, v);
+    } else {
+        for (int i = 0; i < n; ++i)
+            if (out + i < a.out_width) y[i] = (T)sum[i];
+    }
 }
 
 template <int BM, int BN, int WM, int WN, int D, class T> static int32_t launch_tiles(const ProductArgs &a, int64_t tiles, hipStream_t st)
@@ -320,10 +336,6 @@ template <class T> static int32_t launch_product(ProductArgs a, const Choice &c,
     return CL_OK;
 }
 
-static bool wide_rows(const ProductArgs &a, int32_t y_type) { return a.out_width % 4 == 0 && aligned(a.Y, 4 * type_bytes(y_type)); }
-
-static int wide_input(const cl_mx_input &X) { return aligned(X.d_X, 16) && X.stride * (int64_t)type_bytes(X.type) % 16 == 0; }
-
 // Whether few_kernel takes a call.  One matrix: up to four rows.  Experts: where reading a matrix once for every token that
 // is sent to it, and not once, costs less than the launches that sort the tokens by expert.
 static bool few_fc(int blocks, int batch, int32_t x_type)
@@ -359,7 +371,6 @@ static int32_t run_product(ProductArgs a, const Choice &c, const ExpertLists *L,
                            const float *weights, hipStream_t st)
 {
     a.Y = Y;
-    a.y_wide = wide_rows(a, y_type);
     if (!a.part) return with_type(y_type, [&](auto t) { return launch_product<decltype(t)>(a, c, L, st); });
     if (int32_t rc = launch_product<float>(a, c, L, st)) return rc;
     const FinishArgs f{a.part, a.bias, weights, experts_of, Y, (int64_t)a.rows * a.pitch, tokens, k, experts_of ? a.experts : 1, a.M, a.pitch, c.splits, a.act, a.out_width};
@@ -500,8 +511,7 @@ extern "C" int32_t cl_mx_fc_forward(const cl_mx_matrix *W, const cl_mx_input *X,
     a.out_width = act == CL_ACT_GATED ? W->rows / 2 : W->rows;
     if (few_fc(a.blocks, batch, X->type)) {
         a.Y = d_Y;
-        a.y_wide = wide_rows(a, y_type);
-        const FewArgs f{a, X->d_X, X->stride, W->K, batch, nullptr, nullptr, 1, 0, 0, wide_input(*X)};
+        const FewArgs f{a, X->d_X, X->stride, W->K, batch, nullptr, nullptr, 1, 0, 0};
         if (int32_t rc = launch_few(f, X->type, y_type, false, dim3((unsigned)((a.M + 15) / 16)), st)) return rc;
         clear_error();
         return CL_OK;
@@ -561,7 +571,7 @@ extern "C" int32_t cl_mx_experts_forward(const cl_mx_matrix *W, int32_t experts,
     if (few_experts(a.blocks, a.M, X->type, experts, *call)) {
         a.Y = d_Y;
         const int rows_each = 32 / k / 2 * 2;                // (even: a gated product's rows come in pairs)
-        const FewArgs f{a, X->d_X, X->stride, W->K, call->x_per_pair ? k : 1, call->d_experts, call->d_weights, k, rows_each, call->x_per_pair, wide_input(*X)};
+        const FewArgs f{a, X->d_X, X->stride, W->K, call->x_per_pair ? k : 1, call->d_experts, call->d_weights, k, rows_each, call->x_per_pair};
         if (int32_t rc = launch_few(f, X->type, y_type, true, dim3((unsigned)((a.M + rows_each - 1) / rows_each), (unsigned)tokens), st)) return rc;
         clear_error();
         return CL_OK;

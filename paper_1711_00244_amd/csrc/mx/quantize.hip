@@ -30,13 +30,21 @@ static Div make_div(uint32_t d)
 // values a lane - two stores that each fill half of every line - and through the caches it was 223, back alone 133.
 constexpr int kUnits = 2;
 
-template <class T> struct Unit {
-    static constexpr int kValues = 16 / (int)sizeof(T);
-    typedef typename std::conditional<sizeof(T) == 4, uint16_t, uint32_t>::type Codes;
-    typedef uint32_t Bytes __attribute__((ext_vector_type(4)));
+// (An element's alignment is enough for an access of 16 bytes.)
+template <int BYTES> struct UnitOf;
+template <> struct UnitOf<4> {
+    static constexpr int kValues = 4;
+    typedef uint16_t Codes;
+    typedef uint32_t Bytes __attribute__((ext_vector_type(4), aligned(4)));
 };
+template <> struct UnitOf<2> {
+    static constexpr int kValues = 8;
+    typedef uint32_t Codes;
+    typedef uint32_t Bytes __attribute__((ext_vector_type(4), aligned(2)));
+};
+template <class T> using Unit = UnitOf<(int)sizeof(T)>;
 
-template <class T, bool ALIGNED, bool STREAM>
+template <class T, bool STREAM>
 __global__ __launch_bounds__(256) void mx_quantize_kernel(const T *__restrict__ X, int64_t stride, uint32_t units, Div per_row, int K,
                                                           void *__restrict__ codes, uint8_t *__restrict__ scales)
 {
@@ -49,14 +57,14 @@ __global__ __launch_bounds__(256) void mx_quantize_kernel(const T *__restrict__ 
         const uint32_t u = min(first + i * 256u, units - 1), row = per_row.quotient(u);
         const int k0 = (int)(u - row * per_row.d) * V, left = K - k0;
         const T *p = X + (int64_t)row * stride + k0;
-        if (ALIGNED && STREAM && left >= V) {
+        if (STREAM && left >= V) {
             const typename U::Bytes v = __builtin_nontemporal_load((const typename U::Bytes *)p);
             T t[V];
             __builtin_memcpy(t, &v, 16);
 #pragma unroll
             for (int j = 0; j < V; ++j) x[i][j] = to_float(t[j]);
         } else {
-            load_unit<V>(p, left, ALIGNED, x[i]);
+            load_unit<V>(p, left, x[i]);
         }
     }
 #pragma unroll
@@ -71,7 +79,7 @@ __global__ __launch_bounds__(256) void mx_quantize_kernel(const T *__restrict__ 
     }
 }
 
-template <class T, bool ALIGNED, bool STREAM>
+template <class T, bool STREAM>
 __global__ __launch_bounds__(256) void mx_dequantize_kernel(const void *__restrict__ codes, const uint8_t *__restrict__ scales, uint32_t units,
                                                             Div per_row, int K, T *__restrict__ Y, int64_t stride)
 {
@@ -104,7 +112,7 @@ __global__ __launch_bounds__(256) void mx_dequantize_kernel(const void *__restri
 #pragma unroll
         for (int j = 0; j < V; ++j) y[j] = (T)(v[j / 2][j % 2] * s);
         T *out = Y + (int64_t)row * stride + k0;
-        if (ALIGNED && left >= V) {
+        if (left >= V) {
             typename U::Bytes b;
             __builtin_memcpy(&b, y, 16);
             if (STREAM) __builtin_nontemporal_store(b, (typename U::Bytes *)out);
@@ -119,17 +127,16 @@ __global__ __launch_bounds__(256) void mx_dequantize_kernel(const void *__restri
 
 // launch(rows before it, units, kernel of these types) for pieces of at most 2^30 units, so that their numbers and the grid fit 32
 // bits.  Numbers go past the caches where they take more than a quarter of the last one (256 MB).
-template <class T, class F> static int32_t in_pieces(const void *x, int64_t stride, int64_t rows, int32_t K, F launch)
+template <class T, class F> static int32_t in_pieces(int64_t rows, int32_t K, F launch)
 {
     const uint32_t per_row = (uint32_t)(row_blocks(K) * (32 / Unit<T>::kValues));
     const int64_t step = std::max<int64_t>(1, ((int64_t)1 << 30) / per_row);
-    const bool wide = aligned(x, 16) && (stride * (int64_t)sizeof(T)) % 16 == 0, stream = rows * K * (int64_t)sizeof(T) > (64 << 20);
+    const bool stream = rows * K * (int64_t)sizeof(T) > (64 << 20);
     for (int64_t r = 0; r < rows; r += step) {
         const uint32_t units = (uint32_t)std::min(step, rows - r) * per_row;
         const dim3 grid((units + 256 * kUnits - 1) / (256 * kUnits));
-        if (!wide) launch(std::false_type{}, std::false_type{}, grid, r, units, make_div(per_row));
-        else if (!stream) launch(std::true_type{}, std::false_type{}, grid, r, units, make_div(per_row));
-        else launch(std::true_type{}, std::true_type{}, grid, r, units, make_div(per_row));
+        if (stream) launch(std::true_type{}, grid, r, units, make_div(per_row));
+        else launch(std::false_type{}, grid, r, units, make_div(per_row));
         MX_HIP_TRY(hipGetLastError());
     }
     return CL_OK;
@@ -140,8 +147,8 @@ int32_t launch_quantize(const void *X, int32_t type, int64_t stride, int64_t row
     const int64_t kb = row_blocks(K);
     return with_type(type, [&](auto t) -> int32_t {
         using T = decltype(t);
-        return in_pieces<T>(X, stride, rows, K, [&](auto wide, auto stream, dim3 grid, int64_t r, uint32_t units, Div per_row) {
-            hipLaunchKernelGGL((mx_quantize_kernel<T, wide.value, stream.value>), grid, dim3(256), 0, st, (const T *)X + r * stride, stride, units, per_row, K,
+        return in_pieces<T>(rows, K, [&](auto stream, dim3 grid, int64_t r, uint32_t units, Div per_row) {
+            hipLaunchKernelGGL((mx_quantize_kernel<T, stream.value>), grid, dim3(256), 0, st, (const T *)X + r * stride, stride, units, per_row, K,
                                (void *)(codes + r * kb * 16), scales + r * kb);
         });
     });
@@ -180,8 +187,8 @@ extern "C" int32_t cl_mx_dequantize(const void *d_codes, const void *d_scales, i
     const int64_t kb = row_blocks(K);
     const int32_t rc = with_type(type, [&](auto t) -> int32_t {
         using T = decltype(t);
-        return in_pieces<T>(d_Y, y_stride, rows, K, [&](auto wide, auto stream_, dim3 grid, int64_t r, uint32_t units, Div per_row) {
-            hipLaunchKernelGGL((mx_dequantize_kernel<T, wide.value, stream_.value>), grid, dim3(256), 0, (hipStream_t)stream,
+        return in_pieces<T>(rows, K, [&](auto past, dim3 grid, int64_t r, uint32_t units, Div per_row) {
+            hipLaunchKernelGGL((mx_dequantize_kernel<T, past.value>), grid, dim3(256), 0, (hipStream_t)stream,
                                (const void *)((const uint8_t *)d_codes + r * kb * 16), (const uint8_t *)d_scales + r * kb, units, per_row, K,
                                (T *)d_Y + r * y_stride, y_stride);
         });

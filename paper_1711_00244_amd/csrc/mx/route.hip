@@ -16,7 +16,6 @@ struct RouteArgs {
     int32_t *experts_out;
     float *weights_out;
     int tokens, experts, k, groups, kept, top2, sigmoid, renormalize;
-    int wide;                                                // rows of logits are 16-byte aligned
     float scale;
 };
 
@@ -192,9 +191,9 @@ template <class T, int C> __global__ __launch_bounds__(256) void route_rows_kern
     const int mine = live ? a.experts - sub * C : 0;         // experts of this lane, or more
     float logit[C], score[C];
     float top = -INFINITY;
-    if (a.wide && mine >= C) {
+    if (mine >= C) {
         T v[C];
-        __builtin_memcpy(v, __builtin_assume_aligned(x, C * sizeof(T) < 16 ? C * sizeof(T) : 16), sizeof v);
+        load_values<C>(x, v);
 #pragma unroll
         for (int j = 0; j < C; ++j) logit[j] = to_float(v[j]);
     } else {
@@ -238,7 +237,7 @@ template <class T, int C> __global__ __launch_bounds__(256) void route_rows_kern
         if (a.bias) {
             float bias[C];
             if (mine >= C) {
-                __builtin_memcpy(bias, a.bias + sub * C, sizeof bias);
+                load_values<C>(a.bias + sub * C, bias);
             } else {
 #pragma unroll
                 for (int j = 0; j < C; ++j) bias[j] = a.bias[min(sub * C + j, a.experts - 1)];
@@ -566,7 +565,7 @@ extern "C" int32_t cl_route_experts(const void *d_logits, int32_t type, int64_t 
     if (!d_logits || !d_experts || !d_weights) return fail(CL_EINVAL, "null pointer");
     if (tokens > 1 && x_stride < d.experts) return fail(CL_EINVAL, "rows of %d logits overlap at a stride of %lld", (int)d.experts, (long long)x_stride);
     RouteArgs a{d_logits, x_stride, d_bias, d_experts, d_weights, tokens, d.experts, d.k, d.groups, d.groups_kept, d.group_score == CL_GROUP_TOP2,
-                d.score == CL_SCORE_SIGMOID, d.renormalize, aligned(d_logits, 16) && x_stride * (int64_t)type_bytes(type) % 16 == 0, d.scale};
+                d.score == CL_SCORE_SIGMOID, d.renormalize, d.scale};
     const int32_t rc = with_type(type, [&](auto t) -> int32_t {
         using T = decltype(t);
         hipStream_t st = (hipStream_t)stream;
