@@ -160,7 +160,15 @@ struct ExpertLists {
 constexpr int kTileWidths = 4;
 constexpr int kTileWidth[kTileWidths] = {16, 64, 128, 256};
 ExpertLists expert_lists_at(void *base, int32_t tokens, int32_t k, int32_t experts);
-int32_t launch_expert_lists(const int32_t *experts_of, int32_t tokens, int32_t k, int32_t experts, const ExpertLists &L, hipStream_t st);
+// Rows to quantise in the same launches.
+struct QuantiseRows {
+    const void *X;
+    int32_t type;
+    int64_t stride, rows;
+    int32_t K;
+    uint8_t *codes, *scales;
+};
+int32_t launch_expert_lists(const int32_t *experts_of, int32_t tokens, int32_t k, int32_t experts, const ExpertLists &L, const QuantiseRows *rows_or_null, hipStream_t st);
 
 }  // namespace mx
 }  // namespace cl

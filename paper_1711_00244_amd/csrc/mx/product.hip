@@ -581,9 +581,17 @@ extern "C" int32_t cl_mx_experts_forward(const cl_mx_matrix *W, int32_t experts,
     const Scratch s = experts_scratch(c, W->rows, W->K, X->type, experts, *call);
     if (int32_t rc = check_scratch(s, d_workspace, workspace_bytes)) return rc;
     const ExpertLists L = expert_lists_at(call->d_lists ? const_cast<void *>(call->d_lists) : (uint8_t *)d_workspace + s.lists, tokens, k, experts);
-    if (!call->d_lists)
-        if (int32_t rc = launch_expert_lists(call->d_experts, tokens, k, experts, L, st)) return rc;
-    if (int32_t rc = quantised_input(a, X, x_rows, W->K, s, d_workspace, st)) return rc;
+    if (call->d_lists) {
+        if (int32_t rc = quantised_input(a, X, x_rows, W->K, s, d_workspace, st)) return rc;
+    } else if (X->type == CL_MX4) {
+        if (int32_t rc = launch_expert_lists(call->d_experts, tokens, k, experts, L, nullptr, st)) return rc;
+        if (int32_t rc = quantised_input(a, X, x_rows, W->K, s, d_workspace, st)) return rc;
+    } else {
+        const QuantiseRows rows{X->d_X, X->type, X->stride, x_rows, W->K, (uint8_t *)d_workspace + s.x_codes, (uint8_t *)d_workspace + s.x_scales};
+        a.x_codes = rows.codes;
+        a.x_scales = rows.scales;
+        if (int32_t rc = launch_expert_lists(call->d_experts, tokens, k, experts, L, &rows, st)) return rc;
+    }
     a.x_div = call->x_per_pair ? 1 : k;
     a.order = L.order;
     a.offsets = L.offsets;

@@ -1,83 +1,10 @@
 // Rows of numbers to blocks of 32 four-bit floats under one power-of-two scale (OCP MXFP4: E2M1 elements, E8M0 scale), and back.
-#include <algorithm>
-#include <type_traits>
-
-#include "mx_common.hpp"
+#include "quantize_kernel.hpp"
 
 namespace cl {
 namespace mx {
 
-// Division of a 32-bit number by a run-time constant: a high product and two shifts (round-up method; exact for all n).
-struct Div {
-    uint32_t mul, shift1, shift2, d;
-    __device__ __forceinline__ uint32_t quotient(uint32_t n) const
-    {
-        const uint32_t t = __umulhi(n, mul);
-        return (t + ((n - t) >> shift1)) >> shift2;
-    }
-};
-
-static Div make_div(uint32_t d)
-{
-    uint32_t s = 0;
-    while (s < 32 && (1ull << s) < d) ++s;
-    return Div{(uint32_t)((((1ull << s) - d) << 32) / d + 1), s > 0 ? 1u : 0u, s > 0 ? s - 1 : 0u, d};
-}
-
-// A lane has 16 bytes of numbers at a time - a unit: four or eight, eight or four lanes to a block - so that each load and store
-// of a wavefront is consecutive, and kUnits of those.  STREAM: numbers go past the caches (matrices that would not stay in
-// them).  Memory bounds both: 4096 x 25088 fp32, there and back, 142 us, 931 MB at 6.5 TB/s (a large copy: 5.1).  With eight
-// values a lane - two stores that each fill half of every line - and through the caches it was 223, back alone 133.
-constexpr int kUnits = 2;
-
-// (An element's alignment is enough for an access of 16 bytes.)
-template <int BYTES> struct UnitOf;
-template <> struct UnitOf<4> {
-    static constexpr int kValues = 4;
-    typedef uint16_t Codes;
-    typedef uint32_t Bytes __attribute__((ext_vector_type(4), aligned(4)));
-};
-template <> struct UnitOf<2> {
-    static constexpr int kValues = 8;
-    typedef uint32_t Codes;
-    typedef uint32_t Bytes __attribute__((ext_vector_type(4), aligned(2)));
-};
-template <class T> using Unit = UnitOf<(int)sizeof(T)>;
-
-template <class T, bool STREAM>
-__global__ __launch_bounds__(256) void mx_quantize_kernel(const T *__restrict__ X, int64_t stride, uint32_t units, Div per_row, int K,
-                                                          void *__restrict__ codes, uint8_t *__restrict__ scales)
-{
-    typedef Unit<T> U;
-    constexpr int V = U::kValues, kLanes = 32 / V;
-    float x[kUnits][V];
-    const uint32_t first = blockIdx.x * (256u * kUnits) + threadIdx.x;
-#pragma unroll
-    for (int i = 0; i < kUnits; ++i) {
-        const uint32_t u = min(first + i * 256u, units - 1), row = per_row.quotient(u);
-        const int k0 = (int)(u - row * per_row.d) * V, left = K - k0;
-        const T *p = X + (int64_t)row * stride + k0;
-        if (STREAM && left >= V) {
-            const typename U::Bytes v = __builtin_nontemporal_load((const typename U::Bytes *)p);
-            T t[V];
-            __builtin_memcpy(t, &v, 16);
-#pragma unroll
-            for (int j = 0; j < V; ++j) x[i][j] = to_float(t[j]);
-        } else {
-            load_unit<V>(p, left, x[i]);
-        }
-    }
-#pragma unroll
-    for (int i = 0; i < kUnits; ++i) {
-        const uint32_t u = first + i * 256u;
-        uint32_t byte;
-        const uint32_t c = quantise_unit<V>(x[i], byte);     // (a row has whole blocks: the lanes of one are beyond the end together)
-        if (u < units) {
-            ((typename U::Codes *)codes)[u] = (typename U::Codes)c;
-            if (u % kLanes == 0) scales[u / kLanes] = (uint8_t)byte;
-        }
-    }
-}
+template <class T, bool STREAM> __global__ __launch_bounds__(256) void mx_quantize_kernel(QuantiseArgs a) { quantise_units<T, STREAM>(blockIdx.x, a); }
 
 template <class T, bool STREAM>
 __global__ __launch_bounds__(256) void mx_dequantize_kernel(const void *__restrict__ codes, const uint8_t *__restrict__ scales, uint32_t units,
@@ -126,12 +53,12 @@ __global__ __launch_bounds__(256) void mx_dequantize_kernel(const void *__restri
 }
 
 // launch(rows before it, units, kernel of these types) for pieces of at most 2^30 units, so that their numbers and the grid fit 32
-// bits.  Numbers go past the caches where they take more than a quarter of the last one (256 MB).
+// bits.
 template <class T, class F> static int32_t in_pieces(int64_t rows, int32_t K, F launch)
 {
     const uint32_t per_row = (uint32_t)(row_blocks(K) * (32 / Unit<T>::kValues));
     const int64_t step = std::max<int64_t>(1, ((int64_t)1 << 30) / per_row);
-    const bool stream = rows * K * (int64_t)sizeof(T) > (64 << 20);
+    const bool stream = past_caches(rows * K * (int64_t)sizeof(T));
     for (int64_t r = 0; r < rows; r += step) {
         const uint32_t units = (uint32_t)std::min(step, rows - r) * per_row;
         const dim3 grid((units + 256 * kUnits - 1) / (256 * kUnits));
@@ -148,8 +75,8 @@ int32_t launch_quantize(const void *X, int32_t type, int64_t stride, int64_t row
     return with_type(type, [&](auto t) -> int32_t {
         using T = decltype(t);
         return in_pieces<T>(rows, K, [&](auto stream, dim3 grid, int64_t r, uint32_t units, Div per_row) {
-            hipLaunchKernelGGL((mx_quantize_kernel<T, stream.value>), grid, dim3(256), 0, st, (const T *)X + r * stride, stride, units, per_row, K,
-                               (void *)(codes + r * kb * 16), scales + r * kb);
+            const QuantiseArgs a{(const T *)X + r * stride, codes + r * kb * 16, scales + r * kb, stride, per_row, units, K};
+            hipLaunchKernelGGL((mx_quantize_kernel<T, stream.value>), grid, dim3(256), 0, st, a);
         });
     });
 }

@@ -1,7 +1,7 @@
 // The choice of experts for tokens, and the lists of tokens that each expert is given.
 #include <algorithm>
 
-#include "mx_common.hpp"
+#include "quantize_kernel.hpp"
 
 namespace cl {
 namespace mx {
@@ -388,9 +388,18 @@ ExpertLists expert_lists_at(void *base, int32_t tokens, int32_t k, int32_t exper
 
 __device__ __forceinline__ int bucket_of(int e, int experts) { return e >= 0 && e < experts ? e : experts; }
 
-__global__ __launch_bounds__(kListThreads) void lists_count_kernel(const int32_t *__restrict__ experts_of, int pairs, int chunk, int experts, int32_t *counts)
+struct ListArgs {
+    ExpertLists L;
+    const int32_t *experts_of;
+    int pairs, chunk, chunks, experts;
+};
+
+__device__ __forceinline__ void lists_count(const ListArgs &a)
 {
-    __shared__ int32_t n[CL_ROUTE_MAX_EXPERTS + 1];
+    extern __shared__ int32_t list_lds[];
+    const int32_t *experts_of = a.experts_of;
+    const int pairs = a.pairs, chunk = a.chunk, experts = a.experts;
+    int32_t *counts = a.L.chunk_counts, *n = list_lds;
     for (int b = threadIdx.x; b <= experts; b += kListThreads) n[b] = 0;
     __syncthreads();
     const int64_t p0 = (int64_t)blockIdx.x * chunk, p1 = min((int64_t)pairs, p0 + chunk);
@@ -401,9 +410,12 @@ __global__ __launch_bounds__(kListThreads) void lists_count_kernel(const int32_t
 
 // Every workgroup finds where its own pairs of each expert go (the first: also the tiles), and puts them there.  Wavefront w has the
 // w-th sixteenth of the chunk.
-__global__ __launch_bounds__(kListThreads) void lists_place_kernel(ExpertLists L, const int32_t *__restrict__ experts_of, int pairs, int chunk, int chunks, int experts)
+__device__ __forceinline__ void lists_place(const ListArgs &a)
 {
     extern __shared__ int32_t list_lds[];
+    const ExpertLists &L = a.L;
+    const int32_t *experts_of = a.experts_of;
+    const int pairs = a.pairs, chunk = a.chunk, chunks = a.chunks, experts = a.experts;
     const int buckets = experts + 1, wave = (int)threadIdx.x / 64, lane = (int)threadIdx.x & 63;
     int32_t *at = list_lds;                                  // [wavefront][bucket]: how many, then where the next goes
     int32_t *starts = at + kListWaves * buckets;             // [1 + kTileWidths][bucket + 1]: first pair, first tile of each width
@@ -524,20 +536,59 @@ __global__ __launch_bounds__(kListThreads) void lists_place_kernel(ExpertLists L
     }
 }
 
-int32_t launch_expert_lists(const int32_t *experts_of, int32_t tokens, int32_t k, int32_t experts, const ExpertLists &L, hipStream_t st)
+__global__ __launch_bounds__(kListThreads) void lists_count_kernel(ListArgs a) { lists_count(a); }
+__global__ __launch_bounds__(kListThreads) void lists_place_kernel(ListArgs a) { lists_place(a); }
+
+// The first launch of the lists (COUNT: of two) and the quantisation of the rows that are multiplied next, which do not need each
+// other, in one: the first `chunks` workgroups have the lists.
+template <class T, bool STREAM, bool COUNT> __global__ __launch_bounds__(kListThreads) void mx_prepare_kernel(ListArgs a, QuantiseArgs q)
 {
-    const int pairs = tokens * k, chunk = (int)list_chunk(pairs), chunks = std::max(1, (int)(((int64_t)pairs + chunk - 1) / chunk));
-    if (chunks > 1) {
-        hipLaunchKernelGGL(lists_count_kernel, dim3((unsigned)chunks), dim3(kListThreads), 0, st, experts_of, pairs, chunk, experts, L.chunk_counts);
-        MX_HIP_TRY(hipGetLastError());
-    }
-    const size_t lds = ((size_t)kListWaves * (experts + 1) + (1 + kTileWidths) * ((size_t)experts + 2)) * 4;
+    if ((int)blockIdx.x >= a.chunks) quantise_units<T, STREAM>(blockIdx.x - (uint32_t)a.chunks, q);
+    else if (COUNT) lists_count(a);
+    else lists_place(a);
+}
+
+static size_t list_lds_bytes(int experts) { return ((size_t)kListWaves * (experts + 1) + (1 + kTileWidths) * ((size_t)experts + 2)) * 4; }
+
+static int32_t launch_place(const ListArgs &a, hipStream_t st)
+{
+    const size_t lds = list_lds_bytes(a.experts);
     static LdsLimit seen;
     if (lds > 32768)
-        if (int32_t rc = allow_lds((const void *)lists_place_kernel, ((size_t)kListWaves * (CL_ROUTE_MAX_EXPERTS + 1) + (1 + kTileWidths) * (CL_ROUTE_MAX_EXPERTS + 2)) * 4, seen)) return rc;
-    hipLaunchKernelGGL(lists_place_kernel, dim3((unsigned)chunks), dim3(kListThreads), lds, st, L, experts_of, pairs, chunk, chunks, experts);
+        if (int32_t rc = allow_lds((const void *)lists_place_kernel, list_lds_bytes(CL_ROUTE_MAX_EXPERTS), seen)) return rc;
+    hipLaunchKernelGGL(lists_place_kernel, dim3((unsigned)a.chunks), dim3(kListThreads), lds, st, a);
     MX_HIP_TRY(hipGetLastError());
     return CL_OK;
+}
+
+int32_t launch_expert_lists(const int32_t *experts_of, int32_t tokens, int32_t k, int32_t experts, const ExpertLists &L, const QuantiseRows *rows, hipStream_t st)
+{
+    const int pairs = tokens * k, chunk = (int)list_chunk(pairs), chunks = std::max(1, (int)(((int64_t)pairs + chunk - 1) / chunk));
+    const ListArgs a{L, experts_of, pairs, chunk, chunks, experts};
+    const size_t lds = list_lds_bytes(experts);
+    const uint32_t per_row = rows ? (uint32_t)(row_blocks(rows->K) * (rows->type == CL_F32 ? 8 : 4)) : 0;
+    if (rows && (lds > 32768 || rows->rows * per_row > 1 << 30)) {       // (more LDS would keep the quantising workgroups few)
+        if (int32_t rc = launch_quantize(rows->X, rows->type, rows->stride, rows->rows, rows->K, rows->codes, rows->scales, st)) return rc;
+        rows = nullptr;
+    }
+    if (rows) {
+        const QuantiseArgs q{rows->X, rows->codes, rows->scales, rows->stride, make_div(per_row), (uint32_t)(rows->rows * per_row), rows->K};
+        const unsigned wgs = (q.units + kListThreads * kUnits - 1) / (kListThreads * kUnits);
+        const bool stream = past_caches(rows->rows * rows->K * (int64_t)type_bytes(rows->type));
+        const int32_t rc = with_type(rows->type, [&](auto t) -> int32_t {
+            using T = decltype(t);
+            auto kernel = chunks > 1 ? (stream ? mx_prepare_kernel<T, true, true> : mx_prepare_kernel<T, false, true>)
+                                     : (stream ? mx_prepare_kernel<T, true, false> : mx_prepare_kernel<T, false, false>);
+            hipLaunchKernelGGL(kernel, dim3((unsigned)chunks + wgs), dim3(kListThreads), lds, st, a, q);
+            MX_HIP_TRY(hipGetLastError());
+            return CL_OK;
+        });
+        if (rc) return rc;
+    } else if (chunks > 1) {
+        hipLaunchKernelGGL(lists_count_kernel, dim3((unsigned)chunks), dim3(kListThreads), ((size_t)experts + 1) * 4, st, a);
+        MX_HIP_TRY(hipGetLastError());
+    }
+    return rows && chunks == 1 ? (int32_t)CL_OK : launch_place(a, st);
 }
 
 }  // namespace mx
@@ -610,7 +661,7 @@ extern "C" int32_t cl_expert_lists(const int32_t *d_experts, int32_t tokens, int
     if (!d_lists || (tokens && !d_experts)) return fail(CL_EINVAL, "null pointer");
     if (!aligned(d_lists, 256)) return fail(CL_EINVAL, "lists must be 256-byte aligned");
     if (lists_bytes < L.bytes) return fail(CL_EINVAL, "lists need %zu bytes, got %zu", L.bytes, lists_bytes);
-    if (int32_t rc = launch_expert_lists(d_experts, tokens, k, experts, L, (hipStream_t)stream)) return rc;
+    if (int32_t rc = launch_expert_lists(d_experts, tokens, k, experts, L, nullptr, (hipStream_t)stream)) return rc;
     clear_error();
     return CL_OK;
 }

@@ -106,6 +106,13 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void mx_tile_kernel(ProductArgs a,
     };
     auto shift = [&](int q) { return all_steps < 4 ? 0 : t_first + 4 * q - min(t_first + 4 * q, all_steps - 4); };
 
+    // the row of Y of the wavefront's column `lane`
+    static_assert(TJ * 16 <= 64, "");
+    int y_row;
+    {
+        const int at = c.first + min((wave % WN) * TJ * 16 + lane, c.count - 1);
+        y_row = a.order ? a.order[at] : at;
+    }
     const bool idle = (wave % WN) * TJ * 16 >= c.count;      // no columns: the wavefront loads, and multiplies nothing
     const int wi = (wave / WN) * TI * 16 + r, wj = BM + (wave % WN) * TJ * 16 + r;        // the lane's rows of the buffer
     const int at_code = (g ^ (r >> 2)) * 16;
@@ -264,15 +271,14 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void mx_tile_kernel(ProductArgs a,
         for (int i = 0; i < TI; ++i) *(f32x4 *)(mine + r * kPitch + i * 16 + 4 * g) = acc[i][j];
         __builtin_amdgcn_wave_barrier();
         const int first = (wave % WN) * TJ * 16 + j * 16, m = m0 + (wave / WN) * kWide + lane % kLanes * 4;
-#pragma unroll 1
-        for (int n = lane / kLanes; n < 16; n += 64 / kLanes)
-            if (first + n < c.count) {
-                const int at = c.first + first + n;
-                const f32x4 v = *(const f32x4 *)(mine + n * kPitch + lane % kLanes * 4);
-                const int64_t row = a.order ? a.order[at] : at;
-                if (a.part) store_part(a, split, row, m, v);
-                else finish_outputs<T>(a, c.expert, row, m, v);
-            }
+#pragma unroll 2
+        for (int n = lane / kLanes; n < 16; n += 64 / kLanes) {
+            const f32x4 v = *(const f32x4 *)(mine + n * kPitch + lane % kLanes * 4);
+            const int row = __shfl(y_row, j * 16 + n);
+            if (first + n >= c.count) continue;
+            if (a.part) store_part(a, split, row, m, v);
+            else finish_outputs<T>(a, c.expert, row, m, v);
+        }
         __builtin_amdgcn_wave_barrier();
     }
 }
