@@ -2,15 +2,19 @@
 // namespace cl::mx.
 #pragma once
 
-// A workgroup of up to sixteen wavefronts makes the sums of 16 F rows of matrices and up to kFewColumns rows of X.  It quantises
-// those into LDS - every workgroup all of them, which for so few costs less than a launch of its own - while its first weights
-// are on their way; then the wavefronts share out the runs of 16 blocks as in mx_rows_kernel, and their sums meet in LDS.
+// A workgroup of up to sixteen wavefronts makes the sums of 16 F rows of matrices and a few rows of X.  It quantises those into
+// LDS - every workgroup all of them, which for so few costs less than a launch of its own - while its first weights are on
+// their way; then the wavefronts share out the runs of 16 blocks as in mx_rows_kernel, and their sums meet in LDS.
 //
-// One matrix: 16 F consecutive rows of it.  Experts: one token (blockIdx.y), `rows_each` rows of each of its k experts' matrices,
-// which are rows of one matrix instruction like any others, so that a token's weighted sum needs no second launch either.
-// (One token, 64 experts of 1024 x 4096, eight chosen: lists, quantisation, product and sum apart took 33 us in five launches.)
-constexpr int kUnit = 8;                                     // values that a lane quantises at a time
-constexpr int kFewColumns = 4, kFewWaves = kRowsWaves;
+// One matrix: 16 consecutive rows of it, up to kFewColumns rows of X of kFewBlocks blocks together.  (4096 rows, microseconds, here
+// and in two launches: K 4096, one row 4.5 and 6.1, eight 6.1 and 6.5, twelve 7.7 and 6.7; K 9216, one 7.0 and 8.4 - 21 MB, which
+// a large copy moves in 4.1 -, four 8.6 and 8.9; K 25088, one 13.2 and 14.2, two 14.8 and 14.4.  A launch less is some 3 us
+// of the host's time besides.)  What bounds it is how much a compute unit can have on its way.
+// Experts: one token (blockIdx.y), `rows_each` rows of each of its k experts' matrices, which are rows of one matrix instruction
+// like any others, so that a token's weighted sum needs no second launch either.  (One token, 64 experts of 1024 x 4096, eight
+// chosen, 17.8 MB: 8.6 us; lists, quantisation, product and sum apart took 33 in five launches.)
+constexpr int kUnit = 8, kBatch = 4;                         // values that a lane quantises; how often before it asks for more
+constexpr int kFewColumns = 16, kFewBlocks = 1536, kFewWaves = kRowsWaves;
 constexpr size_t kFewLds = 64 << 10;
 
 struct FewArgs {
@@ -21,6 +25,7 @@ struct FewArgs {
     const int32_t *experts_of;
     const float *weights;
     int k, rows_each, x_per_pair;
+    int waves;                                               // wavefronts that multiply; the others only quantise
 };
 
 inline size_t few_lds(int blocks, int columns) { return (size_t)columns * blocks * 17; }
@@ -32,27 +37,33 @@ template <class X, class T, bool EXPERTS> __global__ __launch_bounds__(kFewWaves
     __shared__ f32x4 part[kFewWaves][kFewF][64];
     __shared__ float sums[kFewF * 16];
     const ProductArgs &p = a.p;
-    const int waves = (int)blockDim.x / 64, wave = threadIdx.x / 64, lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
+    const int waves = a.waves, wave = threadIdx.x / 64, lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
     const int64_t token = EXPERTS ? blockIdx.y : 0;
     const int m0 = (int)blockIdx.x * (EXPERTS ? a.rows_each : 16 * kFewF);
     uint8_t *codes = lds, *scales = lds + (size_t)a.columns * p.blocks * 16;
 
-    // the values of this thread's first two units, then the weights of the wavefront's first two runs, then the other units: what
-    // is asked for first arrives first
+    // the values of this thread's first units, then the weights of the wavefront's first two runs, then the other units: what is
+    // asked for first arrives first
     const int per_row = p.blocks * 4, units = a.columns * per_row, threads = (int)blockDim.x;
-    auto load = [&](int u, float *x) {
-        const int row = u / per_row, k0 = (u - row * per_row) * kUnit;
-        load_unit<kUnit>((const X *)a.X + (EXPERTS ? token * (a.x_per_pair ? a.k : 1) + row : row) * a.x_stride + k0, a.K - k0, x);
+    float x[kBatch][kUnit];
+    auto load = [&](int u0) {
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) {
+            const int u = u0 + i * threads, row = u / per_row, k0 = (u - row * per_row) * kUnit;
+            if (u < units) load_unit<kUnit>((const X *)a.X + (EXPERTS ? token * (a.x_per_pair ? a.k : 1) + row : row) * a.x_stride + k0, a.K - k0, x[i]);
+        }
     };
-    auto quantise = [&](int u, const float *x) {             // (a row has whole blocks: a quad's lanes stay together)
-        uint32_t byte;
-        ((uint32_t *)codes)[u] = quantise_unit<kUnit>(x, byte);
-        if ((u & 3) == 0) scales[u >> 2] = (uint8_t)byte;
+    auto quantise = [&](int u0) {                            // (a row has whole blocks: a quad's lanes stay together)
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) {
+            const int u = u0 + i * threads;
+            if (u >= units) continue;
+            uint32_t byte;
+            ((uint32_t *)codes)[u] = quantise_unit<kUnit>(x[i], byte);
+            if ((u & 3) == 0) scales[u >> 2] = (uint8_t)byte;
+        }
     };
-    float x0[kUnit], x1[kUnit];
-    const int u0 = (int)threadIdx.x, u1 = u0 + threads;
-    if (u0 < units) load(u0, x0);
-    if (u1 < units) load(u1, x1);
+    load((int)threadIdx.x);
 
     const uint8_t *w_codes[kFewF], *w_scales[kFewF];
 #pragma unroll
@@ -81,17 +92,16 @@ template <class X, class T, bool EXPERTS> __global__ __launch_bounds__(kFewWaves
             run.scales[f] = in ? *(const int *)(w_scales[f] + b) : 0;
         }
     };
-    const int b0 = wave * 16 + g * 4, stride = (int)blockDim.x / 4;      // (sixteen blocks a wavefront)
+    const int b0 = wave < waves ? wave * 16 + g * 4 : p.blocks + g * 4, stride = waves * 16;
     constexpr bool kTwo = !EXPERTS;                          // (two runs of two rows' fragments do not fit the registers)
     Run even, odd;
     load_run(even, b0);
     if (kTwo) load_run(odd, b0 + stride);
 
-    if (u0 < units) quantise(u0, x0);
-    if (u1 < units) quantise(u1, x1);
-    for (int u = u1 + threads; u < units; u += threads) {
-        load(u, x0);
-        quantise(u, x0);
+    quantise((int)threadIdx.x);
+    for (int u = (int)threadIdx.x + kBatch * threads; u < units; u += kBatch * threads) {
+        load(u);
+        quantise(u);
     }
     __syncthreads();
 
@@ -125,7 +135,8 @@ template <class X, class T, bool EXPERTS> __global__ __launch_bounds__(kFewWaves
         }
     }
 #pragma unroll
-    for (int f = 0; f < kFewF; ++f) part[wave][f][lane] = acc[f];
+    for (int f = 0; f < kFewF; ++f)
+        if (wave < waves) part[wave][f][lane] = acc[f];
     __syncthreads();
     for (int at = threadIdx.x; at < kFewF * 64; at += (int)blockDim.x) {
         const int f = at / 64, l = at & 63;

@@ -25,6 +25,7 @@ struct ProductArgs {
     int x_div;                                               // pair / x_div is its row of X
     float *part;                                             // not null: sums of a share of k, [split][row of Y][pitch], to be finished
     int splits, pitch;
+    int past_caches;                                         // part would not stay in the caches until it is read
     int tile0;                                               // tile of the launch's blockIdx.y of 0
     int skip_unrouted;                                       // the rows of Y of pairs without an expert are not read
 };
@@ -97,7 +98,10 @@ template <class T> __device__ __forceinline__ void finish_outputs(const ProductA
 // Four sums of a share of k.  (A row of partial sums is padded to whole fours.)
 __device__ __forceinline__ void store_part(const ProductArgs &a, int split, int64_t row, int m, f32x4 v)
 {
-    if (m < a.M) *(f32x4 *)(a.part + ((int64_t)split * a.rows + row) * a.pitch + m) = v;
+    if (m >= a.M) return;
+    f32x4 *at = (f32x4 *)(a.part + ((int64_t)split * a.rows + row) * a.pitch + m);
+    if (a.past_caches) __builtin_nontemporal_store(v, at);
+    else *at = v;
 }
 
 // A workgroup of up to sixteen wavefronts makes 16 outputs (blockIdx.x) of 16 NT columns (blockIdx.y).  The wavefronts share out the
@@ -336,11 +340,11 @@ template <class T> static int32_t launch_product(ProductArgs a, const Choice &c,
     return CL_OK;
 }
 
-// Whether few_kernel takes a call.  One matrix: up to four rows.  Experts: where reading a matrix once for every token that
+// Whether few_kernel takes a call.  One matrix: by its measurements.  Experts: where reading a matrix once for every token that
 // is sent to it, and not once, costs less than the launches that sort the tokens by expert.
 static bool few_fc(int blocks, int batch, int32_t x_type)
 {
-    return x_type != CL_MX4 && batch <= kFewColumns && few_lds(blocks, batch) <= kFewLds;
+    return x_type != CL_MX4 && batch <= kFewColumns && batch * blocks <= kFewBlocks && few_lds(blocks, batch) <= kFewLds;
 }
 static bool few_experts(int blocks, int M, int32_t x_type, int experts, const cl_mx_experts_call &call)
 {
@@ -349,9 +353,11 @@ static bool few_experts(int blocks, int M, int32_t x_type, int experts, const cl
            few_lds(blocks, call.x_per_pair ? call.k : 1) <= kFewLds;
 }
 
-static int32_t launch_few(const FewArgs &a, int32_t x_type, int32_t y_type, bool experts, dim3 grid, hipStream_t st)
+static int32_t launch_few(FewArgs a, int32_t x_type, int32_t y_type, bool experts, dim3 grid, hipStream_t st)
 {
     const size_t lds = few_lds(a.p.blocks, a.columns);
+    a.waves = run_waves(a.p.blocks);
+    const int units = a.columns * a.p.blocks * 4, threads = std::max(a.waves * 64, std::min(kFewWaves * 64, (units + 255) / 256 * 64));
     return with_type(x_type, [&](auto x) -> int32_t {
         return with_type(y_type, [&](auto y) -> int32_t {
             using X = decltype(x);
@@ -359,7 +365,7 @@ static int32_t launch_few(const FewArgs &a, int32_t x_type, int32_t y_type, bool
             auto kernel = experts ? mx_few_kernel<X, Y, true> : mx_few_kernel<X, Y, false>;
             static LdsLimit seen[2];
             if (int32_t rc = allow_lds((const void *)kernel, kFewLds, seen[experts])) return rc;
-            hipLaunchKernelGGL(kernel, grid, dim3(run_waves(a.p.blocks) * 64), lds, st, a);
+            hipLaunchKernelGGL(kernel, grid, dim3((unsigned)threads), lds, st, a);
             MX_HIP_TRY(hipGetLastError());
             return CL_OK;
         });
@@ -371,6 +377,7 @@ static int32_t run_product(ProductArgs a, const Choice &c, const ExpertLists *L,
                            const float *weights, hipStream_t st)
 {
     a.Y = Y;
+    a.past_caches = (int64_t)c.splits * a.rows * a.pitch * 4 > (128 << 20);
     if (!a.part) return with_type(y_type, [&](auto t) { return launch_product<decltype(t)>(a, c, L, st); });
     if (int32_t rc = launch_product<float>(a, c, L, st)) return rc;
     const FinishArgs f{a.part, a.bias, weights, experts_of, Y, (int64_t)a.rows * a.pitch, tokens, k, experts_of ? a.experts : 1, a.M, a.pitch, c.splits, a.act, a.out_width};
@@ -511,7 +518,7 @@ extern "C" int32_t cl_mx_fc_forward(const cl_mx_matrix *W, const cl_mx_input *X,
     a.out_width = act == CL_ACT_GATED ? W->rows / 2 : W->rows;
     if (few_fc(a.blocks, batch, X->type)) {
         a.Y = d_Y;
-        const FewArgs f{a, X->d_X, X->stride, W->K, batch, nullptr, nullptr, 1, 0, 0};
+        const FewArgs f{a, X->d_X, X->stride, W->K, batch, nullptr, nullptr, 1, 0, 0, 0};
         if (int32_t rc = launch_few(f, X->type, y_type, false, dim3((unsigned)((a.M + 15) / 16)), st)) return rc;
         clear_error();
         return CL_OK;
@@ -571,7 +578,7 @@ extern "C" int32_t cl_mx_experts_forward(const cl_mx_matrix *W, int32_t experts,
     if (few_experts(a.blocks, a.M, X->type, experts, *call)) {
         a.Y = d_Y;
         const int rows_each = 32 / k / 2 * 2;                // (even: a gated product's rows come in pairs)
-        const FewArgs f{a, X->d_X, X->stride, W->K, call->x_per_pair ? k : 1, call->d_experts, call->d_weights, k, rows_each, call->x_per_pair};
+        const FewArgs f{a, X->d_X, X->stride, W->K, call->x_per_pair ? k : 1, call->d_experts, call->d_weights, k, rows_each, call->x_per_pair, 0};
         if (int32_t rc = launch_few(f, X->type, y_type, true, dim3((unsigned)((a.M + rows_each - 1) / rows_each), (unsigned)tokens), st)) return rc;
         clear_error();
         return CL_OK;

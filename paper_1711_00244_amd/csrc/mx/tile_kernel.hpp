@@ -271,7 +271,6 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void mx_tile_kernel(ProductArgs a,
         for (int i = 0; i < TI; ++i) *(f32x4 *)(mine + r * kPitch + i * 16 + 4 * g) = acc[i][j];
         __builtin_amdgcn_wave_barrier();
         const int first = (wave % WN) * TJ * 16 + j * 16, m = m0 + (wave / WN) * kWide + lane % kLanes * 4;
-#pragma unroll 2
         for (int n = lane / kLanes; n < 16; n += 64 / kLanes) {
             const f32x4 v = *(const f32x4 *)(mine + n * kPitch + lane % kLanes * 4);
             const int row = __shfl(y_row, j * 16 + n);
