@@ -143,7 +143,7 @@ template <class X, class T, bool EXPERTS> __global__ __launch_bounds__(kFewWaves
         f32x4 v = part[0][f][l];
         for (int i = 1; i < waves; ++i) v += part[i][f][l];
         if (!EXPERTS) {
-            if ((l & 15) < a.columns) store_outputs<T>(p, 0, l & 15, m0 + f * 16 + 4 * (l >> 4), v);
+            if ((l & 15) < a.columns) store_outputs<T>(p, l & 15, m0 + f * 16 + 4 * (l >> 4), v, bias_of(p, 0, m0 + f * 16 + 4 * (l >> 4)));
         } else {
             // every column has the token's row, or column j the row of its j-th pair
 #pragma unroll

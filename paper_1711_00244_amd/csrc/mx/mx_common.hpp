@@ -128,6 +128,23 @@ template <class F> static int32_t with_type(int32_t type, F f)
     }
 }
 
+// Division of a 32-bit number by a run-time constant: a high product and two shifts (round-up method; exact for all n).
+struct Div {
+    uint32_t mul, shift1, shift2, d;
+    __device__ __forceinline__ uint32_t quotient(uint32_t n) const
+    {
+        const uint32_t t = __umulhi(n, mul);
+        return (t + ((n - t) >> shift1)) >> shift2;
+    }
+};
+
+static Div make_div(uint32_t d)
+{
+    uint32_t s = 0;
+    while (s < 32 && (1ull << s) < d) ++s;
+    return Div{(uint32_t)((((1ull << s) - d) << 32) / d + 1), s > 0 ? 1u : 0u, s > 0 ? s - 1 : 0u, d};
+}
+
 inline size_t round_up(size_t n, size_t to) { return (n + to - 1) / to * to; }
 inline bool aligned(const void *p, size_t to) { return ((uintptr_t)p & (to - 1)) == 0; }
 

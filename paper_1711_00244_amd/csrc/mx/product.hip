@@ -25,7 +25,7 @@ struct ProductArgs {
     int x_div;                                               // pair / x_div is its row of X
     float *part;                                             // not null: sums of a share of k, [split][row of Y][pitch], to be finished
     int splits, pitch;
-    int past_caches;                                         // part would not stay in the caches until it is read
+    int past_caches;                                         // what the product stores would not stay in the caches until it is read again
     int tile0;                                               // tile of the launch's blockIdx.y of 0
     int skip_unrouted;                                       // the rows of Y of pairs without an expert are not read
 };
@@ -47,52 +47,43 @@ template <int WIDTH> __device__ __forceinline__ bool columns_of(const ProductArg
     return !(c.expert == a.experts && a.skip_unrouted);
 }
 
-// Four consecutive outputs of one row of Y, from output m on.
-template <class T> __device__ __forceinline__ void store_outputs(const ProductArgs &a, int expert, int64_t row, int m, f32x4 v)
+// The bias of four consecutive rows of the matrix from m on (zero where there is no expert, whose sums are zero as well).
+__device__ __forceinline__ f32x4 bias_of(const ProductArgs &a, int expert, int m)
+{
+    f32x4 b = {0, 0, 0, 0};
+    if (!a.bias || (a.order && expert >= a.experts)) return b;
+    const float *at = a.bias + (int64_t)expert * a.M;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) b[i] = at[min(m + i, a.M - 1)];          // (nothing waits for them here, as it would at a branch of lanes)
+    return b;
+}
+
+// The outputs of four consecutive rows of the matrix, from m on, in one row of Y.
+template <class T> __device__ __forceinline__ void store_outputs(const ProductArgs &a, int64_t row, int m, f32x4 v, f32x4 bias)
 {
     if (m >= a.M) return;
-    if (a.bias) {
-        const float *at = a.bias + (int64_t)expert * a.M + m;
-        float b[4];
-        if (m + 4 <= a.M) {
-            load_values<4>(at, b);
-        } else {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) b[i] = m + i < a.M ? at[i] : 0.0f;
-        }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] += b[i];
-    }
+    if (a.bias) v += bias;
     T *y = (T *)a.Y + row * a.out_width;
     if (a.act == CL_ACT_GATED) {
         // rows 2 i and 2 i + 1 of the matrix: gate and value of output i
+        const T out[2] = {(T)(v[0] / (1.0f + expf(-v[0])) * v[1]), (T)(v[2] / (1.0f + expf(-v[2])) * v[3])};
         y += m / 2;
-#pragma unroll
-        for (int i = 0; i < 4; i += 2)
-            if (m + i + 1 < a.M) y[i / 2] = (T)(v[i] / (1.0f + expf(-v[i])) * v[i + 1]);
+        if (m / 2 + 2 <= a.out_width) store_values<2>(y, out);
+        else y[0] = out[0];
         return;
     }
-    y += m;
     T out[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) out[i] = (T)(a.act == CL_ACT_RELU && v[i] < 0.0f ? 0.0f : v[i]);      // (NaN stays)
-    if (m + 4 <= a.M) {
-        store_values<4>(y, out);
+    y += m;
+    if (m + 4 <= a.out_width) {
+        if (std::is_same_v<T, float> && a.past_caches) __builtin_nontemporal_store(f32x4{(float)out[0], (float)out[1], (float)out[2], (float)out[3]}, (f32x4 *)y);
+        else store_values<4>(y, out);
     } else {
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (m + i < a.M) y[i] = out[i];
+        for (int i = 0; i < 3; ++i)
+            if (m + i < a.out_width) y[i] = out[i];
     }
-}
-
-// The same for any column: the pairs without an expert get zeros, whatever the activation would make of a bias.
-template <class T> __device__ __forceinline__ void finish_outputs(const ProductArgs &a, int expert, int64_t row, int m, f32x4 v)
-{
-    if (!a.order || expert < a.experts) return store_outputs<T>(a, expert, row, m, v);
-    const int step = a.act == CL_ACT_GATED ? 2 : 1;
-    T *y = (T *)a.Y + row * a.out_width;
-    for (int i = 0; i < 4; i += step)
-        if (m + i + step <= a.M) y[(m + i) / step] = (T)0.0f;
 }
 
 // Four sums of a share of k.  (A row of partial sums is padded to whole fours.)
@@ -159,90 +150,73 @@ template <int NT, class T> __global__ __launch_bounds__(kRowsWaves * 64) void mx
         for (int w = 1; w < waves; ++w) v += part[w][t][l];
         const int64_t y_row = a.order ? a.order[c.first + n] : c.first + n;
         if (a.part) store_part(a, 0, y_row, m0 + 4 * (l >> 4), v);
-        else finish_outputs<T>(a, c.expert, y_row, m0 + 4 * (l >> 4), v);
+        else store_outputs<T>(a, y_row, m0 + 4 * (l >> 4), v, bias_of(a, c.expert, m0 + 4 * (l >> 4)));
     }
 }
 
 #include "few_kernel.hpp"
 #include "tile_kernel.hpp"
 
-// Y[t] = sum over j of weights[t][j] act(sum over the splits of a pair's parts + bias), both in order, of the pairs that have an
-// expert.  A thread makes four consecutive outputs of one row (two, of a gated product).
-struct FinishArgs {
-    const float *part, *bias, *weights;
-    const int32_t *experts_of;                               // null: one matrix
+// The sum over the splits of a product's parts, in order, and from it four outputs of one row (two, of a gated product).
+template <class T> __global__ __launch_bounds__(256) void mx_finish_kernel(ProductArgs a, Div quads, int row0, int rows)
+{
+    const uint32_t at = blockIdx.x * 256 + threadIdx.x, row = quads.quotient(at);
+    if (row >= (uint32_t)rows) return;
+    const int m = (int)(at - row * quads.d) * 4;
+    const int64_t t = (int64_t)row0 + row, stride = (int64_t)a.rows * a.pitch;
+    const float *p = a.part + t * a.pitch + m;
+    f32x4 part[8];                                           // (at most eight)
+#pragma unroll
+    for (int s = 0; s < 8; ++s) part[s] = *(const f32x4 *)(p + min(s, a.splits - 1) * stride);
+#pragma unroll
+    for (int s = 1; s < 8; ++s)
+        if (s < a.splits) part[0] += part[s];
+    store_outputs<T>(a, t, m, part[0], bias_of(a, 0, m));
+}
+
+// Y[t] = sum over j, in order, of weights[t][j] times what the product made of pair t k + j, of the pairs that have an expert.
+// A thread makes four consecutive outputs of one token and has asked for TOGETHER pairs' before it uses the first.
+struct JoinArgs {
+    const float *pairs, *weights;                            // rows of pitch elements
+    const int32_t *experts_of;
     void *Y;
-    int64_t split_stride;
-    int tokens, k, experts, M, pitch, splits, act, out_width;
+    int token0, tokens, k, experts, width, pitch;
+    Div quads;                                               // fours of a row
 };
 
-constexpr int kTogether = 4;
-
-template <class T> __global__ __launch_bounds__(256) void mx_finish_kernel(FinishArgs a, int quads)
+template <class T, int TOGETHER> __global__ __launch_bounds__(256) void mx_join_kernel(JoinArgs a)
 {
-    const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    const int64_t t = at / quads;
-    if (t >= a.tokens) return;
-    const int m = (int)(at - t * quads) * 4;
+    const uint32_t at = blockIdx.x * 256 + threadIdx.x, token = a.quads.quotient(at);
+    if (token >= (uint32_t)a.tokens) return;
+    const int m = (int)(at - token * a.quads.d) * 4;
+    const int64_t t = (int64_t)a.token0 + token;
     f32x4 sum = {0, 0, 0, 0};
-    for (int j0 = 0; j0 < a.k; j0 += kTogether) {
-        // what kTogether pairs need, on its way together
-        int e[kTogether];
-        float weight[kTogether];
-        f32x4 v[kTogether], bias[kTogether];
+    for (int j0 = 0; j0 < a.k; j0 += TOGETHER) {
+        int e[TOGETHER];
+        float weight[TOGETHER];
+        f32x4 v[TOGETHER];
 #pragma unroll
-        for (int i = 0; i < kTogether; ++i) {
+        for (int i = 0; i < TOGETHER; ++i) {
             const int64_t pair = t * a.k + min(j0 + i, a.k - 1);
-            e[i] = a.experts_of ? a.experts_of[pair] : 0;
-            weight[i] = a.weights ? a.weights[pair] : 1.0f;
-            v[i] = *(const f32x4 *)(a.part + pair * a.pitch + m);
-        }
-        if (a.splits > 1) {                                  // (at most eight; then k is 1)
-            const float *p = a.part + t * a.pitch + m;
-            f32x4 more[7];
-#pragma unroll
-            for (int s = 1; s < 8; ++s) more[s - 1] = *(const f32x4 *)(p + min(s, a.splits - 1) * a.split_stride);
-#pragma unroll
-            for (int s = 1; s < 8; ++s)
-                if (s < a.splits) v[0] += more[s - 1];
-        }
-        if (a.bias) {
-#pragma unroll
-            for (int i = 0; i < kTogether; ++i) {
-                const float *at = a.bias + (int64_t)(e[i] >= 0 && e[i] < a.experts ? e[i] : 0) * a.M + m;
-                float b[4];
-                if (m + 4 <= a.M) {
-                    load_values<4>(at, b);
-                } else {
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) b[c] = at[min(c, a.M - 1 - m)];
-                }
-                bias[i] = f32x4{b[0], b[1], b[2], b[3]};
-            }
+            e[i] = a.experts_of[pair];
+            weight[i] = a.weights[pair];
+            v[i] = *(const f32x4 *)(a.pairs + pair * a.pitch + m);
         }
 #pragma unroll
-        for (int i = 0; i < kTogether; ++i) {
+        for (int i = 0; i < TOGETHER; ++i) {
             if (j0 + i >= a.k || e[i] < 0 || e[i] >= a.experts) continue;
-            if (a.bias) v[i] += bias[i];
-            if (a.act == CL_ACT_GATED) {
-                v[i][0] = v[i][0] / (1.0f + expf(-v[i][0])) * v[i][1];
-                v[i][1] = v[i][2] / (1.0f + expf(-v[i][2])) * v[i][3];
-            } else if (a.act == CL_ACT_RELU) {
-#pragma unroll
-                for (int c = 0; c < 4; ++c) v[i][c] = v[i][c] < 0.0f ? 0.0f : v[i][c];
-            }
 #pragma unroll
             for (int c = 0; c < 4; ++c) sum[c] = fmaf(weight[i], v[i][c], sum[c]);
         }
     }
-    const int n = a.act == CL_ACT_GATED ? 2 : 4, out = a.act == CL_ACT_GATED ? m / 2 : m;
-    T *y = (T *)a.Y + t * a.out_width + out;
-    if (out + 4 <= a.out_width && n == 4) {
+    T *y = (T *)a.Y + t * a.width + m;
+    if (m + 4 <= a.width) {
         const T v[4] = {(T)sum[0], (T)sum[1], (T)sum[2], (T)sum[3]};
         store_values<4>(y, v);
     } else {
-        for (int i = 0; i < n; ++i)
-            if (out + i < a.out_width) y[i] = (T)sum[i];
+#pragma unroll
+        for (int i = 0; i < 3; ++i)
+            if (m + i < a.width) y[i] = (T)sum[i];
     }
 }
 
@@ -278,6 +252,7 @@ struct Price { int bm, bn, width; float start, alone, shared, shared_experts; };
 constexpr Price kPrices[] = {{64, 64, 1, 3.5f, 0.15f, 0.18f, 0.25f}, {128, 128, 2, 4.5f, 0.50f, 0.40f, 0.45f}, {256, 128, 2, 6.0f, 0.70f, 0.70f, 0.70f},
                              {256, 256, 3, 8.0f, 0.90f, 1.05f, 1.05f}};
 constexpr int kCus = 256;
+constexpr int64_t kCaches = 128 << 20;                       // half of what the caches hold
 
 // rows: columns of the product in all; lists: how many runs they are cut into (experts, or 1), each of which fills its last tile
 // half on average; part: a finishing launch follows in any case.
@@ -372,22 +347,53 @@ static int32_t launch_few(FewArgs a, int32_t x_type, int32_t y_type, bool expert
     });
 }
 
-// The product, and what is left to do where it gives partial sums: rows of Y (k pairs to each) from a.part.
-static int32_t run_product(ProductArgs a, const Choice &c, const ExpertLists *L, void *Y, int32_t y_type, int32_t tokens, int32_t k, const int32_t *experts_of,
-                           const float *weights, hipStream_t st)
+// launch(row0, rows, workgroups) over rows of `quads` threads each, in pieces whose threads' numbers have 32 bits.
+template <class F> static int32_t launch_rows(int32_t rows, uint32_t quads, F launch)
 {
-    a.Y = Y;
-    a.past_caches = (int64_t)c.splits * a.rows * a.pitch * 4 > (128 << 20);
-    if (!a.part) return with_type(y_type, [&](auto t) { return launch_product<decltype(t)>(a, c, L, st); });
-    if (int32_t rc = launch_product<float>(a, c, L, st)) return rc;
-    const FinishArgs f{a.part, a.bias, weights, experts_of, Y, (int64_t)a.rows * a.pitch, tokens, k, experts_of ? a.experts : 1, a.M, a.pitch, c.splits, a.act, a.out_width};
-    const int quads = a.pitch / 4;
-    const int64_t wgs = ((int64_t)tokens * quads + 255) / 256;
-    if (wgs > INT32_MAX) return fail(CL_EUNSUPPORTED, "a launch of %lld workgroups does not fit a grid", (long long)wgs);
-    return with_type(y_type, [&](auto t) -> int32_t {
-        hipLaunchKernelGGL(mx_finish_kernel<decltype(t)>, dim3((unsigned)wgs), dim3(256), 0, st, f, quads);
+    const int32_t most = (int32_t)std::min<int64_t>(rows, (1ll << 31) / quads);
+    for (int32_t row0 = 0, n; row0 < rows; row0 += n) {
+        n = std::min(most, rows - row0);
+        launch(row0, n, dim3((uint32_t)(((int64_t)n * quads + 255) / 256)));
         MX_HIP_TRY(hipGetLastError());
-        return CL_OK;
+    }
+    return CL_OK;
+}
+
+// The product of one matrix; a.part is where the sums of a split product go.
+static int32_t run_product(const ProductArgs &a, const Choice &c, int32_t y_type, hipStream_t st)
+{
+    if (!a.part) return with_type(y_type, [&](auto t) { return launch_product<decltype(t)>(a, c, nullptr, st); });
+    ProductArgs p = a;
+    p.splits = c.splits;
+    p.past_caches = (int64_t)c.splits * a.rows * a.pitch * 4 > kCaches;
+    if (int32_t rc = launch_product<float>(p, c, nullptr, st)) return rc;
+    p.past_caches = 0;
+    const Div quads = make_div((uint32_t)a.pitch / 4);
+    return with_type(y_type, [&](auto t) -> int32_t {
+        return launch_rows(a.rows, quads.d, [&](int row0, int rows, dim3 grid) {
+            hipLaunchKernelGGL(mx_finish_kernel<decltype(t)>, grid, dim3(256), 0, st, p, quads, row0, rows);
+        });
+    });
+}
+
+// The products of the pairs, to `pairs` (fp32) and from there to the weighted sums, or straight to Y.
+static int32_t run_experts(const ProductArgs &a, const Choice &c, const ExpertLists &L, const cl_mx_experts_call &call, float *pairs, int32_t y_type, hipStream_t st)
+{
+    if (!call.d_weights) return with_type(y_type, [&](auto t) { return launch_product<decltype(t)>(a, c, &L, st); });
+    ProductArgs p = a;
+    p.Y = pairs;
+    p.out_width = (int)round_up(a.out_width, 4);
+    p.skip_unrouted = 1;
+    p.past_caches = (int64_t)a.rows * p.out_width * 4 > kCaches;
+    if (int32_t rc = launch_product<float>(p, c, &L, st)) return rc;
+    JoinArgs f{pairs, call.d_weights, call.d_experts, a.Y, 0, 0, call.k, a.experts, a.out_width, p.out_width, make_div((uint32_t)p.out_width / 4)};
+    return with_type(y_type, [&](auto t) -> int32_t {
+        return launch_rows(call.tokens, f.quads.d, [&](int row0, int rows, dim3 grid) {
+            f.token0 = row0;
+            f.tokens = rows;
+            if (f.k <= 2) hipLaunchKernelGGL((mx_join_kernel<decltype(t), 2>), grid, dim3(256), 0, st, f);
+            else hipLaunchKernelGGL((mx_join_kernel<decltype(t), 4>), grid, dim3(256), 0, st, f);
+        });
     });
 }
 
@@ -468,11 +474,11 @@ static Scratch fc_scratch(const Choice &c, int32_t M, int32_t K, int32_t x_type,
     return s;
 }
 
-static Scratch experts_scratch(const Choice &c, int32_t M, int32_t K, int32_t x_type, int32_t experts, const cl_mx_experts_call &call)
+static Scratch experts_scratch(int32_t M, int32_t K, int32_t x_type, int32_t experts, const cl_mx_experts_call &call)
 {
     Scratch s;
     scratch_input(s, x_type, (int64_t)call.tokens * (call.x_per_pair ? call.k : 1), K);
-    if (call.d_weights) s.pairs = s.take(part_bytes(M, (int64_t)call.tokens * call.k, c.splits));
+    if (call.d_weights) s.pairs = s.take(part_bytes(call.act == CL_ACT_GATED ? M / 2 : M, (int64_t)call.tokens * call.k, 1));
     if (!call.d_lists) s.lists = s.take(expert_lists_at(nullptr, call.tokens, call.k, experts).bytes);
     return s;
 }
@@ -529,7 +535,8 @@ extern "C" int32_t cl_mx_fc_forward(const cl_mx_matrix *W, const cl_mx_input *X,
     if (int32_t rc = quantised_input(a, X, batch, W->K, s, d_workspace, st)) return rc;
     a.part = c.splits > 1 ? (float *)((uint8_t *)d_workspace + s.pairs) : nullptr;
     a.pitch = (int)round_up(W->rows, 4);
-    if (int32_t rc = run_product(a, c, nullptr, d_Y, y_type, batch, 1, nullptr, nullptr, st)) return rc;
+    a.Y = d_Y;
+    if (int32_t rc = run_product(a, c, y_type, st)) return rc;
     clear_error();
     return CL_OK;
 }
@@ -547,7 +554,7 @@ extern "C" int32_t cl_mx_experts_workspace_bytes(const cl_mx_matrix *W, int32_t 
     if (!out || !call) return fail(CL_EINVAL, "null pointer");
     if (int32_t rc = check_forward(W, x_type, CL_F32, call->act)) return rc;
     if (int32_t rc = check_experts(W, experts, call->tokens, call->k)) return rc;
-    *out = few_experts(row_blocks(W->K), W->rows, x_type, experts, *call) ? 0 : experts_scratch(choose_experts(W->rows, W->K, experts, *call), W->rows, W->K, x_type, experts, *call).bytes;
+    *out = few_experts(row_blocks(W->K), W->rows, x_type, experts, *call) ? 0 : experts_scratch(W->rows, W->K, x_type, experts, *call).bytes;
     clear_error();
     return CL_OK;
 }
@@ -583,9 +590,8 @@ extern "C" int32_t cl_mx_experts_forward(const cl_mx_matrix *W, int32_t experts,
         clear_error();
         return CL_OK;
     }
-    const bool join = call->d_weights != nullptr;
     const Choice c = choose_experts(W->rows, W->K, experts, *call);
-    const Scratch s = experts_scratch(c, W->rows, W->K, X->type, experts, *call);
+    const Scratch s = experts_scratch(W->rows, W->K, X->type, experts, *call);
     if (int32_t rc = check_scratch(s, d_workspace, workspace_bytes)) return rc;
     const ExpertLists L = expert_lists_at(call->d_lists ? const_cast<void *>(call->d_lists) : (uint8_t *)d_workspace + s.lists, tokens, k, experts);
     if (call->d_lists) {
@@ -602,10 +608,8 @@ extern "C" int32_t cl_mx_experts_forward(const cl_mx_matrix *W, int32_t experts,
     a.x_div = call->x_per_pair ? 1 : k;
     a.order = L.order;
     a.offsets = L.offsets;
-    a.skip_unrouted = join;
-    a.part = join ? (float *)((uint8_t *)d_workspace + s.pairs) : nullptr;
-    a.pitch = (int)round_up(W->rows, 4);
-    if (int32_t rc = run_product(a, c, &L, d_Y, y_type, tokens, k, call->d_experts, call->d_weights, st)) return rc;
+    a.Y = d_Y;
+    if (int32_t rc = run_experts(a, c, L, *call, (float *)((uint8_t *)d_workspace + s.pairs), y_type, st)) return rc;
     clear_error();
     return CL_OK;
 }

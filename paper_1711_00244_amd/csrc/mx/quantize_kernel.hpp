@@ -8,23 +8,6 @@
 namespace cl {
 namespace mx {
 
-// Division of a 32-bit number by a run-time constant: a high product and two shifts (round-up method; exact for all n).
-struct Div {
-    uint32_t mul, shift1, shift2, d;
-    __device__ __forceinline__ uint32_t quotient(uint32_t n) const
-    {
-        const uint32_t t = __umulhi(n, mul);
-        return (t + ((n - t) >> shift1)) >> shift2;
-    }
-};
-
-static Div make_div(uint32_t d)
-{
-    uint32_t s = 0;
-    while (s < 32 && (1ull << s) < d) ++s;
-    return Div{(uint32_t)((((1ull << s) - d) << 32) / d + 1), s > 0 ? 1u : 0u, s > 0 ? s - 1 : 0u, d};
-}
-
 // A lane has 16 bytes of numbers at a time - a unit: four or eight, eight or four lanes to a block - so that each load and store
 // of a wavefront is consecutive, and kUnits of those.  STREAM: numbers go past the caches (matrices that would not stay in
 // them).  Memory bounds both: 4096 x 25088 fp32, there and back, 142 us, 931 MB at 6.5 TB/s (a large copy: 5.1).  With eight

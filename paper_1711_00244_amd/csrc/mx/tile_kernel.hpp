@@ -113,6 +113,10 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void mx_tile_kernel(ProductArgs a,
         const int at = c.first + min((wave % WN) * TJ * 16 + lane, c.count - 1);
         y_row = a.order ? a.order[at] : at;
     }
+    // its first output of each row of Y, and the bias from there on
+    constexpr int kWide = TI * 16, kLanes = kWide / 4;
+    const int m = m0 + (wave / WN) * kWide + lane % kLanes * 4;
+    const f32x4 bias = bias_of(a, c.expert, m);
     const bool idle = (wave % WN) * TJ * 16 >= c.count;      // no columns: the wavefront loads, and multiplies nothing
     const int wi = (wave / WN) * TI * 16 + r, wj = BM + (wave % WN) * TJ * 16 + r;        // the lane's rows of the buffer
     const int at_code = (g ^ (r >> 2)) * 16;
@@ -262,7 +266,7 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void mx_tile_kernel(ProductArgs a,
     }
 
     // A wavefront's outputs go through LDS, sixteen columns at a time, so that what it stores of a row of Y is consecutive.
-    constexpr int kWide = TI * 16, kPitch = kWide + 4, kLanes = kWide / 4;
+    constexpr int kPitch = kWide + 4;
     static_assert(C::kWaves * 16 * kPitch * 4 <= C::kLds, "");
     float *mine = (float *)lds + wave * 16 * kPitch;
 #pragma unroll
@@ -270,13 +274,13 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void mx_tile_kernel(ProductArgs a,
 #pragma unroll
         for (int i = 0; i < TI; ++i) *(f32x4 *)(mine + r * kPitch + i * 16 + 4 * g) = acc[i][j];
         __builtin_amdgcn_wave_barrier();
-        const int first = (wave % WN) * TJ * 16 + j * 16, m = m0 + (wave / WN) * kWide + lane % kLanes * 4;
+        const int first = (wave % WN) * TJ * 16 + j * 16;
         for (int n = lane / kLanes; n < 16; n += 64 / kLanes) {
             const f32x4 v = *(const f32x4 *)(mine + n * kPitch + lane % kLanes * 4);
             const int row = __shfl(y_row, j * 16 + n);
             if (first + n >= c.count) continue;
             if (a.part) store_part(a, split, row, m, v);
-            else finish_outputs<T>(a, c.expert, row, m, v);
+            else store_outputs<T>(a, row, m, v, bias);
         }
         __builtin_amdgcn_wave_barrier();
     }
