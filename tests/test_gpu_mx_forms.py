@@ -1,0 +1,141 @@
+"""Products large enough for each tile of the output, whole and split along k, against fp64 products on the device of the same quantised operands (the
+quantisation itself is tested bit by bit elsewhere)."""
+import pytest
+import torch
+
+import mx_ref as ref
+import paper_1711_00244_amd as cl
+
+pytestmark = pytest.mark.gpu
+
+
+def within(y, want, size, terms):
+    """mx_ref's bound: fp32 sums of `terms` terms of absolute sum `size`, then the rounding to y's type."""
+    err = (terms + 4) * 2.0 ** -23 * size
+    bound = err + ref.HALF_ULP[y.dtype] * (want.abs() + err) + ref.SMALLEST[y.dtype]
+    off = (y.double() - want).abs()
+    assert bool((off <= bound).all()), (float(off.max()), float((off / bound).max()))
+
+
+def operands(B, M, K, dtype, experts=None, seed=0):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    x = torch.randn((B, K), generator=g, device="cuda").to(dtype)
+    W = cl.mx_quantize(torch.randn((M, K) if experts is None else (experts, M, K), generator=g, device="cuda") * 0.05)
+    bias = torch.randn(W.shape[:-1], generator=g, device="cuda")
+    return x, W, bias, cl.mx_dequantize(cl.mx_quantize(x)).double(), cl.mx_dequantize(W).double()
+
+
+@pytest.mark.parametrize("B,M,K", [(37, 1000, 4096), (150, 130, 9000),                                 # sixteen columns at a time
+                                   (1500, 1500, 600), (265, 962, 7400), (257, 438, 6681), (241, 453, 6814), (250, 400, 8200),      # 64 x 64; of 2, 4, 8 parts
+                                   (4629, 747, 1), (3000, 2100, 700), (4100, 4100, 1030), (2002, 1230, 7328),    # 128 x 128; of 2 parts
+                                   (2135, 3816, 1994), (5161, 2950, 257), (4000, 4100, 4200)])         # the larger ones
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_matrix(B, M, K, dtype):
+    x, W, bias, xq, wq = operands(B, M, K, dtype)
+    want, size = xq @ wq.T + bias.double(), xq.abs() @ wq.abs().T + bias.double().abs()
+    within(cl.mx_fc_forward(W, x, bias=bias, relu=True), want.clamp_min(0), size, K)
+    within(cl.mx_fc_forward(W, cl.mx_quantize(x), dtype=dtype), want - bias.double(), size, K)
+
+
+@pytest.mark.parametrize("T,E,k,M,K", [(40, 30, 4, 66, 1700), (400, 9, 3, 300, 300), (2100, 3, 4, 402, 1), (1300, 5, 4, 1300, 900), (31, 40, 3, 1470, 1299), (2926, 3, 2, 2700, 142),
+                                       (4000, 3, 2, 2040, 1500)])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.float16])
+def test_experts(T, E, k, M, K, dtype):
+    x, W, bias, xq, wq = operands(T, M, K, dtype, E)
+    g = torch.Generator(device="cuda").manual_seed(1)
+    chosen = torch.randint(-1, E, (T, k), generator=g, device="cuda", dtype=torch.int32)
+    weights = torch.rand((T, k), generator=g, device="cuda")
+    lists = cl.expert_lists(chosen, E)
+    pre, size = torch.zeros((T * k, M), device="cuda", dtype=torch.float64), torch.zeros((T * k, M), device="cuda", dtype=torch.float64)
+    of = chosen.reshape(-1)
+    for e in range(E):
+        at = (of == e).nonzero()[:, 0]
+        pre[at] = xq[at // k] @ wq[e].T + bias[e].double()
+        size[at] = xq[at // k].abs() @ wq[e].abs().T + bias[e].double().abs()
+    within(cl.mx_experts_forward(W, x, chosen, bias=bias, act="relu", lists=lists), pre.clamp_min(0), size, K)
+    w = weights.double().reshape(T * k, 1)
+    total, sizes = (w * pre).reshape(T, k, M).sum(1), (w * size).reshape(T, k, M).sum(1)
+    # (+ k + 1: the products with the weights and their sum)
+    within(cl.mx_experts_forward(W, x, chosen, weights, bias=bias), total, sizes, K + k + 1)
+    gate, value = pre[:, 0::2], pre[:, 1::2]
+    silu = gate / (1 + torch.exp(-gate))
+    out = silu * value
+    err = (K + 4) * 2.0 ** -23 * size
+    err = 1.1 * value.abs() * err[:, 0::2] + (silu.abs() + 1.1 * err[:, 0::2]) * err[:, 1::2] + out.abs() * (8 + gate.abs()) * 2.0 ** -23
+    total, err = (w * out).reshape(T, k, M // 2).sum(1), (w * (err + (k + 1) * 2.0 ** -23 * out.abs())).reshape(T, k, M // 2).sum(1)
+    y = cl.mx_experts_forward(W, x, chosen, weights, bias=bias, act="gated")
+    off = (y.double() - total).abs()
+    assert bool((off <= err + ref.HALF_ULP[dtype] * (total.abs() + err) + ref.SMALLEST[dtype]).all()), float(off.max())
+
+
+@pytest.mark.parametrize("T,k,E", [(8192, 4, 64), (8193, 4, 64), (16381, 2, 1), (16385, 2, 1024), (70001, 3, 17), (350003, 4, 300)])
+def test_lists_of_many_pairs(T, k, E):
+    """Counted by every workgroup, in a launch of their own, and in chunks of more than 4096."""
+    g = torch.Generator(device="cuda").manual_seed(T)
+    chosen = torch.randint(-1, E + 1, (T, k), generator=g, device="cuda", dtype=torch.int32)
+    lists = cl.expert_lists(chosen, E)
+    bucket = torch.where((chosen >= 0) & (chosen < E), chosen, E).reshape(-1)
+    starts = torch.zeros(E + 2, dtype=torch.int64, device="cuda")
+    starts[1:] = torch.bincount(bucket, minlength=E + 1).cumsum(0)
+    assert torch.equal(lists.offsets.long(), starts)
+    # the pairs in the order of their experts, and within one in their own: what a product that returns its row's number gives
+    ident = torch.sort(bucket, dim=0, stable=True).indices
+    at = (4 * (E + 2) + 255) // 256 * 256 + 256
+    assert torch.equal(lists.buffer[at:at + 4 * T * k].view(torch.int32).long(), ident)
+
+
+@pytest.mark.parametrize("weighted", [False, True])
+def test_experts_of_many_pairs(weighted):
+    T, E, k, M, K = 12001, 6, 3, 34, 70
+    x, W, bias, xq, wq = operands(T, M, K, torch.bfloat16, E)
+    chosen = torch.randint(-1, E, (T, k), device="cuda", dtype=torch.int32, generator=torch.Generator(device="cuda").manual_seed(2))
+    weights = torch.rand((T, k), device="cuda")
+    at, rows = chosen.reshape(-1).clamp_min(0).long(), xq.repeat_interleave(k, 0)
+    live = (chosen.reshape(-1, 1) >= 0).double()
+    want = live * ((rows[:, None, :] * wq[at]).sum(2) + bias.double()[at])
+    size = live * ((rows[:, None, :] * wq[at]).abs().sum(2) + bias.double()[at].abs())
+    if weighted:
+        w = weights.double().reshape(-1, 1)
+        want, size = (w * want).reshape(T, k, M).sum(1), (w * size).reshape(T, k, M).sum(1)
+    within(cl.mx_experts_forward(W, x, chosen, weights if weighted else None, bias=bias), want, size, K + k + 1)
+
+
+def test_offsets_beyond_32_bits():
+    # elements, codes and partial sums at offsets that 32 bits do not hold; what lies there is what it is at the start of memory
+    rows, K = 1100003, 4096
+    x = torch.empty((rows, K), dtype=torch.bfloat16, device="cuda")
+    x[:1000].normal_()
+    for at in range(1000, rows, 1000):
+        x[at:at + 1000] = x[:min(1000, rows - at)]
+    Q = cl.mx_quantize(x)
+    alone = cl.mx_quantize(x[-1000:].clone())
+    assert torch.equal(Q.codes[-1000:], alone.codes) and torch.equal(Q.scales[-1000:], alone.scales)
+    back = cl.mx_dequantize(Q, torch.bfloat16)
+    assert torch.equal(back[-1000:], cl.mx_dequantize(alone, torch.bfloat16))
+    del back, x
+
+    # the last of 1024 matrices of 1074 rows, whose codes begin past 2^31 bytes
+    E, M = 1024, 1074
+    W = cl.MxTensor(Q.codes[:E * M].view(E, M, -1), Q.scales[:E * M].view(E, M, -1), K)
+    g = torch.Generator(device="cuda").manual_seed(3)
+    for T in (2, 80):
+        X = torch.randn((T, K), generator=g, device="cuda")
+        chosen = torch.full((T, 1), E - 1, dtype=torch.int32, device="cuda")
+        last = cl.MxTensor(W.codes[-1].clone(), W.scales[-1].clone(), K)
+        xq, wq = cl.mx_dequantize(cl.mx_quantize(X)).double(), cl.mx_dequantize(last).double()
+        within(cl.mx_experts_forward(W, X, chosen, torch.ones((T, 1), device="cuda")), xq @ wq.T, xq.abs() @ wq.abs().T, K)
+    del W, Q
+
+    # 4.9 GB of pairs' sums
+    T, k, M, K = 150001, 2, 4096, 64
+    x, W, bias, xq, wq = operands(T, M, K, torch.bfloat16, 2)
+    chosen = torch.randint(0, 2, (T, k), generator=g, device="cuda", dtype=torch.int32)
+    weights = torch.rand((T, k), generator=g, device="cuda")
+    y = cl.mx_experts_forward(W, x, chosen, weights)
+    for s in (slice(0, 100), slice(T - 100, T)):
+        each = torch.stack([xq[s] @ wq[e].T for e in (0, 1)])
+        size = torch.stack([xq[s].abs() @ wq[e].abs().T for e in (0, 1)])
+        n = torch.arange(100, device="cuda")
+        want = sum(weights[s, j:j + 1].double() * each[chosen[s, j].long(), n] for j in range(k))
+        sizes = sum(weights[s, j:j + 1].double() * size[chosen[s, j].long(), n] for j in range(k))
+        within(y[s], want, sizes, K + k + 1)
