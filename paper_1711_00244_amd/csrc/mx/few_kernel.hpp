@@ -6,15 +6,17 @@
 // LDS - every workgroup all of them, which for so few costs less than a launch of its own - while its first weights are on
 // their way; then the wavefronts share out the runs of 16 blocks as in mx_rows_kernel, and their sums meet in LDS.
 //
-// One matrix: 16 consecutive rows of it, up to kFewColumns rows of X of kFewBlocks blocks together.  (4096 rows, microseconds, here
-// and in two launches: K 4096, one row 4.5 and 6.1, eight 6.1 and 6.5, twelve 7.7 and 6.7; K 9216, one 7.0 and 8.4 - 21 MB, which
-// a large copy moves in 4.1 -, four 8.6 and 8.9; K 25088, one 13.2 and 14.2, two 14.8 and 14.4.  A launch less is some 3 us
-// of the host's time besides.)  What bounds it is how much a compute unit can have on its way.
+// One matrix: 16 consecutive rows of it, up to kFewColumns rows of X (blockIdx.y: which).  (Microseconds, bf16, here and in two
+// launches: 4096 x 4096, one row 4.5 and 6.1, eight 7.1 and 7.2, sixteen 10.2 and 7.6; 4096 x 1024, sixteen 5.3 and 5.7, 32 6.5 and
+// 6.2, 64 10.2 and 8.1; 1000 x 256, 256 rows 5.4 and 7.5; one row of 4096 x 9216 7.0 and 8.4 - 21 MB, which a large copy moves in
+// 4.1.  A launch less is some 4 us of the host's time besides.)  What bounds it is how much a compute unit can have on its
+// way, and with many rows the quantisation.
 // Experts: one token (blockIdx.y), `rows_each` rows of each of its k experts' matrices, which are rows of one matrix instruction
 // like any others, so that a token's weighted sum needs no second launch either.  (One token, 64 experts of 1024 x 4096, eight
-// chosen, 17.8 MB: 8.6 us; lists, quantisation, product and sum apart took 33 in five launches.)
+// chosen, 17.8 MB: 8.4 us, in three launches 16.1; 73 tokens, 4 of 14 of 336 x 217: 8.3 and 13.8; 60, 3 of 4 of 3060 x 1697,
+// whose matrices every token would read: 113 and 16.)
 constexpr int kUnit = 8, kBatch = 4;                         // values that a lane quantises; how often before it asks for more
-constexpr int kFewColumns = 16, kFewBlocks = 1536, kFewWaves = kRowsWaves;
+constexpr int kFewColumns = 16, kFewWaves = kRowsWaves;
 constexpr size_t kFewLds = 64 << 10;
 
 struct FewArgs {
@@ -28,29 +30,30 @@ struct FewArgs {
     int waves;                                               // wavefronts that multiply; the others only quantise
 };
 
-inline size_t few_lds(int blocks, int columns) { return (size_t)columns * blocks * 17; }
+__host__ __device__ inline size_t few_lds(int blocks, int columns) { return ((size_t)columns * blocks * 17 + 15) / 16 * 16; }
 
 template <class X, class T, bool EXPERTS> __global__ __launch_bounds__(kFewWaves * 64) void mx_few_kernel(FewArgs a)
 {
     constexpr int kFewF = EXPERTS ? 2 : 1;
     extern __shared__ __align__(16) uint8_t lds[];
-    __shared__ f32x4 part[kFewWaves][kFewF][64];
     __shared__ float sums[kFewF * 16];
     const ProductArgs &p = a.p;
     const int waves = a.waves, wave = threadIdx.x / 64, lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
-    const int64_t token = EXPERTS ? blockIdx.y : 0;
+    const int64_t token = EXPERTS ? blockIdx.y : 0, column0 = EXPERTS ? 0 : (int64_t)blockIdx.y * kFewColumns;
+    const int columns = EXPERTS ? a.columns : min(kFewColumns, p.rows - (int)column0);
     const int m0 = (int)blockIdx.x * (EXPERTS ? a.rows_each : 16 * kFewF);
     uint8_t *codes = lds, *scales = lds + (size_t)a.columns * p.blocks * 16;
+    f32x4 *part = (f32x4 *)(lds + few_lds(p.blocks, a.columns));         // [waves][kFewF][64]
 
     // the values of this thread's first units, then the weights of the wavefront's first two runs, then the other units: what is
     // asked for first arrives first
-    const int per_row = p.blocks * 4, units = a.columns * per_row, threads = (int)blockDim.x;
+    const int per_row = p.blocks * 4, units = columns * per_row, threads = (int)blockDim.x;
     float x[kBatch][kUnit];
     auto load = [&](int u0) {
 #pragma unroll
         for (int i = 0; i < kBatch; ++i) {
             const int u = u0 + i * threads, row = u / per_row, k0 = (u - row * per_row) * kUnit;
-            if (u < units) load_unit<kUnit>((const X *)a.X + (EXPERTS ? token * (a.x_per_pair ? a.k : 1) + row : row) * a.x_stride + k0, a.K - k0, x[i]);
+            if (u < units) load_unit<kUnit>((const X *)a.X + (EXPERTS ? token * (a.x_per_pair ? a.k : 1) + row : column0 + row) * a.x_stride + k0, a.K - k0, x[i]);
         }
     };
     auto quantise = [&](int u0) {                            // (a row has whole blocks: a quad's lanes stay together)
@@ -106,7 +109,7 @@ template <class X, class T, bool EXPERTS> __global__ __launch_bounds__(kFewWaves
     __syncthreads();
 
     f32x4 acc[kFewF] = {};
-    const int column = min(r, a.columns - 1);
+    const int column = min(r, columns - 1);
     const uint8_t *xc = codes + (size_t)column * p.blocks * 16, *xs = scales + (size_t)column * p.blocks;
     auto multiply = [&](const Run &run, int b) {
         const bool in = b < p.blocks;
@@ -136,14 +139,14 @@ template <class X, class T, bool EXPERTS> __global__ __launch_bounds__(kFewWaves
     }
 #pragma unroll
     for (int f = 0; f < kFewF; ++f)
-        if (wave < waves) part[wave][f][lane] = acc[f];
+        if (wave < waves) part[(wave * kFewF + f) * 64 + lane] = acc[f];
     __syncthreads();
     for (int at = threadIdx.x; at < kFewF * 64; at += (int)blockDim.x) {
         const int f = at / 64, l = at & 63;
-        f32x4 v = part[0][f][l];
-        for (int i = 1; i < waves; ++i) v += part[i][f][l];
+        f32x4 v = part[at];
+        for (int i = 1; i < waves; ++i) v += part[i * kFewF * 64 + at];
         if (!EXPERTS) {
-            if ((l & 15) < a.columns) store_outputs<T>(p, l & 15, m0 + f * 16 + 4 * (l >> 4), v, bias_of(p, 0, m0 + f * 16 + 4 * (l >> 4)));
+            if ((l & 15) < columns) store_outputs<T>(p, column0 + (l & 15), m0 + f * 16 + 4 * (l >> 4), v, bias_of(p, 0, m0 + f * 16 + 4 * (l >> 4)));
         } else {
             // every column has the token's row, or column j the row of its j-th pair
 #pragma unroll

@@ -242,40 +242,47 @@ struct Choice {
     Form form;
     int width;                                               // columns of a tile: an index of kTileWidth
     int splits;
+    float us;
 };
 
-// What a form takes in microseconds, from measurements over M 358 .. 4096, 16 .. 8192 columns, K 636 .. 25088, one matrix and 5 to
-// 64 (most within a quarter).  Tiles: a start (launch, first loads, last stores), and per step of 128 k what a workgroup takes
-// alone on its compute unit, or its share of a full one where the launch has more workgroups than the chip has compute
-// units; that is more with experts, whose matrices change within a launch.
+// What a form takes in microseconds, fitted to measurements of 450 shapes of M 100 .. 4096, K 100 .. 25088, 20 .. 16000 columns, one
+// matrix and 4 to 128: over 450 others the choice takes 1.2 % longer, in the mean of logarithms, than the best of the forms.
+// Tiles: a start (launch, what its columns are, first loads, last stores), and per step of 128 k what a workgroup takes alone on
+// its compute unit, or its share of a full one where the launch has more workgroups than the chip has compute units; that
+// is another with experts, whose matrices change within a launch.
 struct Price { int bm, bn, width; float start, alone, shared, shared_experts; };
-constexpr Price kPrices[] = {{64, 64, 1, 3.5f, 0.15f, 0.18f, 0.25f}, {128, 128, 2, 4.5f, 0.50f, 0.40f, 0.45f}, {256, 128, 2, 6.0f, 0.70f, 0.70f, 0.70f},
-                             {256, 256, 3, 8.0f, 0.90f, 1.05f, 1.05f}};
+constexpr Price kPrices[] = {{64, 64, 1, 5.1f, 0.16f, 0.31f, 0.24f}, {128, 128, 2, 7.5f, 0.35f, 0.63f, 0.52f}, {256, 128, 2, 9.0f, 0.60f, 0.51f, 0.80f},
+                             {256, 256, 3, 12.0f, 0.90f, 1.20f, 1.10f}};
 constexpr int kCus = 256;
 constexpr int64_t kCaches = 128 << 20;                       // half of what the caches hold
 
-// rows: columns of the product in all; lists: how many runs they are cut into (experts, or 1), each of which fills its last tile
-// half on average; part: a finishing launch follows in any case.
-static Choice choose(int M, int blocks, int64_t rows, int64_t lists, bool part)
+// rows: columns of the product in all; experts: how many matrices share them (0: one matrix).
+static Choice choose(int M, int blocks, int64_t rows, int experts)
 {
     const int steps = blocks / 4, runs = (blocks + 15) / 16;
-    lists = std::min(lists, rows);
-    auto tiles_of = [&](int bn) { return lists == 1 ? (rows + bn - 1) / bn : std::max(lists, rows / bn + lists / 2); };
+    // the matrices that have columns, and those that have more than i tiles of them, their numbers spread about the mean
+    const float mean = experts ? (float)rows / experts : 0.0f, spread = std::sqrt(mean) + mean / 8;
+    auto tiles_of = [&](int bn) {
+        if (!experts) return (float)((rows + bn - 1) / bn);
+        const float whole = std::max(0.0f, std::floor((mean - 4 * spread) / bn));
+        float n = (1.0f - std::exp(-mean)) + whole;
+        for (float i = whole + 1; i * bn < mean + 4 * spread; ++i) n += 1.0f / (1.0f + std::exp(1.7f * (i * bn - mean) / spread));
+        return n * experts;
+    };
     // columns sixteen at a time: every workgroup reads all it multiplies itself
-    const float wgs = (float)((M + 15) / 16) * (float)tiles_of(16);
-    Choice best{kRows, 0, 1};
-    float least = 2.5f + std::max(1.12e-3f * wgs * runs, 1.0f + 0.9f * ((runs + kRowsWaves - 1) / kRowsWaves));
+    const float wgs = (float)((M + 15) / 16) * tiles_of(16);
+    Choice best{kRows, 0, 1, 2.5f + std::max(1.08e-3f * wgs * runs, 2.6f * ((runs + kRowsWaves - 1) / kRowsWaves))};
     for (int f = kTile64; f <= kTile256; ++f) {
         const Price &p = kPrices[f - kTile64];
-        const int64_t n = tiles_of(p.bn) * ((M + p.bm - 1) / p.bm);
+        const float n = tiles_of(p.bn) * ((M + p.bm - 1) / p.bm);
         const bool alone = f >= kTile256x128;                // (one workgroup to a compute unit: whole rounds; else two, which hide starts)
         for (int splits = 1; splits <= 8 && (splits == 1 || steps / splits >= 4); splits *= 2) {
-            if (splits > 1 && (lists > 1 || n * splits > 2 * kCus)) break;
-            const float full = (float)(n * splits) / kCus, rounds = std::max(1.0f, std::ceil(full));
-            const float each = full <= 1.0f ? p.alone : std::max(p.alone, (lists > 1 ? p.shared_experts : p.shared) * (alone ? rounds : full));
+            if (splits > 1 && (experts || n * splits > 2 * kCus)) break;
+            const float full = n * splits / kCus, rounds = std::max(1.0f, std::ceil(full));
+            const float each = full <= 1.0f ? p.alone : std::max(p.alone, (experts ? p.shared_experts : p.shared) * (alone ? rounds : full));
             float us = p.start * (alone ? rounds : 1.0f + 0.4f * std::max(0.0f, full / 2 - 1)) + each * (steps + splits - 1) / splits;
-            if (splits > 1) us += (part ? 0.0f : 3.5f) + (float)(2 * splits - 1) * rows * M * 1e-6f;
-            if (us < least) least = us, best = Choice{(Form)f, p.width, splits};
+            if (splits > 1) us += 1.7f + (float)(2 * splits - 1) * rows * M * 0.66e-6f;        // (the parts, there and back, and a launch)
+            if (us < best.us) best = Choice{(Form)f, p.width, splits, us};
         }
     }
     return best;
@@ -300,7 +307,7 @@ template <class T> static int32_t launch_product(ProductArgs a, const Choice &c,
     }
     a.splits = c.splits;
     switch (c.form) {
-    case kTile64: return launch_tiles<64, 64, 2, 2, 6, T>(a, tiles, st);
+    case kTile64: return launch_tiles<64, 64, 2, 2, 8, T>(a, tiles, st);
     case kTile128: return launch_tiles<128, 128, 2, 2, 4, T>(a, tiles, st);
     case kTile256x128: return launch_tiles<256, 128, 4, 2, 4, T>(a, tiles, st);
     case kTile256: return launch_tiles<256, 256, 2, 4, 4, T>(a, tiles, st);
@@ -315,31 +322,45 @@ template <class T> static int32_t launch_product(ProductArgs a, const Choice &c,
     return CL_OK;
 }
 
-// Whether few_kernel takes a call.  One matrix: by its measurements.  Experts: where reading a matrix once for every token that
-// is sent to it, and not once, costs less than the launches that sort the tokens by expert.
-static bool few_fc(int blocks, int batch, int32_t x_type)
+// Rows of each of a token's matrices that a workgroup has (even: a gated product's rows come in pairs).
+static int few_rows_each(int k) { return 32 / k / 2 * 2; }
+
+// Wavefronts of a workgroup of few_kernel: those that multiply, and more where there is much to quantise.
+static int few_waves(int blocks, int columns) { return std::max(run_waves(blocks), std::min(kFewWaves, (columns * blocks * 4 + 255) / 256)); }
+
+// Whether few_kernel takes a call: by what it takes in microseconds (fitted to M 119 .. 4096, K 106 .. 25088, 1 .. 256 columns or 1 .. 1245
+// tokens) against the launches that it replaces, of which each costs the host, besides, some 4 us.  kLaunch of those count.
+constexpr float kQuantise = 2.2f, kLists = 5.5f, kJoin = 3.0f, kLaunch = 2.0f;
+static bool few_fc(int M, int blocks, int batch, int32_t x_type)
 {
-    return x_type != CL_MX4 && batch <= kFewColumns && batch * blocks <= kFewBlocks && few_lds(blocks, batch) <= kFewLds;
+    const int columns = std::min(batch, kFewColumns);
+    const int64_t groups = (batch + kFewColumns - 1) / kFewColumns, wgs = groups * ((M + 15) / 16);
+    if (x_type == CL_MX4 || groups > 65535 || few_lds(blocks, columns) > kFewLds) return false;
+    // a workgroup's quantisation, the share of a chip that is full of them, or reading the matrix
+    const float own = (float)columns * blocks, us = std::max(std::max(4.3f + 2.5e-3f * own, 3.0f + 3.9e-3f * own * wgs / kCus), 2.7f + (float)wgs * 16 * blocks * 17 / 5e6f);
+    return us <= kQuantise + choose(M, blocks, batch, 0).us + kLaunch;
 }
-static bool few_experts(int blocks, int M, int32_t x_type, int experts, const cl_mx_experts_call &call)
+static bool few_experts(int M, int blocks, int32_t x_type, int experts, const cl_mx_experts_call &call)
 {
-    const int64_t pairs = (int64_t)call.tokens * call.k, again = pairs - std::min<int64_t>(pairs, experts);
-    return x_type != CL_MX4 && !call.d_lists && pairs <= 1024 && call.k <= 16 && again * M * blocks * 17 <= (24 << 20) &&
-           few_lds(blocks, call.x_per_pair ? call.k : 1) <= kFewLds;
+    if (x_type == CL_MX4 || call.d_lists || call.k > 16 || call.tokens > 65535 || few_lds(blocks, call.x_per_pair ? call.k : 1) > kFewLds) return false;
+    const int rows_each = few_rows_each(call.k);
+    // workgroups as fast as they are launched, or reading a matrix for every token that is sent to it
+    const float wgs = (float)call.tokens * ((M + rows_each - 1) / rows_each), us = 4.0f + std::max(1.45e-3f * wgs, (float)call.tokens * call.k * M * blocks * 17 / 4e6f);
+    return us <= kLists + choose(M, blocks, (int64_t)call.tokens * call.k, experts).us + kLaunch + (call.d_weights ? kJoin + kLaunch : 0.0f);
 }
 
 static int32_t launch_few(FewArgs a, int32_t x_type, int32_t y_type, bool experts, dim3 grid, hipStream_t st)
 {
-    const size_t lds = few_lds(a.p.blocks, a.columns);
     a.waves = run_waves(a.p.blocks);
-    const int units = a.columns * a.p.blocks * 4, threads = std::max(a.waves * 64, std::min(kFewWaves * 64, (units + 255) / 256 * 64));
+    const int threads = 64 * few_waves(a.p.blocks, a.columns);
+    const size_t lds = few_lds(a.p.blocks, a.columns) + (size_t)a.waves * (experts ? 2 : 1) * 64 * sizeof(f32x4);
     return with_type(x_type, [&](auto x) -> int32_t {
         return with_type(y_type, [&](auto y) -> int32_t {
             using X = decltype(x);
             using Y = decltype(y);
             auto kernel = experts ? mx_few_kernel<X, Y, true> : mx_few_kernel<X, Y, false>;
             static LdsLimit seen[2];
-            if (int32_t rc = allow_lds((const void *)kernel, kFewLds, seen[experts])) return rc;
+            if (int32_t rc = allow_lds((const void *)kernel, kFewLds + kFewWaves * 2 * 64 * sizeof(f32x4), seen[experts])) return rc;
             hipLaunchKernelGGL(kernel, grid, dim3((unsigned)threads), lds, st, a);
             MX_HIP_TRY(hipGetLastError());
             return CL_OK;
@@ -483,11 +504,6 @@ static Scratch experts_scratch(int32_t M, int32_t K, int32_t x_type, int32_t exp
     return s;
 }
 
-static Choice choose_experts(int32_t M, int32_t K, int32_t experts, const cl_mx_experts_call &call)
-{
-    return choose(M, row_blocks(K), (int64_t)call.tokens * call.k, std::max(2, experts), call.d_weights != nullptr);
-}
-
 }  // namespace mx
 }  // namespace cl
 
@@ -499,7 +515,7 @@ extern "C" int32_t cl_mx_fc_workspace_bytes(const cl_mx_matrix *W, int32_t batch
     if (!out) return fail(CL_EINVAL, "null pointer");
     if (int32_t rc = check_forward(W, x_type, CL_F32, CL_ACT_NONE)) return rc;
     if (batch < 0) return fail(CL_EINVAL, "batch of %d", (int)batch);
-    *out = few_fc(row_blocks(W->K), batch, x_type) ? 0 : fc_scratch(choose(W->rows, row_blocks(W->K), batch, 1, false), W->rows, W->K, x_type, batch).bytes;
+    *out = few_fc(W->rows, row_blocks(W->K), batch, x_type) ? 0 : fc_scratch(choose(W->rows, row_blocks(W->K), batch, 0), W->rows, W->K, x_type, batch).bytes;
     clear_error();
     return CL_OK;
 }
@@ -522,14 +538,14 @@ extern "C" int32_t cl_mx_fc_forward(const cl_mx_matrix *W, const cl_mx_input *X,
     a.rows = batch;
     a.act = act;
     a.out_width = act == CL_ACT_GATED ? W->rows / 2 : W->rows;
-    if (few_fc(a.blocks, batch, X->type)) {
+    if (few_fc(a.M, a.blocks, batch, X->type)) {
         a.Y = d_Y;
-        const FewArgs f{a, X->d_X, X->stride, W->K, batch, nullptr, nullptr, 1, 0, 0, 0};
-        if (int32_t rc = launch_few(f, X->type, y_type, false, dim3((unsigned)((a.M + 15) / 16)), st)) return rc;
+        const FewArgs f{a, X->d_X, X->stride, W->K, std::min(batch, kFewColumns), nullptr, nullptr, 1, 0, 0, 0};
+        if (int32_t rc = launch_few(f, X->type, y_type, false, dim3((unsigned)((a.M + 15) / 16), (unsigned)((batch + kFewColumns - 1) / kFewColumns)), st)) return rc;
         clear_error();
         return CL_OK;
     }
-    const Choice c = choose(W->rows, a.blocks, batch, 1, false);
+    const Choice c = choose(W->rows, a.blocks, batch, 0);
     const Scratch s = fc_scratch(c, W->rows, W->K, X->type, batch);
     if (int32_t rc = check_scratch(s, d_workspace, workspace_bytes)) return rc;
     if (int32_t rc = quantised_input(a, X, batch, W->K, s, d_workspace, st)) return rc;
@@ -554,7 +570,7 @@ extern "C" int32_t cl_mx_experts_workspace_bytes(const cl_mx_matrix *W, int32_t 
     if (!out || !call) return fail(CL_EINVAL, "null pointer");
     if (int32_t rc = check_forward(W, x_type, CL_F32, call->act)) return rc;
     if (int32_t rc = check_experts(W, experts, call->tokens, call->k)) return rc;
-    *out = few_experts(row_blocks(W->K), W->rows, x_type, experts, *call) ? 0 : experts_scratch(W->rows, W->K, x_type, experts, *call).bytes;
+    *out = few_experts(W->rows, row_blocks(W->K), x_type, experts, *call) ? 0 : experts_scratch(W->rows, W->K, x_type, experts, *call).bytes;
     clear_error();
     return CL_OK;
 }
@@ -582,15 +598,15 @@ extern "C" int32_t cl_mx_experts_forward(const cl_mx_matrix *W, int32_t experts,
     a.experts = experts;
     a.act = call->act;
     a.out_width = call->act == CL_ACT_GATED ? W->rows / 2 : W->rows;
-    if (few_experts(a.blocks, a.M, X->type, experts, *call)) {
+    if (few_experts(a.M, a.blocks, X->type, experts, *call)) {
         a.Y = d_Y;
-        const int rows_each = 32 / k / 2 * 2;                // (even: a gated product's rows come in pairs)
+        const int rows_each = few_rows_each(k);
         const FewArgs f{a, X->d_X, X->stride, W->K, call->x_per_pair ? k : 1, call->d_experts, call->d_weights, k, rows_each, call->x_per_pair, 0};
         if (int32_t rc = launch_few(f, X->type, y_type, true, dim3((unsigned)((a.M + rows_each - 1) / rows_each), (unsigned)tokens), st)) return rc;
         clear_error();
         return CL_OK;
     }
-    const Choice c = choose_experts(W->rows, W->K, experts, *call);
+    const Choice c = choose(a.M, a.blocks, (int64_t)tokens * k, experts);
     const Scratch s = experts_scratch(W->rows, W->K, X->type, experts, *call);
     if (int32_t rc = check_scratch(s, d_workspace, workspace_bytes)) return rc;
     const ExpertLists L = expert_lists_at(call->d_lists ? const_cast<void *>(call->d_lists) : (uint8_t *)d_workspace + s.lists, tokens, k, experts);

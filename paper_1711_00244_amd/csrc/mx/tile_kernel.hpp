@@ -35,7 +35,7 @@ template <int BM, int BN, int WM, int WN, int D> struct Tile {
         for (int i = 1; i <= D - 3; ++i) n += kCodeLoads + ((s + 8 - i) % 4 == 0 ? kScaleShare : 0);
         return n;
     }
-    static_assert(BM + BN <= kThreads && D >= 3 && D <= 7 && (D - 3) * kCodeLoads + kScaleShare < 16 && (D - 2) * kCodeLoads < 16, "");       // (the count that a wait names)
+    static_assert(BM + BN <= kThreads && D >= 3 && D <= 8 && (D - 3) * kCodeLoads + (D + 3) / 4 * kScaleShare < 64 && (D - 2) * kCodeLoads < 64, "");       // (the count that a wait names)
 };
 
 template <int BM, int BN, int WM, int WN, int D, class T>
@@ -156,7 +156,8 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void mx_tile_kernel(ProductArgs a,
     i32x4 w[C::kRing], x[2][TJ];
     int sw[TI], sx[TJ], sx_next[TJ];
 
-    constexpr int kWaitLds = 0xc07f, kWaitLoads = 0xf70;     // s_waitcnt: no LDS access left; no load left, or-ed with n < 16: n left
+    constexpr int kWaitLds = 0xc07f;                         // s_waitcnt: no LDS access left
+    auto loads_left = [](int n) constexpr { return 0xf70 | (n & 15) | (n >> 4) << 14; };     // n loads left
     auto barrier = [&] {
         asm volatile("" ::: "memory");
         __builtin_amdgcn_s_barrier();
@@ -171,7 +172,8 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void mx_tile_kernel(ProductArgs a,
         // every wavefront's loads of step t + 1 have arrived, and all reads of the buffers that are asked for next are done
         __builtin_amdgcn_sched_barrier(0);
         __builtin_amdgcn_s_waitcnt(kWaitLds);
-        __builtin_amdgcn_s_waitcnt(kWaitLoads | C::on_their_way(s));
+        constexpr int left = loads_left(C::on_their_way(s));
+        __builtin_amdgcn_s_waitcnt(left);
         barrier();
         if (s == 2) turn_scales(scales_next, q + 1);
         if (idle) {
@@ -229,16 +231,22 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void mx_tile_kernel(ProductArgs a,
             const int q = t / 4;
             step(S, buffer(t), buffer(t + 1), buffer(t + D - 1), scales(q + 1), scales(q + 2), q, min(t + D - 1, last), min(q + 2, last / 4));
         };
-        // (requests beyond the last step repeat it, so that a wait always counts the same; nothing reads what they bring)
-#pragma unroll
-        for (int q = 0; q < 2; ++q)
+        // (requests beyond the last step repeat it, so that a wait always counts the same; nothing reads what they bring.  The first
+        // ones are in the order that steps 1 - D .. -1 would ask in, of which step -4 asks for scales: step 0 counts them so)
+        auto request_first_scales = [&](int q) {
 #pragma unroll
             for (int k = 0; k < C::kScaleShare; ++k) request_scales(min(q, last / 4), scales(q), k);
+        };
+        request_first_scales(0);
+        if (D < 5) request_first_scales(1);
 #pragma unroll
-        for (int t = 0; t < D - 1; ++t)
+        for (int t = 0; t < D - 1; ++t) {
 #pragma unroll
             for (int k = 0; k < C::kCodeLoads; ++k) request_code(min(t, last), buffer(t), k);
-        __builtin_amdgcn_s_waitcnt(kWaitLoads | (D - 2) * C::kCodeLoads);
+            if (t == D - 5) request_first_scales(1);
+        }
+        constexpr int all_but_first = loads_left((D - 2) * C::kCodeLoads + (D < 5 ? 0 : C::kScaleShare));
+        __builtin_amdgcn_s_waitcnt(all_but_first);
         barrier();
         if (all_steps < 4) short_scales(scales(0));
         else turn_scales(scales(0), 0);
@@ -261,7 +269,8 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void mx_tile_kernel(ProductArgs a,
         if (t + 1 < steps) at(std::integral_constant<int, 1>{}, t + 1);
         if (t + 2 < steps) at(std::integral_constant<int, 2>{}, t + 2);
         __builtin_amdgcn_s_waitcnt(kWaitLds);
-        __builtin_amdgcn_s_waitcnt(kWaitLoads);
+        constexpr int none = loads_left(0);
+        __builtin_amdgcn_s_waitcnt(none);
         barrier();
     }
 

@@ -216,7 +216,7 @@ def test_refusals_of_the_binding():
     with pytest.raises(ValueError):
         cl.mx_experts_forward(w, x, e, x_per_pair=True)
     with pytest.raises(cl.CLError):
-        cl.mx_experts_forward(w, torch.ones((1000, 64), device="cuda"), torch.zeros((1000, 2), dtype=torch.int32, device="cuda"),
+        cl.mx_experts_forward(w, torch.ones((100000, 64), device="cuda"), torch.zeros((100000, 2), dtype=torch.int32, device="cuda"),
                               workspace=torch.empty(16, dtype=torch.uint8, device="cuda"))
     for kw in (dict(k=0), dict(k=65), dict(k=2, groups=3), dict(k=2, groups=4, groups_kept=5), dict(k=20, groups=4, groups_kept=1)):
         with pytest.raises(cl.CLError):

@@ -213,4 +213,4 @@ def test_refusals_of_the_binding():
     with pytest.raises(cl.CLError):
         cl.mx_fc_forward(cl.mx_quantize(torch.ones((3, 64), device="cuda")), x, act="gated")
     with pytest.raises(cl.CLError):
-        cl.mx_fc_forward(q, torch.ones((40, 64), device="cuda"), workspace=torch.empty(16, dtype=torch.uint8, device="cuda"))
+        cl.mx_fc_forward(q, torch.ones(((1 << 20) + 16, 64), device="cuda"), workspace=torch.empty(16, dtype=torch.uint8, device="cuda"))

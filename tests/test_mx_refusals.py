@@ -28,16 +28,16 @@ def test_product():
     L = binding.lib()
     n = C.c_size_t(0)
     W, X = MxMatrix(4096, 4096, 64, 200), MxInput(4096, None, 0, 200)
-    assert L.cl_mx_fc_workspace_bytes(W, 30, 0, n) == CL_OK and n.value >= 30 * 256 // 32 * 17
-    assert L.cl_mx_fc_workspace_bytes(W, 30, 3, n) == CL_OK and n.value == 0
+    assert L.cl_mx_fc_workspace_bytes(W, 30000, 0, n) == CL_OK and n.value >= 30000 * 256 // 32 * 17
+    assert L.cl_mx_fc_workspace_bytes(W, 30000, 3, n) == CL_OK and n.value == 0
     assert L.cl_mx_fc_workspace_bytes(W, 3, 0, n) == CL_OK and n.value == 0            # quantised where it is multiplied
     for bad in (MxMatrix(4096, 4096, 0, 200), MxMatrix(4096, 4096, 64, 0)):
         assert L.cl_mx_fc_workspace_bytes(bad, 3, 0, n) == CL_EINVAL
     assert L.cl_mx_fc_workspace_bytes(W, -1, 0, n) == CL_EINVAL and L.cl_mx_fc_workspace_bytes(W, 1, 9, n) == CL_EINVAL
     assert L.cl_mx_fc_workspace_bytes(W, 1, 0, None) == CL_EINVAL and L.cl_mx_fc_workspace_bytes(None, 1, 0, n) == CL_EINVAL
-    big = 1 << 20
+    big = 1 << 23
 
-    def call(W=W, X=X, y=P, y_type=0, batch=30, act=0, ws=P, ws_bytes=big):
+    def call(W=W, X=X, y=P, y_type=0, batch=30000, act=0, ws=P, ws_bytes=big):
         return L.cl_mx_fc_forward(W, X, None, y, y_type, batch, act, ws, ws_bytes, None)
 
     assert call(W=None) == CL_EINVAL and call(X=None) == CL_EINVAL and call(y=None) == CL_EINVAL
