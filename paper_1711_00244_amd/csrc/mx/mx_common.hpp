@@ -169,7 +169,7 @@ struct ExpertLists {
     int32_t *offsets;                // experts + 2: first pair of each expert, of the pairs without one, and the end
     int32_t *order;                  // tokens * k pairs (token * k + j), expert by expert, ascending within one
     int32_t *tile_count;             // kTileWidths: tiles of each width
-    int2 *tiles[4];                  // per width: (expert, first pair) of each tile; an expert's pairs begin a tile
+    int2 *tiles[4];                  // per width: (expert << 16 | pairs, first pair) of each tile; an expert's pairs begin a tile
     int32_t *chunk_counts;           // scratch of the launches that build it
     int64_t max_tiles[4];
     size_t bytes;

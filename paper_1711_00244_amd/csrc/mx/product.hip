@@ -19,7 +19,7 @@ struct ProductArgs {
     void *Y;
     const int32_t *order;                                    // pairs in the order of the experts; null: row n of X makes row n of Y
     const int2 *tiles;
-    const int32_t *tile_count, *offsets;
+    const int32_t *tile_count;
     int blocks, M, rows, experts, act;
     int out_width;                                           // elements of a row of Y
     int x_div;                                               // pair / x_div is its row of X
@@ -43,7 +43,7 @@ template <int WIDTH> __device__ __forceinline__ bool columns_of(const ProductArg
     }
     if (tile >= *a.tile_count) return false;
     const int2 t = a.tiles[tile];
-    c = Columns{t.y, min(WIDTH, a.offsets[t.x + 1] - t.y), t.x};
+    c = Columns{t.y, t.x & 0xffff, t.x >> 16};
     return !(c.expert == a.experts && a.skip_unrouted);
 }
 
@@ -623,7 +623,6 @@ extern "C" int32_t cl_mx_experts_forward(const cl_mx_matrix *W, int32_t experts,
     }
     a.x_div = call->x_per_pair ? 1 : k;
     a.order = L.order;
-    a.offsets = L.offsets;
     a.Y = d_Y;
     if (int32_t rc = run_experts(a, c, L, *call, (float *)((uint8_t *)d_workspace + s.pairs), y_type, st)) return rc;
     clear_error();

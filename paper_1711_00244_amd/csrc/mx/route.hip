@@ -536,7 +536,10 @@ __device__ __forceinline__ void lists_place(const ListArgs &a)
 #pragma unroll
             for (int v = 1; v <= kTileWidths; ++v) {
                 const int t0 = starts[v * (buckets + 1) + b], t1 = starts[v * (buckets + 1) + b + 1];
-                for (int t = t0 + lane; t < t1; t += 64) L.tiles[v - 1][t] = make_int2(b, starts[b] + (t - t0) * kTileWidth[v - 1]);
+                for (int t = t0 + lane; t < t1; t += 64) {
+                    const int first = starts[b] + (t - t0) * kTileWidth[v - 1];
+                    L.tiles[v - 1][t] = make_int2(b << 16 | min(kTileWidth[v - 1], starts[b + 1] - first), first);
+                }
             }
     }
     __syncthreads();

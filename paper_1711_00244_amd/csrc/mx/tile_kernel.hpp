@@ -106,19 +106,22 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void mx_tile_kernel(ProductArgs a,
     };
     auto shift = [&](int q) { return all_steps < 4 ? 0 : t_first + 4 * q - min(t_first + 4 * q, all_steps - 4); };
 
+    // Which rows and columns the wavefront has.  A SIMD gets wavefronts s and s + 4: those have different columns, so that a tile
+    // that is not full leaves every SIMD some.
+    const int wm = wave / WN, wn = (wave + wave / 4 * (WN / 2)) % WN;
     // the row of Y of the wavefront's column `lane`
     static_assert(TJ * 16 <= 64, "");
     int y_row;
     {
-        const int at = c.first + min((wave % WN) * TJ * 16 + lane, c.count - 1);
+        const int at = c.first + min(wn * TJ * 16 + lane, c.count - 1);
         y_row = a.order ? a.order[at] : at;
     }
     // its first output of each row of Y, and the bias from there on
     constexpr int kWide = TI * 16, kLanes = kWide / 4;
-    const int m = m0 + (wave / WN) * kWide + lane % kLanes * 4;
+    const int m = m0 + wm * kWide + lane % kLanes * 4;
     const f32x4 bias = bias_of(a, c.expert, m);
-    const bool idle = (wave % WN) * TJ * 16 >= c.count;      // no columns: the wavefront loads, and multiplies nothing
-    const int wi = (wave / WN) * TI * 16 + r, wj = BM + (wave % WN) * TJ * 16 + r;        // the lane's rows of the buffer
+    const bool idle = wn * TJ * 16 >= c.count;      // no columns: the wavefront loads, and multiplies nothing
+    const int wi = wm * TI * 16 + r, wj = BM + wn * TJ * 16 + r;        // the lane's rows of the buffer
     const int at_code = (g ^ (r >> 2)) * 16;
     auto read_code = [&](const uint8_t *buf, int row) { return *(const i32x4 *)(buf + row * 64 + at_code); };
     // The scales of a row's four steps, by step when they arrive, are turned in place (a thread per row) so that the word of
@@ -283,7 +286,7 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void mx_tile_kernel(ProductArgs a,
 #pragma unroll
         for (int i = 0; i < TI; ++i) *(f32x4 *)(mine + r * kPitch + i * 16 + 4 * g) = acc[i][j];
         __builtin_amdgcn_wave_barrier();
-        const int first = (wave % WN) * TJ * 16 + j * 16;
+        const int first = wn * TJ * 16 + j * 16;
         for (int n = lane / kLanes; n < 16; n += 64 / kLanes) {
             const f32x4 v = *(const f32x4 *)(mine + n * kPitch + lane % kLanes * 4);
             const int row = __shfl(y_row, j * 16 + n);
