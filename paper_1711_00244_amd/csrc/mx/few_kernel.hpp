@@ -146,7 +146,7 @@ template <class X, class T, bool EXPERTS> __global__ __launch_bounds__(kFewWaves
         f32x4 v = part[at];
         for (int i = 1; i < waves; ++i) v += part[i * kFewF * 64 + at];
         if (!EXPERTS) {
-            if ((l & 15) < columns) store_outputs<T>(p, column0 + (l & 15), m0 + f * 16 + 4 * (l >> 4), v, bias_of(p, 0, m0 + f * 16 + 4 * (l >> 4)));
+            if ((l & 15) < columns) store_outputs<T, false>(p, column0 + (l & 15), m0 + f * 16 + 4 * (l >> 4), v, bias_of(p, 0, m0 + f * 16 + 4 * (l >> 4)), 1.0f);
         } else {
             // every column has the token's row, or column j the row of its j-th pair
 #pragma unroll

@@ -20,6 +20,7 @@ struct ProductArgs {
     const int32_t *order;                                    // pairs in the order of the experts; null: row n of X makes row n of Y
     const int2 *tiles;
     const int32_t *tile_count;
+    const float *weights;                                    // of rows of Y, where outputs are WEIGHTED
     int blocks, M, rows, experts, act;
     int out_width;                                           // elements of a row of Y
     int x_div;                                               // pair / x_div is its row of X
@@ -58,15 +59,25 @@ __device__ __forceinline__ f32x4 bias_of(const ProductArgs &a, int expert, int m
     return b;
 }
 
-// The outputs of four consecutive rows of the matrix, from m on, in one row of Y.
-template <class T> __device__ __forceinline__ void store_outputs(const ProductArgs &a, int64_t row, int m, f32x4 v, f32x4 bias)
+// w v, rounded to 32 bits before it is rounded to a type of sixteen (in one step the last bit would not always be the same as that of
+// the kernels that sum over k pairs).
+__device__ __forceinline__ float weighted(float w, float v)
+{
+    float r = w * v;
+    asm("" : "+v"(r));
+    return r;
+}
+
+// The outputs of four consecutive rows of the matrix, from m on, in one row of Y; WEIGHTED: times its weight.
+template <class T, bool WEIGHTED> __device__ __forceinline__ void store_outputs(const ProductArgs &a, int64_t row, int m, f32x4 v, f32x4 bias, float weight)
 {
     if (m >= a.M) return;
     if (a.bias) v += bias;
     T *y = (T *)a.Y + row * a.out_width;
     if (a.act == CL_ACT_GATED) {
         // rows 2 i and 2 i + 1 of the matrix: gate and value of output i
-        const T out[2] = {(T)(v[0] / (1.0f + expf(-v[0])) * v[1]), (T)(v[2] / (1.0f + expf(-v[2])) * v[3])};
+        const float g[2] = {v[0] / (1.0f + expf(-v[0])) * v[1], v[2] / (1.0f + expf(-v[2])) * v[3]};
+        const T out[2] = {(T)(WEIGHTED ? weighted(weight, g[0]) : g[0]), (T)(WEIGHTED ? weighted(weight, g[1]) : g[1])};
         y += m / 2;
         if (m / 2 + 2 <= a.out_width) store_values<2>(y, out);
         else y[0] = out[0];
@@ -74,7 +85,10 @@ template <class T> __device__ __forceinline__ void store_outputs(const ProductAr
     }
     T out[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) out[i] = (T)(a.act == CL_ACT_RELU && v[i] < 0.0f ? 0.0f : v[i]);      // (NaN stays)
+    for (int i = 0; i < 4; ++i) {
+        const float r = a.act == CL_ACT_RELU && v[i] < 0.0f ? 0.0f : v[i];       // (NaN stays)
+        out[i] = (T)(WEIGHTED ? weighted(weight, r) : r);
+    }
     y += m;
     if (m + 4 <= a.out_width) {
         if (std::is_same_v<T, float> && a.past_caches) __builtin_nontemporal_store(f32x4{(float)out[0], (float)out[1], (float)out[2], (float)out[3]}, (f32x4 *)y);
@@ -101,7 +115,7 @@ __device__ __forceinline__ void store_part(const ProductArgs &a, int split, int6
 // Their sums meet in LDS and are added in the order of the wavefronts.
 constexpr int kRowsWaves = 16;
 
-template <int NT, class T> __global__ __launch_bounds__(kRowsWaves * 64) void mx_rows_kernel(ProductArgs a)
+template <int NT, class T, bool WEIGHTED> __global__ __launch_bounds__(kRowsWaves * 64) void mx_rows_kernel(ProductArgs a)
 {
     __shared__ f32x4 part[kRowsWaves][NT][64];
     Columns c;
@@ -150,7 +164,7 @@ template <int NT, class T> __global__ __launch_bounds__(kRowsWaves * 64) void mx
         for (int w = 1; w < waves; ++w) v += part[w][t][l];
         const int64_t y_row = a.order ? a.order[c.first + n] : c.first + n;
         if (a.part) store_part(a, 0, y_row, m0 + 4 * (l >> 4), v);
-        else store_outputs<T>(a, y_row, m0 + 4 * (l >> 4), v, bias_of(a, c.expert, m0 + 4 * (l >> 4)));
+        else store_outputs<T, WEIGHTED>(a, y_row, m0 + 4 * (l >> 4), v, bias_of(a, c.expert, m0 + 4 * (l >> 4)), WEIGHTED && c.expert < a.experts ? a.weights[y_row] : 0.0f);
     }
 }
 
@@ -171,7 +185,7 @@ template <class T> __global__ __launch_bounds__(256) void mx_finish_kernel(Produ
 #pragma unroll
     for (int s = 1; s < 8; ++s)
         if (s < a.splits) part[0] += part[s];
-    store_outputs<T>(a, t, m, part[0], bias_of(a, 0, m));
+    store_outputs<T, false>(a, t, m, part[0], bias_of(a, 0, m), 1.0f);
 }
 
 // Y[t] = sum over j, in order, of weights[t][j] times what the product made of pair t k + j, of the pairs that have an expert.
@@ -220,10 +234,10 @@ template <class T, int TOGETHER> __global__ __launch_bounds__(256) void mx_join_
     }
 }
 
-template <int BM, int BN, int WM, int WN, int D, class T> static int32_t launch_tiles(const ProductArgs &a, int64_t tiles, hipStream_t st)
+template <int BM, int BN, int WM, int WN, int D, class T, bool WEIGHTED> static int32_t launch_tiles(const ProductArgs &a, int64_t tiles, hipStream_t st)
 {
     using C = Tile<BM, BN, WM, WN, D>;
-    auto kernel = mx_tile_kernel<BM, BN, WM, WN, D, T>;
+    auto kernel = mx_tile_kernel<BM, BN, WM, WN, D, T, WEIGHTED>;
     static LdsLimit seen;
     if (int32_t rc = allow_lds((const void *)kernel, C::kLds, seen)) return rc;
     const int64_t row_tiles = (a.M + BM - 1) / BM;
@@ -297,7 +311,7 @@ static int run_waves(int blocks)
 }
 
 // The tiles of a product: rows of X in order, or what the lists have.
-template <class T> static int32_t launch_product(ProductArgs a, const Choice &c, const ExpertLists *L, hipStream_t st)
+template <class T, bool WEIGHTED> static int32_t launch_product(ProductArgs a, const Choice &c, const ExpertLists *L, hipStream_t st)
 {
     int64_t tiles = ((int64_t)a.rows + kTileWidth[c.width] - 1) / kTileWidth[c.width];
     if (L) {
@@ -307,16 +321,16 @@ template <class T> static int32_t launch_product(ProductArgs a, const Choice &c,
     }
     a.splits = c.splits;
     switch (c.form) {
-    case kTile64: return launch_tiles<64, 64, 2, 2, 8, T>(a, tiles, st);
-    case kTile128: return launch_tiles<128, 128, 2, 2, 4, T>(a, tiles, st);
-    case kTile256x128: return launch_tiles<256, 128, 4, 2, 4, T>(a, tiles, st);
-    case kTile256: return launch_tiles<256, 256, 2, 4, 4, T>(a, tiles, st);
+    case kTile64: return launch_tiles<64, 64, 2, 2, 8, T, WEIGHTED>(a, tiles, st);
+    case kTile128: return launch_tiles<128, 128, 2, 2, 4, T, WEIGHTED>(a, tiles, st);
+    case kTile256x128: return launch_tiles<256, 128, 4, 2, 4, T, WEIGHTED>(a, tiles, st);
+    case kTile256: return launch_tiles<256, 256, 2, 4, 4, T, WEIGHTED>(a, tiles, st);
     default: break;
     }
     // (a grid is at most 65535 high: taller ones go in pieces)
     for (int64_t t0 = 0; t0 < tiles; t0 += 65535) {
         a.tile0 = (int)t0;
-        hipLaunchKernelGGL((mx_rows_kernel<1, T>), dim3((unsigned)((a.M + 15) / 16), (unsigned)std::min<int64_t>(tiles - t0, 65535)), dim3(run_waves(a.blocks) * 64), 0, st, a);
+        hipLaunchKernelGGL((mx_rows_kernel<1, T, WEIGHTED>), dim3((unsigned)((a.M + 15) / 16), (unsigned)std::min<int64_t>(tiles - t0, 65535)), dim3(run_waves(a.blocks) * 64), 0, st, a);
         MX_HIP_TRY(hipGetLastError());
     }
     return CL_OK;
@@ -346,7 +360,7 @@ static bool few_experts(int M, int blocks, int32_t x_type, int experts, const cl
     const int rows_each = few_rows_each(call.k);
     // workgroups as fast as they are launched, or reading a matrix for every token that is sent to it
     const float wgs = (float)call.tokens * ((M + rows_each - 1) / rows_each), us = 4.0f + std::max(1.45e-3f * wgs, (float)call.tokens * call.k * M * blocks * 17 / 4e6f);
-    return us <= kLists + choose(M, blocks, (int64_t)call.tokens * call.k, experts).us + kLaunch + (call.d_weights ? kJoin + kLaunch : 0.0f);
+    return us <= kLists + choose(M, blocks, (int64_t)call.tokens * call.k, experts).us + kLaunch + (call.d_weights && call.k > 1 ? kJoin + kLaunch : 0.0f);
 }
 
 static int32_t launch_few(FewArgs a, int32_t x_type, int32_t y_type, bool experts, dim3 grid, hipStream_t st)
@@ -383,11 +397,11 @@ template <class F> static int32_t launch_rows(int32_t rows, uint32_t quads, F la
 // The product of one matrix; a.part is where the sums of a split product go.
 static int32_t run_product(const ProductArgs &a, const Choice &c, int32_t y_type, hipStream_t st)
 {
-    if (!a.part) return with_type(y_type, [&](auto t) { return launch_product<decltype(t)>(a, c, nullptr, st); });
+    if (!a.part) return with_type(y_type, [&](auto t) { return launch_product<decltype(t), false>(a, c, nullptr, st); });
     ProductArgs p = a;
     p.splits = c.splits;
     p.past_caches = (int64_t)c.splits * a.rows * a.pitch * 4 > kCaches;
-    if (int32_t rc = launch_product<float>(p, c, nullptr, st)) return rc;
+    if (int32_t rc = launch_product<float, false>(p, c, nullptr, st)) return rc;
     p.past_caches = 0;
     const Div quads = make_div((uint32_t)a.pitch / 4);
     return with_type(y_type, [&](auto t) -> int32_t {
@@ -400,13 +414,17 @@ static int32_t run_product(const ProductArgs &a, const Choice &c, int32_t y_type
 // The products of the pairs, to `pairs` (fp32) and from there to the weighted sums, or straight to Y.
 static int32_t run_experts(const ProductArgs &a, const Choice &c, const ExpertLists &L, const cl_mx_experts_call &call, float *pairs, int32_t y_type, hipStream_t st)
 {
-    if (!call.d_weights) return with_type(y_type, [&](auto t) { return launch_product<decltype(t)>(a, c, &L, st); });
+    if (!call.d_weights) return with_type(y_type, [&](auto t) { return launch_product<decltype(t), false>(a, c, &L, st); });
     ProductArgs p = a;
+    if (call.k == 1) {                                       // nothing to join
+        p.weights = call.d_weights;
+        return with_type(y_type, [&](auto t) { return launch_product<decltype(t), true>(p, c, &L, st); });
+    }
     p.Y = pairs;
     p.out_width = (int)round_up(a.out_width, 4);
     p.skip_unrouted = 1;
     p.past_caches = (int64_t)a.rows * p.out_width * 4 > kCaches;
-    if (int32_t rc = launch_product<float>(p, c, &L, st)) return rc;
+    if (int32_t rc = launch_product<float, false>(p, c, &L, st)) return rc;
     JoinArgs f{pairs, call.d_weights, call.d_experts, a.Y, 0, 0, call.k, a.experts, a.out_width, p.out_width, make_div((uint32_t)p.out_width / 4)};
     return with_type(y_type, [&](auto t) -> int32_t {
         return launch_rows(call.tokens, f.quads.d, [&](int row0, int rows, dim3 grid) {
@@ -499,7 +517,7 @@ static Scratch experts_scratch(int32_t M, int32_t K, int32_t x_type, int32_t exp
 {
     Scratch s;
     scratch_input(s, x_type, (int64_t)call.tokens * (call.x_per_pair ? call.k : 1), K);
-    if (call.d_weights) s.pairs = s.take(part_bytes(call.act == CL_ACT_GATED ? M / 2 : M, (int64_t)call.tokens * call.k, 1));
+    if (call.d_weights && call.k > 1) s.pairs = s.take(part_bytes(call.act == CL_ACT_GATED ? M / 2 : M, (int64_t)call.tokens * call.k, 1));
     if (!call.d_lists) s.lists = s.take(expert_lists_at(nullptr, call.tokens, call.k, experts).bytes);
     return s;
 }

@@ -38,7 +38,8 @@ template <int BM, int BN, int WM, int WN, int D> struct Tile {
     static_assert(BM + BN <= kThreads && D >= 3 && D <= 8 && (D - 3) * kCodeLoads + (D + 3) / 4 * kScaleShare < 64 && (D - 2) * kCodeLoads < 64, "");       // (the count that a wait names)
 };
 
-template <int BM, int BN, int WM, int WN, int D, class T>
+// WEIGHTED: outputs times a weight of their row of Y.
+template <int BM, int BN, int WM, int WN, int D, class T, bool WEIGHTED>
 __global__ __launch_bounds__(WM * WN * 64, 2) void mx_tile_kernel(ProductArgs a, int row_tiles)
 {
     using C = Tile<BM, BN, WM, WN, D>;
@@ -109,12 +110,14 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void mx_tile_kernel(ProductArgs a,
     // Which rows and columns the wavefront has.  A SIMD gets wavefronts s and s + 4: those have different columns, so that a tile
     // that is not full leaves every SIMD some.
     const int wm = wave / WN, wn = (wave + wave / 4 * (WN / 2)) % WN;
-    // the row of Y of the wavefront's column `lane`
+    // the row of Y of the wavefront's column `lane`, and its weight
     static_assert(TJ * 16 <= 64, "");
     int y_row;
+    float weight = 1.0f;
     {
         const int at = c.first + min(wn * TJ * 16 + lane, c.count - 1);
         y_row = a.order ? a.order[at] : at;
+        if (WEIGHTED) weight = routed ? a.weights[y_row] : 0.0f;
     }
     // its first output of each row of Y, and the bias from there on
     constexpr int kWide = TI * 16, kLanes = kWide / 4;
@@ -290,9 +293,10 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void mx_tile_kernel(ProductArgs a,
         for (int n = lane / kLanes; n < 16; n += 64 / kLanes) {
             const f32x4 v = *(const f32x4 *)(mine + n * kPitch + lane % kLanes * 4);
             const int row = __shfl(y_row, j * 16 + n);
+            const float scale = WEIGHTED ? __shfl(weight, j * 16 + n) : 1.0f;
             if (first + n >= c.count) continue;
             if (a.part) store_part(a, split, row, m, v);
-            else store_outputs<T>(a, row, m, v, bias);
+            else store_outputs<T, WEIGHTED>(a, row, m, v, bias, scale);
         }
         __builtin_amdgcn_wave_barrier();
     }

@@ -38,7 +38,7 @@ def test_matrix(B, M, K, dtype):
 
 
 @pytest.mark.parametrize("T,E,k,M,K", [(40, 30, 4, 66, 1700), (400, 9, 3, 300, 300), (2100, 3, 4, 402, 1), (1300, 5, 4, 1300, 900), (31, 40, 3, 1470, 1299), (2926, 3, 2, 2700, 142),
-                                       (4000, 3, 2, 2040, 1500)])
+                                       (4000, 3, 2, 2040, 1500), (900, 4, 1, 514, 700), (9000, 3, 1, 1030, 300), (6000, 3, 1, 2700, 142)])       # k = 1: nothing to join
 @pytest.mark.parametrize("dtype", [torch.float32, torch.float16])
 def test_experts(T, E, k, M, K, dtype):
     x, W, bias, xq, wq = operands(T, M, K, dtype, E)
