@@ -11,8 +11,9 @@
 // multiplies stay in program order (scheduling barriers): in a bunch behind the step's barrier they would fill their queues
 // and the multiplies would wait behind them.
 //
-// In LDS a row's four blocks are 64 consecutive bytes, block c of row r in place c ^ (r / 4 % 4): sixteen lanes that read one
-// block of sixteen rows then touch each of the 64 banks once.
+// In LDS a row's four blocks are 64 consecutive bytes, block c of row r in place c ^ (r / 2 % 4).  A read of 16 bytes a lane is
+// served sixteen lanes at a time, of which eight are from one half of a half-wave and eight from the other's; those then touch each of
+// the 64 banks once.  (Otherwise - in order, or with r or r / 4 - reads take twice as long, but are not what a step waits for.)
 template <int BM, int BN, int WM, int WN, int D> struct Tile {
     static constexpr int kWaves = WM * WN, kThreads = kWaves * 64;
     static constexpr int TI = BM / WM / 16, TJ = BN / WN / 16;
@@ -85,7 +86,7 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void mx_tile_kernel(ProductArgs a,
     const uint8_t *code_at[C::kCodeLoads], *scale_at[C::kScaleShare];
 #pragma unroll
     for (int i = 0; i < C::kCodeLoads; ++i) {
-        const int q = i * C::kWaves + wave, row = q * 16 + (lane >> 2), chunk = (lane & 3) ^ (lane >> 4 & 3);
+        const int q = i * C::kWaves + wave, row = q * 16 + (lane >> 2), chunk = (lane & 3) ^ (lane >> 3 & 3);
         code_at[i] = (q < BM / 16 ? a.w_codes + (w_first + min(m0 + row, a.M - 1)) * row_bytes : a.x_codes + x_row(row - BM) * row_bytes) + chunk * 16;
     }
     auto scale_load = [&](int i) { return min(i * C::kWaves + wave, C::kScaleLoads - 1); };
@@ -125,7 +126,7 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void mx_tile_kernel(ProductArgs a,
     const f32x4 bias = bias_of(a, c.expert, m);
     const bool idle = wn * TJ * 16 >= c.count;      // no columns: the wavefront loads, and multiplies nothing
     const int wi = wm * TI * 16 + r, wj = BM + wn * TJ * 16 + r;        // the lane's rows of the buffer
-    const int at_code = (g ^ (r >> 2)) * 16;
+    const int at_code = (g ^ (r >> 1 & 3)) * 16;
     auto read_code = [&](const uint8_t *buf, int row) { return *(const i32x4 *)(buf + row * 64 + at_code); };
     // The scales of a row's four steps, by step when they arrive, are turned in place (a thread per row) so that the word of
     // block g has its bytes of the four steps: one read for four multiplies, which pick their byte.  (Reading a byte a
