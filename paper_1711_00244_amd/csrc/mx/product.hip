@@ -23,9 +23,11 @@ struct ProductArgs {
     const float *weights;                                    // of rows of Y, where outputs are WEIGHTED
     int blocks, M, rows, experts, act;
     int out_width;                                           // elements of a row of Y
-    int x_div;                                               // pair / x_div is its row of X
+    Div x_div;                                               // pair / x_div is its row of X
     float *part;                                             // not null: sums of a share of k, [split][row of Y][pitch], to be finished
     int splits, pitch;
+    int split_steps, split_more;                             // steps of 128 k of a share of k, and how many shares have one more
+    Div row_tiles, band_tiles;                               // tiles of a column of tiles, and of a band of columns
     int past_caches;                                         // what the product stores would not stay in the caches until it is read again
     int tile0;                                               // tile of the launch's blockIdx.y of 0
     int skip_unrouted;                                       // the rows of Y of pairs without an expert are not read
@@ -130,7 +132,7 @@ template <int NT, class T, bool WEIGHTED> __global__ __launch_bounds__(kRowsWave
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
             const int n = c.first + min(t * 16 + r, c.count - 1);
-            const int64_t x_row = a.order ? a.order[n] / a.x_div : n;
+            const int64_t x_row = a.order ? (int64_t)a.x_div.quotient((uint32_t)a.order[n]) : n;
             xc[t] = a.x_codes + x_row * a.blocks * 16;
             xs[t] = a.x_scales + x_row * a.blocks;
         }
@@ -234,7 +236,7 @@ template <class T, int TOGETHER> __global__ __launch_bounds__(256) void mx_join_
     }
 }
 
-template <int BM, int BN, int WM, int WN, int D, class T, bool WEIGHTED> static int32_t launch_tiles(const ProductArgs &a, int64_t tiles, hipStream_t st)
+template <int BM, int BN, int WM, int WN, int D, class T, bool WEIGHTED> static int32_t launch_tiles(ProductArgs a, int64_t tiles, hipStream_t st)
 {
     using C = Tile<BM, BN, WM, WN, D>;
     auto kernel = mx_tile_kernel<BM, BN, WM, WN, D, T, WEIGHTED>;
@@ -242,6 +244,10 @@ template <int BM, int BN, int WM, int WN, int D, class T, bool WEIGHTED> static 
     if (int32_t rc = allow_lds((const void *)kernel, C::kLds, seen)) return rc;
     const int64_t row_tiles = (a.M + BM - 1) / BM;
     if (row_tiles * tiles > INT32_MAX - 8) return fail(CL_EUNSUPPORTED, "a launch of %lld workgroups does not fit a grid", (long long)(row_tiles * tiles));
+    a.row_tiles = make_div((uint32_t)row_tiles);
+    a.band_tiles = make_div((uint32_t)row_tiles * (a.order ? 1u : 4u));
+    a.split_steps = a.blocks / 4 / a.splits;
+    a.split_more = a.blocks / 4 % a.splits;
     hipLaunchKernelGGL(kernel, dim3((unsigned)round_up(row_tiles * tiles, 8), (unsigned)a.splits), dim3(C::kThreads), C::kLds, st, a, (int)row_tiles);
     MX_HIP_TRY(hipGetLastError());
     return CL_OK;
@@ -639,7 +645,7 @@ extern "C" int32_t cl_mx_experts_forward(const cl_mx_matrix *W, int32_t experts,
         a.x_scales = rows.scales;
         if (int32_t rc = launch_expert_lists(call->d_experts, tokens, k, experts, L, &rows, st)) return rc;
     }
-    a.x_div = call->x_per_pair ? 1 : k;
+    a.x_div = make_div(call->x_per_pair ? 1u : (uint32_t)k);
     a.order = L.order;
     a.Y = d_Y;
     if (int32_t rc = run_experts(a, c, L, *call, (float *)((uint8_t *)d_workspace + s.pairs), y_type, st)) return rc;

@@ -61,40 +61,69 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void mx_tile_kernel(ProductArgs a,
         const int per = tiles / 8, more = tiles % 8, die = (int)blockIdx.x % 8, i = (int)blockIdx.x / 8;
         if (i >= per + (die < more)) return;
         const int tile = die * per + min(die, more) + i, band = a.order ? 1 : 4;
-        const int first = tile / (band * row_tiles) * band, in = tile - first * row_tiles, across = min(band, columns - first);
-        column = first + in % across;
-        m0 = in / across * BM;
+        const int first = (int)a.band_tiles.quotient((uint32_t)tile) * band, in = tile - first * row_tiles, across = min(band, columns - first);
+        const int down = across == 1 ? in : across == 2 ? in / 2 : across == 3 ? in / 3 : in / 4;
+        column = first + in - down * across;
+        m0 = down * BM;
     } else {
         if ((int)blockIdx.x >= tiles) return;
-        column = (int)blockIdx.x / row_tiles;
+        column = (int)a.row_tiles.quotient(blockIdx.x);
         m0 = ((int)blockIdx.x - column * row_tiles) * BM;
     }
     Columns c;
     if (!columns_of<BN>(a, column, c)) return;
     const bool routed = !a.order || c.expert < a.experts;
     const int split = (int)blockIdx.y, all_steps = a.blocks / 4;
-    const int t_first = (int)((int64_t)all_steps * split / a.splits), t_end = (int)((int64_t)all_steps * (split + 1) / a.splits);
-    const int steps = routed ? t_end - t_first : 0;
+    const int t_first = split * a.split_steps + min(split, a.split_more);
+    const int steps = routed ? a.split_steps + (split < a.split_more) : 0;
 
-    // where each load of a wavefront reads: rows of W beyond the last and columns beyond the last repeat the last one
-    const int64_t row_bytes = (int64_t)a.blocks * 16;
-    const int64_t w_first = routed ? (int64_t)c.expert * a.M : 0;
-    auto x_row = [&](int n) -> int64_t {
-        const int at = c.first + min(n, c.count - 1);
-        return a.order ? a.order[at] / a.x_div : at;
-    };
+    // Which rows and columns the wavefront has.  A SIMD gets wavefronts s and s + 4: those have different columns, so that a tile
+    // that is not full leaves every SIMD some.
+    const int wm = wave / WN, wn = (wave + wave / 4 * (WN / 2)) % WN;
+    // The rows of X of what the wavefront loads, and the row of Y of its column `lane`: all asked for before the first is used.  (The
+    // kernel's start is what short rows take longest for: 6 x 64 columns, each in an expert of its own, DIGITS us, one after the other
+    // DIGITS.)  Columns beyond the last repeat it.
+    auto place = [&](int n) { return c.first + min(max(n, 0), c.count - 1); };
+    auto load_row = [&](int i) { return (i * C::kWaves + wave) * 16 + (lane >> 2); };
+    auto scale_load = [&](int i) { return min(i * C::kWaves + wave, C::kScaleLoads - 1); };
+    int x_code[C::kCodeLoads], x_scale[C::kScaleShare], y_row = place(wn * TJ * 16 + lane);
+#pragma unroll
+    for (int i = 0; i < C::kCodeLoads; ++i) x_code[i] = place(load_row(i) - BM);
+#pragma unroll
+    for (int i = 0; i < C::kScaleShare; ++i) x_scale[i] = place(scale_load(i) * 64 + lane - BM);
+    static_assert(TJ * 16 <= 64, "");
+    if (a.order) {
+#pragma unroll
+        for (int i = 0; i < C::kCodeLoads; ++i) x_code[i] = a.order[x_code[i]];
+#pragma unroll
+        for (int i = 0; i < C::kScaleShare; ++i) x_scale[i] = a.order[x_scale[i]];
+        y_row = a.order[y_row];
+        if (a.x_div.d > 1) {
+#pragma unroll
+            for (int i = 0; i < C::kCodeLoads; ++i) x_code[i] = (int)a.x_div.quotient((uint32_t)x_code[i]);
+#pragma unroll
+            for (int i = 0; i < C::kScaleShare; ++i) x_scale[i] = (int)a.x_div.quotient((uint32_t)x_scale[i]);
+        }
+    }
+    float weight = 1.0f;
+    if (WEIGHTED) weight = routed ? a.weights[y_row] : 0.0f;
+
+    // where each load of a wavefront reads: rows of W beyond the last repeat it (a tile's rows have less than 4 GB)
+    const uint32_t row_bytes = (uint32_t)a.blocks * 16;
+    const int64_t w_first = (routed ? (int64_t)c.expert * a.M : 0) + m0;
+    const uint8_t *w_tile = a.w_codes + w_first * row_bytes, *w_tile_scales = a.w_scales + w_first * a.blocks;
+    auto w_row = [&](int row) { return (uint32_t)min(row, a.M - 1 - m0); };
     const uint8_t *code_at[C::kCodeLoads], *scale_at[C::kScaleShare];
 #pragma unroll
     for (int i = 0; i < C::kCodeLoads; ++i) {
-        const int q = i * C::kWaves + wave, row = q * 16 + (lane >> 2), chunk = (lane & 3) ^ (lane >> 3 & 3);
-        code_at[i] = (q < BM / 16 ? a.w_codes + (w_first + min(m0 + row, a.M - 1)) * row_bytes : a.x_codes + x_row(row - BM) * row_bytes) + chunk * 16;
+        const int chunk = (lane & 3) ^ (lane >> 3 & 3);
+        code_at[i] = (i * C::kWaves + wave < BM / 16 ? w_tile + w_row(load_row(i)) * row_bytes : a.x_codes + (uint64_t)(uint32_t)x_code[i] * row_bytes) + chunk * 16;
     }
-    auto scale_load = [&](int i) { return min(i * C::kWaves + wave, C::kScaleLoads - 1); };
 #pragma unroll
     for (int i = 0; i < C::kScaleShare; ++i) {
         const int row = scale_load(i) * 64 + lane;
         // (a row of fewer than four steps is read below, and what these loads bring is not used)
-        scale_at[i] = all_steps < 4 ? a.w_codes : row < BM ? a.w_scales + (w_first + min(m0 + row, a.M - 1)) * a.blocks : a.x_scales + x_row(row - BM) * a.blocks;
+        scale_at[i] = all_steps < 4 ? a.w_codes : row < BM ? w_tile_scales + w_row(row) * (uint32_t)a.blocks : a.x_scales + (uint64_t)(uint32_t)x_scale[i] * (uint32_t)a.blocks;
     }
     // code load k of step t into its buffer
     auto request_code = [&](int t, uint8_t *buf, int k) {
@@ -108,18 +137,6 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void mx_tile_kernel(ProductArgs a,
     };
     auto shift = [&](int q) { return all_steps < 4 ? 0 : t_first + 4 * q - min(t_first + 4 * q, all_steps - 4); };
 
-    // Which rows and columns the wavefront has.  A SIMD gets wavefronts s and s + 4: those have different columns, so that a tile
-    // that is not full leaves every SIMD some.
-    const int wm = wave / WN, wn = (wave + wave / 4 * (WN / 2)) % WN;
-    // the row of Y of the wavefront's column `lane`, and its weight
-    static_assert(TJ * 16 <= 64, "");
-    int y_row;
-    float weight = 1.0f;
-    {
-        const int at = c.first + min(wn * TJ * 16 + lane, c.count - 1);
-        y_row = a.order ? a.order[at] : at;
-        if (WEIGHTED) weight = routed ? a.weights[y_row] : 0.0f;
-    }
     // its first output of each row of Y, and the bias from there on
     constexpr int kWide = TI * 16, kLanes = kWide / 4;
     const int m = m0 + wm * kWide + lane % kLanes * 4;
@@ -146,7 +163,8 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void mx_tile_kernel(ProductArgs a,
     auto short_scales = [&](uint8_t *buf) {
         if (threadIdx.x >= BM + BN) return;
         const int row = (int)threadIdx.x;
-        const uint8_t *from = row < BM ? a.w_scales + (w_first + min(m0 + row, a.M - 1)) * a.blocks : a.x_scales + x_row(row - BM) * a.blocks;
+        const int at = place(row - BM), x = a.order ? (int)a.x_div.quotient((uint32_t)a.order[at]) : at;
+        const uint8_t *from = row < BM ? w_tile_scales + w_row(row) * (uint32_t)a.blocks : a.x_scales + (uint64_t)(uint32_t)x * (uint32_t)a.blocks;
         u32x4 v = {0, 0, 0, 0};
 #pragma unroll
         for (int i = 0; i < 3; ++i)
