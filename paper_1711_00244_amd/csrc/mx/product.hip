@@ -328,7 +328,7 @@ template <class T, bool WEIGHTED> static int32_t launch_product(ProductArgs a, c
     a.splits = c.splits;
     switch (c.form) {
     case kTile64: return launch_tiles<64, 64, 2, 2, 8, T, WEIGHTED>(a, tiles, st);
-    case kTile128: return launch_tiles<128, 128, 2, 2, 4, T, WEIGHTED>(a, tiles, st);
+    case kTile128: return launch_tiles<128, 128, 2, 4, 4, T, WEIGHTED>(a, tiles, st);
     case kTile256x128: return launch_tiles<256, 128, 4, 2, 4, T, WEIGHTED>(a, tiles, st);
     case kTile256: return launch_tiles<256, 256, 2, 4, 4, T, WEIGHTED>(a, tiles, st);
     default: break;
