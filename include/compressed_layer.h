@@ -525,7 +525,8 @@ enum {
  * rounding to Y's type at the end.
  *  X         batch rows of W->K             d_bias   W->rows fp32 or NULL
  *  d_Y       batch rows of W->rows (CL_ACT_GATED: half as many) of y_type (CL_F32, CL_BF16, CL_F16), overwritten
- *  d_workspace  at least cl_mx_fc_workspace_bytes() (0 for X in CL_MX4), 256-byte aligned
+ *  d_workspace  at least cl_mx_fc_workspace_bytes() - for X's codes and partial sums; 0, and then NULL will do, where the batch is so
+ *            small that one launch does all -, 256-byte aligned
  * Run-to-run identical.  A batch of 0 is no error.
  * Errors: CL_EINVAL (null pointers, sizes, alignment, workspace too small), CL_EUNSUPPORTED (CL_MX_MAX_K, a launch that does
  * not fit a grid) - nothing is launched then; CL_EHIP. */
@@ -586,7 +587,7 @@ typedef struct {
  * and, with d_weights, Y[t] = sum over j of d_weights[t][j] P[t k + j], added in fp32 in the order of j.
  *  d_Y       with d_weights tokens rows, else tokens x k rows, of W->rows (CL_ACT_GATED: half as many), overwritten; pairs
  *            without an expert add nothing, and without d_weights their rows are zeros
- *  d_workspace  at least cl_mx_experts_workspace_bytes() for this call, 256-byte aligned
+ *  d_workspace  at least cl_mx_experts_workspace_bytes() for this call (of the pointers only whether they are NULL counts), 256-byte aligned
  * Sums, rounding, errors as cl_mx_fc_forward; run-to-run identical.  Zero tokens are no error. */
 int32_t cl_mx_experts_workspace_bytes(const cl_mx_matrix *W, int32_t experts, const cl_mx_experts_call *call, int32_t x_type, size_t *out);
 int32_t cl_mx_experts_forward(const cl_mx_matrix *W, int32_t experts, const cl_mx_input *X, const cl_mx_experts_call *call, void *d_Y,

@@ -37,7 +37,7 @@ KERNELS = {"wide_mul_kernel": "wide", "wide_expand_kernel": "wide_expand", "fc_m
 
 
 def source_hash() -> str:
-    """sha256 over the kernel and host sources of the library, in name order."""
+    """sha256 over the sources of the kernels that are counted here (those at the top of csrc) and of the host side, in name order."""
     h = hashlib.sha256()
     for name in sorted(os.listdir(CSRC)):
         if name.endswith((".hip", ".hpp", ".cpp")):

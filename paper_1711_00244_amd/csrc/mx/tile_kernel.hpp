@@ -11,6 +11,13 @@
 // multiplies stay in program order (scheduling barriers): in a bunch behind the step's barrier they would fill their queues
 // and the multiplies would wait behind them.
 //
+// What bounds it.  256 x 256 (eight wavefronts, one workgroup to a compute unit): 4096 x 4096 x 25088 204 us, 4.1 PFLOP/s, of which
+// the loads into LDS cost 25 (measured without them) and start and stores 8; the rest are multiplies with the reads that feed
+// them, at the rate that power leaves.  With experts, stores of 32-bit rows of pairs: 32768 pairs of 2048 outputs, 268 MB, are 54 of 251
+// us.  64 x 64 (four wavefronts): 256 x 4096 x 9216 18.3 us - 2 to the first step, 0.18 a step, 1.3 to store -; a step takes as
+// long with its loads alone and with its multiplies alone, and with two steps to a barrier.  128 x 128: eight wavefronts, two to a
+// SIMD, which take over from each other: 3000 x 3000 x 300 17.3 us, on four 20.0.  More (256 x 256 on sixteen) do not fit the registers.
+//
 // In LDS a row's four blocks are 64 consecutive bytes, block c of row r in place c ^ (r / 2 % 4).  A read of 16 bytes a lane is
 // served sixteen lanes at a time, of which eight are from one half of a half-wave and eight from the other's; those then touch each of
 // the 64 banks once.  (Otherwise - in order, or with r or r / 4 - reads take twice as long, but are not what a step waits for.)
@@ -80,9 +87,8 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void mx_tile_kernel(ProductArgs a,
     // Which rows and columns the wavefront has.  A SIMD gets wavefronts s and s + 4: those have different columns, so that a tile
     // that is not full leaves every SIMD some.
     const int wm = wave / WN, wn = (wave + wave / 4 * (WN / 2)) % WN;
-    // The rows of X of what the wavefront loads, and the row of Y of its column `lane`: all asked for before the first is used.  (The
-    // kernel's start is what short rows take longest for: 6 x 64 columns, each in an expert of its own, DIGITS us, one after the other
-    // DIGITS.)  Columns beyond the last repeat it.
+    // The rows of X of what the wavefront loads, and the row of Y of its column `lane`: all asked for before the first is used.  (2194
+    // tokens, 8 of 55 experts of 2238 x 1965: 149.7 us in all, one after the other 152.1.)  Columns beyond the last repeat it.
     auto place = [&](int n) { return c.first + min(max(n, 0), c.count - 1); };
     auto load_row = [&](int i) { return (i * C::kWaves + wave) * 16 + (lane >> 2); };
     auto scale_load = [&](int i) { return min(i * C::kWaves + wave, C::kScaleLoads - 1); };
@@ -147,7 +153,7 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void mx_tile_kernel(ProductArgs a,
     auto read_code = [&](const uint8_t *buf, int row) { return *(const i32x4 *)(buf + row * 64 + at_code); };
     // The scales of a row's four steps, by step when they arrive, are turned in place (a thread per row) so that the word of
     // block g has its bytes of the four steps: one read for four multiplies, which pick their byte.  (Reading a byte a
-    // step, the LDS reads of scales took a third of the time: 4096 x 4096 x 25088 240 us.)
+    // step, the LDS reads of scales took a third of the time: 4096 x 4096 x 25088 240 us, now 204.)
     auto turned = [&](u32x4 v, int late) {
         const uint32_t ab01 = __builtin_amdgcn_perm(v[1], v[0], 0x05010400), ab23 = __builtin_amdgcn_perm(v[1], v[0], 0x07030602);
         const uint32_t cd01 = __builtin_amdgcn_perm(v[3], v[2], 0x05010400), cd23 = __builtin_amdgcn_perm(v[3], v[2], 0x07030602);
