@@ -279,7 +279,7 @@ struct Price { int bm, bn, width; float start, alone, shared, shared_experts; };
 constexpr Price kPrices[] = {{64, 64, 1, 5.1f, 0.16f, 0.31f, 0.24f}, {128, 128, 2, 7.5f, 0.35f, 0.63f, 0.52f}, {256, 128, 2, 9.0f, 0.60f, 0.51f, 0.80f},
                              {256, 256, 3, 12.0f, 0.90f, 1.20f, 1.10f}};
 constexpr int kCus = 256;
-constexpr int64_t kCaches = 128 << 20;                       // half of what the caches hold
+constexpr int64_t kCaches = 128 << 20;                       // half of what the caches hold (past them 268 MB of pairs: 312 us in all, through them 325)
 
 // rows: columns of the product in all; experts: how many matrices share them (0: one matrix).
 static Choice choose(int M, int blocks, int64_t rows, int experts)
@@ -289,6 +289,7 @@ static Choice choose(int M, int blocks, int64_t rows, int experts)
     const float mean = experts ? (float)rows / experts : 0.0f, spread = std::sqrt(mean) + mean / 8;
     auto tiles_of = [&](int bn) {
         if (!experts) return (float)((rows + bn - 1) / bn);
+        if (spread > bn) return (mean / bn + 0.5f) * experts;            // (what the sum comes to, with many terms)
         const float whole = std::max(0.0f, std::floor((mean - 4 * spread) / bn));
         float n = (1.0f - std::exp(-mean)) + whole;
         for (float i = whole + 1; i * bn < mean + 4 * spread; ++i) n += 1.0f / (1.0f + std::exp(1.7f * (i * bn - mean) / spread));

@@ -6,7 +6,7 @@
 // 16 x 16.  A step is one matrix instruction deep: 128 k, four blocks, 64 bytes and one word of scales of each row.
 //
 // LDS holds D steps.  Step t is multiplied while t + 1 lies there and t + 2 .. t + D - 1 are on their way, written by the
-// loads themselves.  Its fragments are read from LDS between the multiplies: a row's fragment two pieces before its use, the
+// loads themselves.  Its fragments are read from LDS between the multiplies: a row's fragment up to four pieces before its use, the
 // columns' fragments, which a whole step uses, during the step before (a second set of registers).  Requests, reads and
 // multiplies stay in program order (scheduling barriers): in a bunch behind the step's barrier they would fill their queues
 // and the multiplies would wait behind them.
@@ -43,6 +43,7 @@ template <int BM, int BN, int WM, int WN, int D> struct Tile {
         for (int i = 1; i <= D - 3; ++i) n += kCodeLoads + ((s + 8 - i) % 4 == 0 ? kScaleShare : 0);
         return n;
     }
+    // (scales are asked for six steps before they have to be there: D - 3 less than that)
     static_assert(BM + BN <= kThreads && D >= 3 && D <= 8 && (D - 3) * kCodeLoads + (D + 3) / 4 * kScaleShare < 64 && (D - 2) * kCodeLoads < 64, "");       // (the count that a wait names)
 };
 
