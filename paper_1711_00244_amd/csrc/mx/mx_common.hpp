@@ -72,6 +72,15 @@ __device__ __forceinline__ float to_float(float x) { return x; }
 __device__ __forceinline__ float to_float(bf16_t x) { return (float)x; }
 __device__ __forceinline__ float to_float(f16_t x) { return (float)x; }
 
+// Between accesses of a wavefront's lanes to what its other lanes have in LDS.  A wavefront's LDS accesses are served in order, so this
+// costs nothing at run time; it keeps the compiler from exchanging them.  (A wave barrier alone is no fence for memory.)
+__device__ __forceinline__ void lanes_exchange()
+{
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
 // N consecutive values at any element's address, with one access (gfx950 takes any alignment).
 template <int N, class T> __device__ __forceinline__ void load_values(const T *p, T *v) { __builtin_memcpy(v, p, N * sizeof(T)); }
 template <int N, class T> __device__ __forceinline__ void store_values(T *p, const T *v) { __builtin_memcpy(p, v, N * sizeof(T)); }

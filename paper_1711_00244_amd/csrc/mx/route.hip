@@ -270,7 +270,7 @@ template <class T, int C> __global__ __launch_bounds__(256) void route_rows_kern
             const int size = a.experts / a.groups;
 #pragma unroll
             for (int j = 0; j < C; ++j) s_score[local][sub * C + j] = biased[j];
-            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            lanes_exchange();
             best = second = -INFINITY;
             if (sub < a.groups)
                 for (int i = 0; i < size; ++i) {
@@ -278,7 +278,7 @@ template <class T, int C> __global__ __launch_bounds__(256) void route_rows_kern
                     second = fmaxf(second, fminf(best, v));
                     best = fmaxf(best, v);
                 }
-            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            lanes_exchange();
             const float v = a.top2 && second != -INFINITY ? best + second : best;
             int before = 0;
             groups_before<1>(v, sub, sub, 1, before);
@@ -329,7 +329,7 @@ template <class T, int C> __global__ __launch_bounds__(256) void route_rows_kern
             if (best == 0 && most != 0 && i + 1 < a.k) look();
         }
     }
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");   // (a token's lanes are one wavefront's: its LDS accesses are in order)
+    lanes_exchange();                                        // (a token's lanes are one wavefront's: its LDS accesses are in order)
     int chosen = -1;
     float weight = 0.0f;
     if (sub < a.k) {
@@ -555,9 +555,9 @@ __device__ __forceinline__ void lists_place(const ListArgs &a)
                 same &= b[i] >> bit & 1 ? set : ~set;
             }
             if (b[i] >= 0) L.order[at[wave * buckets + b[i]] + __popcll(same & ((1ull << lane) - 1))] = (int32_t)(p0 + i * 64 + lane);
-            __builtin_amdgcn_wave_barrier();
+            lanes_exchange();
             if (b[i] >= 0 && (same >> lane) == 1) at[wave * buckets + b[i]] += __popcll(same);        // the highest of them
-            __builtin_amdgcn_wave_barrier();
+            lanes_exchange();
         }
     }
 }

@@ -314,7 +314,7 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void mx_tile_kernel(ProductArgs a,
     for (int j = 0; j < TJ; ++j) {
 #pragma unroll
         for (int i = 0; i < TI; ++i) *(f32x4 *)(mine + r * kPitch + i * 16 + 4 * g) = acc[i][j];
-        __builtin_amdgcn_wave_barrier();
+        lanes_exchange();
         const int first = wn * TJ * 16 + j * 16;
         for (int n = lane / kLanes; n < 16; n += 64 / kLanes) {
             const f32x4 v = *(const f32x4 *)(mine + n * kPitch + lane % kLanes * 4);
@@ -324,6 +324,6 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void mx_tile_kernel(ProductArgs a,
             if (a.part) store_part(a, split, row, m, v);
             else store_outputs<T, WEIGHTED>(a, row, m, v, bias, scale);
         }
-        __builtin_amdgcn_wave_barrier();
+        lanes_exchange();
     }
 }
