@@ -540,7 +540,8 @@ int32_t cl_mx_fc_forward(const cl_mx_matrix *W, const cl_mx_input *X, const floa
  *   groups  the experts in `groups` runs of equal length; the groups_kept with the largest group score stay: their largest
  *           score + bias (CL_GROUP_MAX) or the sum of their two largest (CL_GROUP_TOP2)
  *   chosen  the k experts of those groups with the largest keys, in descending order; equal keys (and groups): the lower first
- *   weights the scores - without the bias - of the chosen, divided by their sum if renormalize, times scale
+ *   weights the scores - without the bias - of the chosen, divided by their sum if renormalize, times scale (the quotients are right also
+ *           where the scores are below what fp32 holds; all 0 where every one of them is, beside an infinite logit)
  * A logit that is -inf, the lowest finite value of its type or NaN, and a bias that is NaN or -inf, mask an expert: its
  * score is 0 (as a logit) and it is never chosen.  Where fewer than k experts are left, the last places have expert -1 and
  * weight 0; so has every place of a token whose experts are all masked.  Keys that differ by less than the rounding of

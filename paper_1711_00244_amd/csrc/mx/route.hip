@@ -26,6 +26,11 @@ template <int L, class F> __device__ __forceinline__ float over_lanes(float v, F
     return v;
 }
 
+// Chosen experts whose scores come to less than this together take their weights from their logits instead, as exp(x_j - largest): some scores
+// may be below what fp32 holds, and their ratios are not.  (Softmax: the common denominator cancels.  Logistic function: it is exp(x)
+// there, to one part in 2^60.)
+constexpr float kSmallScores = 0x1p-60f;
+
 // L lanes to a token, C consecutive experts to a lane, so that the lower of two lanes has the lower experts.  k rounds: the
 // largest key of the lanes' own largest, the lowest lane that has it, which then leaves its expert out.
 template <class T, int L, int C> __global__ __launch_bounds__(256) void route_kernel(RouteArgs a)
@@ -121,7 +126,14 @@ template <class T, int L, int C> __global__ __launch_bounds__(256) void route_ke
             if (sub == winner && j == at) key[j] = -INFINITY;
     }
     if (a.renormalize) {
-        const float sum = over_lanes<L>(weight, [](float p, float q) { return p + q; });
+        float sum = over_lanes<L>(weight, [](float p, float q) { return p + q; });
+        if (sum < kSmallScores) {                            // (the same for all lanes of a token)
+            const float logit = live && chosen >= 0 ? to_float(x[chosen]) : -INFINITY;
+            const float most = over_lanes<L>(logit, [](float p, float q) { return fmaxf(p, q); });
+            // (beside an infinite logit the others' scores are 0)
+            weight = logit == -INFINITY || (!a.sigmoid && top == INFINITY) ? 0.0f : expf(logit - most);
+            sum = over_lanes<L>(weight, [](float p, float q) { return p + q; });
+        }
         weight = sum > 0.0f ? weight / sum : 0.0f;
     }
     if (live && sub < a.k) {
@@ -337,7 +349,14 @@ template <class T, int C> __global__ __launch_bounds__(256) void route_rows_kern
         weight = chosen >= 0 ? s_score[local][chosen] : 0.0f;
     }
     if (a.renormalize) {
-        const float sum = over_row(weight, [](float p, float q) { return p + q; });
+        float sum = over_row(weight, [](float p, float q) { return p + q; });
+        if (sum < kSmallScores) {                            // (the same for all lanes of a token)
+            const float l = live && chosen >= 0 ? to_float(x[chosen - sub * C]) : -INFINITY;
+            const float most = over_row(l, [](float p, float q) { return fmaxf(p, q); });
+            // (beside an infinite logit the others' scores are 0)
+            weight = l == -INFINITY || (!a.sigmoid && top == INFINITY) ? 0.0f : exp_of(fmaxf(l - most, -200.0f));
+            sum = over_row(weight, [](float p, float q) { return p + q; });
+        }
         weight = sum > 0.0f ? weight / sum : 0.0f;
     }
     if (live && sub < a.k) {
