@@ -241,14 +241,18 @@ template <class T, int TOGETHER> __global__ __launch_bounds__(256) void mx_join_
     }
 }
 
-template <int BM, int BN, int WM, int WN, int D, class T, bool WEIGHTED> static int32_t launch_tiles(ProductArgs a, int64_t tiles, hipStream_t st)
+enum Form { kRows, kTile64, kTile128, kTile256x128, kTile256 };
+constexpr int kFormRows[] = {16, 64, 128, 256, 256}, kFormThreads[] = {0, 256, 512, 512, 512};      // of a workgroup (kRows: as many as run_waves says)
+
+template <Form F, int BN, int WM, int WN, int D, class T, bool WEIGHTED> static int32_t launch_tiles(ProductArgs a, int64_t tiles, hipStream_t st)
 {
+    constexpr int BM = kFormRows[F];
     using C = Tile<BM, BN, WM, WN, D>;
+    static_assert(C::kThreads == kFormThreads[F], "");
     auto kernel = mx_tile_kernel<BM, BN, WM, WN, D, T, WEIGHTED>;
     static LdsLimit seen;
     if (int32_t rc = allow_lds((const void *)kernel, C::kLds, seen)) return rc;
     const int64_t row_tiles = (a.M + BM - 1) / BM;
-    if (row_tiles * tiles > INT32_MAX - 8) return fail(CL_EUNSUPPORTED, "a launch of %lld workgroups does not fit a grid", (long long)(row_tiles * tiles));
     a.row_tiles = make_div((uint32_t)row_tiles);
     a.band_tiles = make_div((uint32_t)row_tiles * (a.order ? 1u : 4u));
     a.split_steps = a.blocks / 4 / a.splits;
@@ -261,8 +265,6 @@ template <int BM, int BN, int WM, int WN, int D, class T, bool WEIGHTED> static 
 // ------------------------------------------------------------------------- //
 // which kernel
 // ------------------------------------------------------------------------- //
-enum Form { kRows, kTile64, kTile128, kTile256x128, kTile256 };
-
 struct Choice {
     Form form;
     int width;                                               // columns of a tile: an index of kTileWidth
@@ -296,11 +298,11 @@ static Choice choose(int M, int blocks, int64_t rows, int experts)
         return n * experts;
     };
     // columns sixteen at a time: every workgroup reads all it multiplies itself
-    const float wgs = (float)((M + 15) / 16) * tiles_of(16);
+    const float wgs = (float)(((int64_t)M + 15) / 16) * tiles_of(16);
     Choice best{kRows, 0, 1, 2.5f + std::max(1.08e-3f * wgs * runs, 2.6f * ((runs + kRowsWaves - 1) / kRowsWaves))};
     for (int f = kTile64; f <= kTile256; ++f) {
         const Price &p = kPrices[f - kTile64];
-        const float n = tiles_of(p.bn) * ((M + p.bm - 1) / p.bm);
+        const float n = tiles_of(p.bn) * (((int64_t)M + p.bm - 1) / p.bm);
         const bool alone = f >= kTile256x128;                // (one workgroup to a compute unit: whole rounds; else two, which hide starts)
         for (int splits = 1; splits <= 8 && (splits == 1 || steps / splits >= 4); splits *= 2) {
             if (splits > 1 && (experts || n * splits > 2 * kCus)) break;
@@ -322,10 +324,20 @@ static int run_waves(int blocks)
     return (runs + rounds - 1) / rounds;
 }
 
+// Whether the launch has less than 2^32 threads along each axis, for `tiles` columns of tiles.
+static int32_t check_grid(const Choice &c, int32_t M, int blocks, int64_t tiles)
+{
+    const int64_t rows = kFormRows[c.form], row_tiles = (M + rows - 1) / rows;
+    const int64_t wgs = c.form == kRows ? row_tiles : (int64_t)round_up(row_tiles * tiles, 8), threads = c.form == kRows ? run_waves(blocks) * 64 : kFormThreads[c.form];
+    if (wgs > (int64_t)UINT32_MAX / threads) return fail(CL_EUNSUPPORTED, "a launch of %lld workgroups does not fit a grid", (long long)wgs);
+    return CL_OK;
+}
+static int64_t column_tiles(const Choice &c, int64_t rows) { return (rows + kTileWidth[c.width] - 1) / kTileWidth[c.width]; }
+
 // The tiles of a product: rows of X in order, or what the lists have.
 template <class T, bool WEIGHTED> static int32_t launch_product(ProductArgs a, const Choice &c, const ExpertLists *L, hipStream_t st)
 {
-    int64_t tiles = ((int64_t)a.rows + kTileWidth[c.width] - 1) / kTileWidth[c.width];
+    int64_t tiles = column_tiles(c, a.rows);
     if (L) {
         a.tiles = L->tiles[c.width];
         a.tile_count = L->tile_count + c.width;
@@ -333,10 +345,10 @@ template <class T, bool WEIGHTED> static int32_t launch_product(ProductArgs a, c
     }
     a.splits = c.splits;
     switch (c.form) {
-    case kTile64: return launch_tiles<64, 64, 2, 2, 8, T, WEIGHTED>(a, tiles, st);
-    case kTile128: return launch_tiles<128, 128, 2, 4, 4, T, WEIGHTED>(a, tiles, st);
-    case kTile256x128: return launch_tiles<256, 128, 4, 2, 4, T, WEIGHTED>(a, tiles, st);
-    case kTile256: return launch_tiles<256, 256, 2, 4, 4, T, WEIGHTED>(a, tiles, st);
+    case kTile64: return launch_tiles<kTile64, 64, 2, 2, 8, T, WEIGHTED>(a, tiles, st);
+    case kTile128: return launch_tiles<kTile128, 128, 2, 4, 4, T, WEIGHTED>(a, tiles, st);
+    case kTile256x128: return launch_tiles<kTile256x128, 128, 4, 2, 4, T, WEIGHTED>(a, tiles, st);
+    case kTile256: return launch_tiles<kTile256, 256, 2, 4, 4, T, WEIGHTED>(a, tiles, st);
     default: break;
     }
     // (a grid is at most 65535 high: taller ones go in pieces)
@@ -356,12 +368,13 @@ static int few_waves(int blocks, int columns) { return std::max(run_waves(blocks
 
 // Whether few_kernel takes a call: by what it takes in microseconds (fitted to M 119 .. 4096, K 106 .. 25088, 1 .. 256 columns or 1 .. 1245
 // tokens) against the launches that it replaces, of which each costs the host, besides, some 4 us.  kLaunch of those count.
+constexpr int64_t kFewMostWgs = UINT32_MAX / (kFewWaves * 64);         // (a launch has less than 2^32 threads along an axis)
 constexpr float kQuantise = 2.2f, kLists = 5.5f, kJoin = 3.0f, kLaunch = 2.0f;
 static bool few_fc(int M, int blocks, int batch, int32_t x_type)
 {
     const int columns = std::min(batch, kFewColumns);
-    const int64_t groups = (batch + kFewColumns - 1) / kFewColumns, wgs = groups * ((M + 15) / 16);
-    if (x_type == CL_MX4 || groups > 65535 || few_lds(blocks, columns) > kFewLds) return false;
+    const int64_t groups = ((int64_t)batch + kFewColumns - 1) / kFewColumns, row_wgs = ((int64_t)M + 15) / 16, wgs = groups * row_wgs;
+    if (x_type == CL_MX4 || groups > 65535 || row_wgs > kFewMostWgs || few_lds(blocks, columns) > kFewLds) return false;
     // a workgroup's quantisation, the share of a chip that is full of them, or reading the matrix
     const float own = (float)columns * blocks, us = std::max(std::max(4.3f + 2.5e-3f * own, 3.0f + 3.9e-3f * own * wgs / kCus), 2.7f + (float)wgs * 16 * blocks * 17 / 5e6f);
     return us <= kQuantise + choose(M, blocks, batch, 0).us + kLaunch;
@@ -369,9 +382,10 @@ static bool few_fc(int M, int blocks, int batch, int32_t x_type)
 static bool few_experts(int M, int blocks, int32_t x_type, int experts, const cl_mx_experts_call &call)
 {
     if (x_type == CL_MX4 || call.d_lists || call.k > 16 || call.tokens > 65535 || few_lds(blocks, call.x_per_pair ? call.k : 1) > kFewLds) return false;
-    const int rows_each = few_rows_each(call.k);
+    const int64_t rows_each = few_rows_each(call.k), row_wgs = (M + rows_each - 1) / rows_each;
+    if (row_wgs > kFewMostWgs) return false;
     // workgroups as fast as they are launched, or reading a matrix for every token that is sent to it
-    const float wgs = (float)call.tokens * ((M + rows_each - 1) / rows_each), us = 4.0f + std::max(1.45e-3f * wgs, (float)call.tokens * call.k * M * blocks * 17 / 4e6f);
+    const float wgs = (float)call.tokens * row_wgs, us = 4.0f + std::max(1.45e-3f * wgs, (float)call.tokens * call.k * M * blocks * 17 / 4e6f);
     return us <= kLists + choose(M, blocks, (int64_t)call.tokens * call.k, experts).us + kLaunch + (call.d_weights && call.k > 1 ? kJoin + kLaunch : 0.0f);
 }
 
@@ -545,7 +559,12 @@ extern "C" int32_t cl_mx_fc_workspace_bytes(const cl_mx_matrix *W, int32_t batch
     if (!out) return fail(CL_EINVAL, "null pointer");
     if (int32_t rc = check_forward(W, x_type, CL_F32, CL_ACT_NONE)) return rc;
     if (batch < 0) return fail(CL_EINVAL, "batch of %d", (int)batch);
-    *out = few_fc(W->rows, row_blocks(W->K), batch, x_type) ? 0 : fc_scratch(choose(W->rows, row_blocks(W->K), batch, 0), W->rows, W->K, x_type, batch).bytes;
+    *out = 0;
+    if (!few_fc(W->rows, row_blocks(W->K), batch, x_type)) {
+        const Choice c = choose(W->rows, row_blocks(W->K), batch, 0);
+        if (int32_t rc = check_grid(c, W->rows, row_blocks(W->K), column_tiles(c, batch))) return rc;
+        *out = fc_scratch(c, W->rows, W->K, x_type, batch).bytes;
+    }
     clear_error();
     return CL_OK;
 }
@@ -576,6 +595,7 @@ extern "C" int32_t cl_mx_fc_forward(const cl_mx_matrix *W, const cl_mx_input *X,
         return CL_OK;
     }
     const Choice c = choose(W->rows, a.blocks, batch, 0);
+    if (int32_t rc = check_grid(c, a.M, a.blocks, column_tiles(c, batch))) return rc;
     const Scratch s = fc_scratch(c, W->rows, W->K, X->type, batch);
     if (int32_t rc = check_scratch(s, d_workspace, workspace_bytes)) return rc;
     if (int32_t rc = quantised_input(a, X, batch, W->K, s, d_workspace, st)) return rc;
@@ -600,7 +620,12 @@ extern "C" int32_t cl_mx_experts_workspace_bytes(const cl_mx_matrix *W, int32_t 
     if (!out || !call) return fail(CL_EINVAL, "null pointer");
     if (int32_t rc = check_forward(W, x_type, CL_F32, call->act)) return rc;
     if (int32_t rc = check_experts(W, experts, call->tokens, call->k)) return rc;
-    *out = few_experts(W->rows, row_blocks(W->K), x_type, experts, *call) ? 0 : experts_scratch(W->rows, W->K, x_type, experts, *call).bytes;
+    *out = 0;
+    if (!few_experts(W->rows, row_blocks(W->K), x_type, experts, *call)) {
+        const Choice c = choose(W->rows, row_blocks(W->K), (int64_t)call->tokens * call->k, experts);
+        if (int32_t rc = check_grid(c, W->rows, row_blocks(W->K), expert_lists_at(nullptr, call->tokens, call->k, experts).max_tiles[c.width])) return rc;
+        *out = experts_scratch(W->rows, W->K, x_type, experts, *call).bytes;
+    }
     clear_error();
     return CL_OK;
 }
@@ -637,6 +662,7 @@ extern "C" int32_t cl_mx_experts_forward(const cl_mx_matrix *W, int32_t experts,
         return CL_OK;
     }
     const Choice c = choose(a.M, a.blocks, (int64_t)tokens * k, experts);
+    if (int32_t rc = check_grid(c, a.M, a.blocks, expert_lists_at(nullptr, tokens, k, experts).max_tiles[c.width])) return rc;
     const Scratch s = experts_scratch(W->rows, W->K, X->type, experts, *call);
     if (int32_t rc = check_scratch(s, d_workspace, workspace_bytes)) return rc;
     const ExpertLists L = expert_lists_at(call->d_lists ? const_cast<void *>(call->d_lists) : (uint8_t *)d_workspace + s.lists, tokens, k, experts);
