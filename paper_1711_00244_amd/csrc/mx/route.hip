@@ -365,19 +365,29 @@ template <class T, int C> __global__ __launch_bounds__(256) void route_rows_kern
     }
 }
 
+// launch(arguments, workgroups) over the tokens, `per` of them to a workgroup of 256, in pieces whose threads number less than 2^32.
+template <class T, class F> static int32_t in_pieces(RouteArgs a, int per, F launch)
+{
+    const int64_t tokens = a.tokens, step = (int64_t)per << 23;
+    for (int64_t t0 = 0; t0 < tokens; t0 += step) {
+        a.tokens = (int)std::min(step, tokens - t0);
+        launch(a, dim3((unsigned)(((int64_t)a.tokens + per - 1) / per)));
+        MX_HIP_TRY(hipGetLastError());
+        a.logits = (const T *)a.logits + step * a.stride;
+        a.experts_out += step * a.k;
+        a.weights_out += step * a.k;
+    }
+    return CL_OK;
+}
+
 template <class T, int C> static int32_t launch_route_rows(const RouteArgs &a, int group_lanes, hipStream_t st)
 {
-    hipLaunchKernelGGL((route_rows_kernel<T, C>), dim3((unsigned)((a.tokens + 15) / 16)), dim3(256), 0, st, a, group_lanes);
-    MX_HIP_TRY(hipGetLastError());
-    return CL_OK;
+    return in_pieces<T>(a, 16, [&](const RouteArgs &p, dim3 grid) { hipLaunchKernelGGL((route_rows_kernel<T, C>), grid, dim3(256), 0, st, p, group_lanes); });
 }
 
 template <class T, int L, int C> static int32_t launch_route(const RouteArgs &a, hipStream_t st)
 {
-    const int per = 256 / L;
-    hipLaunchKernelGGL((route_kernel<T, L, C>), dim3((unsigned)((a.tokens + per - 1) / per)), dim3(256), 0, st, a);
-    MX_HIP_TRY(hipGetLastError());
-    return CL_OK;
+    return in_pieces<T>(a, 256 / L, [&](const RouteArgs &p, dim3 grid) { hipLaunchKernelGGL((route_kernel<T, L, C>), grid, dim3(256), 0, st, p); });
 }
 
 // ------------------------------------------------------------------------- //
