@@ -526,7 +526,9 @@ enum {
  *  X         batch rows of W->K             d_bias   W->rows fp32 or NULL
  *  d_Y       batch rows of W->rows (CL_ACT_GATED: half as many) of y_type (CL_F32, CL_BF16, CL_F16), overwritten
  *  d_workspace  at least cl_mx_fc_workspace_bytes() - for X's codes and partial sums; 0, and then NULL will do, where the batch is so
- *            small that one launch does all -, 256-byte aligned
+ *            small that one launch does all -, 256-byte aligned.  What is asked for a batch is enough for every smaller one: a call that
+ *            would split its sums, and whose workspace has room for X's codes only, does not split them (slower, and another order
+ *            of the sums)
  * Run-to-run identical.  A batch of 0 is no error.
  * Errors: CL_EINVAL (null pointers, sizes, alignment, workspace too small), CL_EUNSUPPORTED (CL_MX_MAX_K, a launch that does
  * not fit a grid) - nothing is launched then; CL_EHIP. */
@@ -569,7 +571,8 @@ int32_t cl_route_experts(const void *d_logits, int32_t type, int64_t x_stride, c
 
 /* The pairs (token, j) of d_experts[tokens][k] in the order of their experts, for the products of several matrices with one
  * choice of experts.  Starts with experts + 2 int32: where each expert's pairs begin, where the pairs without an expert
- * (any value outside 0 .. experts - 1) begin, and the end; the rest is the library's own.  256-byte aligned. */
+ * (any value outside 0 .. experts - 1) begin, and the end; the rest is the library's own.  256-byte aligned.  What is asked for some
+ * tokens is enough for fewer. */
 int32_t cl_expert_lists_bytes(int32_t tokens, int32_t k, int32_t experts, size_t *out);
 int32_t cl_expert_lists(const int32_t *d_experts, int32_t tokens, int32_t k, int32_t experts, void *d_lists, size_t lists_bytes, void *stream);
 
@@ -588,7 +591,8 @@ typedef struct {
  * and, with d_weights, Y[t] = sum over j of d_weights[t][j] P[t k + j], added in fp32 in the order of j.
  *  d_Y       with d_weights tokens rows, else tokens x k rows, of W->rows (CL_ACT_GATED: half as many), overwritten; pairs
  *            without an expert add nothing, and without d_weights their rows are zeros
- *  d_workspace  at least cl_mx_experts_workspace_bytes() for this call (of the pointers only whether they are NULL counts), 256-byte aligned
+ *  d_workspace  at least cl_mx_experts_workspace_bytes() for this call (of the pointers only whether they are NULL counts), 256-byte aligned;
+ *            what is asked for a call is enough for the same one with fewer tokens
  * Sums, rounding, errors as cl_mx_fc_forward; run-to-run identical.  Zero tokens are no error. */
 int32_t cl_mx_experts_workspace_bytes(const cl_mx_matrix *W, int32_t experts, const cl_mx_experts_call *call, int32_t x_type, size_t *out);
 int32_t cl_mx_experts_forward(const cl_mx_matrix *W, int32_t experts, const cl_mx_input *X, const cl_mx_experts_call *call, void *d_Y,

@@ -707,7 +707,7 @@ def _mx_fc_need(M, K, batch, x_type):
 
 
 def mx_fc_workspace_bytes(W: MxTensor, batch: int, dtype=None) -> int:
-    """Scratch of mx_fc_forward for `batch` rows of dtype (None: an MxTensor)."""
+    """Scratch of mx_fc_forward for `batch` rows of dtype (None: an MxTensor), or fewer."""
     _start()
     return _mx_fc_need(W.shape[0], W.K, batch, MX4 if dtype is None else _element_type(dtype, "X"))
 

@@ -283,8 +283,8 @@ constexpr Price kPrices[] = {{64, 64, 1, 5.1f, 0.16f, 0.31f, 0.24f}, {128, 128, 
 constexpr int kCus = 256;
 constexpr int64_t kCaches = 128 << 20;                       // half of what the caches hold (past them 268 MB of pairs: 312 us in all, through them 325)
 
-// rows: columns of the product in all; experts: how many matrices share them (0: one matrix).
-static Choice choose(int M, int blocks, int64_t rows, int experts)
+// rows: columns of the product in all; experts: how many matrices share them (0: one matrix); most_splits: 1 where there is no room for parts.
+static Choice choose(int M, int blocks, int64_t rows, int experts, int most_splits = 8)
 {
     const int steps = blocks / 4, runs = (blocks + 15) / 16;
     // the matrices that have columns, and those that have more than i tiles of them, their numbers spread about the mean
@@ -304,7 +304,7 @@ static Choice choose(int M, int blocks, int64_t rows, int experts)
         const Price &p = kPrices[f - kTile64];
         const float n = tiles_of(p.bn) * (((int64_t)M + p.bm - 1) / p.bm);
         const bool alone = f >= kTile256x128;                // (one workgroup to a compute unit: whole rounds; else two, which hide starts)
-        for (int splits = 1; splits <= 8 && (splits == 1 || steps / splits >= 4); splits *= 2) {
+        for (int splits = 1; splits <= most_splits && (splits == 1 || steps / splits >= 4); splits *= 2) {
             if (splits > 1 && (experts || n * splits > 2 * kCus)) break;
             const float full = n * splits / kCus, rounds = std::max(1.0f, std::ceil(full));
             const float each = full <= 1.0f ? p.alone : std::max(p.alone, (experts ? p.shared_experts : p.shared) * (alone ? rounds : full));
@@ -539,6 +539,18 @@ static Scratch fc_scratch(const Choice &c, int32_t M, int32_t K, int32_t x_type,
     return s;
 }
 
+// What is asked for a batch is enough for all smaller ones: X's codes grow with it, where they have no room beside them for parts a product is not
+// split, and where one launch would do it is asked what a smaller batch needs that takes more.
+static size_t fc_need(const Choice &c, const cl_mx_matrix &W, int32_t x_type, int32_t batch)
+{
+    const int blocks = row_blocks(W.K);
+    if (!few_fc(W.rows, blocks, batch, x_type)) return fc_scratch(c, W.rows, W.K, x_type, batch).bytes;
+    // (from kFewColumns on, few_kernel takes as long for all batches of a group, and the other forms at least as long as for its first)
+    for (int32_t b = batch - 1; b > 0; b = b <= kFewColumns ? b - 1 : std::max((b - 2) / kFewColumns * kFewColumns + 1, kFewColumns))
+        if (!few_fc(W.rows, blocks, b, x_type)) return fc_scratch(Choice{kRows, 0, 1, 0.0f}, W.rows, W.K, x_type, batch).bytes;
+    return 0;
+}
+
 static Scratch experts_scratch(int32_t M, int32_t K, int32_t x_type, int32_t experts, const cl_mx_experts_call &call)
 {
     Scratch s;
@@ -559,12 +571,10 @@ extern "C" int32_t cl_mx_fc_workspace_bytes(const cl_mx_matrix *W, int32_t batch
     if (!out) return fail(CL_EINVAL, "null pointer");
     if (int32_t rc = check_forward(W, x_type, CL_F32, CL_ACT_NONE)) return rc;
     if (batch < 0) return fail(CL_EINVAL, "batch of %d", (int)batch);
-    *out = 0;
-    if (!few_fc(W->rows, row_blocks(W->K), batch, x_type)) {
-        const Choice c = choose(W->rows, row_blocks(W->K), batch, 0);
+    const Choice c = choose(W->rows, row_blocks(W->K), batch, 0);
+    if (!few_fc(W->rows, row_blocks(W->K), batch, x_type))
         if (int32_t rc = check_grid(c, W->rows, row_blocks(W->K), column_tiles(c, batch))) return rc;
-        *out = fc_scratch(c, W->rows, W->K, x_type, batch).bytes;
-    }
+    *out = fc_need(c, *W, x_type, batch);
     clear_error();
     return CL_OK;
 }
@@ -594,9 +604,13 @@ extern "C" int32_t cl_mx_fc_forward(const cl_mx_matrix *W, const cl_mx_input *X,
         clear_error();
         return CL_OK;
     }
-    const Choice c = choose(W->rows, a.blocks, batch, 0);
+    Choice c = choose(W->rows, a.blocks, batch, 0);
+    Scratch s = fc_scratch(c, W->rows, W->K, X->type, batch);
+    if (c.splits > 1 && workspace_bytes < s.bytes) {
+        c = choose(W->rows, a.blocks, batch, 0, 1);
+        s = fc_scratch(c, W->rows, W->K, X->type, batch);
+    }
     if (int32_t rc = check_grid(c, a.M, a.blocks, column_tiles(c, batch))) return rc;
-    const Scratch s = fc_scratch(c, W->rows, W->K, X->type, batch);
     if (int32_t rc = check_scratch(s, d_workspace, workspace_bytes)) return rc;
     if (int32_t rc = quantised_input(a, X, batch, W->K, s, d_workspace, st)) return rc;
     a.part = c.splits > 1 ? (float *)((uint8_t *)d_workspace + s.pairs) : nullptr;
@@ -620,12 +634,14 @@ extern "C" int32_t cl_mx_experts_workspace_bytes(const cl_mx_matrix *W, int32_t 
     if (!out || !call) return fail(CL_EINVAL, "null pointer");
     if (int32_t rc = check_forward(W, x_type, CL_F32, call->act)) return rc;
     if (int32_t rc = check_experts(W, experts, call->tokens, call->k)) return rc;
-    *out = 0;
-    if (!few_experts(W->rows, row_blocks(W->K), x_type, experts, *call)) {
+    // (enough for fewer tokens too: where one launch would do, what the most tokens below need that take more)
+    cl_mx_experts_call most = *call;
+    while (most.tokens > 0 && few_experts(W->rows, row_blocks(W->K), x_type, experts, most)) --most.tokens;
+    if (most.tokens == call->tokens) {
         const Choice c = choose(W->rows, row_blocks(W->K), (int64_t)call->tokens * call->k, experts);
         if (int32_t rc = check_grid(c, W->rows, row_blocks(W->K), expert_lists_at(nullptr, call->tokens, call->k, experts).max_tiles[c.width])) return rc;
-        *out = experts_scratch(W->rows, W->K, x_type, experts, *call).bytes;
     }
+    *out = most.tokens > 0 ? experts_scratch(W->rows, W->K, x_type, experts, most).bytes : 0;
     clear_error();
     return CL_OK;
 }

@@ -403,7 +403,7 @@ static int64_t list_chunk(int64_t pairs) { return std::max<int64_t>(1, (pairs + 
 ExpertLists expert_lists_at(void *base, int32_t tokens, int32_t k, int32_t experts)
 {
     ExpertLists L;
-    const int64_t pairs = (int64_t)tokens * k, chunk = list_chunk(pairs), chunks = (pairs + chunk - 1) / chunk;
+    const int64_t pairs = (int64_t)tokens * k, chunks = std::min<int64_t>(256, (pairs + 4095) / 4096);       // (not fewer than there are, and not fewer for more pairs)
     size_t at = 0;
     auto take = [&](size_t bytes) { char *p = (char *)base + at; at += round_up(bytes, 256); return p; };
     L.offsets = (int32_t *)take(((size_t)experts + 2) * 4);
