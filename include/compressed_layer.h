@@ -536,6 +536,19 @@ int32_t cl_mx_fc_workspace_bytes(const cl_mx_matrix *W, int32_t batch, int32_t x
 int32_t cl_mx_fc_forward(const cl_mx_matrix *W, const cl_mx_input *X, const float *d_bias_or_null, void *d_Y, int32_t y_type, int32_t batch,
                          int32_t act, void *d_workspace, size_t workspace_bytes, void *stream);
 
+/* How a product is made. */
+enum {
+    CL_MX_FORM_FEW = 0,          /* one launch that quantises X itself and multiplies; experts: no lists either           */
+    CL_MX_FORM_ROWS = 1,         /* sixteen rows of the matrix and sixteen columns to a workgroup, no operand shared       */
+    CL_MX_FORM_TILE_64 = 2,      /* tiles of the output with their operands in LDS: 64 x 64,                               */
+    CL_MX_FORM_TILE_128 = 3,     /*   128 x 128,                                                                           */
+    CL_MX_FORM_TILE_256X128 = 4, /*   256 rows of the matrix x 128,                                                        */
+    CL_MX_FORM_TILE_256 = 5      /*   256 x 256                                                                            */
+};
+/* The form that cl_mx_fc_forward takes for W, batch and X's type, given a workspace of cl_mx_fc_workspace_bytes() for that batch, and into how
+ * many sums it splits k.  Errors as cl_mx_fc_workspace_bytes. */
+int32_t cl_mx_fc_resolved_form(const cl_mx_matrix *W, int32_t batch, int32_t x_type, int32_t *form, int32_t *splits);
+
 /* The choice of experts for tokens.  Per token, in fp32:
  *   scores  softmax (CL_SCORE_SOFTMAX) or logistic function (CL_SCORE_SIGMOID) of its logits
  *   keys    scores + bias; without a bias the logits themselves, which have the same order
@@ -595,6 +608,8 @@ typedef struct {
  *            what is asked for a call is enough for the same one with fewer tokens
  * Sums, rounding, errors as cl_mx_fc_forward; run-to-run identical.  Zero tokens are no error. */
 int32_t cl_mx_experts_workspace_bytes(const cl_mx_matrix *W, int32_t experts, const cl_mx_experts_call *call, int32_t x_type, size_t *out);
+/* The form that cl_mx_experts_forward takes for such a call (of the pointers only whether they are NULL counts). */
+int32_t cl_mx_experts_resolved_form(const cl_mx_matrix *W, int32_t experts, const cl_mx_experts_call *call, int32_t x_type, int32_t *form);
 int32_t cl_mx_experts_forward(const cl_mx_matrix *W, int32_t experts, const cl_mx_input *X, const cl_mx_experts_call *call, void *d_Y,
                               int32_t y_type, void *d_workspace, size_t workspace_bytes, void *stream);
 

@@ -23,6 +23,7 @@ MX4 = 3                                # CL_MX4, after the element types of _ele
 ACTIVATIONS = {"none": 0, "relu": 1, "gated": 2}
 SCORES = {"softmax": 0, "sigmoid": 1}
 GROUP_SCORES = {"max": 0, "top2": 1}
+MX_FORMS = ("few", "rows", "tile 64", "tile 128", "tile 256 x 128", "tile 256")       # CL_MX_FORM_*
 
 EXPORTS = [
     "cl_last_error", "cl_compress_layer", "cl_layer_upload", "cl_layer_free", "cl_layer_stats",
@@ -33,7 +34,7 @@ EXPORTS = [
     "cl_compressed_conv_forward", "cl_plan_batches", "cl_maxpool_forward", "cl_lrn_forward",
     "cl_set_kernel_timing", "cl_last_kernel_ms",
     "cl_mx_quantize", "cl_mx_dequantize", "cl_mx_fc_workspace_bytes", "cl_mx_fc_forward", "cl_route_experts", "cl_expert_lists_bytes",
-    "cl_expert_lists", "cl_mx_experts_workspace_bytes", "cl_mx_experts_forward",
+    "cl_expert_lists", "cl_mx_experts_workspace_bytes", "cl_mx_experts_forward", "cl_mx_fc_resolved_form", "cl_mx_experts_resolved_form",
 ]
 
 
@@ -146,6 +147,8 @@ def lib():
     L.cl_expert_lists_bytes.argtypes = [i32, i32, i32, C.POINTER(sz)]
     L.cl_expert_lists.argtypes = [p, i32, i32, i32, p, sz, p]
     L.cl_mx_experts_workspace_bytes.argtypes = [C.POINTER(MxMatrix), i32, C.POINTER(MxExpertsCall), i32, C.POINTER(sz)]
+    L.cl_mx_fc_resolved_form.argtypes = [C.POINTER(MxMatrix), i32, i32, C.POINTER(i32), C.POINTER(i32)]
+    L.cl_mx_experts_resolved_form.argtypes = [C.POINTER(MxMatrix), i32, C.POINTER(MxExpertsCall), i32, C.POINTER(i32)]
     L.cl_mx_experts_forward.argtypes = [C.POINTER(MxMatrix), i32, C.POINTER(MxInput), C.POINTER(MxExpertsCall), p, i32, p, sz, p]
     for name in EXPORTS:
         if name not in ("cl_last_error", "cl_layer_group_free"):
@@ -712,6 +715,14 @@ def mx_fc_workspace_bytes(W: MxTensor, batch: int, dtype=None) -> int:
     return _mx_fc_need(W.shape[0], W.K, batch, MX4 if dtype is None else _element_type(dtype, "X"))
 
 
+def mx_fc_resolved_form(W: MxTensor, batch: int, dtype=None) -> tuple[str, int]:
+    """How mx_fc_forward makes `batch` rows of dtype (None: an MxTensor): one of MX_FORMS, and how many sums k is split into."""
+    _start()
+    form, splits = C.c_int32(0), C.c_int32(0)
+    _check(lib().cl_mx_fc_resolved_form(MxMatrix(None, None, W.shape[0], W.K), batch, MX4 if dtype is None else _element_type(dtype, "X"), form, splits))
+    return MX_FORMS[form.value], splits.value
+
+
 def mx_fc_forward(W: MxTensor, X, bias=None, relu=False, act=None, dtype=None, out=None, workspace=None):
     """act(X W^T + bias) with W (M, K) in 4-bit blocks and X (B, K) - float32, bfloat16 or float16, quantised on the way, or an MxTensor.
     act: "none", "relu" (the same as relu=True) or "gated" (rows 2 i and 2 i + 1 of W give gate and value of output i).  The output is of
@@ -797,6 +808,21 @@ def _mx_experts_need(M, K, E, T, k, weighted, lists, act, x_per_pair, x_type):
     call = MxExpertsCall(T, k, None, 256 if weighted else None, None, 256 if lists else None, act, x_per_pair)
     _check(lib().cl_mx_experts_workspace_bytes(MxMatrix(None, None, M, K), E, call, x_type, n))
     return n.value
+
+
+@functools.lru_cache(maxsize=1024)
+def _mx_experts_form(M, K, E, T, k, weighted, lists, x_per_pair, x_type):
+    form = C.c_int32(0)
+    call = MxExpertsCall(T, k, None, 256 if weighted else None, None, 256 if lists else None, 0, x_per_pair)
+    _check(lib().cl_mx_experts_resolved_form(MxMatrix(None, None, M, K), E, call, x_type, form))
+    return MX_FORMS[form.value]
+
+
+def mx_experts_resolved_form(W: MxTensor, tokens: int, k: int, dtype=None, weighted=True, x_per_pair=False, lists=False) -> str:
+    """How mx_experts_forward makes the products of `tokens` rows of dtype (None: an MxTensor) with k experts each: one of MX_FORMS."""
+    _start()
+    E, M, K = W.shape
+    return _mx_experts_form(M, K, E, tokens, k, weighted, lists, int(x_per_pair), MX4 if dtype is None else _element_type(dtype, "X"))
 
 
 def mx_experts_forward(W: MxTensor, X, experts, weights=None, bias=None, act="none", x_per_pair=False, lists: ExpertLists | None = None, dtype=None,

@@ -579,6 +579,20 @@ extern "C" int32_t cl_mx_fc_workspace_bytes(const cl_mx_matrix *W, int32_t batch
     return CL_OK;
 }
 
+static_assert(CL_MX_FORM_ROWS == 1 + kRows && CL_MX_FORM_TILE_64 == 1 + kTile64 && CL_MX_FORM_TILE_256 == 1 + kTile256, "");
+
+extern "C" int32_t cl_mx_fc_resolved_form(const cl_mx_matrix *W, int32_t batch, int32_t x_type, int32_t *form, int32_t *splits)
+{
+    if (!form || !splits) return fail(CL_EINVAL, "null pointer");
+    size_t bytes;
+    if (int32_t rc = cl_mx_fc_workspace_bytes(W, batch, x_type, &bytes)) return rc;
+    const bool few = few_fc(W->rows, row_blocks(W->K), batch, x_type);
+    const Choice c = choose(W->rows, row_blocks(W->K), batch, 0);
+    *form = few ? CL_MX_FORM_FEW : 1 + c.form;
+    *splits = few ? 1 : c.splits;
+    return CL_OK;
+}
+
 extern "C" int32_t cl_mx_fc_forward(const cl_mx_matrix *W, const cl_mx_input *X, const float *d_bias, void *d_Y, int32_t y_type, int32_t batch, int32_t act,
                                     void *d_workspace, size_t workspace_bytes, void *stream)
 {
@@ -643,6 +657,16 @@ extern "C" int32_t cl_mx_experts_workspace_bytes(const cl_mx_matrix *W, int32_t 
     }
     *out = most.tokens > 0 ? experts_scratch(W->rows, W->K, x_type, experts, most).bytes : 0;
     clear_error();
+    return CL_OK;
+}
+
+extern "C" int32_t cl_mx_experts_resolved_form(const cl_mx_matrix *W, int32_t experts, const cl_mx_experts_call *call, int32_t x_type, int32_t *form)
+{
+    if (!form) return fail(CL_EINVAL, "null pointer");
+    size_t bytes;
+    if (int32_t rc = cl_mx_experts_workspace_bytes(W, experts, call, x_type, &bytes)) return rc;
+    const bool few = few_experts(W->rows, row_blocks(W->K), x_type, experts, *call);
+    *form = few ? CL_MX_FORM_FEW : 1 + choose(W->rows, row_blocks(W->K), (int64_t)call->tokens * call->k, experts).form;
     return CL_OK;
 }
 
