@@ -595,7 +595,8 @@ typedef struct {
     const int32_t *d_experts;      /* tokens x k: expert of each pair; any value outside 0 .. experts - 1: none                */
     const float *d_weights;        /* tokens x k, or NULL                                                                      */
     const float *d_bias;           /* experts x rows fp32, or NULL                                                             */
-    const void *d_lists;           /* cl_expert_lists() of d_experts, or NULL: made on the way                                 */
+    const void *d_lists;           /* cl_expert_lists() of d_experts, or NULL: made on the way, or not at all where one launch */
+                                   /*   does without (CL_MX_FORM_FEW, which a call with lists does not take)               */
     int32_t act;                   /* CL_ACT_*                                                                                 */
     int32_t x_per_pair;            /* X has a row for each pair (token * k + j), else for each token                           */
 } cl_mx_experts_call;

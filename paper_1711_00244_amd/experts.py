@@ -3,7 +3,7 @@ the experts are gated two-matrix networks in 4-bit blocks.  One call is
 
     logits = compressed_fc_forward(router, X)                       float32, (tokens, experts)
     chosen, weights = route_experts(logits, k, ...)
-    lists = expert_lists(chosen, experts)                           once for both products
+    lists = expert_lists(chosen, experts)                           once for both products; not where both are one launch without
     hidden = mx_experts_forward(up, X, chosen, act="gated")         a row per pair
     Y = mx_experts_forward(down, hidden, chosen, weights, ...)      a row per token
 
@@ -23,7 +23,7 @@ import numpy as np
 from . import binding as cl
 from . import workloads as wl
 
-SHARED_QUANTISE_TOKENS = 64      # below, the products quantise X themselves, most of them in the launch that multiplies
+SHARED_QUANTISE_TOKENS = 64      # below, each product quantises X itself: the few rows of those that are one launch, in that launch
 
 
 class ExpertLayer:
@@ -53,8 +53,11 @@ class ExpertLayer:
         if X.shape[0] == 0:
             return X.new_empty((0, self.width))              # (a compressed layer takes no empty batch)
         experts, weights = self.route(X)
-        lists = cl.expert_lists(experts, self.experts)
         x = cl.mx_quantize(X) if self.shared is not None and X.shape[0] >= SHARED_QUANTISE_TOKENS else X
+        # (of the default layer up to 15 tokens.  One token, calls recorded in a graph: 29 us, with lists 37; called one by one 63, with lists 80)
+        one_launch = ("few" == cl.mx_experts_resolved_form(self.up, X.shape[0], self.k, None if x is not X else X.dtype, weighted=False)
+                      == cl.mx_experts_resolved_form(self.down, X.shape[0], self.k, X.dtype, x_per_pair=True))
+        lists = None if one_launch else cl.expert_lists(experts, self.experts)
         hidden = cl.mx_experts_forward(self.up, x, experts, act="gated", lists=lists, dtype=X.dtype)
         Y = cl.mx_experts_forward(self.down, hidden, experts, weights, x_per_pair=True, lists=lists)
         if self.shared is not None:
