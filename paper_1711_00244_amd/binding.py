@@ -568,6 +568,13 @@ def _element_type(dtype, what):
     return ty
 
 
+def _int32(*sizes):
+    """What the library takes in 32 bits: ctypes would cut off what is beyond."""
+    for n in sizes:
+        if not -1 << 31 <= n < 1 << 31:
+            raise ValueError(f"{n} does not fit 32 bits")
+
+
 def _rows(t, what, cols=None):
     """A matrix whose rows are contiguous, at any distance from each other -> (element type, distance)."""
     ty = _element_type(t.dtype, what)
@@ -632,6 +639,7 @@ def mx_quantize(X, out: MxTensor | None = None) -> MxTensor:
     if len(shape) > 2:
         X = X.reshape(-1, K)
     ty, stride = _rows(X, "X")
+    _int32(K)
     if out is None:
         kb = mx_row_blocks(K)
         out = MxTensor.__new__(MxTensor)
@@ -656,6 +664,7 @@ def mx_dequantize(Q: MxTensor, dtype=None, out=None):
     elif out.shape != shape or not (out.is_contiguous() or len(shape) == 2) or (dtype is not None and out.dtype != dtype):
         raise ValueError(f"out must be {tuple(shape)}{'' if dtype is None else f' of {dtype}'}, contiguous or a matrix with contiguous rows")
     Y = out if len(shape) == 2 else out.view(-1, Q.K)
+    _int32(Q.K)
     ty, stride = _rows(Y, "out", Q.K)
     stream = _on(codes.device, out)
     _check(L.cl_mx_dequantize(codes.data_ptr(), Q.scales.data_ptr(), Y.shape[0], Q.K, out.data_ptr(), ty, stride, stream))
@@ -704,6 +713,7 @@ def _act(act):
 
 @functools.lru_cache(maxsize=1024)
 def _mx_fc_need(M, K, batch, x_type):
+    _int32(M, K, batch)
     n = C.c_size_t(0)
     _check(lib().cl_mx_fc_workspace_bytes(MxMatrix(None, None, M, K), batch, x_type, n))
     return n.value
@@ -718,6 +728,7 @@ def mx_fc_workspace_bytes(W: MxTensor, batch: int, dtype=None) -> int:
 def mx_fc_resolved_form(W: MxTensor, batch: int, dtype=None) -> tuple[str, int]:
     """How mx_fc_forward makes `batch` rows of dtype (None: an MxTensor): one of MX_FORMS, and how many sums k is split into."""
     _start()
+    _int32(*W.shape, batch)
     form, splits = C.c_int32(0), C.c_int32(0)
     _check(lib().cl_mx_fc_resolved_form(MxMatrix(None, None, W.shape[0], W.K), batch, MX4 if dtype is None else _element_type(dtype, "X"), form, splits))
     return MX_FORMS[form.value], splits.value
@@ -754,15 +765,18 @@ def route_experts(logits, k: int, bias=None, score="softmax", groups: int = 1, g
     L = _start()
     ty, stride = _rows(logits, "logits")
     T, E = logits.shape
+    groups_kept = groups if groups_kept is None else groups_kept
+    _int32(T, E, k, groups, groups_kept)
     if bias is not None:
         _want(bias, (E,), "bias")
     if score not in SCORES or group_score not in GROUP_SCORES:
         raise ValueError(f"score must be one of {', '.join(SCORES)} and group_score of {', '.join(GROUP_SCORES)}, got {score!r} and {group_score!r}")
     device = logits.device
     stream = _on(device, bias)
-    d = RouteDesc(E, k, SCORES[score], groups, groups if groups_kept is None else groups_kept, GROUP_SCORES[group_score], int(renormalize), scale)
-    experts = torch.empty((T, max(k, 0)), dtype=torch.int32, device=device)
-    weights = torch.empty((T, max(k, 0)), dtype=torch.float32, device=device)
+    d = RouteDesc(E, k, SCORES[score], groups, groups_kept, GROUP_SCORES[group_score], int(renormalize), scale)
+    width = k if 0 < k <= E else 0                           # (other k are refused)
+    experts = torch.empty((T, width), dtype=torch.int32, device=device)
+    weights = torch.empty((T, width), dtype=torch.float32, device=device)
     _check(L.cl_route_experts(logits.data_ptr(), ty, stride, None if bias is None else bias.data_ptr(), T, d, experts.data_ptr(), weights.data_ptr(), stream))
     return experts, weights
 
@@ -795,6 +809,7 @@ def expert_lists(experts, n_experts: int) -> ExpertLists:
     _want_experts(experts)
     stream = _on(experts.device)
     T, k = experts.shape
+    _int32(T, k, n_experts)
     n = C.c_size_t(0)
     _check(L.cl_expert_lists_bytes(T, k, n_experts, n))
     buffer = torch.empty(n.value, dtype=torch.uint8, device=experts.device)
@@ -804,6 +819,7 @@ def expert_lists(experts, n_experts: int) -> ExpertLists:
 
 @functools.lru_cache(maxsize=1024)
 def _mx_experts_need(M, K, E, T, k, weighted, lists, act, x_per_pair, x_type):
+    _int32(M, K, E, T, k)
     n = C.c_size_t(0)
     call = MxExpertsCall(T, k, None, 256 if weighted else None, None, 256 if lists else None, act, x_per_pair)
     _check(lib().cl_mx_experts_workspace_bytes(MxMatrix(None, None, M, K), E, call, x_type, n))
@@ -812,6 +828,7 @@ def _mx_experts_need(M, K, E, T, k, weighted, lists, act, x_per_pair, x_type):
 
 @functools.lru_cache(maxsize=1024)
 def _mx_experts_form(M, K, E, T, k, weighted, lists, x_per_pair, x_type):
+    _int32(M, K, E, T, k)
     form = C.c_int32(0)
     call = MxExpertsCall(T, k, None, 256 if weighted else None, None, 256 if lists else None, 0, x_per_pair)
     _check(lib().cl_mx_experts_resolved_form(MxMatrix(None, None, M, K), E, call, x_type, form))
