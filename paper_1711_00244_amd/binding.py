@@ -743,6 +743,8 @@ def mx_fc_forward(W: MxTensor, X, bias=None, relu=False, act=None, dtype=None, o
     if len(codes.shape) != 2:
         raise ValueError(f"W must be a matrix, got {W.shape}")
     M = codes.shape[0]
+    if relu and act not in (None, "relu"):
+        raise ValueError(f"relu=True and act={act!r}")
     act = _act(act or ("relu" if relu else "none"))
     xs, B, own_dtype = _mx_input(X, K)
     if bias is not None:
