@@ -68,6 +68,15 @@ template <int S> __device__ __forceinline__ f32x4 mfma_fp4(i32x4 a, i32x4 b, f32
     return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(widen(a), widen(b), acc, 4, 4, S, scale_a, S, scale_b);
 }
 
+// a b as a 32-bit number before anything else is done with it.  (A product that is rounded to 16 bits next may else become one instruction, a b + 0
+// rounded to fp16, whose last bit can differ and which makes zeros of negative ones.)
+__device__ __forceinline__ float product32(float a, float b)
+{
+    float r = a * b;
+    asm("" : "+v"(r));
+    return r;
+}
+
 __device__ __forceinline__ float to_float(float x) { return x; }
 __device__ __forceinline__ float to_float(bf16_t x) { return (float)x; }
 __device__ __forceinline__ float to_float(f16_t x) { return (float)x; }

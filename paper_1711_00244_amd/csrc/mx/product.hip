@@ -61,16 +61,8 @@ __device__ __forceinline__ f32x4 bias_of(const ProductArgs &a, int expert, int m
     return b;
 }
 
-// w v, rounded to 32 bits before it is rounded to a type of sixteen (in one step the last bit would not always be the same as that of
-// the kernels that sum over k pairs).
-__device__ __forceinline__ float weighted(float w, float v)
-{
-    float r = w * v;
-    asm("" : "+v"(r));
-    return r;
-}
-
-// The outputs of four consecutive rows of the matrix, from m on, in one row of Y; WEIGHTED: times its weight.
+// The outputs of four consecutive rows of the matrix, from m on, in one row of Y; WEIGHTED: times its weight, rounded to 32 bits as in the kernels that
+// sum over k pairs.
 template <class T, bool WEIGHTED> __device__ __forceinline__ void store_outputs(const ProductArgs &a, int64_t row, int m, f32x4 v, f32x4 bias, float weight)
 {
     if (m >= a.M) return;
@@ -79,7 +71,7 @@ template <class T, bool WEIGHTED> __device__ __forceinline__ void store_outputs(
     if (a.act == CL_ACT_GATED) {
         // rows 2 i and 2 i + 1 of the matrix: gate and value of output i
         const float g[2] = {v[0] / (1.0f + expf(-v[0])) * v[1], v[2] / (1.0f + expf(-v[2])) * v[3]};
-        const T out[2] = {(T)(WEIGHTED ? weighted(weight, g[0]) : g[0]), (T)(WEIGHTED ? weighted(weight, g[1]) : g[1])};
+        const T out[2] = {(T)(WEIGHTED ? product32(weight, g[0]) : g[0]), (T)(WEIGHTED ? product32(weight, g[1]) : g[1])};
         y += m / 2;
         if (m / 2 + 2 <= a.out_width) store_values<2>(y, out);
         else y[0] = out[0];
@@ -89,7 +81,7 @@ template <class T, bool WEIGHTED> __device__ __forceinline__ void store_outputs(
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const float r = a.act == CL_ACT_RELU && v[i] < 0.0f ? 0.0f : v[i];       // (NaN stays)
-        out[i] = (T)(WEIGHTED ? weighted(weight, r) : r);
+        out[i] = (T)(WEIGHTED ? product32(weight, r) : r);
     }
     y += m;
     if (m + 4 <= a.out_width) {

@@ -37,7 +37,7 @@ __global__ __launch_bounds__(256) void mx_dequantize_kernel(const void *__restri
         }
         T y[V];
 #pragma unroll
-        for (int j = 0; j < V; ++j) y[j] = (T)(v[j / 2][j % 2] * s);
+        for (int j = 0; j < V; ++j) y[j] = (T)product32(v[j / 2][j % 2], s);
         T *out = Y + (int64_t)row * stride + k0;
         if (left >= V) {
             typename U::Bytes b;
