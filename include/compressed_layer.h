@@ -506,7 +506,8 @@ typedef struct {
 /* Rows of numbers to that form.  The scale of a block is 2^(floor(log2(largest magnitude)) - 2), at least 2^-127, so that the
  * largest magnitude lies between 4 and 8 of it; a value takes the nearest code, ties to the one with an even last bit,
  * what is above 6 takes 6.  A block with a value that is not finite is NaN as a whole.  Zero rows are no error.
- * cl_mx_dequantize gives the values that codes and scales stand for (exact in fp32 and bf16, rounded to nearest in fp16).
+ * cl_mx_dequantize gives the values that codes and scales stand for: rounded to nearest in fp16, exact in fp32 and bf16 but for the larger
+ * codes under the scale bytes 253 and 254, which are infinite there (cl_mx_quantize makes no scale above 252).
  *  type      CL_F32, CL_BF16 or CL_F16    x_stride, y_stride   elements from row to row, at least K
  * Errors: CL_EINVAL (null pointers, sizes, alignment, overlapping rows), CL_EUNSUPPORTED (K above CL_MX_MAX_K) - nothing is
  * launched then; CL_EHIP. */

@@ -265,7 +265,9 @@ struct Choice {
 };
 
 // What a form takes in microseconds, fitted to measurements of 450 shapes of M 100 .. 4096, K 100 .. 25088, 20 .. 16000 columns, one
-// matrix and 4 to 128: over 550 others the choice takes 1.4 % longer, in the mean of logarithms, than the best of the forms.
+// matrix and 4 to 128: over 550 others the choice took 1.4 % longer, in the mean of logarithms, than the best of the forms.  (That was with
+// 128 x 128 on four wavefronts; on eight it is 7-14 % faster at small K, and its row is as it was.  A row fits its shapes on the whole: a step of 64 x 64
+// alone on a compute unit is 0.16 here and 0.18 at 256 x 4096 x 9216.)
 // Tiles: a start (launch, what its columns are, first loads, last stores), and per step of 128 k what a workgroup takes alone on
 // its compute unit, or its share of a full one where the launch has more workgroups than the chip has compute units; that
 // is another with experts, whose matrices change within a launch.
@@ -359,7 +361,9 @@ static int few_rows_each(int k) { return 32 / k / 2 * 2; }
 static int few_waves(int blocks, int columns) { return std::max(run_waves(blocks), std::min(kFewWaves, (columns * blocks * 4 + 255) / 256)); }
 
 // Whether few_kernel takes a call: by what it takes in microseconds (fitted to M 119 .. 4096, K 106 .. 25088, 1 .. 256 columns or 1 .. 1245
-// tokens) against the launches that it replaces, of which each costs the host, besides, some 4 us.  kLaunch of those count.
+// tokens) against the launches that it replaces, of which each costs the host, besides, some 4 us.  kLaunch of those count: between calls one by one,
+// which pay them, and calls recorded in a graph, which do not.  (37 rows of bf16 by 1000 x 4096: 9.4 and 9.3 by price, so two launches, 8.4 of
+// kernels and 13.1 a call.)
 constexpr int64_t kFewMostWgs = UINT32_MAX / (kFewWaves * 64);         // (a launch has less than 2^32 threads along an axis)
 constexpr float kQuantise = 2.2f, kLists = 5.5f, kJoin = 3.0f, kLaunch = 2.0f;
 static bool few_fc(int M, int blocks, int batch, int32_t x_type)

@@ -188,8 +188,9 @@ template <int R> __device__ __forceinline__ void groups_before(float v, int g, i
 // The same for up to sixteen choices among up to 16 C experts: sixteen lanes - a row, within which lanes exchange registers without the LDS -
 // to a token, C experts to a lane, four tokens to a wavefront.  A lane keeps its three largest keys and looks for the next
 // three only when all are taken (8 of 256 experts in half of eight groups: one round of eight, over a wavefront's four tokens).
-// What bounds it is instructions: 16381 tokens of 256 experts, logistic scores, a bias, groups, 8 chosen, 16.5 us - of 16.8 MB,
-// which take 3.5 - where sixty-four lanes to a token, four experts each, and exchanges through LDS took 30.
+// What bounds it is instructions, which have 61 % of the vector units' cycles (counters), and rounds that wait for each other: 16381 tokens
+// of 256 experts, logistic scores, a bias, groups, 8 chosen, 17 us - of 16.8 MB, which take 3.5 - where sixty-four lanes to a token, four
+// experts each, and exchanges through LDS took 30.
 // group_lanes: lanes of a group, a power of two; 0: groups do not end with a lane (16381 tokens, 12 groups of 20 experts: 16 us, 33).
 template <class T, int C> __global__ __launch_bounds__(256) void route_rows_kernel(RouteArgs a, int group_lanes)
 {
