@@ -1,7 +1,7 @@
 """Layers in 8-bit floating point with a scale for each block of 128, as measurable cases: quantising weights (a scale to 128 x 128 values) and
 activations (a scale to 128 of a row), the root-mean-square norm that adds the residual and hands its output on in 8 bits, the product of an 8-bit
-matrix with activations that are quantised on the way, and the gated product of a feed-forward block - both projections, the activation and
-their product.
+matrix with activations that are quantised on the way, the gated product of a feed-forward block - both projections, the activation and
+their product -, and both matrices of such a block, the first's output handed to the second in 8 bits.
 
 Layer shapes are those of workloads.py (AlexNet and VGG-16 fully connected layers) or generic.  What the seed of prepare() changes is everything:
 weights, activations, gains.
@@ -37,23 +37,25 @@ def _norm(name, rows, K, dtype, out, residual):
 
 
 def _product(name, batch, M, K, dtype, bias, act):
-    return dict(name=name, kind="product", batch=batch, M=M, K=K, dtype=dtype, bias=bias, act=act, out=dtype)
+    return dict(name=name, kind="product", batch=batch, M=M, K=K, dtype=dtype, bias=bias, act=act)
 
 
-def _gated(name, batch, hidden, K, dtype, out):
-    return dict(name=name, kind="product", batch=batch, M=2 * hidden, K=K, dtype=dtype, bias=False, act="gated", out=out)
+def _gated(name, batch, hidden, K, dtype):
+    return dict(name=name, kind="product", batch=batch, M=2 * hidden, K=K, dtype=dtype, bias=False, act="gated")
+
+
+def _block(name, batch, hidden, K, dtype):
+    return dict(name=name, kind="block", batch=batch, M=2 * hidden, K=K, dtype=dtype, bias=False, act="gated")
 
 
 def listed():
     return [
-        # the activations of one request between two layers: the launch is all of it
-        _quantise("quantise-1x4096-bf16", 1, 4096, "bf16", 1),
+        # activations whose rows end inside a block and start at odd addresses
+        _quantise("quantise-257x9219-f16", 257, 9219, "f16", 1),
         # the largest weight matrix of the benchmark configurations (VGG-16 fc6), as it is converted when a model is loaded
         _quantise("quantise-4096x25088-f32-w", 4096, 25088, "f32", 128),
         # one new token between two blocks
         _norm("norm-1x4096-bf16-f8", 1, 4096, "bf16", "f8", True),
-        # a ragged batch whose rows end inside a block, handed on as numbers
-        _norm("norm-203x4100-f16", 203, 4100, "f16", "f16", False),
         # a long prompt
         _norm("norm-16384x4096-bf16-f8", 16384, 4096, "bf16", "f8", True),
         # one request through AlexNet's fc6: reading the weights is the cost
@@ -65,11 +67,12 @@ def listed():
         # a long prompt, or a night's batch, through the largest layer
         _product("product-b4096-4096x25088-bf16", 4096, 4096, 25088, "bf16", False, "none"),
         # eight new tokens through both projections of a feed-forward block
-        _gated("gated-b8-4096x4096-bf16", 8, 4096, 4096, "bf16", "bf16"),
+        _gated("gated-b8-4096x4096-bf16", 8, 4096, 4096, "bf16"),
         # a few hundred tokens of ragged sizes
-        _gated("gated-b333-2900x1100-f16", 333, 2900, 1100, "f16", "f16"),
-        # a long prompt's tokens, handed to the second matrix in 8 bits
-        _gated("gated-b4096-9216x4096-bf16-f8", 4096, 9216, 4096, "bf16", "f8"),
+        _gated("gated-b333-2900x1100-f16", 333, 2900, 1100, "f16"),
+        # the whole block for a few tokens, ragged sizes, and for a long prompt's
+        _block("block-b19-2900x1100-bf16", 19, 2900, 1100, "bf16"),
+        _block("block-b4096-9216x4096-bf16", 4096, 9216, 4096, "bf16"),
     ]
 
 
@@ -78,7 +81,7 @@ def _log(rng, lo, hi):
 
 
 def draw(rng):
-    kind = rng.choice(["quantise", "norm", "product", "gated"])
+    kind = rng.choice(["quantise", "norm", "product", "gated", "block"])
     dtype = rng.choice(["f32", "bf16", "f16"])
     if kind == "quantise":
         K = _log(rng, 33, 25088)
@@ -88,10 +91,12 @@ def draw(rng):
         return dict(kind=kind, rows=_log(rng, 1, MOST_NORM // K), K=K, dtype=dtype, out=rng.choice([dtype, "f8"]), residual=rng.random() < 0.5)
     if kind == "product":
         M, K = _log(rng, 100, 4096), _log(rng, 100, 25088)
-        return dict(kind=kind, batch=_log(rng, 1, 4096), M=M, K=K, dtype=dtype, bias=rng.random() < 0.5, act=rng.choice(["none", "relu"]), out=dtype)
+        return dict(kind=kind, batch=_log(rng, 1, 4096), M=M, K=K, dtype=dtype, bias=rng.random() < 0.5, act=rng.choice(["none", "relu"]))
     hidden, K = _log(rng, 100, 9216), _log(rng, 100, 9216)
-    batch = _log(rng, 1, min(4096, int(MOST_FLOPS / (4.0 * hidden * K))))
-    return dict(kind="product", batch=batch, M=2 * hidden, K=K, dtype=dtype, bias=rng.random() < 0.3, act="gated", out=rng.choice([dtype, "f8"]))
+    batch = _log(rng, 1, min(4096, int(MOST_FLOPS / (6.0 * hidden * K))))
+    if kind == "block":
+        return dict(kind=kind, batch=batch, M=2 * hidden, K=K, dtype=rng.choice(["bf16", "f16"]), bias=False, act="gated")
+    return dict(kind="product", batch=batch, M=2 * hidden, K=K, dtype=dtype, bias=rng.random() < 0.3, act="gated")
 
 
 # --------------------------------------------------------------------------- #
@@ -125,9 +130,14 @@ def prepare(case, seed):
     # a matrix as a stored model has it, 8-bit values and scales; of a gated product the gates' and below it the values'
     halves = 2 if case["act"] == "gated" else 1
     rows, K = case["M"] // halves, case["K"]
-    parts = [_to_blocks(torch.randn((rows, K), device="cuda", generator=gen) * torch.exp(0.3 * torch.randn((rows, 1), device="cuda", generator=gen)) * K ** -0.5, 128)
-             for _ in range(halves)]
+
+    def matrix(M, K):
+        return _to_blocks(torch.randn((M, K), device="cuda", generator=gen) * torch.exp(0.3 * torch.randn((M, 1), device="cuda", generator=gen)) * K ** -0.5, 128)
+
+    parts = [matrix(rows, K) for _ in range(halves)]
     state["values"], state["scales"] = torch.cat([v for v, _ in parts]), torch.cat([s for _, s in parts])
+    if kind == "block":
+        state["down"] = matrix(K, rows)
     state["X"] = _activations((case["batch"], K), dtype, gen)
     state["bias"] = 0.1 * torch.randn(case["M"], device="cuda", generator=gen) if case["bias"] else None
     return state
@@ -185,7 +195,9 @@ def _plain_product(s, case):
         y = y[:, :H] / (1 + torch.exp(-y[:, :H])) * y[:, H:]
     elif case["act"] == "relu":
         y = torch.relu(y)
-    return _quantised(*_to_blocks(y, 1), y.shape[1]) if case["out"] == "f8" else y.to(s["X"].dtype)
+    if case["kind"] == "block":
+        y = _values(*_to_blocks(y, 1), H, 1) @ _values(*s["down"], H, 128).t()
+    return y.to(s["X"].dtype)
 
 
 def run(state):
@@ -202,8 +214,10 @@ def run(state):
             out = _quantised(y.values, y.scales, y.K) if case["out"] == "f8" else {"Y": y}
             return out if total is None else {**out, "sum": total}
         W = cl.F8Tensor(state["values"], state["scales"], case["K"], block_rows=128, gated=case["act"] == "gated")
-        y = cl.f8_fc_forward(W, X, state["bias"], act=case["act"], dtype=DTYPES[case["out"]])
-        return _quantised(y.values, y.scales, y.K) if case["out"] == "f8" else y
+        if kind == "block":
+            hidden = cl.f8_fc_forward(W, X, act="gated", dtype=torch.float8_e4m3fn)
+            return cl.f8_fc_forward(cl.F8Tensor(*state["down"], case["M"] // 2, block_rows=128), hidden, dtype=X.dtype)
+        return cl.f8_fc_forward(W, X, state["bias"], act=case["act"])
     if kind == "quantise":
         return _quantised(*_to_blocks(X, case["block_rows"]), case["K"])
     if kind == "norm":
@@ -228,7 +242,9 @@ def work(case):
         return dict(bytes=(3 if case["residual"] else 1) * _bytes(rows, K, dtype) + K * SIZE[dtype] + _bytes(rows, K, case["out"]), flops=6 * rows * K)
     B, M = case["batch"], case["M"]
     width = M // 2 if case["act"] == "gated" else M
-    return dict(bytes=_bytes(M, K, "f8", 128) + _bytes(B, K, case["dtype"]) + _bytes(B, width, case["out"]) + (4 * M if case["bias"] else 0), flops=2 * B * M * K)
+    if kind == "block":
+        return dict(bytes=_bytes(M, K, "f8", 128) + _bytes(K, width, "f8", 128) + 2 * _bytes(B, K, case["dtype"]), flops=2 * B * M * K + 2 * B * K * width)
+    return dict(bytes=_bytes(M, K, "f8", 128) + _bytes(B, K, case["dtype"]) + _bytes(B, width, case["dtype"]) + (4 * M if case["bias"] else 0), flops=2 * B * M * K)
 
 
 # --------------------------------------------------------------------------- #
@@ -294,7 +310,8 @@ def exact(case, seed):
         y = y[:, :H] * torch.sigmoid(y[:, :H]) * y[:, H:]
     elif case["act"] == "relu":
         y = y.clamp_min(0)
-    if case["out"] == "f8":
-        codes, scale = _blocks64(y, 1)
-        return {"values": codes, "scales": scale}
+    if kind == "block":
+        x = _wide64(*_blocks64(y, 1), 1)
+        v, t = s["down"]
+        y = torch.cat([x @ _stored64(v[r:r + 1024], t[r // 128:r // 128 + 8], H).t() for r in range(0, K, 1024)], 1)
     return y
