@@ -20,6 +20,7 @@ PATH_AUTO, PATH_SPARSE, PATH_MFMA_F32, PATH_MFMA_BF16, PATH_SPARSE_WIDE = 0, 1, 
 CHUNK_BITS, RECORD_BITS, RECORDS_PER_CHUNK, MAX_RECORD_ENTRIES, MAX_CODE_LEN = 4096, 64, 64, 15, 12
 STATIC_SCRATCH_BYTES = 16 << 20        # CL_STATIC_SCRATCH_BYTES
 MX4 = 3                                # CL_MX4, after the element types of _element_type
+F8 = 4                                 # CL_F8
 ACTIVATIONS = {"none": 0, "relu": 1, "gated": 2}
 SCORES = {"softmax": 0, "sigmoid": 1}
 GROUP_SCORES = {"max": 0, "top2": 1}
@@ -35,6 +36,7 @@ EXPORTS = [
     "cl_set_kernel_timing", "cl_last_kernel_ms",
     "cl_mx_quantize", "cl_mx_dequantize", "cl_mx_fc_workspace_bytes", "cl_mx_fc_forward", "cl_route_experts", "cl_expert_lists_bytes",
     "cl_expert_lists", "cl_mx_experts_workspace_bytes", "cl_mx_experts_forward", "cl_mx_fc_resolved_form", "cl_mx_experts_resolved_form",
+    "cl_eight_quantize", "cl_eight_dequantize", "cl_rms_norm", "cl_eight_fc_workspace_bytes", "cl_eight_fc_forward",
 ]
 
 
@@ -81,6 +83,20 @@ class RouteDesc(C.Structure):
 class MxExpertsCall(C.Structure):
     _fields_ = [("tokens", C.c_int32), ("k", C.c_int32), ("d_experts", C.c_void_p), ("d_weights", C.c_void_p), ("d_bias", C.c_void_p),
                 ("d_lists", C.c_void_p), ("act", C.c_int32), ("x_per_pair", C.c_int32)]
+
+
+class F8Matrix(C.Structure):
+    _fields_ = [("d_values", C.c_void_p), ("d_scales", C.c_void_p), ("rows", C.c_int32), ("K", C.c_int32)]
+
+
+class F8Input(C.Structure):
+    _fields_ = [("d_X", C.c_void_p), ("d_scales", C.c_void_p), ("type", C.c_int32), ("stride", C.c_int64)]
+
+
+class NormCall(C.Structure):
+    _fields_ = ([(n, C.c_void_p) for n in ("d_X", "d_residual", "d_gain", "d_sum", "d_Y", "d_y_scales")]
+                + [(n, C.c_int64) for n in ("x_stride", "residual_stride", "sum_stride", "y_stride", "rows")]
+                + [(n, C.c_int32) for n in ("K", "type", "gain_type", "y_type")] + [("eps", C.c_float)])
 
 
 class CLError(RuntimeError):
@@ -150,6 +166,11 @@ def lib():
     L.cl_mx_fc_resolved_form.argtypes = [C.POINTER(MxMatrix), i32, i32, C.POINTER(i32), C.POINTER(i32)]
     L.cl_mx_experts_resolved_form.argtypes = [C.POINTER(MxMatrix), i32, C.POINTER(MxExpertsCall), i32, C.POINTER(i32)]
     L.cl_mx_experts_forward.argtypes = [C.POINTER(MxMatrix), i32, C.POINTER(MxInput), C.POINTER(MxExpertsCall), p, i32, p, sz, p]
+    L.cl_eight_quantize.argtypes = [p, i32, i64, i64, i32, i32, p, p, p]
+    L.cl_eight_dequantize.argtypes = [p, p, i64, i32, i32, p, i32, i64, p]
+    L.cl_rms_norm.argtypes = [C.POINTER(NormCall), p]
+    L.cl_eight_fc_workspace_bytes.argtypes = [C.POINTER(F8Matrix), i32, i32, i32, i32, C.POINTER(sz)]
+    L.cl_eight_fc_forward.argtypes = [C.POINTER(F8Matrix), C.POINTER(F8Input), p, p, p, i32, i32, i32, p, sz, p]
     for name in EXPORTS:
         if name not in ("cl_last_error", "cl_layer_group_free"):
             getattr(L, name).restype = i32
@@ -875,6 +896,233 @@ def mx_experts_forward(W: MxTensor, X, experts, weights=None, bias=None, act="no
                          None if lists is None else lists.buffer.data_ptr(), act, int(x_per_pair))
     _check(L.cl_mx_experts_forward(MxMatrix(codes.data_ptr(), W.scales.data_ptr(), M, K), E, xs, call, Y.data_ptr(), y_type, ws, ws_bytes, stream))
     return Y
+
+
+# --------------------------------------------------------------------------- #
+# 8-bit matrices with a scale for each block of 128, and the norm that feeds them
+# --------------------------------------------------------------------------- #
+def f8_row_blocks(K: int) -> int:
+    """Blocks of a row of K elements."""
+    if K < 1:
+        raise ValueError("a row has at least one element")
+    return (K + 127) // 128
+
+
+def f8_row_scales(K: int) -> int:
+    """Scales of a row of K elements: whole fours, of which the first f8_row_blocks(K) are used."""
+    return (f8_row_blocks(K) + 3) // 4 * 4
+
+
+class F8Tensor:
+    """Rows in 8-bit floats with a scale to 128 of them: values (..., rows, blocks * 128) float8_e4m3fn, zeros from K on, and scales float32,
+    (..., rows, f8_row_scales(K)) - or, block_rows=128, a weight matrix: a row of scales to each 128 rows.  gated: the first half of a weight matrix's
+    rows are gates, the second half values, each half with rows of scales of its own (f8_gated makes it of two matrices)."""
+
+    __slots__ = ("values", "scales", "K", "block_rows", "gated")
+
+    def __init__(self, values, scales, K, block_rows=1, gated=False):
+        import torch
+        kb, pitch = f8_row_blocks(K), f8_row_scales(K)
+        if values.dtype != torch.float8_e4m3fn or scales.dtype != torch.float32 or not values.is_cuda or not values.is_contiguous() or not scales.is_contiguous():
+            raise ValueError("values must be contiguous float8_e4m3fn and scales float32 CUDA tensors")
+        shape = values.shape
+        if block_rows not in (1, 128) or len(shape) < 2 or (block_rows == 128 and len(shape) != 2) or (gated and (block_rows != 128 or shape[0] % 2)):
+            raise ValueError(f"{tuple(shape)} with blocks of {block_rows} rows{', gated' if gated else ''}: blocks have 1 row or, of a matrix, 128, and gated ones an even number")
+        if block_rows == 1:
+            lead = shape[:-1]
+        else:
+            halves = 2 if gated else 1
+            lead = (halves * -(-(shape[0] // halves) // 128),)
+        if shape[-1] != kb * 128 or scales.shape != lead + (pitch,) or scales.device != values.device:
+            raise ValueError(f"rows of {K} elements have {kb * 128} values and {pitch} scales, got {tuple(shape)} and {tuple(scales.shape)}")
+        self.values, self.scales, self.K, self.block_rows, self.gated = values, scales, K, block_rows, gated
+
+    @property
+    def shape(self):
+        return tuple(self.values.shape[:-1]) + (self.K,)
+
+    @property
+    def device(self):
+        return self.values.device
+
+
+def _f8_empty(lead, K, block_rows, device):
+    import torch
+    q = F8Tensor.__new__(F8Tensor)
+    q.values = torch.empty(tuple(lead) + ((K + 127) // 128 * 128,), dtype=torch.float8_e4m3fn, device=device)
+    q.scales = torch.empty((tuple(lead) if block_rows == 1 else (-(-lead[0] // 128),)) + ((K + 511) // 512 * 4,), dtype=torch.float32, device=device)
+    q.K, q.block_rows, q.gated = K, block_rows, False
+    return q
+
+
+def f8_quantize(X, block_rows: int = 1, out: F8Tensor | None = None) -> F8Tensor:
+    """Rows of X ((..., K), float32, bfloat16 or float16; a matrix's rows at any distance) -> F8Tensor of the same shape.  block_rows=128: a weight
+    matrix, one scale to 128 x 128."""
+    L = _start()
+    shape = X.shape
+    K, lead = shape[-1], shape[:-1]
+    if len(shape) > 2 and block_rows == 1:
+        X = X.reshape(-1, K)
+    ty, stride = _rows(X, "X")
+    _int32(K, block_rows)
+    if out is None:
+        f8_row_blocks(K)
+        out = _f8_empty(lead, K, block_rows, X.device)
+    elif out.shape != tuple(shape) or out.block_rows != block_rows or out.gated:
+        raise ValueError(f"out must hold {tuple(shape)} in blocks of {block_rows} rows, holds {out.shape} in blocks of {out.block_rows}{', gated' if out.gated else ''}")
+    stream = _on(X.device, out.values)
+    _check(L.cl_eight_quantize(X.data_ptr(), ty, stride, X.shape[0], K, block_rows, out.values.data_ptr(), out.scales.data_ptr(), stream))
+    return out
+
+
+def f8_dequantize(Q: F8Tensor, dtype=None, out=None):
+    """The values Q stands for, (..., K) of dtype (float32 unless given)."""
+    import torch
+    L = _start()
+    if Q.gated and (Q.values.shape[0] // 2) % 128:
+        raise ValueError("halves of a gated matrix that are no multiple of 128 rows are converted one by one")
+    shape = Q.shape
+    if out is None:
+        out = torch.empty(shape, dtype=dtype or torch.float32, device=Q.device)
+    elif tuple(out.shape) != shape or not (out.is_contiguous() or len(shape) == 2) or (dtype is not None and out.dtype != dtype):
+        raise ValueError(f"out must be {shape}{'' if dtype is None else f' of {dtype}'}, contiguous or a matrix with contiguous rows")
+    Y = out if len(shape) == 2 else out.view(-1, Q.K)
+    _int32(Q.K)
+    ty, stride = _rows(Y, "out", Q.K)
+    stream = _on(Q.device, out)
+    _check(L.cl_eight_dequantize(Q.values.data_ptr(), Q.scales.data_ptr(), Y.shape[0], Q.K, Q.block_rows, out.data_ptr(), ty, stride, stream))
+    return out
+
+
+def f8_gated(gate: F8Tensor, up: F8Tensor) -> F8Tensor:
+    """The matrix of a gated product from its gates' and its values', both (rows, K) in blocks of 128 rows."""
+    import torch
+    if gate.block_rows != 128 or up.block_rows != 128 or gate.gated or up.gated or gate.shape != up.shape:
+        raise ValueError(f"gates and values must be matrices of one shape in blocks of 128 rows, got {gate.shape} and {up.shape}")
+    values = torch.cat([gate.values.view(torch.uint8), up.values.view(torch.uint8)]).view(torch.float8_e4m3fn)
+    return F8Tensor(values, torch.cat([gate.scales, up.scales]), gate.K, block_rows=128, gated=True)
+
+
+def _f8_type(dtype, what):
+    """CL_F32, CL_BF16, CL_F16 or CL_F8."""
+    import torch
+    return F8 if dtype == torch.float8_e4m3fn else _element_type(dtype, what)
+
+
+def rms_norm(X, gain=None, eps: float = 1e-6, residual=None, dtype=None, out=None, sum_out=None):
+    """X / sqrt(mean X^2 + eps) * gain over rows of X (..., K; a matrix's rows at any distance), computed in float32.  gain (K): float32 or of X's
+    type.  With a residual: of X + residual, rounded to X's type; -> (Y, that sum).  dtype of Y: X's unless given; float8_e4m3fn makes an F8Tensor.  sum_out may be
+    X or the residual itself, out may be X."""
+    import torch
+    L = _start()
+    shape = X.shape
+    K = shape[-1]
+    flat = len(shape) != 2
+
+    def rows_of(t, what):
+        if tuple(t.shape) != tuple(shape):
+            raise ValueError(f"{what} must be {tuple(shape)}, got {tuple(t.shape)}")
+        return t.view(-1, K) if flat else t
+
+    x = X.reshape(-1, K) if flat else X
+    ty, x_stride = _rows(x, "X")
+    rows = x.shape[0]
+    _int32(K)
+    device = X.device
+    call = NormCall(x.data_ptr(), x_stride=x_stride, rows=rows, K=K, type=ty, eps=eps)
+    if residual is not None:
+        res = residual.reshape(-1, K) if flat and tuple(residual.shape) == tuple(shape) else rows_of(residual, "residual")
+        total = torch.empty(shape, dtype=X.dtype, device=device) if sum_out is None else sum_out
+        t = rows_of(total, "sum_out")
+        if residual.dtype != X.dtype or total.dtype != X.dtype:
+            raise ValueError(f"residual and sum_out must be {X.dtype}, got {residual.dtype} and {total.dtype}")
+        call.d_residual, call.residual_stride = res.data_ptr(), _rows(res, "residual")[1]
+        call.d_sum, call.sum_stride = t.data_ptr(), _rows(t, "sum_out")[1]
+    else:
+        total = None
+        if sum_out is not None:
+            raise ValueError("sum_out without a residual")
+    if gain is not None:
+        if tuple(gain.shape) != (K,) or not gain.is_contiguous() or gain.dtype not in (torch.float32, X.dtype):
+            raise ValueError(f"gain must be ({K},), contiguous, float32 or {X.dtype}, got {gain.dtype} {tuple(gain.shape)}")
+        call.d_gain, call.gain_type = gain.data_ptr(), _element_type(gain.dtype, "gain")
+    if isinstance(out, F8Tensor):
+        if dtype not in (None, torch.float8_e4m3fn) or out.shape != tuple(shape) or out.block_rows != 1:
+            raise ValueError(f"out must hold {tuple(shape)} in blocks of one row, of dtype {dtype}")
+        y_type = F8
+    else:
+        y_type = _f8_type(dtype or (X.dtype if out is None else out.dtype), "out")
+        if out is None:
+            f8_row_blocks(K)
+            out = _f8_empty(shape[:-1], K, 1, device) if y_type == F8 else torch.empty(shape, dtype=dtype or X.dtype, device=device)
+        elif y_type == F8 or out.dtype != (dtype or out.dtype):
+            raise ValueError(f"out must be {'an F8Tensor' if y_type == F8 else f'of {dtype}'}")
+    call.y_type = y_type
+    if y_type == F8:
+        stream = _on(device, residual, total, gain, out.values)
+        call.d_Y, call.d_y_scales = out.values.data_ptr(), out.scales.data_ptr()
+    else:
+        y = rows_of(out, "out")
+        call.d_Y, call.y_stride = y.data_ptr(), _rows(y, "out")[1]
+        stream = _on(device, residual, total, gain, out)
+    _check(L.cl_rms_norm(call, stream))
+    return out if total is None else (out, total)
+
+
+@functools.lru_cache(maxsize=1024)
+def _f8_fc_need(rows, K, batch, x_type, y_type, act):
+    _int32(rows, K, batch)
+    n = C.c_size_t(0)
+    _check(lib().cl_eight_fc_workspace_bytes(F8Matrix(None, None, rows, K), batch, x_type, y_type, act, n))
+    return n.value
+
+
+def f8_fc_workspace_bytes(W: F8Tensor, batch: int, dtype=None, act="none", out_dtype=None) -> int:
+    """Scratch of f8_fc_forward for `batch` rows of dtype (float8_e4m3fn: an F8Tensor; float32 unless given), or fewer; out_dtype: of the output, dtype unless given."""
+    import torch
+    _start()
+    dtype = dtype or torch.float32
+    return _f8_fc_need(W.shape[0], W.K, batch, _f8_type(dtype, "X"), _f8_type(out_dtype or dtype, "out"), _act(act))
+
+
+def f8_fc_forward(W: F8Tensor, X, bias=None, act=None, dtype=None, out=None, workspace=None):
+    """act(X W^T + bias) with W (M, K) in 8 bits with a scale to 128 x 128 and X (B, K) - float32, bfloat16 or float16, quantised on the way, or an F8Tensor.
+    act: "none", "relu" or "gated" (output i from rows i and M / 2 + i of W, gate and value; W as f8_gated makes it).  The output is of dtype, X's own
+    unless given (float32 for an F8Tensor); float8_e4m3fn makes an F8Tensor."""
+    import torch
+    L = _start()
+    values, K = W.values, W.K
+    if W.block_rows != 128:
+        raise ValueError("W must be a matrix in blocks of 128 rows")
+    M = values.shape[0]
+    act = _act(act or "none")
+    width = M // 2 if act == 2 else M
+    if W.gated != (act == 2) and (M % 256 or M == 0):
+        raise ValueError(f"W of {M} rows is {'' if W.gated else 'not '}a gated product's matrix")
+    if isinstance(X, F8Tensor):
+        if len(X.values.shape) != 2 or X.K != K or X.block_rows != 1:
+            raise ValueError(f"X must have rows of {K} in blocks of one row, got {X.shape} in blocks of {X.block_rows}")
+        xs, B, own_dtype = F8Input(X.values.data_ptr(), X.scales.data_ptr(), F8, 0), X.values.shape[0], torch.float32
+    else:
+        ty, stride = _rows(X, "X", K)
+        xs, B, own_dtype = F8Input(X.data_ptr(), None, ty, stride), X.shape[0], X.dtype
+    if bias is not None:
+        _want(bias, (M,), "bias")
+    device = X.device
+    if dtype == torch.float8_e4m3fn or isinstance(out, F8Tensor):
+        if out is None:
+            out = _f8_empty((B,), width, 1, device)
+        elif not isinstance(out, F8Tensor) or dtype not in (None, torch.float8_e4m3fn) or out.shape != (B, width) or out.block_rows != 1:
+            raise ValueError(f"out must be an F8Tensor of ({B}, {width}) in blocks of one row")
+        y, y_scales, y_type = out.values, out.scales.data_ptr(), F8
+    else:
+        out, y_type = _mx_output(out, (B, width), dtype or (own_dtype if out is None else out.dtype), device)
+        y, y_scales = out, None
+    stream = _on(device, values, bias, y, workspace)
+    workspace, ws, ws_bytes = _mx_workspace(workspace, _f8_fc_need(M, K, B, xs.type, y_type, act), device)
+    _check(L.cl_eight_fc_forward(F8Matrix(values.data_ptr(), W.scales.data_ptr(), M, K), xs, None if bias is None else bias.data_ptr(), y.data_ptr(), y_scales, y_type, B,
+                              act, ws, ws_bytes, stream))
+    return out
 
 
 def set_kernel_timing(enable: bool):

@@ -8,7 +8,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libcompressed_layer.so")
-SOURCES = ["compress.cpp", "huffman.cpp", "planner.cpp", "device.hip", "mx/quantize.hip", "mx/route.hip", "mx/product.hip"]
+SOURCES = ["compress.cpp", "huffman.cpp", "planner.cpp", "device.hip", "mx/quantize.hip", "mx/route.hip", "mx/product.hip",
+           "f8/quantize.hip", "f8/norm.hip", "f8/product.hip"]
 
 HIPCC_FLAGS = [
     "-O3", "-std=c++17", "-fPIC", "-shared", "--offload-arch=gfx950",

@@ -1,0 +1,376 @@
+// Products with 8-bit matrices that have a scale for each block of 128 x 128, on the 8-bit matrix instructions.
+#include <algorithm>
+#include <type_traits>
+
+#include "f8_common.hpp"
+
+namespace cl {
+namespace f8 {
+
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+
+// What a product kernel reads and writes.  Rows are `blocks` blocks of 128 bytes; scales have `pitch_scales` numbers to a row of blocks.
+//
+// y[n][o] = act(sum over blocks j of sx[n][j] sw[o / 128][j] p_j + v[o]) with p_j the sum of 128 products of 8-bit values: one matrix instruction, whose
+// sums start at zero, and a multiplication by both scales where its result joins the others.  Rows of a gated product: `width` gates and
+// as many values, each with blocks of its own.
+struct ProductArgs {
+    const uint8_t *w, *x;
+    const float *w_scales, *x_scales, *bias;
+    void *Y;
+    float *y_scales;
+    int blocks, pitch_scales;
+    int width;                                               // outputs of a row
+    int rows, act;
+    int value_tall;                                          // gated: where the values' rows of scales start
+    float *part;                                             // not null: sums of a share of k, [split][row of Y][pitch], gates and values apart, to be finished
+    int pitch, value_at;
+    int splits;
+};
+
+// Eight 8-bit values in 16 bits.
+__device__ __forceinline__ bf16x8 wide(int lo, int hi)
+{
+    const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, true);
+    const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, false), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, true);
+    return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+
+// The sum over 128 k of A[row][k] B[col][k], 8 bits each.  Lane l has row (A) and column (B) l % 16 and 32 of the k, whole runs of eight of them (which ones does
+// not matter, as long as it is the same in both).  Of the result, [i] is row 4 (l / 16) + i, column l % 16.
+//
+// The 8-bit instructions line up the products of each run of eight k by the largest and cut off what is more than 13 bits below it (measured: a product of
+// 2^-14 of the largest is lost, beside a product of another run one of 2^-23 is not); sums of runs are 32 bits.  So a run is off by less than 7 * 2^-13 of its
+// largest product - with activations and weights as they are, 1.4e-5 to 5e-5 of a sum (2-norm), a hundredth of the rounding of an output in bf16, a
+// tenth of one in fp16.  An output in fp32 has the bits to show it: WIDE takes the operands to bf16, which is exact, and multiplies on the bf16
+// instructions, whose products and sums are 32 bits, at half the rate.
+template <bool WIDE> __device__ __forceinline__ f32x4 mfma_f8(i32x8 a, i32x8 b)
+{
+    if constexpr (!WIDE) {
+        return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, f32x4{0, 0, 0, 0}, 0, 0, 0, 0, 0, 0);
+    } else {
+        f32x4 acc = {0, 0, 0, 0};
+#pragma unroll
+        for (int i = 0; i < 8; i += 2) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wide(a[i], a[i + 1]), wide(b[i], b[i + 1]), acc, 0, 0, 0);
+        return acc;
+    }
+}
+
+__device__ __forceinline__ i32x8 both(i32x4 lo, i32x4 hi) { return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7); }
+
+struct F8Out {};
+
+// bias of four outputs from o on (of the values: at = width)
+__device__ __forceinline__ f32x4 bias_of(const ProductArgs &a, int at, int o)
+{
+    f32x4 b = {0, 0, 0, 0};
+    if (!a.bias) return b;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) b[i] = a.bias[at + min(o + i, a.width - 1)];
+    return b;
+}
+
+template <bool GATED> __device__ __forceinline__ f32x4 activated(const ProductArgs &a, int o, f32x4 v, f32x4 u)
+{
+    if (a.bias) v += bias_of(a, 0, o);
+    if (GATED) {
+        if (a.bias) u += bias_of(a, a.width, o);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = v[i] / (1.0f + expf(-v[i])) * u[i];
+    } else if (a.act == CL_ACT_RELU) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = v[i] < 0.0f ? 0.0f : v[i];            // (NaN stays)
+    }
+    return v;
+}
+
+// The outputs o .. o + 3 of one row of Y.
+template <class T> __device__ __forceinline__ void store_outputs(const ProductArgs &a, int64_t row, int o, f32x4 v)
+{
+    if (o >= a.width) return;
+    T *y = (T *)a.Y + row * a.width + o;
+    const T out[4] = {(T)product32(v[0], 1.0f), (T)product32(v[1], 1.0f), (T)product32(v[2], 1.0f), (T)product32(v[3], 1.0f)};
+    if (o + 4 <= a.width) {
+        store_values<4>(y, out);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 3; ++i)
+            if (o + i < a.width) y[i] = out[i];
+    }
+}
+
+// Four sums of a share of k.  (A row of partial sums is padded to whole fours.)
+__device__ __forceinline__ void store_part(const ProductArgs &a, int split, int64_t row, int o, f32x4 v, int at)
+{
+    if (o < a.width) *(f32x4 *)(a.part + ((int64_t)split * a.rows + row) * a.pitch + at + o) = v;
+}
+
+// A workgroup of up to sixteen wavefronts makes 16 outputs (blockIdx.x) of 16 columns (blockIdx.y).  The wavefronts share out the row's blocks; their sums
+// meet in LDS and are added in the order of the wavefronts.  No operand is shared, so that nothing waits for a barrier until the end.
+constexpr int kRowsWaves = 16;
+
+template <class T, bool GATED, bool WIDE> __global__ __launch_bounds__(kRowsWaves * 64) void f8_rows_kernel(ProductArgs a, int column0)
+{
+    constexpr int F = GATED ? 2 : 1;
+    __shared__ f32x4 sums[kRowsWaves][F][64];
+    const int waves = (int)blockDim.x / 64, wave = threadIdx.x / 64, lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
+    const int o0 = (int)blockIdx.x * 16;
+    const int64_t c0 = column0 + (int64_t)blockIdx.y * 16, column = min(c0 + r, (int64_t)a.rows - 1), row_bytes = (int64_t)a.blocks * kBlock;
+    const uint8_t *w[F], *x = a.x + column * row_bytes + g * 32;
+    const float *ws[F], *xs = a.x_scales + column * a.pitch_scales;
+#pragma unroll
+    for (int f = 0; f < F; ++f) {
+        w[f] = a.w + ((int64_t)f * a.width + min(o0 + r, a.width - 1)) * row_bytes + g * 32;
+        ws[f] = a.w_scales + (int64_t)(f * a.value_tall + o0 / kBlock) * a.pitch_scales;
+    }
+    f32x4 acc[F] = {};
+    for (int b = wave; b < a.blocks; b += waves) {
+        const i32x4 *xp = (const i32x4 *)(x + (int64_t)b * kBlock);
+        const i32x8 xv = both(xp[0], xp[1]);
+        const float sx = xs[b];
+#pragma unroll
+        for (int f = 0; f < F; ++f) {
+            const i32x4 *wp = (const i32x4 *)(w[f] + (int64_t)b * kBlock);
+            const f32x4 p = mfma_f8<WIDE>(both(wp[0], wp[1]), xv);
+            const float s = sx * ws[f][b];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) acc[f][i] = fmaf(p[i], s, acc[f][i]);
+        }
+    }
+#pragma unroll
+    for (int f = 0; f < F; ++f) sums[wave][f][lane] = acc[f];
+    __syncthreads();
+    if (threadIdx.x >= 64) return;
+    const int64_t row = c0 + r;
+    if (row >= a.rows) return;
+    f32x4 v[F];
+#pragma unroll
+    for (int f = 0; f < F; ++f) {
+        v[f] = sums[0][f][lane];
+        for (int i = 1; i < waves; ++i) v[f] += sums[i][f][lane];
+    }
+    const int o = o0 + 4 * g;
+    if (a.part) {
+#pragma unroll
+        for (int f = 0; f < F; ++f) store_part(a, 0, row, o, v[f], f * a.value_at);
+    } else {
+        store_outputs<T>(a, row, o, activated<GATED>(a, o, v[0], v[F - 1]));
+    }
+}
+
+// The sum over the splits of a product's parts, in order, and from it four outputs of one row.  8-bit outputs: 32 lanes have a block.
+template <class T, bool GATED> __global__ __launch_bounds__(256) void f8_finish_kernel(ProductArgs a, Div quads, int row0, int rows)
+{
+    constexpr bool kF8 = std::is_same_v<T, F8Out>;
+    const uint32_t at = blockIdx.x * 256 + threadIdx.x, row = quads.quotient(at);
+    if (row >= (uint32_t)rows) return;                       // (8-bit outputs: the lanes of a block together)
+    const int o = (int)(at - row * quads.d) * 4;
+    const int64_t t = (int64_t)row0 + row, stride = (int64_t)a.rows * a.pitch;
+    f32x4 v = {0, 0, 0, 0}, u = {0, 0, 0, 0};
+    if (o < a.width) {
+        const float *p = a.part + t * a.pitch + o;
+        v = *(const f32x4 *)p;
+        if (GATED) u = *(const f32x4 *)(p + a.value_at);
+        for (int s = 1; s < a.splits; ++s) {
+            v += *(const f32x4 *)(p + s * stride);
+            if (GATED) u += *(const f32x4 *)(p + a.value_at + s * stride);
+        }
+        v = activated<GATED>(a, o, v, u);
+    }
+    if constexpr (kF8) {
+        float y[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) y[i] = o + i < a.width ? v[i] : 0.0f;
+        const Scale s = scale_of(top_of_lanes<32>(top_bits<4>(y)));
+        const int y_blocks = (int)quads.d / 32, b = o / kBlock;
+        *(uint32_t *)((uint8_t *)a.Y + t * y_blocks * kBlock + o) = to_f8(y, s.inverse);
+        if (o % kBlock == 0) {
+            const int pitch = (y_blocks + 3) / 4 * 4;
+            float *to = a.y_scales + t * pitch;
+            to[b] = s.scale;
+            if (b == y_blocks - 1)
+                for (int i = y_blocks; i < pitch; ++i) to[i] = 0.0f;
+        }
+    } else {
+        store_outputs<T>(a, t, o, v);
+    }
+}
+
+// ------------------------------------------------------------------------- //
+// which kernel
+// ------------------------------------------------------------------------- //
+enum Form { kRows };
+struct Choice {
+    Form form;
+    int splits;
+};
+
+static Choice choose(int, int, int64_t) { return Choice{kRows, 1}; }
+
+// Wavefronts that share out the blocks of a row.
+static int rows_waves(int blocks) { return std::min(kRowsWaves, blocks); }
+
+// Whether the launch has less than 2^32 threads along each axis.
+static int32_t check_grid(const Choice &, int32_t width, int blocks, int64_t)
+{
+    const int64_t wgs = ((int64_t)width + 15) / 16, threads = rows_waves(blocks) * 64;
+    if (wgs > (int64_t)UINT32_MAX / threads) return fail(CL_EUNSUPPORTED, "a launch of %lld workgroups does not fit a grid", (long long)wgs);
+    return CL_OK;
+}
+
+template <class T, bool GATED, bool WIDE> static int32_t launch_product(ProductArgs a, const Choice &c, hipStream_t st)
+{
+    a.splits = c.splits;
+    // (a grid is at most 65535 high: taller ones go in pieces)
+    const int64_t tiles = ((int64_t)a.rows + 15) / 16;
+    for (int64_t t0 = 0; t0 < tiles; t0 += 65535) {
+        hipLaunchKernelGGL((f8_rows_kernel<T, GATED, WIDE>), dim3((unsigned)((a.width + 15) / 16), (unsigned)std::min<int64_t>(tiles - t0, 65535)), dim3(rows_waves(a.blocks) * 64), 0, st, a,
+                           (int)(t0 * 16));
+        MX_HIP_TRY(hipGetLastError());
+    }
+    return CL_OK;
+}
+
+// launch(row0, rows, workgroups) over rows of `quads` threads each, in pieces whose threads' numbers have 32 bits.
+template <class F> static int32_t launch_rows(int32_t rows, uint32_t quads, F launch)
+{
+    const int32_t most = (int32_t)std::min<int64_t>(rows, std::max<int64_t>(1, (1ll << 31) / quads));
+    for (int32_t row0 = 0, n; row0 < rows; row0 += n) {
+        n = std::min(most, rows - row0);
+        launch(row0, n, dim3((uint32_t)(((int64_t)n * quads + 255) / 256)));
+        MX_HIP_TRY(hipGetLastError());
+    }
+    return CL_OK;
+}
+
+template <bool GATED> static int32_t run_product(const ProductArgs &a, const Choice &c, int32_t y_type, hipStream_t st)
+{
+    if (!a.part) return with_type(y_type, [&](auto t) { return launch_product<decltype(t), GATED, std::is_same_v<decltype(t), float>>(a, c, st); });
+    if (int32_t rc = y_type == CL_F32 ? launch_product<float, GATED, true>(a, c, st) : launch_product<float, GATED, false>(a, c, st)) return rc;
+    ProductArgs p = a;
+    p.splits = c.splits;
+    auto finish = [&](auto t, uint32_t quads) {
+        return launch_rows(a.rows, quads, [&](int row0, int rows, dim3 grid) {
+            hipLaunchKernelGGL((f8_finish_kernel<decltype(t), GATED>), grid, dim3(256), 0, st, p, make_div(quads), row0, rows);
+        });
+    };
+    if (y_type == CL_F8) return finish(F8Out{}, (uint32_t)blocks_of(a.width) * 32);
+    return with_type(y_type, [&](auto t) { return finish(t, (uint32_t)(a.width + 3) / 4); });
+}
+
+static int32_t check_forward(const cl_f8_matrix *W, int32_t batch, int32_t x_type, int32_t y_type, int32_t act)
+{
+    if (!W) return fail(CL_EINVAL, "null pointer");
+    if (W->rows < 1 || W->K < 1) return fail(CL_EINVAL, "bad matrix: %d x %d", (int)W->rows, (int)W->K);
+    if (W->K > CL_F8_MAX_K) return fail(CL_EUNSUPPORTED, "rows of more than %d elements", (int)CL_F8_MAX_K);
+    if (W->rows > INT_MAX - 512) return fail(CL_EUNSUPPORTED, "a matrix of %d rows", (int)W->rows);
+    if (batch < 0) return fail(CL_EINVAL, "batch of %d", (int)batch);
+    if (!known_type(x_type) && x_type != CL_F8) return fail(CL_EINVAL, "unknown element type %d", (int)x_type);
+    if (!known_type(y_type) && y_type != CL_F8) return fail(CL_EINVAL, "unknown element type %d", (int)y_type);
+    if (act != CL_ACT_NONE && act != CL_ACT_RELU && act != CL_ACT_GATED) return fail(CL_EINVAL, "unknown activation %d", (int)act);
+    if (act == CL_ACT_GATED && W->rows % 2) return fail(CL_EINVAL, "a gated product needs an even number of rows, got %d", (int)W->rows);
+    return CL_OK;
+}
+
+static int32_t check_pointers(const cl_f8_matrix *W, const cl_f8_input *X, const void *Y, const void *y_scales, int32_t y_type, int64_t rows)
+{
+    if (!W->d_values || !W->d_scales || !X->d_X || !Y) return fail(CL_EINVAL, "null pointer");
+    if (!aligned(W->d_values, 16) || !aligned(W->d_scales, 16)) return fail(CL_EINVAL, "values and scales must be 16-byte aligned");
+    if (X->type == CL_F8) {
+        if (!X->d_scales) return fail(CL_EINVAL, "null pointer");
+        if (!aligned(X->d_X, 16) || !aligned(X->d_scales, 16)) return fail(CL_EINVAL, "values and scales must be 16-byte aligned");
+    } else {
+        if (!aligned(X->d_X, type_bytes(X->type))) return fail(CL_EINVAL, "elements are not aligned");
+        if (rows > 1 && X->stride < W->K) return fail(CL_EINVAL, "rows of %d elements overlap at a stride of %lld", (int)W->K, (long long)X->stride);
+    }
+    if (y_type == CL_F8) {
+        if (!y_scales) return fail(CL_EINVAL, "null pointer");
+        if (!aligned(Y, 16) || !aligned(y_scales, 16)) return fail(CL_EINVAL, "values and scales must be 16-byte aligned");
+    } else if (!aligned(Y, type_bytes(y_type))) {
+        return fail(CL_EINVAL, "elements are not aligned");
+    }
+    return CL_OK;
+}
+
+// Scratch of a call, by what is in it.
+struct Scratch {
+    size_t x_values = 0, x_scales = 0, parts = 0, bytes = 0;
+    size_t take(size_t n) { const size_t at = bytes; bytes += round_up(n, 256); return at; }
+};
+
+static size_t part_pitch(int32_t width, bool gated) { return round_up(width, 4) * (gated ? 2 : 1); }
+
+static Scratch scratch_of(const Choice &c, const cl_f8_matrix &W, int32_t batch, int32_t x_type, int32_t y_type, int32_t act)
+{
+    Scratch s;
+    if (x_type != CL_F8) {
+        s.x_values = s.take((size_t)batch * blocks_of(W.K) * kBlock);
+        s.x_scales = s.take((size_t)batch * scales_of(W.K) * 4);
+    }
+    const bool gated = act == CL_ACT_GATED;
+    if (c.splits > 1 || y_type == CL_F8) s.parts = s.take((size_t)c.splits * batch * part_pitch(gated ? W.rows / 2 : W.rows, gated) * 4);
+    return s;
+}
+
+}  // namespace f8
+}  // namespace cl
+
+using namespace cl;
+using namespace cl::f8;
+
+extern "C" int32_t cl_eight_fc_workspace_bytes(const cl_f8_matrix *W, int32_t batch, int32_t x_type, int32_t y_type, int32_t act, size_t *out)
+{
+    if (!out) return fail(CL_EINVAL, "null pointer");
+    if (int32_t rc = check_forward(W, batch, x_type, y_type, act)) return rc;
+    const int32_t width = act == CL_ACT_GATED ? W->rows / 2 : W->rows;
+    const Choice c = choose(width, blocks_of(W->K), batch);
+    if (int32_t rc = check_grid(c, width, blocks_of(W->K), batch)) return rc;
+    *out = scratch_of(c, *W, batch, x_type, y_type, act).bytes;
+    clear_error();
+    return CL_OK;
+}
+
+extern "C" int32_t cl_eight_fc_forward(const cl_f8_matrix *W, const cl_f8_input *X, const float *d_bias, void *d_Y, float *d_y_scales, int32_t y_type, int32_t batch, int32_t act,
+                                    void *d_workspace, size_t workspace_bytes, void *stream)
+{
+    if (!X) return fail(CL_EINVAL, "null pointer");
+    if (int32_t rc = check_forward(W, batch, X->type, y_type, act)) return rc;
+    if (batch == 0) return CL_OK;
+    if (int32_t rc = check_pointers(W, X, d_Y, d_y_scales, y_type, batch)) return rc;
+    hipStream_t st = (hipStream_t)stream;
+    const bool gated = act == CL_ACT_GATED;
+    ProductArgs a{};
+    a.w = (const uint8_t *)W->d_values;
+    a.w_scales = W->d_scales;
+    a.bias = d_bias;
+    a.Y = d_Y;
+    a.y_scales = d_y_scales;
+    a.blocks = blocks_of(W->K);
+    a.pitch_scales = scales_of(W->K);
+    a.width = gated ? W->rows / 2 : W->rows;
+    a.rows = batch;
+    a.act = act;
+    a.value_tall = (a.width + kBlock - 1) / kBlock;
+    const Choice c = choose(a.width, a.blocks, batch);
+    if (int32_t rc = check_grid(c, a.width, a.blocks, batch)) return rc;
+    const Scratch s = scratch_of(c, *W, batch, X->type, y_type, act);
+    if (s.bytes && !d_workspace) return fail(CL_EINVAL, "null workspace");
+    if (workspace_bytes < s.bytes) return fail(CL_EINVAL, "workspace needs %zu bytes, got %zu", s.bytes, workspace_bytes);
+    if (s.bytes && !aligned(d_workspace, 256)) return fail(CL_EINVAL, "workspace must be 256-byte aligned");
+    uint8_t *ws = (uint8_t *)d_workspace;
+    if (X->type == CL_F8) {
+        a.x = (const uint8_t *)X->d_X;
+        a.x_scales = X->d_scales;
+    } else {
+        a.x = ws + s.x_values;
+        a.x_scales = (const float *)(ws + s.x_scales);
+        if (int32_t rc = launch_rows_to_f8(X->d_X, X->type, X->stride, batch, W->K, ws + s.x_values, (float *)(ws + s.x_scales), st)) return rc;
+    }
+    if (c.splits > 1 || y_type == CL_F8) a.part = (float *)(ws + s.parts);
+    a.pitch = (int)part_pitch(a.width, gated);
+    a.value_at = (int)round_up(a.width, 4);
+    if (int32_t rc = gated ? run_product<true>(a, c, y_type, st) : run_product<false>(a, c, y_type, st)) return rc;
+    clear_error();
+    return CL_OK;
+}

@@ -156,7 +156,7 @@ struct Div {
     }
 };
 
-static Div make_div(uint32_t d)
+inline Div make_div(uint32_t d)
 {
     uint32_t s = 0;
     while (s < 32 && (1ull << s) < d) ++s;
