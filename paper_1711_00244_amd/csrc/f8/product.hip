@@ -1,6 +1,7 @@
 // Products with 8-bit matrices that have a scale for each block of 128 x 128, on the 8-bit matrix instructions.
 #include <algorithm>
 #include <type_traits>
+#include <utility>
 
 #include "f8_common.hpp"
 
@@ -27,6 +28,8 @@ struct ProductArgs {
     float *part;                                             // not null: sums of a share of k, [split][row of Y][pitch], gates and values apart, to be finished
     int pitch, value_at;
     int splits;
+    int split_fours, split_more;                             // fours of steps of 128 k of a share of k, and how many shares have one more
+    Div row_tiles, band_tiles;                               // tiles of a column of tiles, and of a band of columns
 };
 
 // Eight 8-bit values in 16 bits.
@@ -45,14 +48,24 @@ __device__ __forceinline__ bf16x8 wide(int lo, int hi)
 // largest product - with activations and weights as they are, 1.4e-5 to 5e-5 of a sum (2-norm), a hundredth of the rounding of an output in bf16, a
 // tenth of one in fp16.  An output in fp32 has the bits to show it: WIDE takes the operands to bf16, which is exact, and multiplies on the bf16
 // instructions, whose products and sums are 32 bits, at half the rate.
-template <bool WIDE> __device__ __forceinline__ f32x4 mfma_f8(i32x8 a, i32x8 b)
+template <bool WIDE> struct OperandOf { typedef i32x8 type; };
+template <> struct OperandOf<true> { struct type { bf16x8 v[4]; }; };
+template <bool WIDE> using Operand = typename OperandOf<WIDE>::type;
+
+template <bool WIDE> __device__ __forceinline__ Operand<WIDE> operand(i32x8 a)
+{
+    if constexpr (!WIDE) return a;
+    else return {{wide(a[0], a[1]), wide(a[2], a[3]), wide(a[4], a[5]), wide(a[6], a[7])}};
+}
+
+template <bool WIDE> __device__ __forceinline__ f32x4 mfma_f8(const Operand<WIDE> &a, const Operand<WIDE> &b)
 {
     if constexpr (!WIDE) {
         return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, f32x4{0, 0, 0, 0}, 0, 0, 0, 0, 0, 0);
     } else {
         f32x4 acc = {0, 0, 0, 0};
 #pragma unroll
-        for (int i = 0; i < 8; i += 2) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wide(a[i], a[i + 1]), wide(b[i], b[i + 1]), acc, 0, 0, 0);
+        for (int i = 0; i < 4; ++i) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.v[i], b.v[i], acc, 0, 0, 0);
         return acc;
     }
 }
@@ -127,12 +140,12 @@ template <class T, bool GATED, bool WIDE> __global__ __launch_bounds__(kRowsWave
     f32x4 acc[F] = {};
     for (int b = wave; b < a.blocks; b += waves) {
         const i32x4 *xp = (const i32x4 *)(x + (int64_t)b * kBlock);
-        const i32x8 xv = both(xp[0], xp[1]);
+        const Operand<WIDE> xv = operand<WIDE>(both(xp[0], xp[1]));
         const float sx = xs[b];
 #pragma unroll
         for (int f = 0; f < F; ++f) {
             const i32x4 *wp = (const i32x4 *)(w[f] + (int64_t)b * kBlock);
-            const f32x4 p = mfma_f8<WIDE>(both(wp[0], wp[1]), xv);
+            const f32x4 p = mfma_f8<WIDE>(operand<WIDE>(both(wp[0], wp[1])), xv);
             const float s = sx * ws[f][b];
 #pragma unroll
             for (int i = 0; i < 4; ++i) acc[f][i] = fmaf(p[i], s, acc[f][i]);
@@ -158,6 +171,8 @@ template <class T, bool GATED, bool WIDE> __global__ __launch_bounds__(kRowsWave
         store_outputs<T>(a, row, o, activated<GATED>(a, o, v[0], v[F - 1]));
     }
 }
+
+#include "tile_kernel.hpp"
 
 // The sum over the splits of a product's parts, in order, and from it four outputs of one row.  8-bit outputs: 32 lanes have a block.
 template <class T, bool GATED> __global__ __launch_bounds__(256) void f8_finish_kernel(ProductArgs a, Div quads, int row0, int rows)
@@ -200,28 +215,71 @@ template <class T, bool GATED> __global__ __launch_bounds__(256) void f8_finish_
 // ------------------------------------------------------------------------- //
 // which kernel
 // ------------------------------------------------------------------------- //
-enum Form { kRows };
+enum Form { kRows, kTile64, kTile128, kTile256 };
+constexpr int kFormSide[] = {16, 64, 128, 256}, kFormThreads[] = {0, 256, 512, 512};        // of a workgroup: rows of W and of X, threads (kRows: as many as rows_waves says)
 struct Choice {
     Form form;
     int splits;
 };
 
-static Choice choose(int, int, int64_t) { return Choice{kRows, 1}; }
+static Choice choose(int width, int blocks, int64_t rows, bool gated, bool wide)
+{
+    (void)blocks;
+    const int64_t M = (int64_t)width * (gated ? 2 : 1);
+    if (rows <= 32) return Choice{kRows, 1};
+    const int64_t n = ((M + 255) / 256) * ((rows + 255) / 256);
+    if (n >= 128 && !wide) return Choice{kTile256, 1};
+    if (((M + 127) / 128) * ((rows + 127) / 128) >= 128) return Choice{kTile128, 1};
+    return Choice{kTile64, 1};
+}
 
 // Wavefronts that share out the blocks of a row.
 static int rows_waves(int blocks) { return std::min(kRowsWaves, blocks); }
 
-// Whether the launch has less than 2^32 threads along each axis.
-static int32_t check_grid(const Choice &, int32_t width, int blocks, int64_t)
+static int64_t row_tiles_of(const Choice &c, int32_t width, bool gated)
 {
-    const int64_t wgs = ((int64_t)width + 15) / 16, threads = rows_waves(blocks) * 64;
-    if (wgs > (int64_t)UINT32_MAX / threads) return fail(CL_EUNSUPPORTED, "a launch of %lld workgroups does not fit a grid", (long long)wgs);
+    const int64_t outputs = c.form == kRows || !gated ? kFormSide[c.form] : kFormSide[c.form] / 2;
+    return (width + outputs - 1) / outputs;
+}
+
+// Whether the launch has less than 2^32 threads along each axis.
+static int32_t check_grid(const Choice &c, int32_t width, int blocks, int64_t rows, bool gated)
+{
+    const int64_t row_tiles = row_tiles_of(c, width, gated), columns = (rows + kFormSide[c.form] - 1) / kFormSide[c.form];
+    const int64_t wgs = c.form == kRows ? row_tiles : (int64_t)round_up(row_tiles * columns, 8), threads = c.form == kRows ? rows_waves(blocks) * 64 : kFormThreads[c.form];
+    if (wgs > (int64_t)UINT32_MAX / threads || wgs > INT_MAX) return fail(CL_EUNSUPPORTED, "a launch of %lld workgroups does not fit a grid", (long long)wgs);
+    return CL_OK;
+}
+
+template <Form F, int WM, int WN, int D, class T, bool GATED, bool WIDE> static int32_t launch_tiles(ProductArgs a, const Choice &c, hipStream_t st)
+{
+    constexpr int SIDE = kFormSide[F];
+    using C = Tile<SIDE, SIDE, WM, WN, D>;
+    static_assert(C::kThreads == kFormThreads[F], "");
+    auto kernel = f8_tile_kernel<SIDE, SIDE, WM, WN, D, T, GATED, WIDE>;
+    static LdsLimit seen;
+    if (int32_t rc = allow_lds((const void *)kernel, C::kLds, seen)) return rc;
+    const int64_t row_tiles = row_tiles_of(c, a.width, GATED), columns = ((int64_t)a.rows + SIDE - 1) / SIDE;
+    a.row_tiles = make_div((uint32_t)row_tiles);
+    a.band_tiles = make_div((uint32_t)row_tiles * 4u);
+    const int fours = (a.blocks + 3) / 4;
+    a.split_fours = fours / c.splits;
+    a.split_more = fours % c.splits;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)round_up(row_tiles * columns, 8), (unsigned)c.splits), dim3(C::kThreads), C::kLds, st, a, (int)row_tiles);
+    MX_HIP_TRY(hipGetLastError());
     return CL_OK;
 }
 
 template <class T, bool GATED, bool WIDE> static int32_t launch_product(ProductArgs a, const Choice &c, hipStream_t st)
 {
     a.splits = c.splits;
+    switch (c.form) {
+    case kTile64: return launch_tiles<kTile64, 2, 2, 4, T, GATED, WIDE>(a, c, st);
+    case kTile128: return launch_tiles<kTile128, 2, 4, 2, T, GATED, WIDE>(a, c, st);
+    case kTile256:
+        if constexpr (!WIDE) return launch_tiles<kTile256, 2, 4, 2, T, GATED, false>(a, c, st);
+    default: break;
+    }
     // (a grid is at most 65535 high: taller ones go in pieces)
     const int64_t tiles = ((int64_t)a.rows + 15) / 16;
     for (int64_t t0 = 0; t0 < tiles; t0 += 65535) {
@@ -324,8 +382,9 @@ extern "C" int32_t cl_eight_fc_workspace_bytes(const cl_f8_matrix *W, int32_t ba
     if (!out) return fail(CL_EINVAL, "null pointer");
     if (int32_t rc = check_forward(W, batch, x_type, y_type, act)) return rc;
     const int32_t width = act == CL_ACT_GATED ? W->rows / 2 : W->rows;
-    const Choice c = choose(width, blocks_of(W->K), batch);
-    if (int32_t rc = check_grid(c, width, blocks_of(W->K), batch)) return rc;
+    const bool gated = act == CL_ACT_GATED;
+    const Choice c = choose(width, blocks_of(W->K), batch, gated, y_type == CL_F32);
+    if (int32_t rc = check_grid(c, width, blocks_of(W->K), batch, gated)) return rc;
     *out = scratch_of(c, *W, batch, x_type, y_type, act).bytes;
     clear_error();
     return CL_OK;
@@ -352,8 +411,8 @@ extern "C" int32_t cl_eight_fc_forward(const cl_f8_matrix *W, const cl_f8_input 
     a.rows = batch;
     a.act = act;
     a.value_tall = (a.width + kBlock - 1) / kBlock;
-    const Choice c = choose(a.width, a.blocks, batch);
-    if (int32_t rc = check_grid(c, a.width, a.blocks, batch)) return rc;
+    const Choice c = choose(a.width, a.blocks, batch, gated, y_type == CL_F32);
+    if (int32_t rc = check_grid(c, a.width, a.blocks, batch, gated)) return rc;
     const Scratch s = scratch_of(c, *W, batch, X->type, y_type, act);
     if (s.bytes && !d_workspace) return fail(CL_EINVAL, "null workspace");
     if (workspace_bytes < s.bytes) return fail(CL_EINVAL, "workspace needs %zu bytes, got %zu", s.bytes, workspace_bytes);
