@@ -6,9 +6,13 @@
 // gates, the other half their values, so that a lane has both of an output.  A step is one block of 128 k.
 //
 // LDS holds D steps.  The loads themselves write it.  A wavefront's rows go through registers R pieces at a time, its columns, which a whole step uses, stay
-// there.  When it has read the step's last rows, R pieces before the step ends, it waits for the next step's loads and for the other wavefronts: from there on the next step
-// may be read, and the buffer of this one is asked for again; what is left of the step's multiplies hides both.  Columns are replaced one by one behind their last
-// use.  A piece's sum (it starts at zero in each step) is multiplied by the scales when its register is needed for the piece after it.
+// there, replaced one by one behind their last use.  A piece's sum (it starts at zero in each step) is multiplied by the scales when its register is needed for the piece
+// after it.
+//
+// What bounds it are loads: all workgroups of a die want the same lines at about the same time, and wait for the first of them to come from beyond its cache.  So a
+// buffer is asked for again in two parts, each as soon as it has been read: the columns and each wavefront's first half of rows halfway through the step, the
+// second halves at its end; and either part is waited for when it is to be read, one and a half steps (of two) later.  At both points the wavefronts wait for each
+// other.  (4096 x 4096 x 25088, 256 x 256: without loads 222 us; all of a buffer asked for at once behind the step 343, in four bunches 336.)
 //
 // In LDS a row's eight units of 16 bytes are 128 consecutive bytes, unit c of row r in place c ^ (r % 8).  A read of 16 bytes a lane is served sixteen lanes at a time,
 // of which eight are from one half of a half-wave and eight from the other's; those have units of either parity, and touch each of the 64 banks once.
@@ -17,23 +21,29 @@ template <int BM, int BN, int WM, int WN, int D> struct Tile {
     static constexpr int TI = BM / WM / 16, TJ = BN / WN / 16, R = 2;
     static constexpr int kRun = TI * 8;                      // rows under one scale: half of a wavefront's
     static constexpr int kLoads = (BM + BN) / 8 / kWaves;    // of a wavefront and step
+    static constexpr bool kHalves = TI > R;                  // a buffer in two parts; else as one
+    static constexpr int kLate = kHalves ? BM / 16 / kWaves : 0, kEarly = kLoads - kLate;       // second halves of rows; all others
+    // Where the wavefronts wait for each other: before piece row kFree the second halves have to be there, and what is early may be asked for again; before kNext
+    // the next step's early part has to be there, and the second halves may be asked for again.
+    static constexpr int kNext = TI - R, kFree = kHalves ? TI / 2 - R : -1;
+    // loads behind piece row i: the early ones from early(i) to early(i + 1), the late ones likewise
+    static constexpr int share(int n, int of, int i) { return n * (i < 0 ? 0 : i < of ? i : of) / of; }
+    static constexpr int early(int i) { return kHalves ? share(kEarly, TI / 2, i - kFree) : share(kEarly, R, i - kNext); }
+    static constexpr int late(int i) { return share(kLate, R, i - kNext); }
     static constexpr int kScaleLoads = BN / 64 + 1;          // of the workgroup and four steps: columns, then the wavefronts' rows
     static constexpr int kScaleShare = (kScaleLoads + kWaves - 1) / kWaves;      // (wavefronts beyond that number repeat the last)
     static constexpr int kBuffer = (BM + BN) * kBlock;
-    static constexpr int kScales = D * kBuffer;              // where the scales start: two buffers of four steps
+    static constexpr int kScales = D * kBuffer;              // where the scales start: D buffers of four steps
     static constexpr int kScaleBuffer = (BN + 64) * 16;
-    static constexpr int kLds = kScales + 2 * kScaleBuffer;
+    static constexpr int kLds = kScales + D * kScaleBuffer;
     static_assert(TI % R == 0 && TI % 2 == 0 && TI > 0 && TJ > 0 && 128 % kRun == 0, "");
     static_assert(BM % (8 * kWaves) == 0 && BN % (8 * kWaves) == 0 && kRun % 8 == 0 && BN % 64 == 0 && 2 * WM <= 64, "");
-    static_assert(D >= 2 && D <= 4 && 4 % D == 0, "");
-    // loads of a wavefront that may be on their way when step t + 1 has to be there, t % 4 = s: those of the steps t + 2 .. t + D - 1
-    static constexpr int on_their_way(int s)
-    {
-        int n = 0;
-        for (int j = s + 2; j <= s + D - 1; ++j) n += kLoads + (j % 4 == 0 ? kScaleShare : 0);
-        return n;
-    }
-    static_assert((D - 2) * kLoads + kScaleShare < 64, "");  // (the count that a wait names)
+    static_assert(D == 2 || D == 4, "");
+    static_assert(!kHalves || (TI / 2 >= R && BM / 16 % kWaves == 0), "");
+    // Loads of a wavefront that may be on their way, at the least those asked for after the next step's early part, or after this one's second halves.  (Those of scales
+    // not counted: there may be one or two more.)
+    static constexpr int kBeforeNext = (kHalves ? D - 1 : D - 2) * kLoads, kBeforeLate = (D - 1) * kLoads;
+    static_assert(kBeforeLate + kLate < 64, "");             // (the count that a wait names)
 };
 
 // f(I), ..., f(N - 1), numbers that are known when it is compiled.
@@ -43,6 +53,14 @@ template <int I, int N, class F> __device__ __forceinline__ void each(F f)
         f(std::integral_constant<int, I>{});
         each<I + 1, N>(f);
     }
+}
+
+// Sixteen 16-bit outputs of a lane's column, of two neighbouring pieces, so that a lane has eight consecutive ones: even sixteens of lanes of the first piece, odd ones of the
+// second; lo, hi: four outputs of each as they come from the matrix instructions.
+__device__ __forceinline__ u32x4 eight_outputs(u32x2 first, u32x2 second)
+{
+    const auto a = __builtin_amdgcn_permlane16_swap(first[0], second[0], false, false), b = __builtin_amdgcn_permlane16_swap(first[1], second[1], false, false);
+    return u32x4{(uint32_t)a[0], (uint32_t)b[0], (uint32_t)a[1], (uint32_t)b[1]};
 }
 
 template <int BM, int BN, int WM, int WN, int D, class T, bool GATED, bool WIDE>
@@ -57,102 +75,122 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void f8_tile_kernel(ProductArgs a,
     constexpr int kOutputs = GATED ? BM / 2 : BM;            // of the tile
 
     // Workgroups go to the eight dies in turn.  Each die takes a run of tiles, of large ones four columns of tiles at a time, so that what it has in flight shares rows
-    // of W and of X in its cache.
-    int column, o0;
-    const int columns = (a.rows + BN - 1) / BN, tiles = columns * row_tiles;
-    if (BM * BN >= 128 * 128) {
-        const int per = tiles / 8, more = tiles % 8, die = (int)blockIdx.x % 8, i = (int)blockIdx.x / 8;
-        if (i >= per + (die < more)) return;
-        const int tile = die * per + min(die, more) + i;
-        const int first = (int)a.band_tiles.quotient((uint32_t)tile) * 4, in = tile - first * row_tiles, across = min(4, columns - first);
-        const int down = across == 1 ? in : across == 2 ? in / 2 : across == 3 ? in / 3 : in / 4;
-        column = first + in - down * across;
-        o0 = down * kOutputs;
-    } else {
-        if ((int)blockIdx.x >= tiles) return;
-        column = (int)a.row_tiles.quotient(blockIdx.x);
-        o0 = ((int)blockIdx.x - column * row_tiles) * kOutputs;
-    }
-    const int c0 = column * BN, count = min(BN, a.rows - c0);
+    // of W and of X in its cache.  A workgroup takes every gridDim.x / 8-th tile of its die's run, and asks for its next tile's first steps while it multiplies the
+    // last of the one before.
+    const int columns = (a.rows + BN - 1) / BN, tiles = columns * row_tiles, die = (int)blockIdx.x % 8, dies_run = tiles / 8 + (die < tiles % 8);
+    const int run_first = die * (tiles / 8) + min(die, tiles % 8), stride = (int)gridDim.x / 8;
+    int nth = (int)blockIdx.x / 8;
+    if (nth >= dies_run) return;
     const int split = (int)blockIdx.y;
     const int t_first = 4 * (split * a.split_fours + min(split, a.split_more));
-    const int steps = min(4 * (a.split_fours + (split < a.split_more)), a.blocks - t_first), last = steps - 1;
+    const int steps = min(4 * (a.split_fours + (split < a.split_more)), a.blocks - t_first);
 
     const int wm = wave / WN, wn = wave % WN;
     const uint32_t row_bytes = (uint32_t)a.blocks * kBlock;
-    // Where run n of a tile's rows begins - the first output that it has, and whether it has values -, for runs of kRun rows, two to a wavefront's.
-    auto run_output = [&](int n) { return o0 + (GATED ? n / 2 : n) * C::kRun; };
-    auto run_value = [&](int n) { return GATED ? n % 2 : 0; };
-
-    // What each load of a wavefront reads: eight rows.  (Rows beyond the last repeat it; a tile's have less than 4 GB.)
+    // which of the buffer's rows load k of the wavefront writes: columns, then first halves of rows, then second halves
+    auto load_row = [&](int k) {
+        constexpr int kColumns = BN / 8 / C::kWaves, kRows = C::kHalves ? C::kLate : BM / 8 / C::kWaves;
+        if (k < kColumns) return BM + (k * C::kWaves + wave) * 8;
+        const int n = (k - kColumns) % kRows * C::kWaves + wave, half = (k - kColumns) / kRows;
+        return C::kHalves ? n / TI * (TI * 16) + half * C::kRun + n % TI * 8 : n * 8;
+    };
+    struct Place { int o, c; };                              // a tile's first output and column
+    auto place = [&](int nth) {
+        const int tile = run_first + nth;
+        int column, down;
+        if (BM * BN >= 128 * 128) {
+            const int first = (int)a.band_tiles.quotient((uint32_t)tile) * 4, in = tile - first * row_tiles, across = min(4, columns - first);
+            down = across == 1 ? in : across == 2 ? in / 2 : across == 3 ? in / 3 : in / 4;
+            column = first + in - down * across;
+        } else {
+            column = (int)a.row_tiles.quotient((uint32_t)tile);
+            down = tile - column * row_tiles;
+        }
+        return Place{down * kOutputs, column * BN};
+    };
+    // The tile that is asked for: what each load of a wavefront reads, eight rows (those beyond the last repeat it; a tile's have less than 4 GB).
     const uint8_t *base[C::kLoads];
     uint32_t offset[C::kLoads];
-    const uint32_t unit = (uint32_t)((lane & 7) ^ (lane >> 3)) * 16;
-#pragma unroll
-    for (int k = 0; k < C::kLoads; ++k) {
-        const int row = (k * C::kWaves + wave) * 8;
-        if (k < BM / 8 / C::kWaves) {
-            const int run = row / C::kRun, o = min(run_output(run) + row % C::kRun, a.width - 1);
-            base[k] = a.w + ((int64_t)run_value(run) * a.width + o) * row_bytes + (int64_t)t_first * kBlock;
-            offset[k] = (uint32_t)min(lane >> 3, a.width - 1 - o) * row_bytes + unit;
-        } else {
-            const int n = min(row - BM, count - 1);
-            base[k] = a.x + (int64_t)(c0 + n) * row_bytes + (int64_t)t_first * kBlock;
-            offset[k] = (uint32_t)min(lane >> 3, count - 1 - n) * row_bytes + unit;
-        }
-    }
     const float *scale_at[C::kScaleShare];
+    auto take = [&](int nth) __attribute__((always_inline)) {
+        const Place at = place(nth);
+        const int o0 = at.o, c0 = at.c, count = min(BN, a.rows - c0);
+        // where run n of a tile's rows begins - the first output that it has, and whether it has values -, for runs of kRun rows, two to a wavefront
+        auto run_output = [&](int n) { return o0 + (GATED ? n / 2 : n) * C::kRun; };
+        auto run_value = [&](int n) { return GATED ? n % 2 : 0; };
+        const uint32_t unit = (uint32_t)((lane & 7) ^ (lane >> 3)) * 16;
 #pragma unroll
-    for (int k = 0; k < C::kScaleShare; ++k) {
-        const int load = min(k * C::kWaves + wave, C::kScaleLoads - 1), n = load * 64 + lane;
-        if (n < BN) {
-            scale_at[k] = a.x_scales + (int64_t)(c0 + min(n, count - 1)) * a.pitch_scales + t_first;
-        } else {
-            const int run = min(n - BN, 2 * WM - 1), tall = min(run_output(run), a.width - 1) / kBlock + run_value(run) * a.value_tall;
-            scale_at[k] = a.w_scales + (int64_t)tall * a.pitch_scales + t_first;
+        for (int k = 0; k < C::kLoads; ++k) {
+            const int row = load_row(k);
+            if (k >= BN / 8 / C::kWaves) {
+                const int run = row / C::kRun, o = min(run_output(run) + row % C::kRun, a.width - 1);
+                base[k] = a.w + ((int64_t)run_value(run) * a.width + o) * row_bytes + (int64_t)t_first * kBlock;
+                offset[k] = (uint32_t)min(lane >> 3, a.width - 1 - o) * row_bytes + unit;
+            } else {
+                const int n = min(row - BM, count - 1);
+                base[k] = a.x + (int64_t)(c0 + n) * row_bytes + (int64_t)t_first * kBlock;
+                offset[k] = (uint32_t)min(lane >> 3, count - 1 - n) * row_bytes + unit;
+            }
         }
-    }
+#pragma unroll
+        for (int k = 0; k < C::kScaleShare; ++k) {
+            const int load = min(k * C::kWaves + wave, C::kScaleLoads - 1), n = load * 64 + lane;
+            if (n < BN) {
+                scale_at[k] = a.x_scales + (int64_t)(c0 + min(n, count - 1)) * a.pitch_scales + t_first;
+            } else {
+                const int run = min(n - BN, 2 * WM - 1), tall = min(run_output(run), a.width - 1) / kBlock + run_value(run) * a.value_tall;
+                scale_at[k] = a.w_scales + (int64_t)tall * a.pitch_scales + t_first;
+            }
+        }
+    };
     auto request = [&](int t, uint8_t *buf, int k) {
-        __builtin_amdgcn_global_load_lds((global_ptr)(base[k] + (uint32_t)t * kBlock + offset[k]), (lds_ptr)(buf + (k * C::kWaves + wave) * 1024), 16, 0, 0);
+        const uint8_t *at = base[k] + (uint32_t)t * kBlock;
+        asm("" : "+s"(at));                                  // (the same for all lanes, and added up there: half the registers)
+        __builtin_amdgcn_global_load_lds((global_ptr)(at + offset[k]), (lds_ptr)(buf + load_row(k) * kBlock), 16, 0, 0);
     };
     auto request_scales = [&](int q, uint8_t *buf, int k) {
         __builtin_amdgcn_global_load_lds((global_ptr)(scale_at[k] + (int64_t)q * 4), (lds_ptr)(buf + min(k * C::kWaves + wave, C::kScaleLoads - 1) * 1024), 16, 0, 0);
     };
 
-    const bool idle = wn * TJ * 16 >= count;                 // no columns: the wavefront loads, and multiplies nothing
     const int wi = wm * TI * 16 + r, wj = BM + wn * TJ * 16 + r;        // the lane's rows of the buffer
     const int lo = (g ^ (r & 7)) * 16, hi = ((g + 4) ^ (r & 7)) * 16;
     auto read_piece = [&](const uint8_t *buf, int row) { return both(*(const i32x4 *)(buf + row * kBlock + lo), *(const i32x4 *)(buf + row * kBlock + hi)); };
-    auto scale_of_column = [&](const uint8_t *buf, int s, int j) { return *(const float *)(buf + (wn * TJ * 16 + j * 16 + r) * 16 + s * 4); };
-    auto scale_of_run = [&](const uint8_t *buf, int s, int h) { return *(const float *)(buf + (BN + wm * 2 + h) * 16 + s * 4); };
+    auto scale_of_column = [&](const uint8_t *buf, int j) { return *(const float *)(buf + (wn * TJ * 16 + j * 16 + r) * 16); };
+    auto scale_of_run = [&](const uint8_t *buf, int h) { return *(const float *)(buf + (BN + wm * 2 + h) * 16); };
 
     f32x4 acc[TI][TJ], p[TJ];
-#pragma unroll
-    for (auto &x : acc)
-#pragma unroll
-        for (auto &y : x) y = f32x4{0, 0, 0, 0};
-#pragma unroll
-    for (auto &x : p) x = f32x4{0, 0, 0, 0};
     Operand<WIDE> x[TJ];
     i32x8 w[R];
     float sx[TJ], sw[2], by[TJ];
-#pragma unroll
-    for (auto &s : by) s = 0.0f;
 
     constexpr int kWaitLds = 0xc07f;                         // s_waitcnt: no LDS access left
     auto loads_left = [](int n) constexpr { return 0xf70 | (n & 15) | (n >> 4) << 14; };     // n loads left
-    auto barrier = [&] {
-        asm volatile("" ::: "memory");
-        __builtin_amdgcn_s_barrier();
-        asm volatile("" ::: "memory");
-    };
     auto join = [&](int i, int j) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) acc[i][j][e] = fmaf(p[j][e], by[j], acc[i][j][e]);
+        asm volatile("" : "+v"(acc[i][j]));                  // (here, not where the sum is needed next: p would have to be kept)
+    };
+    // What is asked for: step `ask` of the tile that was taken, and the scales of four into their buffers in turn.  (Behind the last step of the last tile that one again, so
+    // that a wait always counts the same; nothing uses what it brings.)
+    int ask = 0, scales_asked = 0;
+    auto scales = [&](int n) { return lds + C::kScales + n % D * C::kScaleBuffer; };
+    auto ask_scales = [&](uint8_t *__restrict__ to) __attribute__((always_inline)) {
+        if (ask % 4) return;
+#pragma unroll
+        for (int k = 0; k < C::kScaleShare; ++k) request_scales(ask / 4, to, k);
+        ++scales_asked;
+    };
+    auto asked = [&]() __attribute__((always_inline)) {
+        if (++ask < steps) return;
+        ask = steps - 1;
+        if (nth + stride >= dies_run) return;
+        nth += stride;
+        take(nth);
+        ask = 0;
     };
     // Piece row i of a step.  What is read behind it, into the registers that it leaves: rows from `rows`, and, of the last one, columns from `cols`.
-    auto piece = [&](auto I, auto S, const uint8_t *__restrict__ rows, const uint8_t *__restrict__ cols, const uint8_t *__restrict__ scales) __attribute__((always_inline)) {
-        constexpr int i = decltype(I)::value, s = decltype(S)::value;
+    auto piece = [&](auto I, const uint8_t *__restrict__ rows, const uint8_t *__restrict__ cols, const uint8_t *__restrict__ scales, uint8_t *__restrict__ to) __attribute__((always_inline)) {
+        constexpr int i = decltype(I)::value;
         const Operand<WIDE> wi_ = operand<WIDE>(w[i % R]);
 #pragma unroll
         for (int j = 0; j < TJ; ++j) {
@@ -165,119 +203,132 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void f8_tile_kernel(ProductArgs a,
             }
         }
         w[i % R] = read_piece(rows, wi + (i + R) % TI * 16);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int k = C::early(i); k < C::early(i + 1); ++k) request(ask, to, k);
+#pragma unroll
+        for (int k = C::late(i); k < C::late(i + 1); ++k) request(ask, to, C::kEarly + k);
         if (i == 0 || i == TI / 2) {
 #pragma unroll
             for (int j = 0; j < TJ; ++j) by[j] = sx[j] * sw[i == 0 ? 0 : 1];
         }
         if (i == TI - 1) {                                   // (the next step's)
 #pragma unroll
-            for (int j = 0; j < TJ; ++j) sx[j] = scale_of_column(scales, (s + 1) % 4, j);
-            sw[0] = scale_of_run(scales, (s + 1) % 4, 0);
+            for (int j = 0; j < TJ; ++j) sx[j] = scale_of_column(scales, j);
+            sw[0] = scale_of_run(scales, 0);
         }
         __builtin_amdgcn_sched_barrier(0);
     };
-    // Step t, t % 4 = S: `now` has it, `next` the one after, `to` (the same as now) receives step `ask`.
-    auto step = [&](auto S, const uint8_t *now, const uint8_t *next, const uint8_t *scales, const uint8_t *scales_next, uint8_t *to, uint8_t *scales_to, int ask, int ask_scales)
-                    __attribute__((always_inline)) {
-        constexpr int s = decltype(S)::value;
-        auto first = [&](const uint8_t *__restrict__ now, const uint8_t *__restrict__ scales) __attribute__((always_inline)) {
-            sw[1] = scale_of_run(scales, s, 1);
-            each<0, TI - R>([&](auto I) __attribute__((always_inline)) { piece(I, S, now, now, scales); });
-        };
-        auto second = [&](const uint8_t *__restrict__ next, const uint8_t *__restrict__ scales_next, uint8_t *__restrict__ to, uint8_t *__restrict__ scales_to) __attribute__((always_inline)) {
-            if ((s + D) % 4 == 0) {
-#pragma unroll
-                for (int k = 0; k < C::kScaleShare; ++k) request_scales(ask_scales, scales_to, k);
-            }
-#pragma unroll
-            for (int k = 0; k < C::kLoads; ++k) request(ask, to, k);
-            if (idle) return;
-            __builtin_amdgcn_sched_barrier(0);
-            each<TI - R, TI>([&](auto I) __attribute__((always_inline)) { piece(I, S, next, next, scales_next); });
-        };
-        if (!idle) first(now, scales);
-        // every wavefront's loads of step t + 1 have arrived, and all reads of this step's buffer are done
+    auto meet = [&](auto LEFT) __attribute__((always_inline)) {
         __builtin_amdgcn_sched_barrier(0);
         __builtin_amdgcn_s_waitcnt(kWaitLds);
-        constexpr int left = loads_left(C::on_their_way(s));
+        constexpr int left = loads_left(decltype(LEFT)::value);
         __builtin_amdgcn_s_waitcnt(left);
-        barrier();
-        second(next, scales_next, to, scales_to);
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+    };
+    // A step.  `now` has it, `next` the one after; `to`, which is `now`, receives step `ask`.  `scales_now` and `scales_next` are at the word of their step.
+    auto step = [&](const uint8_t *now, const uint8_t *next, uint8_t *to, const uint8_t *scales_now, const uint8_t *scales_next) __attribute__((always_inline)) {
+        sw[1] = scale_of_run(scales_now, 1);
+        if (C::kHalves) {
+            each<0, C::kFree>([&](auto I) __attribute__((always_inline)) { piece(I, now, now, scales_now, to); });
+            meet(std::integral_constant<int, C::kBeforeLate>{});
+            ask_scales(scales(scales_asked));
+        }
+        each<(C::kHalves ? C::kFree : 0), C::kNext>([&](auto I) __attribute__((always_inline)) { piece(I, now, now, scales_now, to); });
+        meet(std::integral_constant<int, C::kBeforeNext>{});
+        if (!C::kHalves) ask_scales(scales(scales_asked));
+        each<C::kNext, TI>([&](auto I) __attribute__((always_inline)) { piece(I, next, next, scales_next, to); });
     };
 
-    auto buffer = [&](int t) { return lds + t % D * C::kBuffer; };
-    auto scales = [&](int q) { return lds + C::kScales + q % 2 * C::kScaleBuffer; };
-    // (requests beyond the last step repeat it, so that a wait always counts the same; nothing uses what they bring)
-#pragma unroll
-    for (int k = 0; k < C::kScaleShare; ++k) request_scales(0, scales(0), k);
+    const int nth0 = nth;
+    take(nth);
 #pragma unroll
     for (int t = 0; t < D; ++t) {
-        if (t > 0 && t % 4 == 0) {
+        ask_scales(scales(scales_asked));
 #pragma unroll
-            for (int k = 0; k < C::kScaleShare; ++k) request_scales(min(t, last) / 4, scales(t / 4), k);
+        for (int k = 0; k < C::kLoads; ++k) request(ask, lds + t * C::kBuffer, k);
+        asked();
+    }
+    meet(std::integral_constant<int, (D - 1) * C::kLoads + C::kLate>{});
+#pragma unroll
+    for (int j = 0; j < TJ; ++j) x[j] = operand<WIDE>(read_piece(lds, wj + j * 16)), sx[j] = scale_of_column(scales(0), j);
+    sw[0] = scale_of_run(scales(0), 0);
+#pragma unroll
+    for (int i = 0; i < R; ++i) w[i] = read_piece(lds, wi + i * 16);
+
+    int buffer = 0, fours = 0;                               // of the step that is multiplied
+    for (int mth = nth0; mth < dies_run; mth += stride) {
+#pragma unroll
+        for (auto &v : acc)
+#pragma unroll
+            for (auto &y : v) y = f32x4{0, 0, 0, 0};
+#pragma unroll
+        for (int j = 0; j < TJ; ++j) p[j] = f32x4{0, 0, 0, 0}, by[j] = 0.0f;
+        for (int t = 0; t < steps; ++t) {
+            uint8_t *now = lds + buffer * C::kBuffer;
+            buffer = (buffer + 1) % D;
+            const int in = t % 4, in_next = t + 1 < steps ? (t + 1) % 4 : 0;
+            const uint8_t *scales_now = scales(fours) + in * 4;
+            fours += in_next == 0;
+            step(now, lds + buffer * C::kBuffer, now, scales_now, scales(fours) + in_next * 4);
+            asked();
         }
 #pragma unroll
-        for (int k = 0; k < C::kLoads; ++k) request(min(t, last), buffer(t), k);
-    }
-    constexpr int all_but_first = loads_left((D - 1) * C::kLoads);
-    __builtin_amdgcn_s_waitcnt(all_but_first);
-    barrier();
-    if (!idle) {
+        for (int j = 0; j < TJ; ++j) join(TI - 1, j);
+
+        // Straight from the registers: what a wavefront stores of a row at a time are 64 consecutive bytes, and the next tile's loads need not wait.
+        const Place at = place(mth);
+        constexpr int kWide = GATED ? TI * 8 : TI * 16, kPieces = kWide / 16;
+        const int first = at.o + wm * kWide, c_first = at.c + wn * TJ * 16 + r;
+        if (a.part) {
 #pragma unroll
-        for (int j = 0; j < TJ; ++j) x[j] = operand<WIDE>(read_piece(lds, wj + j * 16)), sx[j] = scale_of_column(scales(0), 0, j);
-        sw[0] = scale_of_run(scales(0), 0, 0);
+            for (int i = 0; i < TI; ++i) {
+                const int h = GATED && i >= kPieces, o = first + (i - h * kPieces) * 16 + 4 * g;
 #pragma unroll
-        for (int i = 0; i < R; ++i) w[i] = read_piece(lds, wi + i * 16);
-    }
-    auto at = [&](auto S, int q) __attribute__((always_inline)) {
-        constexpr int s = decltype(S)::value;
-        const int t = 4 * q + s, ask = min(t + D, last);
-        step(S, lds + s % D * C::kBuffer, lds + (s + 1) % D * C::kBuffer, scales(q), scales(q + (s + 1) / 4), lds + s % D * C::kBuffer, scales(q + 1), ask, ask / 4);
-    };
-    int q = 0;
-    for (; 4 * q + 4 <= steps; ++q) {
-        at(std::integral_constant<int, 0>{}, q);
-        at(std::integral_constant<int, 1>{}, q);
-        at(std::integral_constant<int, 2>{}, q);
-        at(std::integral_constant<int, 3>{}, q);
-    }
-    if (4 * q < steps) at(std::integral_constant<int, 0>{}, q);
-    if (4 * q + 1 < steps) at(std::integral_constant<int, 1>{}, q);
-    if (4 * q + 2 < steps) at(std::integral_constant<int, 2>{}, q);
+                for (int j = 0; j < TJ; ++j)
+                    if (c_first + j * 16 < a.rows) store_part(a, split, c_first + j * 16, o, acc[i][j], h * a.value_at);
+            }
+        } else if constexpr (sizeof(T) == 2 && kPieces % 2 == 0) {
 #pragma unroll
-    for (int j = 0; j < TJ; ++j) join(TI - 1, j);
-    __builtin_amdgcn_s_waitcnt(kWaitLds);
+            for (int i = 0; i < kPieces; i += 2) {
+#pragma unroll
+                for (int j = 0; j < TJ; ++j) {
+                    const f32x4 v = activated<GATED>(a, first + i * 16 + 4 * g, acc[i][j], acc[GATED ? kPieces + i : i][j]);
+                    const f32x4 u = activated<GATED>(a, first + i * 16 + 16 + 4 * g, acc[i + 1][j], acc[GATED ? kPieces + i + 1 : i + 1][j]);
+                    const T four[2][4] = {{(T)v[0], (T)v[1], (T)v[2], (T)v[3]}, {(T)u[0], (T)u[1], (T)u[2], (T)u[3]}};
+                    u32x2 lo, hi;
+                    __builtin_memcpy(&lo, four[0], 8);
+                    __builtin_memcpy(&hi, four[1], 8);
+                    const u32x4 eight = eight_outputs(lo, hi);
+                    const int o = first + (i + (g & 1)) * 16 + g / 2 * 8;
+                    if (c_first + j * 16 >= a.rows || o >= a.width) continue;
+                    T *y = (T *)a.Y + (int64_t)(c_first + j * 16) * a.width + o;
+                    if (o + 8 <= a.width) {
+                        __builtin_memcpy(y, &eight, 16);
+                    } else {
+                        T out[8];
+                        __builtin_memcpy(out, &eight, 16);
+#pragma unroll
+                        for (int e = 0; e < 7; ++e)
+                            if (o + e < a.width) y[e] = out[e];
+                    }
+                }
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < kPieces; ++i) {
+                const int o = first + i * 16 + 4 * g;
+#pragma unroll
+                for (int j = 0; j < TJ; ++j) {
+                    const f32x4 v = activated<GATED>(a, o, acc[i][j], acc[GATED ? kPieces + i : i][j]);
+                    if (c_first + j * 16 < a.rows) store_outputs<T>(a, c_first + j * 16, o, v);
+                }
+            }
+        }
+    }
+    // (what is still on its way into LDS has to be there before that is another workgroup's)
     constexpr int none = loads_left(0);
     __builtin_amdgcn_s_waitcnt(none);
-    barrier();
-    if (idle) return;
-
-    // A wavefront's outputs go through LDS, sixteen columns at a time, so that what it stores of a row of Y is consecutive.
-    constexpr int kWide = GATED ? TI * 8 : TI * 16, kPitch = kWide + 4, kLanes = kWide / 4;
-    static_assert(C::kWaves * 16 * kPitch * 4 <= C::kLds && 64 % kLanes == 0, "");
-    float *mine = (float *)lds + wave * 16 * kPitch;
-    const int first = o0 + wm * kWide, o = first + lane % kLanes * 4;
-#pragma unroll
-    for (int j = 0; j < TJ; ++j) {
-        // (parts of a gated product: gates, then values)
-#pragma unroll
-        for (int h = 0; h < (GATED ? 2 : 1); ++h) {
-            if (GATED && h == 1 && !a.part) break;
-            lanes_exchange();
-#pragma unroll
-            for (int i = 0; i < kWide / 16; ++i) {
-                f32x4 v = acc[h * (TI / 2) + i][j];
-                if (!a.part) v = activated<GATED>(a, first + i * 16 + 4 * g, v, acc[GATED ? TI / 2 + i : i][j]);
-                *(f32x4 *)(mine + r * kPitch + i * 16 + 4 * g) = v;
-            }
-            lanes_exchange();
-            for (int n = lane / kLanes; n < 16; n += 64 / kLanes) {
-                const int c = wn * TJ * 16 + j * 16 + n;
-                if (c >= count) continue;
-                const f32x4 v = *(const f32x4 *)(mine + n * kPitch + lane % kLanes * 4);
-                if (a.part) store_part(a, split, c0 + c, o, v, h * a.value_at);
-                else store_outputs<T>(a, c0 + c, o, v);
-            }
-        }
-    }
 }
