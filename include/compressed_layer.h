@@ -689,12 +689,24 @@ int32_t cl_rms_norm(const cl_norm_call *call, void *stream);
  *  d_Y       batch rows of W->rows (CL_ACT_GATED: half as many) of y_type, overwritten; CL_F8: values, and scales at d_y_scales, as
  *            cl_eight_quantize makes them of the fp32 result
  *  d_workspace  at least cl_eight_fc_workspace_bytes(), 256-byte aligned; NULL will do where that is 0.  What is asked for a batch is enough for
- *            every smaller one: a call that would split its sums, and whose workspace has no room for the parts, does not split them (slower, and
- *            another order of the sums)
+ *            every smaller one: a call whose workspace has no room for what its fastest form needs takes another that does with it (slower, and
+ *            with another order of the sums)
  * Run-to-run identical.  A batch of 0 is no error.
  * Errors: CL_EINVAL (null pointers, sizes, alignment, workspace too small), CL_EUNSUPPORTED (CL_F8_MAX_K, a launch that does
  * not fit a grid) - nothing is launched then; CL_EHIP. */
 int32_t cl_eight_fc_workspace_bytes(const cl_f8_matrix *W, int32_t batch, int32_t x_type, int32_t y_type, int32_t act, size_t *out);
+
+/* How a product is made. */
+enum {
+    CL_F8_FORM_FEW_NUMBERS = 0,  /* one launch that quantises X itself and multiplies, sixteen rows of W at a time        */
+    CL_F8_FORM_FEW = 1,          /* the same with X in 8 bits                                                               */
+    CL_F8_FORM_TILE_64 = 2,      /* tiles of the output with their operands in LDS: 64 x 64,                               */
+    CL_F8_FORM_TILE_128 = 3,     /*   128 x 128,                                                                           */
+    CL_F8_FORM_TILE_256 = 4      /*   256 x 256                                                                            */
+};
+/* The form that cl_eight_fc_forward takes for such a call, given a workspace of cl_eight_fc_workspace_bytes() for that batch, and into how many sums it splits
+ * k.  Errors as cl_eight_fc_workspace_bytes. */
+int32_t cl_eight_fc_resolved_form(const cl_f8_matrix *W, int32_t batch, int32_t x_type, int32_t y_type, int32_t act, int32_t *form, int32_t *splits);
 int32_t cl_eight_fc_forward(const cl_f8_matrix *W, const cl_f8_input *X, const float *d_bias_or_null, void *d_Y, float *d_y_scales, int32_t y_type, int32_t batch,
                          int32_t act, void *d_workspace, size_t workspace_bytes, void *stream);
 

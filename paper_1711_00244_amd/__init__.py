@@ -9,5 +9,5 @@ from .binding import (PATH_AUTO, STATIC_SCRATCH_BYTES, PATH_MFMA_BF16, PATH_MFMA
                       fc_resolved_path, fc_stack_workspace_bytes, fc_workspace_bytes, layer_deserialize, lrn_forward, maxpool_forward, plan_batches)
 from .binding import (MX_FORMS, ExpertLists, MxTensor, expert_lists, mx_dequantize, mx_experts_forward, mx_experts_resolved_form, mx_fc_forward,  # noqa: F401
                       mx_fc_resolved_form, mx_fc_workspace_bytes, mx_quantize, mx_row_blocks, route_experts)
-from .binding import (F8Tensor, f8_dequantize, f8_fc_forward, f8_fc_workspace_bytes, f8_gated, f8_quantize, f8_row_blocks, f8_row_scales,  # noqa: F401
+from .binding import (F8_FORMS, F8Tensor, f8_dequantize, f8_fc_forward, f8_fc_resolved_form, f8_fc_workspace_bytes, f8_gated, f8_quantize, f8_row_blocks, f8_row_scales,  # noqa: F401
                       rms_norm)

@@ -24,6 +24,7 @@ F8 = 4                                 # CL_F8
 ACTIVATIONS = {"none": 0, "relu": 1, "gated": 2}
 SCORES = {"softmax": 0, "sigmoid": 1}
 GROUP_SCORES = {"max": 0, "top2": 1}
+F8_FORMS = ("few numbers", "few", "tile 64", "tile 128", "tile 256")                  # CL_F8_FORM_*
 MX_FORMS = ("few", "rows", "tile 64", "tile 128", "tile 256 x 128", "tile 256")       # CL_MX_FORM_*
 
 EXPORTS = [
@@ -36,7 +37,7 @@ EXPORTS = [
     "cl_set_kernel_timing", "cl_last_kernel_ms",
     "cl_mx_quantize", "cl_mx_dequantize", "cl_mx_fc_workspace_bytes", "cl_mx_fc_forward", "cl_route_experts", "cl_expert_lists_bytes",
     "cl_expert_lists", "cl_mx_experts_workspace_bytes", "cl_mx_experts_forward", "cl_mx_fc_resolved_form", "cl_mx_experts_resolved_form",
-    "cl_eight_quantize", "cl_eight_dequantize", "cl_rms_norm", "cl_eight_fc_workspace_bytes", "cl_eight_fc_forward",
+    "cl_eight_quantize", "cl_eight_dequantize", "cl_rms_norm", "cl_eight_fc_workspace_bytes", "cl_eight_fc_forward", "cl_eight_fc_resolved_form",
 ]
 
 
@@ -170,6 +171,7 @@ def lib():
     L.cl_eight_dequantize.argtypes = [p, p, i64, i32, i32, p, i32, i64, p]
     L.cl_rms_norm.argtypes = [C.POINTER(NormCall), p]
     L.cl_eight_fc_workspace_bytes.argtypes = [C.POINTER(F8Matrix), i32, i32, i32, i32, C.POINTER(sz)]
+    L.cl_eight_fc_resolved_form.argtypes = [C.POINTER(F8Matrix), i32, i32, i32, i32, C.POINTER(i32), C.POINTER(i32)]
     L.cl_eight_fc_forward.argtypes = [C.POINTER(F8Matrix), C.POINTER(F8Input), p, p, p, i32, i32, i32, p, sz, p]
     for name in EXPORTS:
         if name not in ("cl_last_error", "cl_layer_group_free"):
@@ -1083,6 +1085,17 @@ def f8_fc_workspace_bytes(W: F8Tensor, batch: int, dtype=None, act="none", out_d
     _start()
     dtype = dtype or torch.float32
     return _f8_fc_need(W.shape[0], W.K, batch, _f8_type(dtype, "X"), _f8_type(out_dtype or dtype, "out"), _act(act))
+
+
+def f8_fc_resolved_form(W: F8Tensor, batch: int, dtype=None, act="none", out_dtype=None) -> tuple[str, int]:
+    """How f8_fc_forward makes `batch` rows of dtype (as in f8_fc_workspace_bytes): one of F8_FORMS, and how many sums k is split into."""
+    import torch
+    _start()
+    dtype = dtype or torch.float32
+    _int32(*W.shape, batch)
+    form, splits = C.c_int32(0), C.c_int32(0)
+    _check(lib().cl_eight_fc_resolved_form(F8Matrix(None, None, W.shape[0], W.K), batch, _f8_type(dtype, "X"), _f8_type(out_dtype or dtype, "out"), _act(act), form, splits))
+    return F8_FORMS[form.value], splits.value
 
 
 def f8_fc_forward(W: F8Tensor, X, bias=None, act=None, dtype=None, out=None, workspace=None):

@@ -1,5 +1,6 @@
 // Products with 8-bit matrices that have a scale for each block of 128 x 128, on the 8-bit matrix instructions.
 #include <algorithm>
+#include <cmath>
 #include <type_traits>
 #include <utility>
 
@@ -121,59 +122,7 @@ __device__ __forceinline__ void store_part(const ProductArgs &a, int split, int6
     if (o < a.width) *(f32x4 *)(a.part + ((int64_t)split * a.rows + row) * a.pitch + at + o) = v;
 }
 
-// A workgroup of up to sixteen wavefronts makes 16 outputs (blockIdx.x) of 16 columns (blockIdx.y).  The wavefronts share out the row's blocks; their sums
-// meet in LDS and are added in the order of the wavefronts.  No operand is shared, so that nothing waits for a barrier until the end.
-constexpr int kRowsWaves = 16;
-
-template <class T, bool GATED, bool WIDE> __global__ __launch_bounds__(kRowsWaves * 64) void f8_rows_kernel(ProductArgs a, int column0)
-{
-    constexpr int F = GATED ? 2 : 1;
-    __shared__ f32x4 sums[kRowsWaves][F][64];
-    const int waves = (int)blockDim.x / 64, wave = threadIdx.x / 64, lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
-    const int o0 = (int)blockIdx.x * 16;
-    const int64_t c0 = column0 + (int64_t)blockIdx.y * 16, column = min(c0 + r, (int64_t)a.rows - 1), row_bytes = (int64_t)a.blocks * kBlock;
-    const uint8_t *w[F], *x = a.x + column * row_bytes + g * 32;
-    const float *ws[F], *xs = a.x_scales + column * a.pitch_scales;
-#pragma unroll
-    for (int f = 0; f < F; ++f) {
-        w[f] = a.w + ((int64_t)f * a.width + min(o0 + r, a.width - 1)) * row_bytes + g * 32;
-        ws[f] = a.w_scales + (int64_t)(f * a.value_tall + o0 / kBlock) * a.pitch_scales;
-    }
-    f32x4 acc[F] = {};
-    for (int b = wave; b < a.blocks; b += waves) {
-        const i32x4 *xp = (const i32x4 *)(x + (int64_t)b * kBlock);
-        const Operand<WIDE> xv = operand<WIDE>(both(xp[0], xp[1]));
-        const float sx = xs[b];
-#pragma unroll
-        for (int f = 0; f < F; ++f) {
-            const i32x4 *wp = (const i32x4 *)(w[f] + (int64_t)b * kBlock);
-            const f32x4 p = mfma_f8<WIDE>(operand<WIDE>(both(wp[0], wp[1])), xv);
-            const float s = sx * ws[f][b];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) acc[f][i] = fmaf(p[i], s, acc[f][i]);
-        }
-    }
-#pragma unroll
-    for (int f = 0; f < F; ++f) sums[wave][f][lane] = acc[f];
-    __syncthreads();
-    if (threadIdx.x >= 64) return;
-    const int64_t row = c0 + r;
-    if (row >= a.rows) return;
-    f32x4 v[F];
-#pragma unroll
-    for (int f = 0; f < F; ++f) {
-        v[f] = sums[0][f][lane];
-        for (int i = 1; i < waves; ++i) v[f] += sums[i][f][lane];
-    }
-    const int o = o0 + 4 * g;
-    if (a.part) {
-#pragma unroll
-        for (int f = 0; f < F; ++f) store_part(a, 0, row, o, v[f], f * a.value_at);
-    } else {
-        store_outputs<T>(a, row, o, activated<GATED>(a, o, v[0], v[F - 1]));
-    }
-}
-
+#include "few_kernel.hpp"
 #include "tile_kernel.hpp"
 
 // The sum over the splits of a product's parts, in order, and from it four outputs of one row.  8-bit outputs: 32 lanes have a block.
@@ -218,38 +167,52 @@ template <class T, bool GATED> __global__ __launch_bounds__(256) void f8_finish_
 // which kernel
 // ------------------------------------------------------------------------- //
 constexpr int kCus = 256;
-enum Form { kRows, kTile64, kTile128, kTile256 };
-constexpr int kFormSide[] = {16, 64, 128, 256}, kFormThreads[] = {0, 256, 512, 512};        // of a workgroup: rows of W and of X, threads (kRows: as many as rows_waves says)
+enum Form { kFew, kTile64, kTile128, kTile256 };
+constexpr int kFormSide[] = {16, 64, 128, 256}, kFormThreads[] = {0, 256, 512, 512};        // of a workgroup: rows of W and of X, threads (kFew: as few_threads says)
+
+// A call, by what the choice of a kernel depends on.
+struct Shape {
+    int32_t width, blocks, batch;
+    bool gated, wide;                                        // wide: sums of 32 bits within a block
+    int32_t x_type, y_type;
+};
 struct Choice {
     Form form;
     int splits;
+    bool own;                                                // kFew: quantises X itself
+    float us;
 };
 
-static Choice choose(int width, int blocks, int64_t rows, bool gated, bool wide)
+// Outputs in fp32 show the 8-bit instruction's sums (see mfma_f8).  8-bit outputs do not; but a value of them next to the middle of two steps goes to one or
+// the other by the last bits of its sum, and of two blocks of a layer one after the other the rounding of outputs in fp16 is fine enough to show that, in bf16 not: so 8-bit outputs
+// of a bf16 input, or of one that has 8 bits already, take the faster instructions.
+static bool is_wide(int32_t x_type, int32_t y_type) { return y_type == CL_F32 || (y_type == CL_F8 && (x_type == CL_F32 || x_type == CL_F16)); }
+
+static bool few_own(const Shape &s) { return s.x_type != CL_F8 && few_lds(s.blocks, std::min(s.batch, kFewColumns)) <= kFewLds; }
+
+// Wavefronts of a workgroup of few_kernel that share out the blocks of a row, and all: more where there is much to quantise.
+static int few_waves(int blocks) { return std::min(kFewWaves, blocks); }
+static int few_threads(const Shape &s, bool own)
 {
-    (void)blocks;
-    const int64_t M = (int64_t)width * (gated ? 2 : 1);
-    if (rows <= 32) return Choice{kRows, 1};
-    const int64_t n = ((M + 255) / 256) * ((rows + 255) / 256);
-    if (n >= 128 && !wide) return Choice{kTile256, 1};
-    if (((M + 127) / 128) * ((rows + 127) / 128) >= 128) return Choice{kTile128, 1};
-    return Choice{kTile64, 1};
+    const int columns = std::min(s.batch, kFewColumns);
+    return 64 * std::max(few_waves(s.blocks), own ? (int)std::min<int64_t>(kFewWaves, ((int64_t)columns * s.blocks * 16 + 127) / 128) : 1);
 }
 
-// Wavefronts that share out the blocks of a row.
-static int rows_waves(int blocks) { return std::min(kRowsWaves, blocks); }
-
-static int64_t row_tiles_of(const Choice &c, int32_t width, bool gated)
+static int64_t row_tiles_of(Form form, int32_t width, bool gated)
 {
-    const int64_t outputs = c.form == kRows || !gated ? kFormSide[c.form] : kFormSide[c.form] / 2;
+    const int64_t outputs = form == kFew || !gated ? kFormSide[form] : kFormSide[form] / 2;
     return (width + outputs - 1) / outputs;
 }
 
+// Whether 8-bit outputs are made where the product ends: where a workgroup has all 128 of a block.
+static bool ends_in_f8(const Shape &s, const Choice &c) { return s.y_type == CL_F8 && c.splits == 1 && (c.form == kTile256 || (c.form == kTile128 && !s.gated)); }
+static bool needs_parts(const Shape &s, const Choice &c) { return c.splits > 1 || (s.y_type == CL_F8 && !ends_in_f8(s, c)); }
+
 // Whether the launch has less than 2^32 threads along each axis.
-static int32_t check_grid(const Choice &c, int32_t width, int blocks, int64_t rows, bool gated)
+static int32_t check_grid(const Choice &c, const Shape &s)
 {
-    const int64_t row_tiles = row_tiles_of(c, width, gated), columns = (rows + kFormSide[c.form] - 1) / kFormSide[c.form];
-    const int64_t wgs = c.form == kRows ? row_tiles : (int64_t)round_up(row_tiles * columns, 8), threads = c.form == kRows ? rows_waves(blocks) * 64 : kFormThreads[c.form];
+    const int64_t row_tiles = row_tiles_of(c.form, s.width, s.gated), columns = ((int64_t)s.batch + kFormSide[c.form] - 1) / kFormSide[c.form];
+    const int64_t wgs = c.form == kFew ? row_tiles : (int64_t)round_up(row_tiles * columns, 8), threads = c.form == kFew ? few_threads(s, c.own) : kFormThreads[c.form];
     if (wgs > (int64_t)UINT32_MAX / threads || wgs > INT_MAX) return fail(CL_EUNSUPPORTED, "a launch of %lld workgroups does not fit a grid", (long long)wgs);
     return CL_OK;
 }
@@ -259,24 +222,46 @@ template <Form F, int WM, int WN, int D, class T, bool GATED, bool WIDE> static 
     constexpr int SIDE = kFormSide[F];
     using C = Tile<SIDE, SIDE, WM, WN, D>;
     static_assert(C::kThreads == kFormThreads[F], "");
+    constexpr size_t kLds = C::kLds + (std::is_same_v<T, F8Out> ? C::kTops : 0);
     auto kernel = f8_tile_kernel<SIDE, SIDE, WM, WN, D, T, GATED, WIDE>;
     static LdsLimit seen;
-    if (int32_t rc = allow_lds((const void *)kernel, C::kLds, seen)) return rc;
-    const int64_t row_tiles = row_tiles_of(c, a.width, GATED), columns = ((int64_t)a.rows + SIDE - 1) / SIDE;
+    if (int32_t rc = allow_lds((const void *)kernel, kLds, seen)) return rc;
+    const int64_t row_tiles = row_tiles_of(F, a.width, GATED), columns = ((int64_t)a.rows + SIDE - 1) / SIDE;
     a.row_tiles = make_div((uint32_t)row_tiles);
     a.band_tiles = make_div((uint32_t)row_tiles * 4u);
     const int fours = (a.blocks + 3) / 4;
     a.split_fours = fours / c.splits;
     a.split_more = fours % c.splits;
     const size_t wgs = round_up(row_tiles * columns, 8);
-    hipLaunchKernelGGL(kernel, dim3((unsigned)(F == kTile256 ? std::min<size_t>(wgs, kCus) : wgs), (unsigned)c.splits), dim3(C::kThreads), C::kLds, st, a, (int)row_tiles);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(F == kTile256 ? std::min<size_t>(wgs, kCus) : wgs), (unsigned)c.splits), dim3(C::kThreads), kLds, st, a, (int)row_tiles);
     MX_HIP_TRY(hipGetLastError());
     return CL_OK;
 }
 
-template <class T, bool GATED, bool WIDE> static int32_t launch_product(ProductArgs a, const Choice &c, hipStream_t st)
+// x: what few_kernel quantises itself; else a.x.
+template <class X, class T, bool GATED, bool WIDE> static int32_t launch_few(const ProductArgs &a, const Shape &s, const cl_f8_input &x, int32_t K, hipStream_t st)
 {
-    a.splits = c.splits;
+    constexpr bool kOwn = !std::is_same_v<X, F8In>;
+    auto kernel = f8_few_kernel<X, T, GATED, WIDE>;
+    const int columns = std::min(s.batch, kFewColumns);
+    const size_t sums = (size_t)few_waves(s.blocks) * (GATED ? 2 : 1) * 64 * sizeof(f32x4);
+    static LdsLimit seen;
+    if (int32_t rc = allow_lds((const void *)kernel, kFewLds + kFewWaves * 2 * 64 * sizeof(f32x4), seen)) return rc;
+    FewArgs f{a, x.d_X, x.stride, make_div((uint32_t)s.blocks * (kBlock / 8)), K, 0, columns, few_waves(s.blocks)};
+    // (a grid is at most 65535 high: taller ones go in pieces)
+    const int64_t groups = ((int64_t)s.batch + kFewColumns - 1) / kFewColumns;
+    for (int64_t g = 0; g < groups; g += 65535) {
+        f.column0 = g * kFewColumns;
+        hipLaunchKernelGGL(kernel, dim3((unsigned)((s.width + 15) / 16), (unsigned)std::min<int64_t>(groups - g, 65535)), dim3((unsigned)few_threads(s, kOwn)),
+                           (kOwn ? few_lds(s.blocks, columns) : 0) + sums, st, f);
+        MX_HIP_TRY(hipGetLastError());
+    }
+    return CL_OK;
+}
+
+// T: what the kernel stores.
+template <class T, bool GATED, bool WIDE> static int32_t launch_product(const ProductArgs &a, const Shape &s, const Choice &c, const cl_f8_input &x, int32_t K, hipStream_t st)
+{
     switch (c.form) {
     case kTile64: return launch_tiles<kTile64, 2, 2, 4, T, GATED, WIDE>(a, c, st);
     case kTile128: return launch_tiles<kTile128, 2, 4, 2, T, GATED, WIDE>(a, c, st);
@@ -284,14 +269,8 @@ template <class T, bool GATED, bool WIDE> static int32_t launch_product(ProductA
         if constexpr (!WIDE) return launch_tiles<kTile256, 2, 4, 2, T, GATED, false>(a, c, st);
     default: break;
     }
-    // (a grid is at most 65535 high: taller ones go in pieces)
-    const int64_t tiles = ((int64_t)a.rows + 15) / 16;
-    for (int64_t t0 = 0; t0 < tiles; t0 += 65535) {
-        hipLaunchKernelGGL((f8_rows_kernel<T, GATED, WIDE>), dim3((unsigned)((a.width + 15) / 16), (unsigned)std::min<int64_t>(tiles - t0, 65535)), dim3(rows_waves(a.blocks) * 64), 0, st, a,
-                           (int)(t0 * 16));
-        MX_HIP_TRY(hipGetLastError());
-    }
-    return CL_OK;
+    if (!c.own) return launch_few<F8In, T, GATED, WIDE>(a, s, x, K, st);
+    return with_type(x.type, [&](auto t) { return launch_few<decltype(t), T, GATED, WIDE>(a, s, x, K, st); });
 }
 
 // launch(row0, rows, workgroups) over rows of `quads` threads each, in pieces whose threads' numbers have 32 bits.
@@ -306,19 +285,24 @@ template <class F> static int32_t launch_rows(int32_t rows, uint32_t quads, F la
     return CL_OK;
 }
 
-template <bool GATED> static int32_t run_product(const ProductArgs &a, const Choice &c, int32_t y_type, hipStream_t st)
+template <bool GATED> static int32_t run_product(ProductArgs a, const Shape &s, const Choice &c, const cl_f8_input &x, int32_t K, hipStream_t st)
 {
-    if (!a.part) return with_type(y_type, [&](auto t) { return launch_product<decltype(t), GATED, std::is_same_v<decltype(t), float>>(a, c, st); });
-    if (int32_t rc = y_type == CL_F32 ? launch_product<float, GATED, true>(a, c, st) : launch_product<float, GATED, false>(a, c, st)) return rc;
-    ProductArgs p = a;
-    p.splits = c.splits;
+    a.splits = c.splits;
+    if (!a.part) {
+        if (s.y_type == CL_F32) return launch_product<float, GATED, true>(a, s, c, x, K, st);
+        if (s.y_type == CL_BF16) return launch_product<bf16_t, GATED, false>(a, s, c, x, K, st);
+        if (s.y_type == CL_F16) return launch_product<f16_t, GATED, false>(a, s, c, x, K, st);
+        if (c.form == kTile256) return launch_tiles<kTile256, 2, 4, 2, F8Out, GATED, false>(a, c, st);
+        if constexpr (!GATED) return s.wide ? launch_tiles<kTile128, 2, 4, 2, F8Out, false, true>(a, c, st) : launch_tiles<kTile128, 2, 4, 2, F8Out, false, false>(a, c, st);
+    }
+    if (int32_t rc = s.wide ? launch_product<float, GATED, true>(a, s, c, x, K, st) : launch_product<float, GATED, false>(a, s, c, x, K, st)) return rc;
     auto finish = [&](auto t, uint32_t quads) {
         return launch_rows(a.rows, quads, [&](int row0, int rows, dim3 grid) {
-            hipLaunchKernelGGL((f8_finish_kernel<decltype(t), GATED>), grid, dim3(256), 0, st, p, make_div(quads), row0, rows);
+            hipLaunchKernelGGL((f8_finish_kernel<decltype(t), GATED>), grid, dim3(256), 0, st, a, make_div(quads), row0, rows);
         });
     };
-    if (y_type == CL_F8) return finish(F8Out{}, (uint32_t)blocks_of(a.width) * 32);
-    return with_type(y_type, [&](auto t) { return finish(t, (uint32_t)(a.width + 3) / 4); });
+    if (s.y_type == CL_F8) return finish(F8Out{}, (uint32_t)blocks_of(a.width) * 32);
+    return with_type(s.y_type, [&](auto t) { return finish(t, (uint32_t)(a.width + 3) / 4); });
 }
 
 static int32_t check_forward(const cl_f8_matrix *W, int32_t batch, int32_t x_type, int32_t y_type, int32_t act)
@@ -363,16 +347,77 @@ struct Scratch {
 
 static size_t part_pitch(int32_t width, bool gated) { return round_up(width, 4) * (gated ? 2 : 1); }
 
-static Scratch scratch_of(const Choice &c, const cl_f8_matrix &W, int32_t batch, int32_t x_type, int32_t y_type, int32_t act)
+static Scratch scratch_of(const Shape &s, const Choice &c, int32_t K)
 {
-    Scratch s;
-    if (x_type != CL_F8) {
-        s.x_values = s.take((size_t)batch * blocks_of(W.K) * kBlock);
-        s.x_scales = s.take((size_t)batch * scales_of(W.K) * 4);
+    Scratch at;
+    if (s.x_type != CL_F8 && !c.own) {
+        at.x_values = at.take((size_t)s.batch * s.blocks * kBlock);
+        at.x_scales = at.take((size_t)s.batch * scales_of(K) * 4);
     }
+    if (needs_parts(s, c)) at.parts = at.take((size_t)c.splits * s.batch * part_pitch(s.width, s.gated) * 4);
+    return at;
+}
+
+// What a form takes in microseconds, fitted to measurements of 700 shapes - 100 .. 4096 rows of W (gated: twice 100 .. 9216), K 100 .. 25088, 1 .. 4096 rows of X, outputs of
+// bf16 and of fp32 -: the choice then takes 1.2 % longer, in the mean of logarithms, than the best of up to thirteen.
+// Tiles: a start (launch, first loads, last stores), and per step of 128 k what a workgroup takes alone on its compute unit, or its share of a full one where the launch has more
+// workgroups than the chip has compute units; what each further workgroup of a compute unit adds.  256 x 256: one workgroup to a compute unit, whole rounds.
+struct Price { float start, alone, shared, more; };
+constexpr Price kPrices[2][4] = {{{}, {3.4f, 0.33f, 0.322f, 1.1f}, {4.0f, 0.545f, 0.644f, 2.2f}, {7.0f, 1.26f, 1.26f, 7.6f}},
+                                 {{}, {3.7f, 0.565f, 0.457f, 1.8f}, {4.9f, 1.05f, 1.27f, 6.6f}, {}}};
+// few_kernel: a start; per block of 128 k and 256 workgroups of rows of W and of X (from 0.6 or 0.7 of that on, which is as fast as a workgroup gets); what it quantises.
+struct FewPrice { float start, row, column, at_least, quantise; };
+constexpr FewPrice kFewPrices[2] = {{2.55f, 0.102f, 0.003f, 0.71f, 0.0015f}, {3.4f, 0.093f, 0.0134f, 0.59f, 0.003f}};      // X in 8 bits; in numbers
+// The quantisation of X, the sum of partial sums.  A launch costs the host, besides, some 4 us, which calls one by one pay, and calls recorded in a graph do not: half of it counts.
+constexpr float kLaunch = 2.0f;
+constexpr int32_t kFewMostRows = 256;                        // (beyond, tiles are always faster)
+
+static float price_of(const Shape &s, const Choice &c)
+{
+    const int64_t row_tiles = row_tiles_of(c.form, s.width, s.gated), columns = ((int64_t)s.batch + kFormSide[c.form] - 1) / kFormSide[c.form];
+    const float M = (float)s.width * (s.gated ? 2 : 1), n = (float)row_tiles * columns * c.splits / kCus;
+    float us;
+    if (c.form == kFew) {
+        const FewPrice &p = kFewPrices[c.own];
+        const int cols = std::min(s.batch, kFewColumns);
+        us = p.start + s.blocks * ((p.row * (s.gated ? 2 : 1) + p.column * cols) * std::max(n, p.at_least) + p.quantise * cols);
+    } else {
+        const Price &p = kPrices[s.wide][c.form];
+        const int fours = (s.blocks + 3) / 4, steps = std::min(s.blocks, (fours + c.splits - 1) / c.splits * 4);
+        if (c.form == kTile256) us = p.start + std::ceil(n) * p.alone * steps + p.more * (std::ceil(n) - 1);
+        else us = p.start + steps * std::max(p.alone, p.shared * n) + p.more * std::max(0.0f, n - 1);
+    }
+    if (s.x_type != CL_F8 && !c.own) us += 2.9f + kLaunch + 2.1e-7f * s.batch * s.blocks * kBlock * type_bytes(s.x_type);
+    if (needs_parts(s, c)) us += 1.9f + kLaunch + 0.85e-6f * (2 * c.splits + 1) * s.batch * M;
+    return us;
+}
+
+// The cheapest form whose scratch has at most `most` bytes; us < 0: there is none.  What one form needs for a batch is enough for the same form, not split, and a smaller batch: so
+// is what is asked for.
+static Choice choose(const Shape &s, int32_t K, size_t most)
+{
+    Choice best{kFew, 1, false, -1.0f};
+    auto offer = [&](Form form, int splits, bool own) {
+        Choice c{form, splits, own, 0.0f};
+        c.us = price_of(s, c);
+        if ((best.us < 0.0f || c.us < best.us) && scratch_of(s, c, K).bytes <= most) best = c;
+    };
+    if (s.batch <= kFewMostRows) {
+        offer(kFew, 1, false);
+        if (few_own(s)) offer(kFew, 1, true);
+    }
+    const int fours = (s.blocks + 3) / 4;
+    for (int form = kTile64; form <= (s.wide ? kTile128 : kTile256); ++form) {
+        const int64_t n = row_tiles_of((Form)form, s.width, s.gated) * (((int64_t)s.batch + kFormSide[form] - 1) / kFormSide[form]);
+        for (int splits = 1; splits <= 8 && splits <= fours && (splits == 1 || n * splits <= 4 * kCus); splits *= 2) offer((Form)form, splits, false);
+    }
+    return best;
+}
+
+static Shape shape_of(const cl_f8_matrix &W, int32_t batch, int32_t x_type, int32_t y_type, int32_t act)
+{
     const bool gated = act == CL_ACT_GATED;
-    if (c.splits > 1 || y_type == CL_F8) s.parts = s.take((size_t)c.splits * batch * part_pitch(gated ? W.rows / 2 : W.rows, gated) * 4);
-    return s;
+    return Shape{gated ? W.rows / 2 : W.rows, blocks_of(W.K), batch, gated, is_wide(x_type, y_type), x_type, y_type};
 }
 
 }  // namespace f8
@@ -385,55 +430,68 @@ extern "C" int32_t cl_eight_fc_workspace_bytes(const cl_f8_matrix *W, int32_t ba
 {
     if (!out) return fail(CL_EINVAL, "null pointer");
     if (int32_t rc = check_forward(W, batch, x_type, y_type, act)) return rc;
-    const int32_t width = act == CL_ACT_GATED ? W->rows / 2 : W->rows;
-    const bool gated = act == CL_ACT_GATED;
-    const Choice c = choose(width, blocks_of(W->K), batch, gated, y_type == CL_F32);
-    if (int32_t rc = check_grid(c, width, blocks_of(W->K), batch, gated)) return rc;
-    *out = scratch_of(c, *W, batch, x_type, y_type, act).bytes;
+    const Shape s = shape_of(*W, batch, x_type, y_type, act);
+    const Choice c = choose(s, W->K, SIZE_MAX);
+    if (int32_t rc = check_grid(c, s)) return rc;
+    *out = scratch_of(s, c, W->K).bytes;
+    clear_error();
+    return CL_OK;
+}
+
+static_assert(CL_F8_FORM_FEW == 1 + kFew && CL_F8_FORM_TILE_64 == 1 + kTile64 && CL_F8_FORM_TILE_256 == 1 + kTile256, "");
+
+extern "C" int32_t cl_eight_fc_resolved_form(const cl_f8_matrix *W, int32_t batch, int32_t x_type, int32_t y_type, int32_t act, int32_t *form, int32_t *splits)
+{
+    if (!form || !splits) return fail(CL_EINVAL, "null pointer");
+    if (int32_t rc = check_forward(W, batch, x_type, y_type, act)) return rc;
+    const Shape s = shape_of(*W, batch, x_type, y_type, act);
+    const Choice c = choose(s, W->K, SIZE_MAX);
+    if (int32_t rc = check_grid(c, s)) return rc;
+    *form = c.own ? CL_F8_FORM_FEW_NUMBERS : 1 + c.form;
+    *splits = c.splits;
     clear_error();
     return CL_OK;
 }
 
 extern "C" int32_t cl_eight_fc_forward(const cl_f8_matrix *W, const cl_f8_input *X, const float *d_bias, void *d_Y, float *d_y_scales, int32_t y_type, int32_t batch, int32_t act,
-                                    void *d_workspace, size_t workspace_bytes, void *stream)
+                                       void *d_workspace, size_t workspace_bytes, void *stream)
 {
     if (!X) return fail(CL_EINVAL, "null pointer");
     if (int32_t rc = check_forward(W, batch, X->type, y_type, act)) return rc;
     if (batch == 0) return CL_OK;
     if (int32_t rc = check_pointers(W, X, d_Y, d_y_scales, y_type, batch)) return rc;
     hipStream_t st = (hipStream_t)stream;
-    const bool gated = act == CL_ACT_GATED;
+    const Shape s = shape_of(*W, batch, X->type, y_type, act);
+    const Choice c = choose(s, W->K, d_workspace ? workspace_bytes : 0);
+    if (c.us < 0.0f) return fail(CL_EINVAL, "workspace needs %zu bytes, got %zu", scratch_of(s, choose(s, W->K, SIZE_MAX), W->K).bytes, d_workspace ? workspace_bytes : 0);
+    if (int32_t rc = check_grid(c, s)) return rc;
+    const Scratch at = scratch_of(s, c, W->K);
+    if (at.bytes && !aligned(d_workspace, 256)) return fail(CL_EINVAL, "workspace must be 256-byte aligned");
+    uint8_t *ws = (uint8_t *)d_workspace;
     ProductArgs a{};
     a.w = (const uint8_t *)W->d_values;
     a.w_scales = W->d_scales;
     a.bias = d_bias;
     a.Y = d_Y;
     a.y_scales = d_y_scales;
-    a.blocks = blocks_of(W->K);
+    a.blocks = s.blocks;
     a.pitch_scales = scales_of(W->K);
-    a.width = gated ? W->rows / 2 : W->rows;
+    a.width = s.width;
     a.rows = batch;
     a.act = act;
-    a.value_tall = (a.width + kBlock - 1) / kBlock;
-    const Choice c = choose(a.width, a.blocks, batch, gated, y_type == CL_F32);
-    if (int32_t rc = check_grid(c, a.width, a.blocks, batch, gated)) return rc;
-    const Scratch s = scratch_of(c, *W, batch, X->type, y_type, act);
-    if (s.bytes && !d_workspace) return fail(CL_EINVAL, "null workspace");
-    if (workspace_bytes < s.bytes) return fail(CL_EINVAL, "workspace needs %zu bytes, got %zu", s.bytes, workspace_bytes);
-    if (s.bytes && !aligned(d_workspace, 256)) return fail(CL_EINVAL, "workspace must be 256-byte aligned");
-    uint8_t *ws = (uint8_t *)d_workspace;
+    a.value_tall = (s.width + kBlock - 1) / kBlock;
     if (X->type == CL_F8) {
         a.x = (const uint8_t *)X->d_X;
         a.x_scales = X->d_scales;
-    } else {
-        a.x = ws + s.x_values;
-        a.x_scales = (const float *)(ws + s.x_scales);
-        if (int32_t rc = launch_rows_to_f8(X->d_X, X->type, X->stride, batch, W->K, ws + s.x_values, (float *)(ws + s.x_scales), st)) return rc;
+    } else if (!c.own) {
+        a.x = ws + at.x_values;
+        a.x_scales = (const float *)(ws + at.x_scales);
+        if (int32_t rc = launch_rows_to_f8(X->d_X, X->type, X->stride, batch, W->K, ws + at.x_values, (float *)(ws + at.x_scales), st)) return rc;
     }
-    if (c.splits > 1 || y_type == CL_F8) a.part = (float *)(ws + s.parts);
-    a.pitch = (int)part_pitch(a.width, gated);
-    a.value_at = (int)round_up(a.width, 4);
-    if (int32_t rc = gated ? run_product<true>(a, c, y_type, st) : run_product<false>(a, c, y_type, st)) return rc;
+    if (needs_parts(s, c)) a.part = (float *)(ws + at.parts);
+    a.pitch = (int)part_pitch(s.width, s.gated);
+    a.value_at = (int)round_up(s.width, 4);
+    if (int32_t rc = s.gated ? run_product<true>(a, s, c, *X, W->K, st) : run_product<false>(a, s, c, *X, W->K, st)) return rc;
     clear_error();
     return CL_OK;
 }

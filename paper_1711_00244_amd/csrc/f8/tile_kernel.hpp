@@ -35,7 +35,7 @@ template <int BM, int BN, int WM, int WN, int D> struct Tile {
     static constexpr int kBuffer = (BM + BN) * kBlock;
     static constexpr int kScales = D * kBuffer;              // where the scales start: D buffers of four steps
     static constexpr int kScaleBuffer = (BN + 64) * 16;
-    static constexpr int kLds = kScales + D * kScaleBuffer;
+    static constexpr int kLds = kScales + D * kScaleBuffer, kTops = 2 * BN * 4;      // (8-bit outputs: the largest of each column, of two wavefronts)
     static_assert(TI % R == 0 && TI % 2 == 0 && TI > 0 && TJ > 0 && 128 % kRun == 0, "");
     static_assert(BM % (8 * kWaves) == 0 && BN % (8 * kWaves) == 0 && kRun % 8 == 0 && BN % 64 == 0 && 2 * WM <= 64, "");
     static_assert(D == 2 || D == 4, "");
@@ -61,6 +61,14 @@ __device__ __forceinline__ u32x4 eight_outputs(u32x2 first, u32x2 second)
 {
     const auto a = __builtin_amdgcn_permlane16_swap(first[0], second[0], false, false), b = __builtin_amdgcn_permlane16_swap(first[1], second[1], false, false);
     return u32x4{(uint32_t)a[0], (uint32_t)b[0], (uint32_t)a[1], (uint32_t)b[1]};
+}
+
+// The same for 8-bit outputs of four pieces, so that a lane has sixteen consecutive ones, lanes of sixteen n those of piece n.
+__device__ __forceinline__ u32x4 sixteen_outputs(const uint32_t *q)
+{
+    const auto a = __builtin_amdgcn_permlane16_swap(q[0], q[1], false, false), b = __builtin_amdgcn_permlane16_swap(q[2], q[3], false, false);
+    const auto c = __builtin_amdgcn_permlane32_swap(a[0], b[0], false, false), d = __builtin_amdgcn_permlane32_swap(a[1], b[1], false, false);
+    return u32x4{(uint32_t)c[0], (uint32_t)d[0], (uint32_t)c[1], (uint32_t)d[1]};
 }
 
 template <int BM, int BN, int WM, int WN, int D, class T, bool GATED, bool WIDE>
@@ -290,6 +298,63 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void f8_tile_kernel(ProductArgs a,
                 for (int j = 0; j < TJ; ++j)
                     if (c_first + j * 16 < a.rows) store_part(a, split, c_first + j * 16, o, acc[i][j], h * a.value_at);
             }
+        } else if constexpr (std::is_same_v<T, F8Out>) {
+            // A block of 128 outputs is a wavefront's, or two wavefronts' that share their columns.
+            static_assert(kWide == 128 || (kWide == 64 && WM == 2), "");
+            float *tops = (float *)(lds + C::kLds);          // [wm][column]
+            uint32_t top[TJ];
+#pragma unroll
+            for (int j = 0; j < TJ; ++j) {
+                top[j] = 0;
+#pragma unroll
+                for (int i = 0; i < kPieces; ++i) {
+                    const int o = first + i * 16 + 4 * g;
+                    f32x4 v = activated<GATED>(a, o, acc[i][j], acc[GATED ? kPieces + i : i][j]);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        v[e] = o + e < a.width ? v[e] : 0.0f;
+                        top[j] = max(top[j], __float_as_uint(v[e]) & 0x7fffffffu);
+                    }
+                    acc[i][j] = v;
+                }
+                top[j] = max(top[j], (uint32_t)__shfl_xor((int)top[j], 16));
+                top[j] = max(top[j], (uint32_t)__shfl_xor((int)top[j], 32));
+                if (kWide == 64 && g == 0) tops[wm * BN + wn * TJ * 16 + j * 16 + r] = __uint_as_float(top[j]);
+            }
+            if (kWide == 64) {
+                // (before these are written again come the barriers of the next tile's steps)
+                __builtin_amdgcn_s_waitcnt(kWaitLds);
+                asm volatile("" ::: "memory");
+                __builtin_amdgcn_s_barrier();
+                asm volatile("" ::: "memory");
+#pragma unroll
+                for (int j = 0; j < TJ; ++j) top[j] = max(top[j], __float_as_uint(tops[(1 - wm) * BN + wn * TJ * 16 + j * 16 + r]));
+            }
+            const int y_blocks = (a.width + kBlock - 1) / kBlock, y_pitch = (y_blocks + 3) / 4 * 4;
+#pragma unroll
+            for (int j = 0; j < TJ; ++j) {
+                const int64_t c = c_first + j * 16;
+                const Scale s = scale_of(top[j]);
+#pragma unroll
+                for (int i = 0; i < kPieces; i += 4) {
+                    uint32_t q[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float v[4] = {acc[i + e][j][0], acc[i + e][j][1], acc[i + e][j][2], acc[i + e][j][3]};
+                        q[e] = to_f8(v, s.inverse);
+                    }
+                    const u32x4 sixteen = sixteen_outputs(q);
+                    const int o = first + (i + g) * 16;
+                    if (c < a.rows && o < y_blocks * kBlock) *(u32x4 *)((uint8_t *)a.Y + c * y_blocks * kBlock + o) = sixteen;
+                }
+                if (c < a.rows && g == 0 && (kWide == 128 || wm == 0) && first < a.width) {
+                    const int b = first / kBlock;
+                    float *to = a.y_scales + c * y_pitch;
+                    to[b] = s.scale;
+                    if (b == y_blocks - 1)
+                        for (int i = y_blocks; i < y_pitch; ++i) to[i] = 0.0f;
+                }
+            }
         } else if constexpr (sizeof(T) == 2 && kPieces % 2 == 0) {
 #pragma unroll
             for (int i = 0; i < kPieces; i += 2) {
@@ -316,7 +381,7 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void f8_tile_kernel(ProductArgs a,
                     }
                 }
             }
-        } else {
+        } else if constexpr (!std::is_same_v<T, F8Out>) {
 #pragma unroll
             for (int i = 0; i < kPieces; ++i) {
                 const int o = first + i * 16 + 4 * g;
