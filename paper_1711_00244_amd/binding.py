@@ -948,11 +948,12 @@ class F8Tensor:
         return self.values.device
 
 
-def _f8_empty(lead, K, block_rows, device):
+def _f8_empty(like, lead, K, block_rows):
+    """Room for rows of K elements, on the device of `like`."""
     import torch
     q = F8Tensor.__new__(F8Tensor)
-    q.values = torch.empty(tuple(lead) + ((K + 127) // 128 * 128,), dtype=torch.float8_e4m3fn, device=device)
-    q.scales = torch.empty((tuple(lead) if block_rows == 1 else (-(-lead[0] // 128),)) + ((K + 511) // 512 * 4,), dtype=torch.float32, device=device)
+    q.values = like.new_empty(lead + ((K + 127) // 128 * 128,), dtype=torch.float8_e4m3fn)
+    q.scales = like.new_empty((lead if block_rows == 1 else (-(-lead[0] // 128),)) + ((K + 511) // 512 * 4,), dtype=torch.float32)
     q.K, q.block_rows, q.gated = K, block_rows, False
     return q
 
@@ -969,7 +970,7 @@ def f8_quantize(X, block_rows: int = 1, out: F8Tensor | None = None) -> F8Tensor
     _int32(K, block_rows)
     if out is None:
         f8_row_blocks(K)
-        out = _f8_empty(lead, K, block_rows, X.device)
+        out = _f8_empty(X, tuple(lead), K, block_rows)
     elif out.shape != tuple(shape) or out.block_rows != block_rows or out.gated:
         raise ValueError(f"out must hold {tuple(shape)} in blocks of {block_rows} rows, holds {out.shape} in blocks of {out.block_rows}{', gated' if out.gated else ''}")
     stream = _on(X.device, out.values)
@@ -1020,54 +1021,52 @@ def rms_norm(X, gain=None, eps: float = 1e-6, residual=None, dtype=None, out=Non
     shape = X.shape
     K = shape[-1]
     flat = len(shape) != 2
+    dt = X.dtype
 
-    def rows_of(t, what):
-        if tuple(t.shape) != tuple(shape):
+    def matrix(t, what):
+        """t, of X's shape, as rows that are read or written -> (address, distance)"""
+        if t.shape != shape:
             raise ValueError(f"{what} must be {tuple(shape)}, got {tuple(t.shape)}")
-        return t.view(-1, K) if flat else t
+        if flat:
+            t = t.view(-1, K)
+        return t.data_ptr(), _rows(t, what)[1]
 
     x = X.reshape(-1, K) if flat else X
     ty, x_stride = _rows(x, "X")
-    rows = x.shape[0]
     _int32(K)
-    device = X.device
-    call = NormCall(x.data_ptr(), x_stride=x_stride, rows=rows, K=K, type=ty, eps=eps)
+    call = NormCall(x.data_ptr(), x_stride=x_stride, rows=x.shape[0], K=K, type=ty, eps=eps)
+    total = None
     if residual is not None:
-        res = residual.reshape(-1, K) if flat and tuple(residual.shape) == tuple(shape) else rows_of(residual, "residual")
-        total = torch.empty(shape, dtype=X.dtype, device=device) if sum_out is None else sum_out
-        t = rows_of(total, "sum_out")
-        if residual.dtype != X.dtype or total.dtype != X.dtype:
-            raise ValueError(f"residual and sum_out must be {X.dtype}, got {residual.dtype} and {total.dtype}")
-        call.d_residual, call.residual_stride = res.data_ptr(), _rows(res, "residual")[1]
-        call.d_sum, call.sum_stride = t.data_ptr(), _rows(t, "sum_out")[1]
-    else:
-        total = None
-        if sum_out is not None:
-            raise ValueError("sum_out without a residual")
+        total = torch.empty_like(X, memory_format=torch.contiguous_format) if sum_out is None else sum_out
+        if residual.dtype != dt or total.dtype != dt:
+            raise ValueError(f"residual and sum_out must be {dt}, got {residual.dtype} and {total.dtype}")
+        if flat:
+            residual = residual.contiguous()
+        call.d_residual, call.residual_stride = matrix(residual, "residual")
+        call.d_sum, call.sum_stride = matrix(total, "sum_out")
+    elif sum_out is not None:
+        raise ValueError("sum_out without a residual")
     if gain is not None:
-        if tuple(gain.shape) != (K,) or not gain.is_contiguous() or gain.dtype not in (torch.float32, X.dtype):
-            raise ValueError(f"gain must be ({K},), contiguous, float32 or {X.dtype}, got {gain.dtype} {tuple(gain.shape)}")
-        call.d_gain, call.gain_type = gain.data_ptr(), _element_type(gain.dtype, "gain")
-    if isinstance(out, F8Tensor):
-        if dtype not in (None, torch.float8_e4m3fn) or out.shape != tuple(shape) or out.block_rows != 1:
-            raise ValueError(f"out must hold {tuple(shape)} in blocks of one row, of dtype {dtype}")
-        y_type = F8
-    else:
-        y_type = _f8_type(dtype or (X.dtype if out is None else out.dtype), "out")
+        if gain.shape != (K,) or not gain.is_contiguous() or gain.dtype not in (torch.float32, dt):
+            raise ValueError(f"gain must be ({K},), contiguous, float32 or {dt}, got {gain.dtype} {tuple(gain.shape)}")
+        call.d_gain, call.gain_type = gain.data_ptr(), _types[gain.dtype]
+    if dtype == torch.float8_e4m3fn or isinstance(out, F8Tensor):
         if out is None:
             f8_row_blocks(K)
-            out = _f8_empty(shape[:-1], K, 1, device) if y_type == F8 else torch.empty(shape, dtype=dtype or X.dtype, device=device)
-        elif y_type == F8 or out.dtype != (dtype or out.dtype):
-            raise ValueError(f"out must be {'an F8Tensor' if y_type == F8 else f'of {dtype}'}")
-    call.y_type = y_type
-    if y_type == F8:
-        stream = _on(device, residual, total, gain, out.values)
-        call.d_Y, call.d_y_scales = out.values.data_ptr(), out.scales.data_ptr()
+            out = _f8_empty(X, tuple(shape[:-1]), K, 1)
+        elif not isinstance(out, F8Tensor) or dtype not in (None, torch.float8_e4m3fn) or out.shape != tuple(shape) or out.block_rows != 1:
+            raise ValueError(f"out must be an F8Tensor of {tuple(shape)} in blocks of one row")
+        y = out.values
+        call.d_Y, call.d_y_scales, call.y_type = y.data_ptr(), out.scales.data_ptr(), F8
     else:
-        y = rows_of(out, "out")
-        call.d_Y, call.y_stride = y.data_ptr(), _rows(y, "out")[1]
-        stream = _on(device, residual, total, gain, out)
-    _check(L.cl_rms_norm(call, stream))
+        if out is None:
+            out = torch.empty_like(X, dtype=dtype, memory_format=torch.contiguous_format)
+        elif dtype not in (None, out.dtype):
+            raise ValueError(f"out must be of {dtype}, got {out.dtype}")
+        y = out
+        call.y_type = _element_type(out.dtype, "out")
+        call.d_Y, call.y_stride = matrix(out, "out")
+    _check(L.cl_rms_norm(call, _on(X.device, residual, total, gain, y)))
     return out if total is None else (out, total)
 
 
@@ -1124,7 +1123,7 @@ def f8_fc_forward(W: F8Tensor, X, bias=None, act=None, dtype=None, out=None, wor
     device = X.device
     if dtype == torch.float8_e4m3fn or isinstance(out, F8Tensor):
         if out is None:
-            out = _f8_empty((B,), width, 1, device)
+            out = _f8_empty(values, (B,), width, 1)
         elif not isinstance(out, F8Tensor) or dtype not in (None, torch.float8_e4m3fn) or out.shape != (B, width) or out.block_rows != 1:
             raise ValueError(f"out must be an F8Tensor of ({B}, {width}) in blocks of one row")
         y, y_scales, y_type = out.values, out.scales.data_ptr(), F8
