@@ -209,12 +209,11 @@ static bool ends_in_f8(const Shape &s, const Choice &c) { return s.y_type == CL_
 static bool needs_parts(const Shape &s, const Choice &c) { return c.splits > 1 || (s.y_type == CL_F8 && !ends_in_f8(s, c)); }
 
 // Whether the launch has less than 2^32 threads along each axis.
-static int32_t check_grid(const Choice &c, const Shape &s)
+static bool fits_grid(const Choice &c, const Shape &s)
 {
     const int64_t row_tiles = row_tiles_of(c.form, s.width, s.gated), columns = ((int64_t)s.batch + kFormSide[c.form] - 1) / kFormSide[c.form];
     const int64_t wgs = c.form == kFew ? row_tiles : (int64_t)round_up(row_tiles * columns, 8), threads = c.form == kFew ? few_threads(s, c.own) : kFormThreads[c.form];
-    if (wgs > (int64_t)UINT32_MAX / threads || wgs > INT_MAX) return fail(CL_EUNSUPPORTED, "a launch of %lld workgroups does not fit a grid", (long long)wgs);
-    return CL_OK;
+    return wgs <= (int64_t)UINT32_MAX / threads;
 }
 
 template <Form F, int WM, int WN, int D, class T, bool GATED, bool WIDE> static int32_t launch_tiles(ProductArgs a, const Choice &c, hipStream_t st)
@@ -384,7 +383,8 @@ static float price_of(const Shape &s, const Choice &c)
     } else {
         const Price &p = kPrices[s.wide][c.form];
         const int fours = (s.blocks + 3) / 4, steps = std::min(s.blocks, (fours + c.splits - 1) / c.splits * 4);
-        if (c.form == kTile256) us = p.start + std::ceil(n) * p.alone * steps + p.more * (std::ceil(n) - 1);
+        const float rounds = std::max(1.0f, std::ceil(n));
+        if (c.form == kTile256) us = p.start + rounds * p.alone * steps + p.more * (rounds - 1);
         else us = p.start + steps * std::max(p.alone, p.shared * n) + p.more * std::max(0.0f, n - 1);
     }
     if (s.x_type != CL_F8 && !c.own) us += 2.9f + kLaunch + 2.1e-7f * s.batch * s.blocks * kBlock * type_bytes(s.x_type);
@@ -392,7 +392,7 @@ static float price_of(const Shape &s, const Choice &c)
     return us;
 }
 
-// The cheapest form whose scratch has at most `most` bytes; us < 0: there is none.  What one form needs for a batch is enough for the same form, not split, and a smaller batch: so
+// The cheapest form that fits a grid and whose scratch has at most `most` bytes; us < 0: there is none.  What one form needs for a batch is enough for the same form, not split, and a smaller batch: so
 // is what is asked for.
 static Choice choose(const Shape &s, int32_t K, size_t most)
 {
@@ -400,7 +400,7 @@ static Choice choose(const Shape &s, int32_t K, size_t most)
     auto offer = [&](Form form, int splits, bool own) {
         Choice c{form, splits, own, 0.0f};
         c.us = price_of(s, c);
-        if ((best.us < 0.0f || c.us < best.us) && scratch_of(s, c, K).bytes <= most) best = c;
+        if ((best.us < 0.0f || c.us < best.us) && fits_grid(c, s) && scratch_of(s, c, K).bytes <= most) best = c;
     };
     if (s.batch <= kFewMostRows) {
         offer(kFew, 1, false);
@@ -413,6 +413,8 @@ static Choice choose(const Shape &s, int32_t K, size_t most)
     }
     return best;
 }
+
+static int32_t fail_with_grid(const Shape &s) { return fail(CL_EUNSUPPORTED, "%d rows of %d outputs do not fit a grid", (int)s.batch, (int)s.width); }
 
 static Shape shape_of(const cl_f8_matrix &W, int32_t batch, int32_t x_type, int32_t y_type, int32_t act)
 {
@@ -432,7 +434,7 @@ extern "C" int32_t cl_eight_fc_workspace_bytes(const cl_f8_matrix *W, int32_t ba
     if (int32_t rc = check_forward(W, batch, x_type, y_type, act)) return rc;
     const Shape s = shape_of(*W, batch, x_type, y_type, act);
     const Choice c = choose(s, W->K, SIZE_MAX);
-    if (int32_t rc = check_grid(c, s)) return rc;
+    if (c.us < 0.0f) return fail_with_grid(s);
     *out = scratch_of(s, c, W->K).bytes;
     clear_error();
     return CL_OK;
@@ -446,7 +448,7 @@ extern "C" int32_t cl_eight_fc_resolved_form(const cl_f8_matrix *W, int32_t batc
     if (int32_t rc = check_forward(W, batch, x_type, y_type, act)) return rc;
     const Shape s = shape_of(*W, batch, x_type, y_type, act);
     const Choice c = choose(s, W->K, SIZE_MAX);
-    if (int32_t rc = check_grid(c, s)) return rc;
+    if (c.us < 0.0f) return fail_with_grid(s);
     *form = c.own ? CL_F8_FORM_FEW_NUMBERS : 1 + c.form;
     *splits = c.splits;
     clear_error();
@@ -463,8 +465,11 @@ extern "C" int32_t cl_eight_fc_forward(const cl_f8_matrix *W, const cl_f8_input 
     hipStream_t st = (hipStream_t)stream;
     const Shape s = shape_of(*W, batch, X->type, y_type, act);
     const Choice c = choose(s, W->K, d_workspace ? workspace_bytes : 0);
-    if (c.us < 0.0f) return fail(CL_EINVAL, "workspace needs %zu bytes, got %zu", scratch_of(s, choose(s, W->K, SIZE_MAX), W->K).bytes, d_workspace ? workspace_bytes : 0);
-    if (int32_t rc = check_grid(c, s)) return rc;
+    if (c.us < 0.0f) {
+        const Choice any = choose(s, W->K, SIZE_MAX);
+        if (any.us < 0.0f) return fail_with_grid(s);
+        return fail(CL_EINVAL, "workspace needs %zu bytes, got %zu", scratch_of(s, any, W->K).bytes, d_workspace ? workspace_bytes : 0);
+    }
     const Scratch at = scratch_of(s, c, W->K);
     if (at.bytes && !aligned(d_workspace, 256)) return fail(CL_EINVAL, "workspace must be 256-byte aligned");
     uint8_t *ws = (uint8_t *)d_workspace;

@@ -7,7 +7,8 @@ the experts are gated two-matrix networks in 4-bit blocks.  One call is
     hidden = mx_experts_forward(up, X, chosen, act="gated")         a row per pair
     Y = mx_experts_forward(down, hidden, chosen, weights, ...)      a row per token
 
-and, where there is a shared expert, mx_fc_forward of its two matrices on X, quantised once for the shared expert and the routed ones.
+and, where there is a shared expert, mx_fc_forward of its two matrices on X, quantised once for the shared expert and the routed ones.  A shared expert, which every
+token goes through, may be in 8 bits instead (f8_fc_forward).
 Host-side control only: the work is in the library's kernels, on the caller's current stream, and nothing is read back, so that a call can be
 recorded in a graph.
 
@@ -21,6 +22,7 @@ import json
 import numpy as np
 
 from . import binding as cl
+from . import feed_forward
 from . import workloads as wl
 
 SHARED_QUANTISE_TOKENS = 64      # below, each product quantises X itself: the few rows of those that are one launch, in that launch
@@ -28,8 +30,8 @@ SHARED_QUANTISE_TOKENS = 64      # below, each product quantises X itself: the f
 
 class ExpertLayer:
     """router: a compressed layer of (experts, width); up: MxTensor (experts, 2 hidden, width), rows 2 i and 2 i + 1 gate and value of hidden
-    unit i; down: MxTensor (experts, width, hidden); shared: None or (MxTensor (2 h, width), MxTensor (width, h)).  routing: keyword
-    arguments of route_experts."""
+    unit i; down: MxTensor (experts, width, hidden); shared: None or (MxTensor (2 h, width), MxTensor (width, h)), or two F8Tensors of these shapes, the
+    first as f8_gated makes it.  routing: keyword arguments of route_experts."""
 
     def __init__(self, router: cl.Layer, up: cl.MxTensor, down: cl.MxTensor, k: int, shared=None, **routing):
         experts, two_hidden, width = up.shape
@@ -39,6 +41,8 @@ class ExpertLayer:
             raise ValueError(f"up {up.shape} and down {down.shape} are not the matrices of gated experts")
         if shared is not None:
             first, second = shared
+            if isinstance(first, cl.F8Tensor):
+                feed_forward.check_gated(first, second)
             if len(first.shape) != 2 or first.K != width or first.shape[0] % 2 or second.shape != (width, first.shape[0] // 2):
                 raise ValueError(f"{first.shape} and {second.shape} are not the matrices of a gated expert of width {width}")
         self.router, self.up, self.down, self.k, self.shared, self.routing = router, up, down, k, shared, routing
@@ -53,14 +57,17 @@ class ExpertLayer:
         if X.shape[0] == 0:
             return X.new_empty((0, self.width))              # (a compressed layer takes no empty batch)
         experts, weights = self.route(X)
-        x = cl.mx_quantize(X) if self.shared is not None and X.shape[0] >= SHARED_QUANTISE_TOKENS else X
+        eight = self.shared is not None and isinstance(self.shared[0], cl.F8Tensor)
+        x = cl.mx_quantize(X) if self.shared is not None and not eight and X.shape[0] >= SHARED_QUANTISE_TOKENS else X
         # (of the default layer up to 15 tokens.  One token, calls recorded in a graph: 29 us, with lists 37; called one by one 63, with lists 80)
         one_launch = ("few" == cl.mx_experts_resolved_form(self.up, X.shape[0], self.k, None if x is not X else X.dtype, weighted=False)
                       == cl.mx_experts_resolved_form(self.down, X.shape[0], self.k, X.dtype, x_per_pair=True))
         lists = None if one_launch else cl.expert_lists(experts, self.experts)
         hidden = cl.mx_experts_forward(self.up, x, experts, act="gated", lists=lists, dtype=X.dtype)
         Y = cl.mx_experts_forward(self.down, hidden, experts, weights, x_per_pair=True, lists=lists)
-        if self.shared is not None:
+        if eight:
+            Y += feed_forward.gated_product(*self.shared, X, X.dtype)
+        elif self.shared is not None:
             first, second = self.shared
             Y += cl.mx_fc_forward(second, cl.mx_fc_forward(first, x, act="gated", dtype=X.dtype))
         return Y
