@@ -124,6 +124,7 @@ __device__ __forceinline__ void store_part(const ProductArgs &a, int split, int6
 
 #include "few_kernel.hpp"
 #include "tile_kernel.hpp"
+#include "small_tile_kernel.hpp"
 
 // The sum over the splits of a product's parts, in order, and from it four outputs of one row.  8-bit outputs: 32 lanes have a block.
 template <class T, bool GATED> __global__ __launch_bounds__(256) void f8_finish_kernel(ProductArgs a, Div quads, int row0, int rows)
@@ -168,7 +169,8 @@ template <class T, bool GATED> __global__ __launch_bounds__(256) void f8_finish_
 // ------------------------------------------------------------------------- //
 constexpr int kCus = 256;
 enum Form { kFew, kTile64, kTile128, kTile256 };
-constexpr int kFormSide[] = {16, 64, 128, 256}, kFormThreads[] = {0, 256, 512, 512};        // of a workgroup: rows of W and of X, threads (kFew: as few_threads says)
+constexpr int kFormRows[] = {16, 64, 128, 256}, kFormThreads[] = {0, 256, 512, 512};        // of a workgroup: rows of W; threads (kFew: as many as few_threads says)
+constexpr int form_columns(Form form, bool wide) { return form == kTile256 && wide ? 128 : kFormRows[form]; }      // rows of X
 
 // A call, by what the choice of a kernel depends on.
 struct Shape {
@@ -200,32 +202,38 @@ static int few_threads(const Shape &s, bool own)
 
 static int64_t row_tiles_of(Form form, int32_t width, bool gated)
 {
-    const int64_t outputs = form == kFew || !gated ? kFormSide[form] : kFormSide[form] / 2;
+    const int64_t outputs = form == kFew || !gated ? kFormRows[form] : kFormRows[form] / 2;
     return (width + outputs - 1) / outputs;
 }
 
+static int64_t columns_of(Form form, int64_t rows, bool wide) { return (rows + form_columns(form, wide) - 1) / form_columns(form, wide); }
+
 // Whether 8-bit outputs are made where the product ends: where a workgroup has all 128 of a block.
-static bool ends_in_f8(const Shape &s, const Choice &c) { return s.y_type == CL_F8 && c.splits == 1 && (c.form == kTile256 || (c.form == kTile128 && !s.gated)); }
+static bool ends_in_f8(const Shape &s, const Choice &c) { return s.y_type == CL_F8 && c.splits == 1 && ((c.form == kTile256 && !s.wide) || (c.form == kTile128 && !s.gated)); }
 static bool needs_parts(const Shape &s, const Choice &c) { return c.splits > 1 || (s.y_type == CL_F8 && !ends_in_f8(s, c)); }
 
 // Whether the launch has less than 2^32 threads along each axis.
 static bool fits_grid(const Choice &c, const Shape &s)
 {
-    const int64_t row_tiles = row_tiles_of(c.form, s.width, s.gated), columns = ((int64_t)s.batch + kFormSide[c.form] - 1) / kFormSide[c.form];
+    const int64_t row_tiles = row_tiles_of(c.form, s.width, s.gated), columns = columns_of(c.form, s.batch, s.wide);
     const int64_t wgs = c.form == kFew ? row_tiles : (int64_t)round_up(row_tiles * columns, 8), threads = c.form == kFew ? few_threads(s, c.own) : kFormThreads[c.form];
     return wgs <= (int64_t)UINT32_MAX / threads;
 }
 
-template <Form F, int WM, int WN, int D, class T, bool GATED, bool WIDE> static int32_t launch_tiles(ProductArgs a, const Choice &c, hipStream_t st)
+template <Form F, class T, bool GATED, bool WIDE> static int32_t launch_tiles(ProductArgs a, const Choice &c, hipStream_t st)
 {
-    constexpr int SIDE = kFormSide[F];
-    using C = Tile<SIDE, SIDE, WM, WN, D>;
+    using C = std::conditional_t<F == kTile256, std::conditional_t<WIDE, Tile<256, 128, 4, 2, 2>, Tile<256, 256, 2, 4, 2>>,
+                                 std::conditional_t<F == kTile128, SmallTile<128, 128, 2, 4, 4>, SmallTile<64, 64, 2, 2, 4>>>;
     static_assert(C::kThreads == kFormThreads[F], "");
     constexpr size_t kLds = C::kLds + (std::is_same_v<T, F8Out> ? C::kTops : 0);
-    auto kernel = f8_tile_kernel<SIDE, SIDE, WM, WN, D, T, GATED, WIDE>;
+    void (*kernel)(ProductArgs, int);
+    if constexpr (F == kTile256 && WIDE) kernel = f8_tile_kernel<256, 128, 4, 2, 2, T, GATED, WIDE>;
+    else if constexpr (F == kTile256) kernel = f8_tile_kernel<256, 256, 2, 4, 2, T, GATED, WIDE>;
+    else if constexpr (F == kTile128) kernel = f8_small_tile_kernel<128, 128, 2, 4, 4, 2, T, GATED, WIDE>;
+    else kernel = f8_small_tile_kernel<64, 64, 2, 2, 4, 2, T, GATED, WIDE>;
     static LdsLimit seen;
     if (int32_t rc = allow_lds((const void *)kernel, kLds, seen)) return rc;
-    const int64_t row_tiles = row_tiles_of(F, a.width, GATED), columns = ((int64_t)a.rows + SIDE - 1) / SIDE;
+    const int64_t row_tiles = row_tiles_of(F, a.width, GATED), columns = columns_of(F, a.rows, WIDE);
     a.row_tiles = make_div((uint32_t)row_tiles);
     a.band_tiles = make_div((uint32_t)row_tiles * 4u);
     const int fours = (a.blocks + 3) / 4;
@@ -262,10 +270,9 @@ template <class X, class T, bool GATED, bool WIDE> static int32_t launch_few(con
 template <class T, bool GATED, bool WIDE> static int32_t launch_product(const ProductArgs &a, const Shape &s, const Choice &c, const cl_f8_input &x, int32_t K, hipStream_t st)
 {
     switch (c.form) {
-    case kTile64: return launch_tiles<kTile64, 2, 2, 4, T, GATED, WIDE>(a, c, st);
-    case kTile128: return launch_tiles<kTile128, 2, 4, 2, T, GATED, WIDE>(a, c, st);
-    case kTile256:
-        if constexpr (!WIDE) return launch_tiles<kTile256, 2, 4, 2, T, GATED, false>(a, c, st);
+    case kTile64: return launch_tiles<kTile64, T, GATED, WIDE>(a, c, st);
+    case kTile128: return launch_tiles<kTile128, T, GATED, WIDE>(a, c, st);
+    case kTile256: return launch_tiles<kTile256, T, GATED, WIDE>(a, c, st);
     default: break;
     }
     if (!c.own) return launch_few<F8In, T, GATED, WIDE>(a, s, x, K, st);
@@ -291,8 +298,8 @@ template <bool GATED> static int32_t run_product(ProductArgs a, const Shape &s, 
         if (s.y_type == CL_F32) return launch_product<float, GATED, true>(a, s, c, x, K, st);
         if (s.y_type == CL_BF16) return launch_product<bf16_t, GATED, false>(a, s, c, x, K, st);
         if (s.y_type == CL_F16) return launch_product<f16_t, GATED, false>(a, s, c, x, K, st);
-        if (c.form == kTile256) return launch_tiles<kTile256, 2, 4, 2, F8Out, GATED, false>(a, c, st);
-        if constexpr (!GATED) return s.wide ? launch_tiles<kTile128, 2, 4, 2, F8Out, false, true>(a, c, st) : launch_tiles<kTile128, 2, 4, 2, F8Out, false, false>(a, c, st);
+        if (c.form == kTile256) return launch_tiles<kTile256, F8Out, GATED, false>(a, c, st);
+        if constexpr (!GATED) return s.wide ? launch_tiles<kTile128, F8Out, false, true>(a, c, st) : launch_tiles<kTile128, F8Out, false, false>(a, c, st);
     }
     if (int32_t rc = s.wide ? launch_product<float, GATED, true>(a, s, c, x, K, st) : launch_product<float, GATED, false>(a, s, c, x, K, st)) return rc;
     auto finish = [&](auto t, uint32_t quads) {
@@ -357,23 +364,24 @@ static Scratch scratch_of(const Shape &s, const Choice &c, int32_t K)
     return at;
 }
 
-// What a form takes in microseconds, fitted to measurements of 700 shapes - 100 .. 4096 rows of W (gated: twice 100 .. 9216), K 100 .. 25088, 1 .. 4096 rows of X, outputs of
-// bf16 and of fp32 -: the choice then takes 1.2 % longer, in the mean of logarithms, than the best of up to thirteen.
-// Tiles: a start (launch, first loads, last stores), and per step of 128 k what a workgroup takes alone on its compute unit, or its share of a full one where the launch has more
-// workgroups than the chip has compute units; what each further workgroup of a compute unit adds.  256 x 256: one workgroup to a compute unit, whole rounds.
-struct Price { float start, alone, shared, more; };
-constexpr Price kPrices[2][4] = {{{}, {3.4f, 0.33f, 0.322f, 1.1f}, {4.0f, 0.545f, 0.644f, 2.2f}, {7.0f, 1.26f, 1.26f, 7.6f}},
-                                 {{}, {3.7f, 0.565f, 0.457f, 1.8f}, {4.9f, 1.05f, 1.27f, 6.6f}, {}}};
+// What a form takes in microseconds, fitted to measurements of 1800 shapes - 100 .. 4096 rows of W (gated: twice 100 .. 9216), K 100 .. 25088, 1 .. 4096 rows of X, outputs of
+// bf16 and of fp32 -: the choice then takes 1.1 % longer, in the mean of logarithms, than the best of up to thirteen.
+// Tiles: a start (launch, first loads, last stores), and per step of 128 k what a workgroup takes alone on its compute unit; 64 x 64: its share of a full one, where the launch has more
+// workgroups than the chip has compute units; the larger, of which a compute unit has one at a time: how much of a last round that is not full counts; what each further
+// workgroup of a compute unit adds.
+struct Price { float start, alone, shared, last, more; };
+constexpr Price kPrices[2][4] = {{{}, {3.1f, 0.273f, 0.259f, 0, 1.0f}, {4.0f, 0.447f, 0, 0.84f, 3.9f}, {7.0f, 1.25f, 0, 0.82f, 8.2f}},
+                                 {{}, {3.35f, 0.535f, 0.432f, 0, 1.7f}, {4.7f, 0.99f, 0, 0.47f, 7.7f}, {6.4f, 1.69f, 0, 0.77f, 9.8f}}};
 // few_kernel: a start; per block of 128 k and 256 workgroups of rows of W and of X (from 0.6 or 0.7 of that on, which is as fast as a workgroup gets); what it quantises.
 struct FewPrice { float start, row, column, at_least, quantise; };
-constexpr FewPrice kFewPrices[2] = {{2.55f, 0.102f, 0.003f, 0.71f, 0.0015f}, {3.4f, 0.093f, 0.0134f, 0.59f, 0.003f}};      // X in 8 bits; in numbers
+constexpr FewPrice kFewPrices[2] = {{2.55f, 0.103f, 0.003f, 0.71f, 0.0015f}, {3.4f, 0.095f, 0.014f, 0.6f, 0.0022f}};       // X in 8 bits; in numbers
 // The quantisation of X, the sum of partial sums.  A launch costs the host, besides, some 4 us, which calls one by one pay, and calls recorded in a graph do not: half of it counts.
 constexpr float kLaunch = 2.0f;
 constexpr int32_t kFewMostRows = 256;                        // (beyond, tiles are always faster)
 
 static float price_of(const Shape &s, const Choice &c)
 {
-    const int64_t row_tiles = row_tiles_of(c.form, s.width, s.gated), columns = ((int64_t)s.batch + kFormSide[c.form] - 1) / kFormSide[c.form];
+    const int64_t row_tiles = row_tiles_of(c.form, s.width, s.gated), columns = columns_of(c.form, s.batch, s.wide);
     const float M = (float)s.width * (s.gated ? 2 : 1), n = (float)row_tiles * columns * c.splits / kCus;
     float us;
     if (c.form == kFew) {
@@ -383,12 +391,15 @@ static float price_of(const Shape &s, const Choice &c)
     } else {
         const Price &p = kPrices[s.wide][c.form];
         const int fours = (s.blocks + 3) / 4, steps = std::min(s.blocks, (fours + c.splits - 1) / c.splits * 4);
-        const float rounds = std::max(1.0f, std::ceil(n));
-        if (c.form == kTile256) us = p.start + rounds * p.alone * steps + p.more * (rounds - 1);
-        else us = p.start + steps * std::max(p.alone, p.shared * n) + p.more * std::max(0.0f, n - 1);
+        if (c.form == kTile64) {
+            us = p.start + steps * std::max(p.alone, p.shared * n) + p.more * std::max(0.0f, n - 1);
+        } else {
+            const float rounds = std::max(1.0f, n + p.last * (std::ceil(n) - n));
+            us = p.start + steps * p.alone * rounds + p.more * (rounds - 1);
+        }
     }
     if (s.x_type != CL_F8 && !c.own) us += 2.9f + kLaunch + 2.1e-7f * s.batch * s.blocks * kBlock * type_bytes(s.x_type);
-    if (needs_parts(s, c)) us += 1.9f + kLaunch + 0.85e-6f * (2 * c.splits + 1) * s.batch * M;
+    if (needs_parts(s, c)) us += 1.7f + kLaunch + 0.85e-6f * (2 * c.splits + 1) * s.batch * M;
     return us;
 }
 
@@ -407,8 +418,8 @@ static Choice choose(const Shape &s, int32_t K, size_t most)
         if (few_own(s)) offer(kFew, 1, true);
     }
     const int fours = (s.blocks + 3) / 4;
-    for (int form = kTile64; form <= (s.wide ? kTile128 : kTile256); ++form) {
-        const int64_t n = row_tiles_of((Form)form, s.width, s.gated) * (((int64_t)s.batch + kFormSide[form] - 1) / kFormSide[form]);
+    for (int form = kTile64; form <= kTile256; ++form) {
+        const int64_t n = row_tiles_of((Form)form, s.width, s.gated) * columns_of((Form)form, s.batch, s.wide);
         for (int splits = 1; splits <= 8 && splits <= fours && (splits == 1 || n * splits <= 4 * kCus); splits *= 2) offer((Form)form, splits, false);
     }
     return best;

@@ -71,6 +71,116 @@ __device__ __forceinline__ u32x4 sixteen_outputs(const uint32_t *q)
     return u32x4{(uint32_t)c[0], (uint32_t)d[0], (uint32_t)c[1], (uint32_t)d[1]};
 }
 
+// What a wavefront has of a tile - outputs from `first` on, columns of X from c0 - to memory, straight from the registers: of a row it stores 64 consecutive bytes at a time, and
+// loads that are on their way into LDS need not be waited for.  tops: room for 2 BN numbers, [wm][column] (8-bit outputs).
+template <int TI, int TJ, int WM, int BN, class T, bool GATED>
+__device__ __forceinline__ void store_tile(const ProductArgs &a, int split, int first, int c0, int wm, int wn, int lane, f32x4 (&acc)[TI][TJ], float *tops)
+{
+    constexpr int kWide = GATED ? TI * 8 : TI * 16, kPieces = kWide / 16;
+    const int r = lane & 15, g = lane >> 4, c_first = c0 + wn * TJ * 16 + r;
+    if (a.part) {
+#pragma unroll
+        for (int i = 0; i < TI; ++i) {
+            const int h = GATED && i >= kPieces, o = first + (i - h * kPieces) * 16 + 4 * g;
+#pragma unroll
+            for (int j = 0; j < TJ; ++j)
+                if (c_first + j * 16 < a.rows) store_part(a, split, c_first + j * 16, o, acc[i][j], h * a.value_at);
+        }
+    } else if constexpr (std::is_same_v<T, F8Out>) {
+        // A block of 128 outputs is a wavefront's, or two wavefronts' that share their columns.
+        static_assert(kWide == 128 || (kWide == 64 && WM == 2), "");
+        uint32_t top[TJ];
+#pragma unroll
+        for (int j = 0; j < TJ; ++j) {
+            top[j] = 0;
+#pragma unroll
+            for (int i = 0; i < kPieces; ++i) {
+                const int o = first + i * 16 + 4 * g;
+                f32x4 v = activated<GATED>(a, o, acc[i][j], acc[GATED ? kPieces + i : i][j]);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    v[e] = o + e < a.width ? v[e] : 0.0f;
+                    top[j] = max(top[j], __float_as_uint(v[e]) & 0x7fffffffu);
+                }
+                acc[i][j] = v;
+            }
+            top[j] = max(top[j], (uint32_t)__shfl_xor((int)top[j], 16));
+            top[j] = max(top[j], (uint32_t)__shfl_xor((int)top[j], 32));
+            if (kWide == 64 && g == 0) tops[wm * BN + wn * TJ * 16 + j * 16 + r] = __uint_as_float(top[j]);
+        }
+        if (kWide == 64) {
+            // (before these are written again come the barriers of the next tile's steps)
+            __builtin_amdgcn_s_waitcnt(0xc07f);              // (no LDS access left)
+            asm volatile("" ::: "memory");
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+#pragma unroll
+            for (int j = 0; j < TJ; ++j) top[j] = max(top[j], __float_as_uint(tops[(1 - wm) * BN + wn * TJ * 16 + j * 16 + r]));
+        }
+        const int y_blocks = (a.width + kBlock - 1) / kBlock, y_pitch = (y_blocks + 3) / 4 * 4;
+#pragma unroll
+        for (int j = 0; j < TJ; ++j) {
+            const int64_t c = c_first + j * 16;
+            const Scale s = scale_of(top[j]);
+#pragma unroll
+            for (int i = 0; i < kPieces; i += 4) {
+                uint32_t q[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float v[4] = {acc[i + e][j][0], acc[i + e][j][1], acc[i + e][j][2], acc[i + e][j][3]};
+                    q[e] = to_f8(v, s.inverse);
+                }
+                const u32x4 sixteen = sixteen_outputs(q);
+                const int o = first + (i + g) * 16;
+                if (c < a.rows && o < y_blocks * kBlock) *(u32x4 *)((uint8_t *)a.Y + c * y_blocks * kBlock + o) = sixteen;
+            }
+            if (c < a.rows && g == 0 && (kWide == 128 || wm == 0) && first < a.width) {
+                const int b = first / kBlock;
+                float *to = a.y_scales + c * y_pitch;
+                to[b] = s.scale;
+                if (b == y_blocks - 1)
+                    for (int i = y_blocks; i < y_pitch; ++i) to[i] = 0.0f;
+            }
+        }
+    } else if constexpr (sizeof(T) == 2 && kPieces % 2 == 0) {
+#pragma unroll
+        for (int i = 0; i < kPieces; i += 2) {
+#pragma unroll
+            for (int j = 0; j < TJ; ++j) {
+                const f32x4 v = activated<GATED>(a, first + i * 16 + 4 * g, acc[i][j], acc[GATED ? kPieces + i : i][j]);
+                const f32x4 u = activated<GATED>(a, first + i * 16 + 16 + 4 * g, acc[i + 1][j], acc[GATED ? kPieces + i + 1 : i + 1][j]);
+                const T four[2][4] = {{(T)v[0], (T)v[1], (T)v[2], (T)v[3]}, {(T)u[0], (T)u[1], (T)u[2], (T)u[3]}};
+                u32x2 lo, hi;
+                __builtin_memcpy(&lo, four[0], 8);
+                __builtin_memcpy(&hi, four[1], 8);
+                const u32x4 eight = eight_outputs(lo, hi);
+                const int o = first + (i + (g & 1)) * 16 + g / 2 * 8;
+                if (c_first + j * 16 >= a.rows || o >= a.width) continue;
+                T *y = (T *)a.Y + (int64_t)(c_first + j * 16) * a.width + o;
+                if (o + 8 <= a.width) {
+                    __builtin_memcpy(y, &eight, 16);
+                } else {
+                    T out[8];
+                    __builtin_memcpy(out, &eight, 16);
+#pragma unroll
+                    for (int e = 0; e < 7; ++e)
+                        if (o + e < a.width) y[e] = out[e];
+                }
+            }
+        }
+    } else if constexpr (!std::is_same_v<T, F8Out>) {
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) {
+            const int o = first + i * 16 + 4 * g;
+#pragma unroll
+            for (int j = 0; j < TJ; ++j) {
+                const f32x4 v = activated<GATED>(a, o, acc[i][j], acc[GATED ? kPieces + i : i][j]);
+                if (c_first + j * 16 < a.rows) store_outputs<T>(a, c_first + j * 16, o, v);
+            }
+        }
+    }
+}
+
 template <int BM, int BN, int WM, int WN, int D, class T, bool GATED, bool WIDE>
 __global__ __launch_bounds__(WM * WN * 64, 2) void f8_tile_kernel(ProductArgs a, int row_tiles)
 {
@@ -199,11 +309,11 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void f8_tile_kernel(ProductArgs a,
     // Piece row i of a step.  What is read behind it, into the registers that it leaves: rows from `rows`, and, of the last one, columns from `cols`.
     auto piece = [&](auto I, const uint8_t *__restrict__ rows, const uint8_t *__restrict__ cols, const uint8_t *__restrict__ scales, uint8_t *__restrict__ to) __attribute__((always_inline)) {
         constexpr int i = decltype(I)::value;
-        const Operand<WIDE> wi_ = operand<WIDE>(w[i % R]);
+        const Operand<WIDE> row = operand<WIDE>(w[i % R]);
 #pragma unroll
         for (int j = 0; j < TJ; ++j) {
             join((i + TI - 1) % TI, j);
-            p[j] = mfma_f8<WIDE>(wi_, x[j]);
+            p[j] = mfma_f8<WIDE>(row, x[j]);
             __builtin_amdgcn_sched_barrier(0);
             if (i == TI - 1) {
                 x[j] = operand<WIDE>(read_piece(cols, wj + j * 16));
@@ -286,112 +396,8 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void f8_tile_kernel(ProductArgs a,
 #pragma unroll
         for (int j = 0; j < TJ; ++j) join(TI - 1, j);
 
-        // Straight from the registers: what a wavefront stores of a row at a time are 64 consecutive bytes, and the next tile's loads need not wait.
         const Place at = place(mth);
-        constexpr int kWide = GATED ? TI * 8 : TI * 16, kPieces = kWide / 16;
-        const int first = at.o + wm * kWide, c_first = at.c + wn * TJ * 16 + r;
-        if (a.part) {
-#pragma unroll
-            for (int i = 0; i < TI; ++i) {
-                const int h = GATED && i >= kPieces, o = first + (i - h * kPieces) * 16 + 4 * g;
-#pragma unroll
-                for (int j = 0; j < TJ; ++j)
-                    if (c_first + j * 16 < a.rows) store_part(a, split, c_first + j * 16, o, acc[i][j], h * a.value_at);
-            }
-        } else if constexpr (std::is_same_v<T, F8Out>) {
-            // A block of 128 outputs is a wavefront's, or two wavefronts' that share their columns.
-            static_assert(kWide == 128 || (kWide == 64 && WM == 2), "");
-            float *tops = (float *)(lds + C::kLds);          // [wm][column]
-            uint32_t top[TJ];
-#pragma unroll
-            for (int j = 0; j < TJ; ++j) {
-                top[j] = 0;
-#pragma unroll
-                for (int i = 0; i < kPieces; ++i) {
-                    const int o = first + i * 16 + 4 * g;
-                    f32x4 v = activated<GATED>(a, o, acc[i][j], acc[GATED ? kPieces + i : i][j]);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        v[e] = o + e < a.width ? v[e] : 0.0f;
-                        top[j] = max(top[j], __float_as_uint(v[e]) & 0x7fffffffu);
-                    }
-                    acc[i][j] = v;
-                }
-                top[j] = max(top[j], (uint32_t)__shfl_xor((int)top[j], 16));
-                top[j] = max(top[j], (uint32_t)__shfl_xor((int)top[j], 32));
-                if (kWide == 64 && g == 0) tops[wm * BN + wn * TJ * 16 + j * 16 + r] = __uint_as_float(top[j]);
-            }
-            if (kWide == 64) {
-                // (before these are written again come the barriers of the next tile's steps)
-                __builtin_amdgcn_s_waitcnt(kWaitLds);
-                asm volatile("" ::: "memory");
-                __builtin_amdgcn_s_barrier();
-                asm volatile("" ::: "memory");
-#pragma unroll
-                for (int j = 0; j < TJ; ++j) top[j] = max(top[j], __float_as_uint(tops[(1 - wm) * BN + wn * TJ * 16 + j * 16 + r]));
-            }
-            const int y_blocks = (a.width + kBlock - 1) / kBlock, y_pitch = (y_blocks + 3) / 4 * 4;
-#pragma unroll
-            for (int j = 0; j < TJ; ++j) {
-                const int64_t c = c_first + j * 16;
-                const Scale s = scale_of(top[j]);
-#pragma unroll
-                for (int i = 0; i < kPieces; i += 4) {
-                    uint32_t q[4];
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const float v[4] = {acc[i + e][j][0], acc[i + e][j][1], acc[i + e][j][2], acc[i + e][j][3]};
-                        q[e] = to_f8(v, s.inverse);
-                    }
-                    const u32x4 sixteen = sixteen_outputs(q);
-                    const int o = first + (i + g) * 16;
-                    if (c < a.rows && o < y_blocks * kBlock) *(u32x4 *)((uint8_t *)a.Y + c * y_blocks * kBlock + o) = sixteen;
-                }
-                if (c < a.rows && g == 0 && (kWide == 128 || wm == 0) && first < a.width) {
-                    const int b = first / kBlock;
-                    float *to = a.y_scales + c * y_pitch;
-                    to[b] = s.scale;
-                    if (b == y_blocks - 1)
-                        for (int i = y_blocks; i < y_pitch; ++i) to[i] = 0.0f;
-                }
-            }
-        } else if constexpr (sizeof(T) == 2 && kPieces % 2 == 0) {
-#pragma unroll
-            for (int i = 0; i < kPieces; i += 2) {
-#pragma unroll
-                for (int j = 0; j < TJ; ++j) {
-                    const f32x4 v = activated<GATED>(a, first + i * 16 + 4 * g, acc[i][j], acc[GATED ? kPieces + i : i][j]);
-                    const f32x4 u = activated<GATED>(a, first + i * 16 + 16 + 4 * g, acc[i + 1][j], acc[GATED ? kPieces + i + 1 : i + 1][j]);
-                    const T four[2][4] = {{(T)v[0], (T)v[1], (T)v[2], (T)v[3]}, {(T)u[0], (T)u[1], (T)u[2], (T)u[3]}};
-                    u32x2 lo, hi;
-                    __builtin_memcpy(&lo, four[0], 8);
-                    __builtin_memcpy(&hi, four[1], 8);
-                    const u32x4 eight = eight_outputs(lo, hi);
-                    const int o = first + (i + (g & 1)) * 16 + g / 2 * 8;
-                    if (c_first + j * 16 >= a.rows || o >= a.width) continue;
-                    T *y = (T *)a.Y + (int64_t)(c_first + j * 16) * a.width + o;
-                    if (o + 8 <= a.width) {
-                        __builtin_memcpy(y, &eight, 16);
-                    } else {
-                        T out[8];
-                        __builtin_memcpy(out, &eight, 16);
-#pragma unroll
-                        for (int e = 0; e < 7; ++e)
-                            if (o + e < a.width) y[e] = out[e];
-                    }
-                }
-            }
-        } else if constexpr (!std::is_same_v<T, F8Out>) {
-#pragma unroll
-            for (int i = 0; i < kPieces; ++i) {
-                const int o = first + i * 16 + 4 * g;
-#pragma unroll
-                for (int j = 0; j < TJ; ++j) {
-                    const f32x4 v = activated<GATED>(a, o, acc[i][j], acc[GATED ? kPieces + i : i][j]);
-                    if (c_first + j * 16 < a.rows) store_outputs<T>(a, c_first + j * 16, o, v);
-                }
-            }
-        }
+        store_tile<TI, TJ, WM, BN, T, GATED>(a, split, at.o + wm * (GATED ? TI * 8 : TI * 16), at.c, wm, wn, lane, acc, (float *)(lds + C::kLds));
     }
     // (what is still on its way into LDS has to be there before that is another workgroup's)
     constexpr int none = loads_left(0);

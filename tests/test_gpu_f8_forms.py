@@ -82,16 +82,18 @@ def draw(B, M, K, gated, seed, dtype=BF16):
 # form, splits, batch, outputs, K, type of X, of the output, activation
 FORMS = [
     ("few numbers", 1, 1, 23, 34, BF16, BF16, "gated"), ("few numbers", 1, 16, 1000, 4096, F32, F32, "relu"), ("few numbers", 1, 5, 333, 1700, F16, F8, "gated"),
-    ("few numbers", 1, 7, 129, 515, BF16, F8, "none"), ("few", 1, 1, 31, 670, F8, F8, "none"), ("few", 1, 29, 38, 4639, BF16, BF16, "none"), ("few", 1, 9, 21, 8278, F32, F32, "gated"),
-    ("few", 1, 4, 27, 17865, F16, F8, "none"),
+    ("few numbers", 1, 7, 129, 515, BF16, F8, "none"), ("few", 1, 9, 5614, 5596, F16, F8, "gated"), ("few", 1, 29, 38, 4639, BF16, BF16, "none"), ("few", 1, 31, 23, 5068, F32, F32, "gated"),
+    ("few", 1, 20, 30, 4358, F16, F8, "none"),
     ("tile 64", 1, 426, 25, 42, BF16, BF16, "gated"), ("tile 64", 1, 343, 18, 69, BF16, BF16, "none"), ("tile 64", 1, 335, 18, 49, F16, F8, "gated"), ("tile 64", 1, 367, 19, 69, F8, F32, "gated"),
     ("tile 64", 2, 284, 31, 722, F16, F8, "gated"), ("tile 64", 4, 351, 17, 3200, BF16, BF16, "relu"), ("tile 64", 8, 3, 32, 24400, F16, F8, "none"), ("tile 64", 8, 6, 17, 15527, F32, F32, "gated"),
-    ("tile 128", 1, 262, 2604, 37, F8, BF16, "gated"), ("tile 128", 1, 561, 2840, 41, BF16, BF16, "none"), ("tile 128", 1, 381, 19, 81, F16, F8, "none"), ("tile 128", 1, 300, 500, 100, F8, F8, "none"),
-    ("tile 128", 1, 197, 4566, 907, F8, F8, "gated"), ("tile 128", 1, 286, 6028, 33, F32, F32, "none"), ("tile 128", 2, 70, 6741, 2513, F16, F8, "gated"), ("tile 128", 4, 66, 6995, 1963, F16, F8, "none"),
+    ("tile 128", 1, 169, 6980, 33, F8, BF16, "gated"), ("tile 128", 1, 258, 7158, 36, BF16, BF16, "none"), ("tile 128", 1, 381, 19, 81, F16, F8, "none"), ("tile 128", 1, 300, 500, 100, F8, F8, "none"),
+    ("tile 128", 1, 197, 4566, 907, F8, F8, "gated"), ("tile 128", 1, 8118, 220, 34, F32, F32, "none"), ("tile 128", 2, 70, 6741, 2513, F16, F8, "gated"), ("tile 128", 4, 66, 6995, 1963, F16, F8, "none"),
     ("tile 128", 8, 71, 3268, 6900, F32, F32, "relu"), ("tile 128", 8, 104, 1555, 10491, F8, F32, "gated"),
     # (more tiles than compute units: workgroups go from one to the next, with one step to a tile, with three, and with more than fours of them)
-    ("tile 256", 1, 2034, 90, 33, F8, F8, "gated"), ("tile 256", 1, 5644, 2196, 38, F8, F8, "none"), ("tile 256", 1, 5537, 1166, 35, BF16, BF16, "gated"), ("tile 256", 1, 4300, 2200, 260, F8, F8, "gated"),
-    ("tile 256", 1, 5000, 2500, 130, BF16, F8, "none"), ("tile 256", 1, 5100, 2470, 900, BF16, BF16, "none"), ("tile 256", 4, 202, 5086, 13781, F8, BF16, "gated"), ("tile 256", 8, 129, 7837, 16532, F8, F8, "none"),
+    ("tile 256", 1, 1258, 223, 33, F8, F8, "gated"), ("tile 256", 1, 5644, 2196, 38, F8, F8, "none"), ("tile 256", 1, 5537, 1166, 35, BF16, BF16, "gated"), ("tile 256", 1, 4300, 2200, 260, F8, F8, "gated"),
+    ("tile 256", 1, 5000, 2500, 130, BF16, F8, "none"), ("tile 256", 1, 5100, 2470, 900, BF16, BF16, "none"), ("tile 256", 4, 148, 4253, 19748, F8, F8, "gated"), ("tile 256", 8, 4704, 131, 24334, BF16, BF16, "none"),
+    # (outputs in fp32, or in 8 bits of an input in fp16: 256 x 128)
+    ("tile 256", 1, 6024, 359, 36, F32, F32, "gated"), ("tile 256", 1, 9000, 1500, 300, F32, F32, "relu"), ("tile 256", 8, 129, 3911, 18938, F32, F32, "none"), ("tile 256", 2, 2657, 530, 10655, F16, F8, "gated"),
 ]
 
 
