@@ -681,8 +681,8 @@ typedef struct {
 int32_t cl_rms_norm(const cl_norm_call *call, void *stream);
 
 /* Y = act(X W^T + v) with W and X in 8 bits.  The sum over a block of 128 is multiplied by fl(X's scale times W's) and added to the others in fp32; one rounding
- * to Y's type at the end.  Where that is CL_F32, products and sums within a block are fp32, too; for the other types, whose rounding is coarser, they are the
- * 8-bit matrix instruction's: of each eight neighbouring k, products are cut off at 2^-13 of the largest.
+ * to Y's type at the end.  Where that is CL_F32 or CL_F8, products and sums within a block are fp32, too; for CL_BF16 and CL_F16 they are the 8-bit matrix
+ * instruction's, twice as fast: of each eight neighbouring k, products are cut off at 2^-13 of the largest.
  *  X         batch rows of W->K             d_bias   W->rows fp32 or NULL
  *  act       CL_ACT_NONE, CL_ACT_RELU, or CL_ACT_GATED: output i is g / (1 + exp(-g)) u with g from row i of W and u from row rows / 2 + i (the rows of
  *            a pair are not neighbours here as they are for 4-bit matrices: a block of 128 of them has one scale)
@@ -702,7 +702,7 @@ enum {
     CL_F8_FORM_FEW = 1,          /* the same with X in 8 bits                                                               */
     CL_F8_FORM_TILE_64 = 2,      /* tiles of the output with their operands in LDS: 64 x 64,                               */
     CL_F8_FORM_TILE_128 = 3,     /*   128 x 128,                                                                           */
-    CL_F8_FORM_TILE_256 = 4      /*   256 x 256                                                                            */
+    CL_F8_FORM_TILE_256 = 4      /*   256 x 256; where sums within a block are fp32, 256 rows of the matrix x 128          */
 };
 /* The form that cl_eight_fc_forward takes for such a call, given a workspace of cl_eight_fc_workspace_bytes() for that batch, and into how many sums it splits
  * k.  Errors as cl_eight_fc_workspace_bytes. */

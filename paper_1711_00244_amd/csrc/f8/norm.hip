@@ -171,7 +171,7 @@ template <class T, class Y> static int32_t launch_norm(NormArgs a, hipStream_t s
     // 91); few: as many lanes as there is work for (512 rows of 4096 5.3, four times 6.5; one row 3.4 and 6.9)
     const int want = a.rows >= (1 << 20) / a.units ? 4 : 1;
     int times = 1;
-    a.lanes = kBlock / V;
+    a.lanes = kBlock / V;                                    // (a block's; whatever the output's type, so that 8 bits are those of the fp32 result)
     while (a.lanes < 1024 && a.lanes * want < a.units) a.lanes *= 2;
     while (times <= 8 && a.lanes * times < a.units) times *= 2;
     const int threads = std::max(256, a.lanes), each = threads / a.lanes;

@@ -30,7 +30,7 @@ struct ProductArgs {
     int pitch, value_at;
     int splits;
     int split_fours, split_more;                             // fours of steps of 128 k of a share of k, and how many shares have one more
-    Div row_tiles, band_tiles;                               // tiles of a column of tiles, and of a band of columns
+    Div band_tiles;                                          // of a band of four columns of tiles
 };
 
 // Eight 8-bit values in 16 bits.
@@ -47,8 +47,10 @@ __device__ __forceinline__ bf16x8 wide(int lo, int hi)
 // The 8-bit instructions line up the products of each run of eight k by the largest and cut off what is more than 13 bits below it (measured: a product of
 // 2^-14 of the largest is lost, beside a product of another run one of 2^-23 is not); sums of runs are 32 bits.  So a run is off by less than 7 * 2^-13 of its
 // largest product - with activations and weights as they are, 1.4e-5 to 5e-5 of a sum (2-norm), a hundredth of the rounding of an output in bf16, a
-// tenth of one in fp16.  An output in fp32 has the bits to show it: WIDE takes the operands to bf16, which is exact, and multiplies on the bf16
-// instructions, whose products and sums are 32 bits, at half the rate.
+// tenth of one in fp16.  An output in fp32 has the bits to show it; so has, behind a second product, one in 8 bits: a value next to the middle of two steps goes to
+// one or the other by the last bits of its sum (outputs in bf16 of two layers one after the other were up to 5.7e-3 off instead of the rounding's 1.7e-3, of 32 rows of
+// 194 numbers).  For these WIDE takes the operands to bf16, which is exact, and multiplies on the bf16 instructions,
+// whose products and sums are 32 bits, at half the rate.
 template <bool WIDE> struct OperandOf { typedef i32x8 type; };
 template <> struct OperandOf<true> { struct type { bf16x8 v[4]; }; };
 template <bool WIDE> using Operand = typename OperandOf<WIDE>::type;
@@ -185,10 +187,8 @@ struct Choice {
     float us;
 };
 
-// Outputs in fp32 show the 8-bit instruction's sums (see mfma_f8).  8-bit outputs do not; but a value of them next to the middle of two steps goes to one or
-// the other by the last bits of its sum, and of two blocks of a layer one after the other the rounding of outputs in fp16 is fine enough to show that, in bf16 not: so 8-bit outputs
-// of a bf16 input, or of one that has 8 bits already, take the faster instructions.
-static bool is_wide(int32_t x_type, int32_t y_type) { return y_type == CL_F32 || (y_type == CL_F8 && (x_type == CL_F32 || x_type == CL_F16)); }
+// Outputs that show the 8-bit instruction's sums (see mfma_f8).
+static bool is_wide(int32_t y_type) { return y_type == CL_F32 || y_type == CL_F8; }
 
 static bool few_own(const Shape &s) { return s.x_type != CL_F8 && few_lds(s.blocks, std::min(s.batch, kFewColumns)) <= kFewLds; }
 
@@ -209,7 +209,7 @@ static int64_t row_tiles_of(Form form, int32_t width, bool gated)
 static int64_t columns_of(Form form, int64_t rows, bool wide) { return (rows + form_columns(form, wide) - 1) / form_columns(form, wide); }
 
 // Whether 8-bit outputs are made where the product ends: where a workgroup has all 128 of a block.
-static bool ends_in_f8(const Shape &s, const Choice &c) { return s.y_type == CL_F8 && c.splits == 1 && ((c.form == kTile256 && !s.wide) || (c.form == kTile128 && !s.gated)); }
+static bool ends_in_f8(const Shape &s, const Choice &c) { return s.y_type == CL_F8 && c.splits == 1 && (c.form == kTile256 || (c.form == kTile128 && !s.gated)); }
 static bool needs_parts(const Shape &s, const Choice &c) { return c.splits > 1 || (s.y_type == CL_F8 && !ends_in_f8(s, c)); }
 
 // Whether the launch has less than 2^32 threads along each axis.
@@ -234,7 +234,6 @@ template <Form F, class T, bool GATED, bool WIDE> static int32_t launch_tiles(Pr
     static LdsLimit seen;
     if (int32_t rc = allow_lds((const void *)kernel, kLds, seen)) return rc;
     const int64_t row_tiles = row_tiles_of(F, a.width, GATED), columns = columns_of(F, a.rows, WIDE);
-    a.row_tiles = make_div((uint32_t)row_tiles);
     a.band_tiles = make_div((uint32_t)row_tiles * 4u);
     const int fours = (a.blocks + 3) / 4;
     a.split_fours = fours / c.splits;
@@ -298,8 +297,8 @@ template <bool GATED> static int32_t run_product(ProductArgs a, const Shape &s, 
         if (s.y_type == CL_F32) return launch_product<float, GATED, true>(a, s, c, x, K, st);
         if (s.y_type == CL_BF16) return launch_product<bf16_t, GATED, false>(a, s, c, x, K, st);
         if (s.y_type == CL_F16) return launch_product<f16_t, GATED, false>(a, s, c, x, K, st);
-        if (c.form == kTile256) return launch_tiles<kTile256, F8Out, GATED, false>(a, c, st);
-        if constexpr (!GATED) return s.wide ? launch_tiles<kTile128, F8Out, false, true>(a, c, st) : launch_tiles<kTile128, F8Out, false, false>(a, c, st);
+        if (c.form == kTile256) return launch_tiles<kTile256, F8Out, GATED, true>(a, c, st);
+        if constexpr (!GATED) return launch_tiles<kTile128, F8Out, false, true>(a, c, st);
     }
     if (int32_t rc = s.wide ? launch_product<float, GATED, true>(a, s, c, x, K, st) : launch_product<float, GATED, false>(a, s, c, x, K, st)) return rc;
     auto finish = [&](auto t, uint32_t quads) {
@@ -430,7 +429,7 @@ static int32_t fail_with_grid(const Shape &s) { return fail(CL_EUNSUPPORTED, "%d
 static Shape shape_of(const cl_f8_matrix &W, int32_t batch, int32_t x_type, int32_t y_type, int32_t act)
 {
     const bool gated = act == CL_ACT_GATED;
-    return Shape{gated ? W.rows / 2 : W.rows, blocks_of(W.K), batch, gated, is_wide(x_type, y_type), x_type, y_type};
+    return Shape{gated ? W.rows / 2 : W.rows, blocks_of(W.K), batch, gated, is_wide(y_type), x_type, y_type};
 }
 
 }  // namespace f8

@@ -16,7 +16,7 @@ template <int BM, int BN, int WM, int WN, int D> struct SmallTile {
     static constexpr int kBuffer = (BM + BN) * kBlock;
     static constexpr int kScales = D * kBuffer;              // where the scales start: two buffers of four steps
     static constexpr int kScaleBuffer = (BN + 64) * 16;
-    static constexpr int kLds = kScales + 2 * kScaleBuffer, kTops = 2 * BN * 4;
+    static constexpr int kLds = kScales + 2 * kScaleBuffer, kTops = WM * BN * 4;
     static constexpr int share(int n, int of, int i) { return n * i / of; }
     static constexpr int kColumnPieces = TI > 2 ? TI / 2 : 1;          // pieces at whose beginning columns of the next step are read
     static_assert(TI % 2 == 0 && TI > 0 && TJ > 0 && 128 % kRun == 0, "");

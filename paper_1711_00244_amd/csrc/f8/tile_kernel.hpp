@@ -21,29 +21,27 @@ template <int BM, int BN, int WM, int WN, int D> struct Tile {
     static constexpr int TI = BM / WM / 16, TJ = BN / WN / 16, R = 2;
     static constexpr int kRun = TI * 8;                      // rows under one scale: half of a wavefront's
     static constexpr int kLoads = (BM + BN) / 8 / kWaves;    // of a wavefront and step
-    static constexpr bool kHalves = TI > R;                  // a buffer in two parts; else as one
-    static constexpr int kLate = kHalves ? BM / 16 / kWaves : 0, kEarly = kLoads - kLate;       // second halves of rows; all others
+    static constexpr int kLate = BM / 16 / kWaves, kEarly = kLoads - kLate;       // second halves of rows; all others
     // Where the wavefronts wait for each other: before piece row kFree the second halves have to be there, and what is early may be asked for again; before kNext
     // the next step's early part has to be there, and the second halves may be asked for again.
-    static constexpr int kNext = TI - R, kFree = kHalves ? TI / 2 - R : -1;
+    static constexpr int kNext = TI - R, kFree = TI / 2 - R;
     // loads behind piece row i: the early ones from early(i) to early(i + 1), the late ones likewise
     static constexpr int share(int n, int of, int i) { return n * (i < 0 ? 0 : i < of ? i : of) / of; }
-    static constexpr int early(int i) { return kHalves ? share(kEarly, TI / 2, i - kFree) : share(kEarly, R, i - kNext); }
+    static constexpr int early(int i) { return share(kEarly, TI / 2, i - kFree); }
     static constexpr int late(int i) { return share(kLate, R, i - kNext); }
     static constexpr int kScaleLoads = BN / 64 + 1;          // of the workgroup and four steps: columns, then the wavefronts' rows
     static constexpr int kScaleShare = (kScaleLoads + kWaves - 1) / kWaves;      // (wavefronts beyond that number repeat the last)
     static constexpr int kBuffer = (BM + BN) * kBlock;
     static constexpr int kScales = D * kBuffer;              // where the scales start: D buffers of four steps
     static constexpr int kScaleBuffer = (BN + 64) * 16;
-    static constexpr int kLds = kScales + D * kScaleBuffer, kTops = 2 * BN * 4;      // (8-bit outputs: the largest of each column, of two wavefronts)
-    static_assert(TI % R == 0 && TI % 2 == 0 && TI > 0 && TJ > 0 && 128 % kRun == 0, "");
+    static constexpr int kLds = kScales + D * kScaleBuffer, kTops = WM * BN * 4;     // (8-bit outputs: the largest of each column, of each wavefront)
+    static_assert(TI % (2 * R) == 0 && TI > 0 && TJ > 0 && 128 % kRun == 0, "");
     static_assert(BM % (8 * kWaves) == 0 && BN % (8 * kWaves) == 0 && kRun % 8 == 0 && BN % 64 == 0 && 2 * WM <= 64, "");
-    static_assert(D == 2 || D == 4, "");
-    static_assert(!kHalves || (TI / 2 >= R && BM / 16 % kWaves == 0), "");
+    static_assert((D == 2 || D == 4) && BM / 16 % kWaves == 0, "");
     // Loads of a wavefront that may be on their way, at the least those asked for after the next step's early part, or after this one's second halves.  (Those of scales
     // not counted: there may be one or two more.)
-    static constexpr int kBeforeNext = (kHalves ? D - 1 : D - 2) * kLoads, kBeforeLate = (D - 1) * kLoads;
-    static_assert(kBeforeLate + kLate < 64, "");             // (the count that a wait names)
+    static constexpr int kInFlight = (D - 1) * kLoads;
+    static_assert(kInFlight + kLate < 64, "");             // (the count that a wait names)
 };
 
 // f(I), ..., f(N - 1), numbers that are known when it is compiled.
@@ -63,7 +61,14 @@ __device__ __forceinline__ u32x4 eight_outputs(u32x2 first, u32x2 second)
     return u32x4{(uint32_t)a[0], (uint32_t)b[0], (uint32_t)a[1], (uint32_t)b[1]};
 }
 
-// The same for 8-bit outputs of four pieces, so that a lane has sixteen consecutive ones, lanes of sixteen n those of piece n.
+// The same for 8-bit outputs.
+__device__ __forceinline__ u32x2 eight_outputs(uint32_t first, uint32_t second)
+{
+    const auto a = __builtin_amdgcn_permlane16_swap(first, second, false, false);
+    return u32x2{(uint32_t)a[0], (uint32_t)a[1]};
+}
+
+// And of four pieces, so that a lane has sixteen consecutive ones, lanes of sixteen n those of piece n.
 __device__ __forceinline__ u32x4 sixteen_outputs(const uint32_t *q)
 {
     const auto a = __builtin_amdgcn_permlane16_swap(q[0], q[1], false, false), b = __builtin_amdgcn_permlane16_swap(q[2], q[3], false, false);
@@ -72,7 +77,7 @@ __device__ __forceinline__ u32x4 sixteen_outputs(const uint32_t *q)
 }
 
 // What a wavefront has of a tile - outputs from `first` on, columns of X from c0 - to memory, straight from the registers: of a row it stores 64 consecutive bytes at a time, and
-// loads that are on their way into LDS need not be waited for.  tops: room for 2 BN numbers, [wm][column] (8-bit outputs).
+// loads that are on their way into LDS need not be waited for.  tops: room for WM BN numbers, [wm][column] (8-bit outputs).
 template <int TI, int TJ, int WM, int BN, class T, bool GATED>
 __device__ __forceinline__ void store_tile(const ProductArgs &a, int split, int first, int c0, int wm, int wn, int lane, f32x4 (&acc)[TI][TJ], float *tops)
 {
@@ -87,8 +92,9 @@ __device__ __forceinline__ void store_tile(const ProductArgs &a, int split, int 
                 if (c_first + j * 16 < a.rows) store_part(a, split, c_first + j * 16, o, acc[i][j], h * a.value_at);
         }
     } else if constexpr (std::is_same_v<T, F8Out>) {
-        // A block of 128 outputs is a wavefront's, or two wavefronts' that share their columns.
-        static_assert(kWide == 128 || (kWide == 64 && WM == 2), "");
+        // A block of 128 outputs belongs to kShare wavefronts that have the same columns.
+        constexpr int kShare = kBlock / kWide;
+        static_assert(kWide * kShare == kBlock && kShare > 1 && WM % kShare == 0, "");
         uint32_t top[TJ];
 #pragma unroll
         for (int j = 0; j < TJ; ++j) {
@@ -106,35 +112,38 @@ __device__ __forceinline__ void store_tile(const ProductArgs &a, int split, int 
             }
             top[j] = max(top[j], (uint32_t)__shfl_xor((int)top[j], 16));
             top[j] = max(top[j], (uint32_t)__shfl_xor((int)top[j], 32));
-            if (kWide == 64 && g == 0) tops[wm * BN + wn * TJ * 16 + j * 16 + r] = __uint_as_float(top[j]);
+            if (g == 0) tops[wm * BN + wn * TJ * 16 + j * 16 + r] = __uint_as_float(top[j]);
         }
-        if (kWide == 64) {
-            // (before these are written again come the barriers of the next tile's steps)
-            __builtin_amdgcn_s_waitcnt(0xc07f);              // (no LDS access left)
-            asm volatile("" ::: "memory");
-            __builtin_amdgcn_s_barrier();
-            asm volatile("" ::: "memory");
+        // (before these are written again come the barriers of the next tile's steps)
+        __builtin_amdgcn_s_waitcnt(0xc07f);                  // (no LDS access left)
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
 #pragma unroll
-            for (int j = 0; j < TJ; ++j) top[j] = max(top[j], __float_as_uint(tops[(1 - wm) * BN + wn * TJ * 16 + j * 16 + r]));
-        }
+        for (int n = 0; n < kShare; ++n)
+#pragma unroll
+            for (int j = 0; j < TJ; ++j) top[j] = max(top[j], __float_as_uint(tops[(wm / kShare * kShare + n) * BN + wn * TJ * 16 + j * 16 + r]));
         const int y_blocks = (a.width + kBlock - 1) / kBlock, y_pitch = (y_blocks + 3) / 4 * 4;
 #pragma unroll
         for (int j = 0; j < TJ; ++j) {
             const int64_t c = c_first + j * 16;
             const Scale s = scale_of(top[j]);
+            uint32_t q[kPieces];
 #pragma unroll
-            for (int i = 0; i < kPieces; i += 4) {
-                uint32_t q[4];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float v[4] = {acc[i + e][j][0], acc[i + e][j][1], acc[i + e][j][2], acc[i + e][j][3]};
-                    q[e] = to_f8(v, s.inverse);
-                }
-                const u32x4 sixteen = sixteen_outputs(q);
-                const int o = first + (i + g) * 16;
-                if (c < a.rows && o < y_blocks * kBlock) *(u32x4 *)((uint8_t *)a.Y + c * y_blocks * kBlock + o) = sixteen;
+            for (int i = 0; i < kPieces; ++i) {
+                const float v[4] = {acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]};
+                q[i] = to_f8(v, s.inverse);
             }
-            if (c < a.rows && g == 0 && (kWide == 128 || wm == 0) && first < a.width) {
+            const int o = first + (kPieces == 4 ? g * 16 : (g & 1) * 16 + g / 2 * 8);
+            uint8_t *y = (uint8_t *)a.Y + c * y_blocks * kBlock + o;
+            if constexpr (kPieces == 4) {
+                const u32x4 sixteen = sixteen_outputs(q);
+                if (c < a.rows && o < y_blocks * kBlock) *(u32x4 *)y = sixteen;
+            } else {
+                const u32x2 eight = eight_outputs(q[0], q[1]);
+                if (c < a.rows && o < y_blocks * kBlock) *(u32x2 *)y = eight;
+            }
+            if (c < a.rows && g == 0 && wm % kShare == 0 && first < a.width) {
                 const int b = first / kBlock;
                 float *to = a.y_scales + c * y_pitch;
                 to[b] = s.scale;
@@ -192,7 +201,7 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void f8_tile_kernel(ProductArgs a,
     const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = (int)(threadIdx.x & 63), r = lane & 15, g = lane >> 4;
     constexpr int kOutputs = GATED ? BM / 2 : BM;            // of the tile
 
-    // Workgroups go to the eight dies in turn.  Each die takes a run of tiles, of large ones four columns of tiles at a time, so that what it has in flight shares rows
+    // Workgroups go to the eight dies in turn.  Each die takes a run of tiles, four columns of tiles at a time, so that what it has in flight shares rows
     // of W and of X in its cache.  A workgroup takes every gridDim.x / 8-th tile of its die's run, and asks for its next tile's first steps while it multiplies the
     // last of the one before.
     const int columns = (a.rows + BN - 1) / BN, tiles = columns * row_tiles, die = (int)blockIdx.x % 8, dies_run = tiles / 8 + (die < tiles % 8);
@@ -207,24 +216,16 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void f8_tile_kernel(ProductArgs a,
     const uint32_t row_bytes = (uint32_t)a.blocks * kBlock;
     // which of the buffer's rows load k of the wavefront writes: columns, then first halves of rows, then second halves
     auto load_row = [&](int k) {
-        constexpr int kColumns = BN / 8 / C::kWaves, kRows = C::kHalves ? C::kLate : BM / 8 / C::kWaves;
+        constexpr int kColumns = BN / 8 / C::kWaves;
         if (k < kColumns) return BM + (k * C::kWaves + wave) * 8;
-        const int n = (k - kColumns) % kRows * C::kWaves + wave, half = (k - kColumns) / kRows;
-        return C::kHalves ? n / TI * (TI * 16) + half * C::kRun + n % TI * 8 : n * 8;
+        const int n = (k - kColumns) % C::kLate * C::kWaves + wave, half = (k - kColumns) / C::kLate;
+        return n / TI * (TI * 16) + half * C::kRun + n % TI * 8;
     };
     struct Place { int o, c; };                              // a tile's first output and column
     auto place = [&](int nth) {
-        const int tile = run_first + nth;
-        int column, down;
-        if (BM * BN >= 128 * 128) {
-            const int first = (int)a.band_tiles.quotient((uint32_t)tile) * 4, in = tile - first * row_tiles, across = min(4, columns - first);
-            down = across == 1 ? in : across == 2 ? in / 2 : across == 3 ? in / 3 : in / 4;
-            column = first + in - down * across;
-        } else {
-            column = (int)a.row_tiles.quotient((uint32_t)tile);
-            down = tile - column * row_tiles;
-        }
-        return Place{down * kOutputs, column * BN};
+        const int tile = run_first + nth, band = (int)a.band_tiles.quotient((uint32_t)tile) * 4, in = tile - band * row_tiles, across = min(4, columns - band);
+        const int down = across == 1 ? in : across == 2 ? in / 2 : across == 3 ? in / 3 : in / 4;
+        return Place{down * kOutputs, (band + in - down * across) * BN};
     };
     // The tile that is asked for: what each load of a wavefront reads, eight rows (those beyond the last repeat it; a tile's have less than 4 GB).
     const uint8_t *base[C::kLoads];
@@ -349,14 +350,11 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void f8_tile_kernel(ProductArgs a,
     // A step.  `now` has it, `next` the one after; `to`, which is `now`, receives step `ask`.  `scales_now` and `scales_next` are at the word of their step.
     auto step = [&](const uint8_t *now, const uint8_t *next, uint8_t *to, const uint8_t *scales_now, const uint8_t *scales_next) __attribute__((always_inline)) {
         sw[1] = scale_of_run(scales_now, 1);
-        if (C::kHalves) {
-            each<0, C::kFree>([&](auto I) __attribute__((always_inline)) { piece(I, now, now, scales_now, to); });
-            meet(std::integral_constant<int, C::kBeforeLate>{});
-            ask_scales(scales(scales_asked));
-        }
-        each<(C::kHalves ? C::kFree : 0), C::kNext>([&](auto I) __attribute__((always_inline)) { piece(I, now, now, scales_now, to); });
-        meet(std::integral_constant<int, C::kBeforeNext>{});
-        if (!C::kHalves) ask_scales(scales(scales_asked));
+        each<0, C::kFree>([&](auto I) __attribute__((always_inline)) { piece(I, now, now, scales_now, to); });
+        meet(std::integral_constant<int, C::kInFlight>{});
+        ask_scales(scales(scales_asked));
+        each<C::kFree, C::kNext>([&](auto I) __attribute__((always_inline)) { piece(I, now, now, scales_now, to); });
+        meet(std::integral_constant<int, C::kInFlight>{});
         each<C::kNext, TI>([&](auto I) __attribute__((always_inline)) { piece(I, next, next, scales_next, to); });
     };
 
@@ -369,7 +367,7 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void f8_tile_kernel(ProductArgs a,
         for (int k = 0; k < C::kLoads; ++k) request(ask, lds + t * C::kBuffer, k);
         asked();
     }
-    meet(std::integral_constant<int, (D - 1) * C::kLoads + C::kLate>{});
+    meet(std::integral_constant<int, C::kInFlight + C::kLate>{});
 #pragma unroll
     for (int j = 0; j < TJ; ++j) x[j] = operand<WIDE>(read_piece(lds, wj + j * 16)), sx[j] = scale_of_column(scales(0), j);
     sw[0] = scale_of_run(scales(0), 0);

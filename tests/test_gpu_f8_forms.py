@@ -87,11 +87,11 @@ FORMS = [
     ("tile 64", 1, 426, 25, 42, BF16, BF16, "gated"), ("tile 64", 1, 343, 18, 69, BF16, BF16, "none"), ("tile 64", 1, 335, 18, 49, F16, F8, "gated"), ("tile 64", 1, 367, 19, 69, F8, F32, "gated"),
     ("tile 64", 2, 284, 31, 722, F16, F8, "gated"), ("tile 64", 4, 351, 17, 3200, BF16, BF16, "relu"), ("tile 64", 8, 3, 32, 24400, F16, F8, "none"), ("tile 64", 8, 6, 17, 15527, F32, F32, "gated"),
     ("tile 128", 1, 169, 6980, 33, F8, BF16, "gated"), ("tile 128", 1, 258, 7158, 36, BF16, BF16, "none"), ("tile 128", 1, 381, 19, 81, F16, F8, "none"), ("tile 128", 1, 300, 500, 100, F8, F8, "none"),
-    ("tile 128", 1, 197, 4566, 907, F8, F8, "gated"), ("tile 128", 1, 8118, 220, 34, F32, F32, "none"), ("tile 128", 2, 70, 6741, 2513, F16, F8, "gated"), ("tile 128", 4, 66, 6995, 1963, F16, F8, "none"),
+    ("tile 128", 1, 150, 6948, 1798, F8, F8, "gated"), ("tile 128", 1, 8118, 220, 34, F32, F32, "none"), ("tile 128", 2, 70, 6741, 2513, F16, F8, "gated"), ("tile 128", 4, 66, 6995, 1963, F16, F8, "none"),
     ("tile 128", 8, 71, 3268, 6900, F32, F32, "relu"), ("tile 128", 8, 104, 1555, 10491, F8, F32, "gated"),
     # (more tiles than compute units: workgroups go from one to the next, with one step to a tile, with three, and with more than fours of them)
     ("tile 256", 1, 1258, 223, 33, F8, F8, "gated"), ("tile 256", 1, 5644, 2196, 38, F8, F8, "none"), ("tile 256", 1, 5537, 1166, 35, BF16, BF16, "gated"), ("tile 256", 1, 4300, 2200, 260, F8, F8, "gated"),
-    ("tile 256", 1, 5000, 2500, 130, BF16, F8, "none"), ("tile 256", 1, 5100, 2470, 900, BF16, BF16, "none"), ("tile 256", 4, 148, 4253, 19748, F8, F8, "gated"), ("tile 256", 8, 4704, 131, 24334, BF16, BF16, "none"),
+    ("tile 256", 1, 5000, 2500, 130, BF16, F8, "none"), ("tile 256", 1, 5100, 2470, 900, BF16, BF16, "none"), ("tile 256", 4, 3485, 141, 14150, F8, F8, "gated"), ("tile 256", 8, 4704, 131, 24334, BF16, BF16, "none"),
     # (outputs in fp32, or in 8 bits of an input in fp16: 256 x 128)
     ("tile 256", 1, 6024, 359, 36, F32, F32, "gated"), ("tile 256", 1, 9000, 1500, 300, F32, F32, "relu"), ("tile 256", 8, 129, 3911, 18938, F32, F32, "none"), ("tile 256", 2, 2657, 530, 10655, F16, F8, "gated"),
 ]
@@ -104,7 +104,7 @@ def test_form(form, splits, B, M, K, x_type, y_type, act):
         X = cl.f8_quantize(X)
     assert cl.f8_fc_resolved_form(W, B, x_type, act, y_type) == (form, splits)
     x = wide(X if x_type == F8 else cl.f8_quantize(X))
-    narrow = not (y_type == F32 or (y_type == F8 and x_type in (F32, F16)))
+    narrow = y_type in (BF16, F16)
     for b in (None, bias):
         want, err = product(x, wide(W), b, act, narrow)
         y = cl.f8_fc_forward(W, X, b, act=act, dtype=y_type)
@@ -123,7 +123,7 @@ def test_the_workspace_of_the_largest_batch_serves_all(M, K, largest, batches, x
     for batch in batches:
         part = X[:batch]
         q = cl.f8_quantize(part)
-        want, err = product(wide(q), w, None, act, not (y_type == F32 or (y_type == F8 and x_type in (F32, F16))))
+        want, err = product(wide(q), w, None, act, y_type in (BF16, F16))
         y = cl.f8_fc_forward(W, q if x_type == F8 else part, act=act, dtype=y_type, workspace=room[:need])
         check(y, want, err, batch)
         assert bool((room[need:] == 255).all())
