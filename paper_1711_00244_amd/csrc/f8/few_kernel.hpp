@@ -6,6 +6,8 @@
 // 16 rows of W - GATED: of gates and of values - is one matrix instruction; their sums meet in LDS and are added in the order of the wavefronts.  No operand of W is
 // shared, so that nothing but the quantisation of X, which is done while the first weights are on their way, waits for a barrier until the end.
 // X in numbers: every workgroup quantises all of its rows into LDS, which for so few costs less than a launch of its own; X in 8 bits comes from the caches.
+// What bounds it are a launch and one trip to memory: one fp32 row of 4096 x 9216, 38 MB, 9.3 us with the launch, 4.1 TB/s (a large copy 5.1); 8 bf16 rows of
+// 2 x 4096 x 4096 gated 10.7.
 constexpr int kFewWaves = 16, kFewColumns = 16, kFewAhead = 3;
 constexpr size_t kFewLds = 72 << 10;
 

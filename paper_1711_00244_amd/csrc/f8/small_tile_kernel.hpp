@@ -6,6 +6,9 @@
 // there, columns at its beginning, into a second set.  So nothing waits for LDS where the wavefronts meet; a buffer is asked for again one step after it was read.
 //
 // WIDE: columns are taken to bf16 when their step begins, and then replaced in their one set.
+//
+// 256 rows of X, 4096 x 9216, fp32 outputs, WIDE: 128 x 128 in four shares of k 33 us with the sum of the shares (a compute unit has one workgroup, of 18 steps), 64 x 64 in
+// two 35, in three 38; 333 rows of 2 x 2900 x 1100 gated, fp16: 128 x 128 8.2 us.
 template <int BM, int BN, int WM, int WN, int D> struct SmallTile {
     static constexpr int kWaves = WM * WN, kThreads = kWaves * 64;
     static constexpr int TI = BM / WM / 16, TJ = BN / WN / 16;
