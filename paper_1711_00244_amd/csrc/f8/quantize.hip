@@ -43,21 +43,23 @@ __device__ __forceinline__ void store_scale(float *row, int b, int blocks, int p
         for (int i = blocks; i < pitch; ++i) row[i] = 0.0f;
 }
 
-// Blocks of one row: a lane has 16 bytes of numbers at a time - 16 or 32 lanes to a block -, kUnits times.  Memory bounds it: 4096 rows of 25088 bf16, 308 MB, 51 us, 6.0 TB/s;
-// 257 rows of 9219 fp16 4.4 us, most of them a launch.
+// Blocks of one row: a lane has 16 bytes of numbers at a time - 16 or 32 lanes to a block -, of what goes past the caches kUnits times (4096 rows of
+// 25088 bf16, 308 MB, 51 us, 6.0 TB/s; once 54), else once (333 rows of 1100 fp16 2.6 us, else 3.5; 4096 of 4096 bf16 9.6, else 10.1).  Memory bounds the first, a launch and
+// one trip there and back the smallest.
 template <class T, bool STREAM> __global__ __launch_bounds__(256) void f8_rows_kernel(ToArgs a)
 {
     constexpr int V = Unit<T>::kValues, kLanes = kBlock / V;
-    float x[kUnits][V];
-    const uint32_t first = blockIdx.x * (256u * kUnits) + threadIdx.x;
+    constexpr int kTimes = STREAM ? kUnits : 1;
+    float x[kTimes][V];
+    const uint32_t first = blockIdx.x * (256u * kTimes) + threadIdx.x;
 #pragma unroll
-    for (int i = 0; i < kUnits; ++i) {
+    for (int i = 0; i < kTimes; ++i) {
         const uint32_t u = min(first + i * 256u, a.units - 1), row = a.per_row.quotient(u);
         const int k0 = (int)(u - row * a.per_row.d) * V;
         load_numbers<T, STREAM>((const T *)a.X + (int64_t)row * a.stride + k0, a.K - k0, x[i]);
     }
 #pragma unroll
-    for (int i = 0; i < kUnits; ++i) {
+    for (int i = 0; i < kTimes; ++i) {
         const uint32_t u = first + i * 256u;
         const Scale s = scale_of(top_of_lanes<kLanes>(top_bits<V>(x[i])));       // (a row has whole blocks: the lanes of one are beyond the end together)
         if (u >= a.units) continue;
@@ -99,23 +101,24 @@ template <class T, bool STREAM> __global__ __launch_bounds__(256) void f8_blocks
     if (threadIdx.x == 0) store_scale(a.scales + (int64_t)tall * a.pitch, b, blocks, a.pitch, s.scale);
 }
 
-// Back: a lane makes 16 bytes of numbers, kUnits times.
+// Back: a lane makes 16 bytes of numbers, of what goes past the caches kUnits times.
 template <class T, bool STREAM>
 __global__ __launch_bounds__(256) void f8_back_kernel(const uint8_t *__restrict__ values, const float *__restrict__ scales, int64_t row0, int block_rows, uint32_t units,
                                                       Div per_row, int K, int pitch, T *__restrict__ Y, int64_t stride)
 {
     constexpr int V = Unit<T>::kValues, kLanes = kBlock / V;
-    uint32_t c[kUnits][V / 4];
-    float s[kUnits];
-    const uint32_t first = blockIdx.x * (256u * kUnits) + threadIdx.x;
+    constexpr int kTimes = STREAM ? kUnits : 1;
+    uint32_t c[kTimes][V / 4];
+    float s[kTimes];
+    const uint32_t first = blockIdx.x * (256u * kTimes) + threadIdx.x;
 #pragma unroll
-    for (int i = 0; i < kUnits; ++i) {
+    for (int i = 0; i < kTimes; ++i) {
         const uint32_t u = min(first + i * 256u, units - 1), row = per_row.quotient(u);
         __builtin_memcpy(c[i], values + (uint64_t)u * V, V);
         s[i] = scales[(row0 + row) / block_rows * pitch + (u - row * per_row.d) / kLanes];
     }
 #pragma unroll
-    for (int i = 0; i < kUnits; ++i) {
+    for (int i = 0; i < kTimes; ++i) {
         const uint32_t u = first + i * 256u;
         if (u >= units) return;
         const uint32_t row = per_row.quotient(u);
@@ -155,7 +158,11 @@ template <class F> static int32_t in_pieces(int64_t rows, uint32_t per_row, F la
     return CL_OK;
 }
 
-static dim3 grid_of(uint32_t units) { return dim3((units + 256 * kUnits - 1) / (256 * kUnits)); }
+static dim3 grid_of(uint32_t units, bool stream)
+{
+    const uint32_t each = 256 * (stream ? kUnits : 1);
+    return dim3((units + each - 1) / each);
+}
 
 int32_t launch_rows_to_f8(const void *X, int32_t type, int64_t stride, int64_t rows, int32_t K, uint8_t *values, float *scales, hipStream_t st)
 {
@@ -167,8 +174,8 @@ int32_t launch_rows_to_f8(const void *X, int32_t type, int64_t stride, int64_t r
         const bool stream = past_caches(rows * K * (int64_t)sizeof(T));
         return in_pieces(rows, per_row, [&](int64_t r, uint32_t units) {
             const ToArgs a{(const T *)X + r * stride, values + r * blocks * kBlock, scales + r * pitch, stride, make_div(per_row), units, K, pitch};
-            if (stream) hipLaunchKernelGGL((f8_rows_kernel<T, true>), grid_of(units), dim3(256), 0, st, a);
-            else hipLaunchKernelGGL((f8_rows_kernel<T, false>), grid_of(units), dim3(256), 0, st, a);
+            if (stream) hipLaunchKernelGGL((f8_rows_kernel<T, true>), grid_of(units, true), dim3(256), 0, st, a);
+            else hipLaunchKernelGGL((f8_rows_kernel<T, false>), grid_of(units, false), dim3(256), 0, st, a);
         });
     });
 }
@@ -232,7 +239,7 @@ extern "C" int32_t cl_eight_dequantize(const void *d_values, const float *d_scal
         const bool stream_it = past_caches(rows * K * (int64_t)sizeof(T));
         return in_pieces(rows, per_row, [&](int64_t r, uint32_t units) {
             auto kernel = stream_it ? f8_back_kernel<T, true> : f8_back_kernel<T, false>;
-            hipLaunchKernelGGL(kernel, grid_of(units), dim3(256), 0, (hipStream_t)stream, (const uint8_t *)d_values + r * blocks * kBlock, d_scales, r, (int)block_rows, units,
+            hipLaunchKernelGGL(kernel, grid_of(units, stream_it), dim3(256), 0, (hipStream_t)stream, (const uint8_t *)d_values + r * blocks * kBlock, d_scales, r, (int)block_rows, units,
                                make_div(per_row), (int)K, (int)scales_of(K), (T *)d_Y + r * y_stride, y_stride);
         });
     });
