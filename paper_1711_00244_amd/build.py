@@ -3,6 +3,7 @@ from __future__ import annotations
 
 import os
 import subprocess
+from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
@@ -34,18 +35,21 @@ def _run(cmd, verbose):
 
 
 def build_library(verbose: bool = False) -> str:
-    """Host sources go through g++, the kernels through hipcc; hipcc links."""
+    """Host sources go through g++, the kernels through hipcc, four at a time; hipcc links."""
     bdir = os.path.join(HERE, "_build")
     os.makedirs(bdir, exist_ok=True)
     inc = ["-I", os.path.join(ROOT, "include"), "-I", CSRC]
-    objs = []
-    for s in SOURCES:
+
+    def compile_one(s):
         obj = os.path.join(bdir, s.replace("/", "_") + ".o")
         if s.endswith(".hip"):
             _run([hipcc(), *[f for f in HIPCC_FLAGS if f != "-shared"], *inc, "-c", os.path.join(CSRC, s), "-o", obj], verbose)
         else:
             _run(["g++", "-O2", "-std=c++17", "-fPIC", "-Wall", *inc, "-c", os.path.join(CSRC, s), "-o", obj], verbose)
-        objs.append(obj)
+        return obj
+
+    with ThreadPoolExecutor(4) as pool:
+        objs = list(pool.map(compile_one, SOURCES))
     _run([hipcc(), "-shared", "-fPIC", "--offload-arch=gfx950", *objs, "-o", LIB], verbose)
     return LIB
 
