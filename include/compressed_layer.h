@@ -668,8 +668,8 @@ int32_t cl_eight_dequantize(const void *d_values, const float *d_scales, int64_t
  *  d_Y, y_type     CL_F32, CL_BF16, CL_F16 (y_stride; may be d_X itself where type and stride are X's), or CL_F8: values, and scales at
  *                  d_y_scales, as cl_eight_quantize makes them of the fp32 result
  * Run-to-run identical.  Zero rows are no error.
- * Errors: CL_EINVAL (null pointers, sizes, alignment, overlapping rows, eps), CL_EUNSUPPORTED (K above CL_F8_MAX_K) - nothing is launched then;
- * CL_EHIP. */
+ * Errors: CL_EINVAL (null pointers, sizes, alignment, overlapping rows, one matrix in place of another of other type or stride, eps), CL_EUNSUPPORTED (K above
+ * CL_F8_MAX_K) - nothing is launched then; CL_EHIP. */
 typedef struct {
     const void *d_X, *d_residual, *d_gain;
     void *d_sum, *d_Y;
@@ -686,8 +686,8 @@ int32_t cl_rms_norm(const cl_norm_call *call, void *stream);
  *  X         batch rows of W->K             d_bias   W->rows fp32 or NULL
  *  act       CL_ACT_NONE, CL_ACT_RELU, or CL_ACT_GATED: output i is g / (1 + exp(-g)) u with g from row i of W and u from row rows / 2 + i (the rows of
  *            a pair are not neighbours here as they are for 4-bit matrices: a block of 128 of them has one scale)
- *  d_Y       batch rows of W->rows (CL_ACT_GATED: half as many) of y_type, overwritten; CL_F8: values, and scales at d_y_scales, as
- *            cl_eight_quantize makes them of the fp32 result
+ *  d_Y       batch rows of W->rows (CL_ACT_GATED: half as many) of y_type, overwritten, apart from X; CL_F8: values, and scales at d_y_scales,
+ *            as cl_eight_quantize makes them of the fp32 result
  *  d_workspace  at least cl_eight_fc_workspace_bytes(), 256-byte aligned; NULL will do where that is 0.  What is asked for a batch is enough for
  *            every smaller one: a call whose workspace has no room for what its fastest form needs takes another that does with it (slower, and
  *            with another order of the sums)

@@ -246,6 +246,13 @@ static int32_t check_operand(const char *name, const void *p, int32_t type, int6
     return CL_OK;
 }
 
+// What is written over what is read has to have its elements where those are.
+static int32_t check_in_place(const char *name, const void *to, int32_t to_type, int64_t to_stride, const void *from, const cl_norm_call &c, int64_t from_stride)
+{
+    if (to == from && (to_type != c.type || (c.rows > 1 && to_stride != from_stride))) return fail(CL_EINVAL, "%s: in place, but of another type or stride", name);
+    return CL_OK;
+}
+
 extern "C" int32_t cl_rms_norm(const cl_norm_call *call, void *stream)
 {
     if (!call) return fail(CL_EINVAL, "null pointer");
@@ -261,7 +268,11 @@ extern "C" int32_t cl_rms_norm(const cl_norm_call *call, void *stream)
         if (int32_t rc = check_operand("residual", c.d_residual, c.type, c.residual_stride, c.rows, c.K)) return rc;
         if (int32_t rc = check_operand("sum", c.d_sum, c.type, c.sum_stride, c.rows, c.K)) return rc;
         if (c.d_sum == c.d_Y) return fail(CL_EINVAL, "the sum and the output are one");
+        if (int32_t rc = check_in_place("sum", c.d_sum, c.type, c.sum_stride, c.d_X, c, c.x_stride)) return rc;
+        if (int32_t rc = check_in_place("sum", c.d_sum, c.type, c.sum_stride, c.d_residual, c, c.residual_stride)) return rc;
+        if (int32_t rc = check_in_place("Y", c.d_Y, c.y_type, c.y_stride, c.d_residual, c, c.residual_stride)) return rc;
     }
+    if (int32_t rc = check_in_place("Y", c.d_Y, c.y_type, c.y_stride, c.d_X, c, c.x_stride)) return rc;
     if (c.d_gain) {
         if (c.gain_type != CL_F32 && c.gain_type != c.type) return fail(CL_EINVAL, "a gain is of type CL_F32 or of X's own, got %d", (int)c.gain_type);
         if (!aligned(c.d_gain, type_bytes(c.gain_type))) return fail(CL_EINVAL, "gain: elements are not aligned");

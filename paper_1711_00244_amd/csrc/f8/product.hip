@@ -327,6 +327,7 @@ static int32_t check_forward(const cl_f8_matrix *W, int32_t batch, int32_t x_typ
 static int32_t check_pointers(const cl_f8_matrix *W, const cl_f8_input *X, const void *Y, const void *y_scales, int32_t y_type, int64_t rows)
 {
     if (!W->d_values || !W->d_scales || !X->d_X || !Y) return fail(CL_EINVAL, "null pointer");
+    if (Y == X->d_X) return fail(CL_EINVAL, "the output and the input are one");
     if (!aligned(W->d_values, 16) || !aligned(W->d_scales, 16)) return fail(CL_EINVAL, "values and scales must be 16-byte aligned");
     if (X->type == CL_F8) {
         if (!X->d_scales) return fail(CL_EINVAL, "null pointer");

@@ -12,6 +12,7 @@ from paper_1711_00244_amd.binding import CL_EINVAL, CL_EUNSUPPORTED, CL_OK, F8In
 
 P = C.c_void_p(4096)              # an aligned address that no refused call touches
 ODD = C.c_void_p(4097)
+Y = C.c_void_p(1 << 20)             # another
 NAN, INF = float("nan"), float("inf")
 
 
@@ -40,6 +41,10 @@ def test_norm():
                dict(d_residual=4096, d_sum=8192, sum_stride=63), dict(d_residual=4097, d_sum=8192), dict(d_residual=8192, d_sum=4096), dict(d_gain=4096, gain_type=2),
                dict(d_gain=4098, gain_type=0), dict(d_gain=4097, gain_type=1), dict(y_type=4), dict(y_type=4, d_y_scales=4104), dict(y_type=4, d_Y=4104, d_y_scales=4096)):
         assert call(**kw) == CL_EINVAL, kw
+    # in place, with elements elsewhere
+    for kw in (dict(y_type=0), dict(y_type=2), dict(y_stride=65), dict(y_type=4, d_y_scales=8192), dict(d_Y=12288, d_residual=8192, d_sum=4096, sum_stride=65),
+               dict(d_Y=12288, d_residual=8192, d_sum=8192, residual_stride=70), dict(d_X=12288, d_residual=4096, d_sum=8192, y_type=0)):
+        assert call(**kw) == CL_EINVAL, kw
     assert call(K=(1 << 24) + 1, x_stride=1 << 25, y_stride=1 << 25) == CL_EUNSUPPORTED
     assert L.cl_rms_norm(None, None) == CL_EINVAL
     assert call(rows=0, d_X=None, d_Y=None) == CL_OK
@@ -59,7 +64,7 @@ def test_product():
     assert L.cl_eight_fc_workspace_bytes(F8Matrix(4096, 4096, 2**31 - 1, 200), 1, 0, 0, 0, n) == CL_EUNSUPPORTED
     big = 1 << 24
 
-    def call(W=W, X=X, y=P, ys=P, y_type=0, batch=30000, act=0, ws=P, ws_bytes=big):
+    def call(W=W, X=X, y=Y, ys=P, y_type=0, batch=30000, act=0, ws=P, ws_bytes=big):
         return L.cl_eight_fc_forward(W, X, None, y, ys, y_type, batch, act, ws, ws_bytes, None)
 
     assert call(W=None) == CL_EINVAL and call(X=None) == CL_EINVAL and call(y=None) == CL_EINVAL
@@ -72,6 +77,7 @@ def test_product():
     assert call(X=F8Input(4096, None, 0, 199)) == CL_EINVAL and call(X=F8Input(4096, None, 4, 0)) == CL_EINVAL and call(X=F8Input(4098, None, 0, 200)) == CL_EINVAL
     assert call(X=F8Input(4104, 4096, 4, 0)) == CL_EINVAL and call(X=F8Input(4096, 4104, 4, 0)) == CL_EINVAL
     assert call(ws=None) == CL_EINVAL and call(ws_bytes=16) == CL_EINVAL and call(ws=C.c_void_p(4096 + 16)) == CL_EINVAL
+    assert call(y=P) == CL_EINVAL and "one" in L.cl_last_error().decode()             # the input's own place
     assert call(batch=0, y=None, ws=None, ws_bytes=0) == CL_OK
 
 
