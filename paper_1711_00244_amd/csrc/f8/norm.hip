@@ -197,12 +197,13 @@ template <class T, class Y> static int32_t launch_norm(NormArgs a, hipStream_t s
     constexpr int V = Unit<T>::kValues;
     a.units = std::is_same_v<Y, F8Out> ? a.blocks * (kBlock / V) : (a.K + V - 1) / V;
     // many rows: a lane has 64 bytes or 16 (16384 rows of 4096 bf16 with sum and 8-bit output, 4 times 77 us, 2 times 81, 8 times 82, once 94; 65536 of 1024 76, once
-    // 91); few: as many lanes as there is work for (512 rows of 4096 5.3, four times 6.5; one row 3.4 and 6.9)
-    const int want = a.rows >= (1 << 20) / a.units ? 4 : 1;
+    // 91); few: as many lanes as there is work for (512 rows of 4096 5.3, four times 6.5; one row 3.4 and 6.9).  Lanes and times, which are the order that squares are added in,
+    // go by the units of whole blocks, a block's at the least, whatever the output's type: so 8 bits are those of the fp32 result.
+    const int whole = a.blocks * (kBlock / V), want = a.rows >= (1 << 20) / whole ? 4 : 1;
     int times = 1;
-    a.lanes = kBlock / V;                                    // (a block's; whatever the output's type, so that 8 bits are those of the fp32 result)
-    while (a.lanes < 1024 && a.lanes * want < a.units) a.lanes *= 2;
-    while (times <= 8 && a.lanes * times < a.units) times *= 2;
+    a.lanes = kBlock / V;
+    while (a.lanes < 1024 && a.lanes * want < whole) a.lanes *= 2;
+    while (times <= 8 && a.lanes * times < whole) times *= 2;
     const int threads = std::max(256, a.lanes), each = threads / a.lanes;
     const int64_t step = (int64_t)(UINT32_MAX / threads) * each, all = a.rows;
     for (int64_t r = 0; r < all; r += step) {
