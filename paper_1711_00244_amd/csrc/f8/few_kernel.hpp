@@ -145,6 +145,6 @@ template <class X, class T, bool GATED, bool WIDE> __global__ __launch_bounds__(
 #pragma unroll
         for (int f = 0; f < F; ++f) store_part(p, 0, row, o, v[f], f * p.value_at);
     } else {
-        store_outputs<T>(p, row, o, activated<GATED>(p, o, v[0], v[F - 1]));
+        store_outputs<T>(p, row, o, activated<T, GATED>(p, o, v[0], v[F - 1]));
     }
 }

@@ -105,7 +105,7 @@ __device__ __forceinline__ void store_tile(const ProductArgs &a, int split, int 
 #pragma unroll
             for (int i = 0; i < kPieces; ++i) {
                 const int o = first + i * 16 + 4 * g;
-                f32x4 v = activated<GATED>(a, o, acc[i][j], acc[GATED ? kPieces + i : i][j]);
+                f32x4 v = activated<T, GATED>(a, o, acc[i][j], acc[GATED ? kPieces + i : i][j]);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     v[e] = o + e < a.width ? v[e] : 0.0f;
@@ -159,8 +159,8 @@ __device__ __forceinline__ void store_tile(const ProductArgs &a, int split, int 
         for (int i = 0; i < kPieces; i += 2) {
 #pragma unroll
             for (int j = 0; j < TJ; ++j) {
-                const f32x4 v = activated<GATED>(a, first + i * 16 + 4 * g, acc[i][j], acc[GATED ? kPieces + i : i][j]);
-                const f32x4 u = activated<GATED>(a, first + i * 16 + 16 + 4 * g, acc[i + 1][j], acc[GATED ? kPieces + i + 1 : i + 1][j]);
+                const f32x4 v = activated<T, GATED>(a, first + i * 16 + 4 * g, acc[i][j], acc[GATED ? kPieces + i : i][j]);
+                const f32x4 u = activated<T, GATED>(a, first + i * 16 + 16 + 4 * g, acc[i + 1][j], acc[GATED ? kPieces + i + 1 : i + 1][j]);
                 const T four[2][4] = {{(T)v[0], (T)v[1], (T)v[2], (T)v[3]}, {(T)u[0], (T)u[1], (T)u[2], (T)u[3]}};
                 u32x2 lo, hi;
                 __builtin_memcpy(&lo, four[0], 8);
@@ -186,7 +186,7 @@ __device__ __forceinline__ void store_tile(const ProductArgs &a, int split, int 
             const int o = first + i * 16 + 4 * g;
 #pragma unroll
             for (int j = 0; j < TJ; ++j) {
-                const f32x4 v = activated<GATED>(a, o, acc[i][j], acc[GATED ? kPieces + i : i][j]);
+                const f32x4 v = activated<T, GATED>(a, o, acc[i][j], acc[GATED ? kPieces + i : i][j]);
                 if (c_first + j * 16 < a.rows) store_outputs<T>(a, c_first + j * 16, o, v);
             }
         }
