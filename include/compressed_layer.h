@@ -651,10 +651,10 @@ typedef struct {
 
 /* Rows of numbers to that form, and back.  The scale of a block is fl(largest magnitude / 448), at least 2^-126; a value becomes the nearest 8-bit
  * float, ties to even, of fl(x fl(448 / largest magnitude)) (x 2^126 under the least scale), fl() rounding to fp32.  A block with a value that is
- * not finite is NaN as a whole.  Zero rows are no error.
+ * not finite is NaN as a whole.  Not in place: numbers, values and scales are apart.  Zero rows are no error.
  *  type      CL_F32, CL_BF16 or CL_F16    x_stride, y_stride   elements from row to row, at least K
  *  block_rows  rows under a scale: 1 or 128 (the last rows of blocks of 128 as many as are left)
- * Errors: CL_EINVAL (null pointers, sizes, alignment, overlapping rows), CL_EUNSUPPORTED (K above CL_F8_MAX_K) - nothing is
+ * Errors: CL_EINVAL (null pointers, sizes, alignment, overlapping rows, one buffer for two), CL_EUNSUPPORTED (K above CL_F8_MAX_K) - nothing is
  * launched then; CL_EHIP. */
 int32_t cl_eight_quantize(const void *d_X, int32_t type, int64_t x_stride, int64_t rows, int32_t K, int32_t block_rows, void *d_values, float *d_scales, void *stream);
 int32_t cl_eight_dequantize(const void *d_values, const float *d_scales, int64_t rows, int32_t K, int32_t block_rows, void *d_Y, int32_t type, int64_t y_stride,

@@ -214,6 +214,7 @@ static int32_t check_rows(const void *x, const void *values, const void *scales,
     if (K > CL_F8_MAX_K) return fail(CL_EUNSUPPORTED, "rows of more than %d elements", (int)CL_F8_MAX_K);
     if (rows == 0) return CL_OK;
     if (!x || !values || !scales) return fail(CL_EINVAL, "null pointer");
+    if (x == values || x == scales || values == scales) return fail(CL_EINVAL, "numbers, values and scales: two of them are one");
     if (rows > 1 && stride < K) return fail(CL_EINVAL, "rows of %d elements overlap at a stride of %lld", (int)K, (long long)stride);
     if (!aligned(values, 16) || !aligned(scales, 16)) return fail(CL_EINVAL, "values and scales must be 16-byte aligned");
     if (!aligned(x, type_bytes(type))) return fail(CL_EINVAL, "elements are not aligned");
