@@ -248,6 +248,7 @@ template <Form F, class T, bool GATED, bool WIDE> static int32_t launch_tiles(Pr
     const int64_t row_tiles = row_tiles_of(F, a.width, GATED), columns = columns_of(F, a.rows, WIDE);
     a.band_tiles = make_div((uint32_t)row_tiles * 4u);
     const int fours = (a.blocks + 3) / 4;
+    if (c.splits < 1 || c.splits > fours) return fail(CL_EINVAL, "%d blocks of k in %d shares", a.blocks, c.splits);      // (a share without steps would read off its operands)
     a.split_fours = fours / c.splits;
     a.split_more = fours % c.splits;
     const size_t wgs = round_up(row_tiles * columns, 8);
