@@ -41,7 +41,7 @@ class ExpertLayer:
             raise ValueError(f"up {up.shape} and down {down.shape} are not the matrices of gated experts")
         if shared is not None:
             first, second = shared
-            if isinstance(first, cl.F8Tensor):
+            if isinstance(first, cl.F8Tensor) or isinstance(second, cl.F8Tensor):
                 feed_forward.check_gated(first, second)
             if len(first.shape) != 2 or first.K != width or first.shape[0] % 2 or second.shape != (width, first.shape[0] // 2):
                 raise ValueError(f"{first.shape} and {second.shape} are not the matrices of a gated expert of width {width}")
