@@ -43,7 +43,7 @@ def check_gated(up, down):
         raise ValueError(f"the matrices of a gated block must be two F8Tensors, are {type(up).__name__} and {type(down).__name__}")
     if up.block_rows != 128 or down.block_rows != 128 or down.gated or len(up.shape) != 2 or up.shape[0] % 2 or tuple(down.shape) != (up.K, up.shape[0] // 2):
         raise ValueError(f"{up.shape} and {down.shape} are not the matrices of a gated block in blocks of 128 rows")
-    if up.shape[0] == 0 or (not up.gated and up.shape[0] % 256):
+    if not up.gated and up.shape[0] % 256:
         raise ValueError(f"{up.shape}: gates and values in halves that are no multiple of 128 rows have to be put together by f8_gated")
 
 

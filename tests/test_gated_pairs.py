@@ -23,7 +23,7 @@ def four(*shape):
 
 
 TAKEN = [(eight(1400, 256, gated=True), eight(256, 700)), (eight(512, 256), eight(256, 256)), (eight(512, 256, gated=True), eight(256, 256)), (eight(2, 256, gated=True), eight(256, 1))]
-REFUSED = [(eight(1400, 256), eight(256, 700)), (eight(2, 256), eight(256, 1)), (eight(0, 256), eight(256, 0)), (eight(512, 256), four(256, 256)), (four(512, 256), eight(256, 256)),
+REFUSED = [(eight(1400, 256), eight(256, 700)), (eight(2, 256), eight(256, 1)), (eight(512, 256), four(256, 256)), (four(512, 256), eight(256, 256)),
            (eight(512, 256), eight(256, 256, gated=True)), (eight(512, 256, 1), eight(256, 256)), (eight(512, 256), eight(256, 256, 1)), (eight(512, 256), eight(256, 384))]
 
 
