@@ -19,7 +19,6 @@ struct FewArgs {
     int64_t x_stride;
     Div per_row;                                             // eights of a row's values
     int K;
-    int64_t column0;
     int columns;                                             // most of a workgroup
     int waves;                                               // wavefronts that multiply; the others only quantise
 };
@@ -36,7 +35,7 @@ template <class X, class T, bool GATED, bool WIDE> __global__ __launch_bounds__(
     const ProductArgs &p = a.p;
     const int waves = a.waves, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
     const int o0 = (int)blockIdx.x * 16;
-    const int64_t c0 = a.column0 + (int64_t)blockIdx.y * kFewColumns;
+    const int64_t c0 = (int64_t)blockIdx.y * kFewColumns;
     const int columns = (int)min((int64_t)a.columns, p.rows - c0);
     const int64_t row_bytes = (int64_t)p.blocks * kBlock;
     uint8_t *codes = lds;

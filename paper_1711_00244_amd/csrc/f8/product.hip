@@ -266,15 +266,10 @@ template <class X, class T, bool GATED, bool WIDE> static int32_t launch_few(con
     const size_t sums = (size_t)few_waves(s.blocks) * (GATED ? 2 : 1) * 64 * sizeof(f32x4);
     static LdsLimit seen;
     if (int32_t rc = allow_lds((const void *)kernel, kFewLds + kFewWaves * 2 * 64 * sizeof(f32x4), seen)) return rc;
-    FewArgs f{a, x.d_X, x.stride, make_div((uint32_t)s.blocks * (kBlock / 8)), K, 0, columns, few_waves(s.blocks)};
-    // (a grid is at most 65535 high: taller ones go in pieces)
-    const int64_t groups = ((int64_t)s.batch + kFewColumns - 1) / kFewColumns;
-    for (int64_t g = 0; g < groups; g += 65535) {
-        f.column0 = g * kFewColumns;
-        hipLaunchKernelGGL(kernel, dim3((unsigned)((s.width + 15) / 16), (unsigned)std::min<int64_t>(groups - g, 65535)), dim3((unsigned)few_threads(s, kOwn)),
-                           (kOwn ? few_lds(s.blocks, columns) : 0) + sums, st, f);
-        MX_HIP_TRY(hipGetLastError());
-    }
+    const FewArgs f{a, x.d_X, x.stride, make_div((uint32_t)s.blocks * (kBlock / 8)), K, columns, few_waves(s.blocks)};
+    hipLaunchKernelGGL(kernel, dim3((unsigned)((s.width + 15) / 16), (unsigned)((s.batch + kFewColumns - 1) / kFewColumns)), dim3((unsigned)few_threads(s, kOwn)),
+                       (kOwn ? few_lds(s.blocks, columns) : 0) + sums, st, f);
+    MX_HIP_TRY(hipGetLastError());
     return CL_OK;
 }
 
@@ -391,6 +386,7 @@ constexpr FewPrice kFewPrices[2] = {{2.55f, 0.103f, 0.003f, 0.71f, 0.0015f}, {3.
 // The quantisation of X, the sum of partial sums.  A launch costs the host, besides, some 4 us, which calls one by one pay, and calls recorded in a graph do not: half of it counts.
 constexpr float kLaunch = 2.0f;
 constexpr int32_t kFewMostRows = 256;                        // (beyond, tiles are always faster)
+static_assert(kFewMostRows / kFewColumns < 65536, "");       // (the height of its grid)
 
 static float price_of(const Shape &s, const Choice &c)
 {
