@@ -234,15 +234,15 @@ static bool fits_grid(const Choice &c, const Shape &s)
 
 template <Form F, class T, bool GATED, bool WIDE> static int32_t launch_tiles(ProductArgs a, const Choice &c, hipStream_t st)
 {
-    using C = std::conditional_t<F == kTile256, std::conditional_t<WIDE, Tile<256, 128, 4, 2, 2>, Tile<256, 256, 2, 4, 2>>,
-                                 std::conditional_t<F == kTile128, SmallTile<128, 128, 2, 4, 4>, SmallTile<64, 64, 2, 2, 4>>>;
+    using C = std::conditional_t<F == kTile256, std::conditional_t<WIDE, Tile<256, 128, 4, 2>, Tile<256, 256, 2, 4>>,
+                                 std::conditional_t<F == kTile128, SmallTile<128, 128, 2, 4>, SmallTile<64, 64, 2, 2>>>;
     static_assert(C::kThreads == kFormThreads[F], "");
     constexpr size_t kLds = C::kLds + (std::is_same_v<T, F8Out> ? C::kTops : 0);
     void (*kernel)(ProductArgs, int);
-    if constexpr (F == kTile256 && WIDE) kernel = f8_tile_kernel<256, 128, 4, 2, 2, T, GATED, WIDE>;
-    else if constexpr (F == kTile256) kernel = f8_tile_kernel<256, 256, 2, 4, 2, T, GATED, WIDE>;
-    else if constexpr (F == kTile128) kernel = f8_small_tile_kernel<128, 128, 2, 4, 4, 2, T, GATED, WIDE>;
-    else kernel = f8_small_tile_kernel<64, 64, 2, 2, 4, 2, T, GATED, WIDE>;
+    if constexpr (F == kTile256 && WIDE) kernel = f8_tile_kernel<256, 128, 4, 2, T, GATED, WIDE>;
+    else if constexpr (F == kTile256) kernel = f8_tile_kernel<256, 256, 2, 4, T, GATED, WIDE>;
+    else if constexpr (F == kTile128) kernel = f8_small_tile_kernel<128, 128, 2, 4, T, GATED, WIDE>;
+    else kernel = f8_small_tile_kernel<64, 64, 2, 2, T, GATED, WIDE>;
     static LdsLimit seen;
     if (int32_t rc = allow_lds((const void *)kernel, kLds, seen)) return rc;
     const int64_t row_tiles = row_tiles_of(F, a.width, GATED), columns = columns_of(F, a.rows, WIDE);

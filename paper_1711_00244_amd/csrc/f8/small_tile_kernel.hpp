@@ -9,29 +9,29 @@
 //
 // 256 rows of X, 4096 x 9216, fp32 outputs, WIDE: 128 x 128 in four shares of k 33 us with the sum of the shares (a compute unit has one workgroup, of 18 steps), 64 x 64 in
 // two 35, in three 38; 333 rows of 2 x 2900 x 1100 gated, fp16: 128 x 128 8.2 us.
-template <int BM, int BN, int WM, int WN, int D> struct SmallTile {
+template <int BM, int BN, int WM, int WN> struct SmallTile {
     static constexpr int kWaves = WM * WN, kThreads = kWaves * 64;
     static constexpr int TI = BM / WM / 16, TJ = BN / WN / 16;
     static constexpr int kRun = TI * 8;                      // rows under one scale: half of a wavefront's
     static constexpr int kLoads = (BM + BN) / 8 / kWaves;    // of a wavefront and step
     static constexpr int kScaleLoads = BN / 64 + 1;          // of the workgroup and four steps: columns, then the wavefronts' rows
     static constexpr int kScaleShare = (kScaleLoads + kWaves - 1) / kWaves;      // (wavefronts beyond that number repeat the last)
-    static constexpr int kBuffer = (BM + BN) * kBlock;
-    static constexpr int kScales = D * kBuffer;              // where the scales start: two buffers of four steps
+    static constexpr int kBuffer = (BM + BN) * kBlock, kSteps = 4;       // of a step, and how many LDS holds
+    static constexpr int kScales = kSteps * kBuffer;         // where the scales start: two buffers of four steps
     static constexpr int kScaleBuffer = (BN + 64) * 16;
     static constexpr int kLds = kScales + 2 * kScaleBuffer, kTops = WM * BN * 4;
     static constexpr int share(int n, int of, int i) { return n * i / of; }
     static constexpr int kColumnPieces = TI > 2 ? TI / 2 : 1;          // pieces at whose beginning columns of the next step are read
     static_assert(TI % 2 == 0 && TI > 0 && TJ > 0 && 128 % kRun == 0, "");
     static_assert(BM % (8 * kWaves) == 0 && BN % (8 * kWaves) == 0 && kRun % 8 == 0 && BN % 64 == 0 && 2 * WM <= 64, "");
-    static_assert(D >= 3 && D <= 5 && (D - 1) * kLoads + 2 * kScaleShare < 64, "");
+    static_assert((kSteps - 1) * kLoads + 2 * kScaleShare < 64, "");             // (the count that a wait names)
 };
 
-template <int BM, int BN, int WM, int WN, int D, int OCCUPANCY, class T, bool GATED, bool WIDE>
-__global__ __launch_bounds__(WM * WN * 64, OCCUPANCY) void f8_small_tile_kernel(ProductArgs a, int row_tiles)
+template <int BM, int BN, int WM, int WN, class T, bool GATED, bool WIDE>
+__global__ __launch_bounds__(WM * WN * 64, 2) void f8_small_tile_kernel(ProductArgs a, int row_tiles)
 {
-    using C = SmallTile<BM, BN, WM, WN, D>;
-    constexpr int TI = C::TI, TJ = C::TJ, kSets = WIDE ? 1 : 2;
+    using C = SmallTile<BM, BN, WM, WN>;
+    constexpr int TI = C::TI, TJ = C::TJ, kSteps = C::kSteps, kSets = WIDE ? 1 : 2;
     extern __shared__ __align__(128) uint8_t lds[];
     typedef __attribute__((address_space(3))) void *lds_ptr;
     typedef const __attribute__((address_space(1))) void *global_ptr;
@@ -163,25 +163,24 @@ __global__ __launch_bounds__(WM * WN * 64, OCCUPANCY) void f8_small_tile_kernel(
         __builtin_amdgcn_sched_barrier(0);
     };
     // (requests beyond the last step repeat it, so that a wait always counts the same; nothing uses what they bring, nor what is read of a step beyond the last)
-    int to = D - 1;                                          // the buffer that is asked for: that of the step before
+    int to = kSteps - 1;                                     // the buffer that is asked for: that of the step before
     auto step = [&](auto P, int t) __attribute__((always_inline)) {
-        // every wavefront's loads of step t + 1 have arrived - those of t + 2 .. t + D - 2 may be on their way -, and what it read of step t - 1 it has multiplied
-        meet(std::integral_constant<int, (D - 3) * C::kLoads>{});
-        const int ask = min(t + D - 1, last);
-        if ((t + D - 1) % 4 == 0) request_scales(ask / 4, scales((t + D - 1) / 4));
-        const uint8_t *next = lds + (to + 2 < D ? to + 2 : to + 2 - D) * C::kBuffer, *scales_next = scales((t + 1) / 4) + (t + 1) % 4 * 4;
+        // every wavefront's loads of step t + 1 have arrived - those of t + 2 may be on their way -, and what it read of step t - 1 it has multiplied
+        meet(std::integral_constant<int, C::kLoads>{});
+        const int ask = min(t + kSteps - 1, last);
+        if ((t + kSteps - 1) % 4 == 0) request_scales(ask / 4, scales((t + kSteps - 1) / 4));
+        const uint8_t *next = lds + (to + 2 < kSteps ? to + 2 : to + 2 - kSteps) * C::kBuffer, *scales_next = scales((t + 1) / 4) + (t + 1) % 4 * 4;
         each<0, TI>([&](auto I) __attribute__((always_inline)) { piece(I, P, next, scales_next, lds + to * C::kBuffer, ask); });
-        to = to + 1 < D ? to + 1 : 0;
+        to = to + 1 < kSteps ? to + 1 : 0;
     };
 
     request_scales(0, scales(0));
 #pragma unroll
-    for (int t = 0; t < D - 1; ++t) {
-        if (t == 4) request_scales(min(t, last) / 4, scales(1));
+    for (int t = 0; t < kSteps - 1; ++t) {
 #pragma unroll
         for (int k = 0; k < C::kLoads; ++k) request(min(t, last), lds + t * C::kBuffer, k);
     }
-    meet(std::integral_constant<int, (D - 2) * C::kLoads>{});
+    meet(std::integral_constant<int, (kSteps - 2) * C::kLoads>{});
 #pragma unroll
     for (int j = 0; j < TJ; ++j) x[0][j] = read_piece(lds, wj + j * 16), sx[j] = scale_of_column(scales(0), j);
     sw[0] = scale_of_run(scales(0), 0);

@@ -5,7 +5,7 @@
 // A workgroup of WM x WN wavefronts makes BM rows of W of BN columns (rows of X), a wavefront TI x TJ pieces of 16 x 16.  GATED: half of a wavefront's rows are
 // gates, the other half their values, so that a lane has both of an output.  A step is one block of 128 k.
 //
-// LDS holds D steps.  The loads themselves write it.  A wavefront's rows go through registers R pieces at a time, its columns, which a whole step uses, stay
+// LDS holds two steps.  The loads themselves write it.  A wavefront's rows go through registers R pieces at a time, its columns, which a whole step uses, stay
 // there, replaced one by one behind their last use.  A piece's sum (it starts at zero in each step) is multiplied by the scales when its register is needed for the piece
 // after it.
 //
@@ -19,7 +19,7 @@
 //
 // In LDS a row's eight units of 16 bytes are 128 consecutive bytes, unit c of row r in place c ^ (r % 8).  A read of 16 bytes a lane is served sixteen lanes at a time,
 // of which eight are from one half of a half-wave and eight from the other's; those have units of either parity, and touch each of the 64 banks once.
-template <int BM, int BN, int WM, int WN, int D> struct Tile {
+template <int BM, int BN, int WM, int WN> struct Tile {
     static constexpr int kWaves = WM * WN, kThreads = kWaves * 64;
     static constexpr int TI = BM / WM / 16, TJ = BN / WN / 16, R = 2;
     static constexpr int kRun = TI * 8;                      // rows under one scale: half of a wavefront's
@@ -34,16 +34,16 @@ template <int BM, int BN, int WM, int WN, int D> struct Tile {
     static constexpr int late(int i) { return share(kLate, R, i - kNext); }
     static constexpr int kScaleLoads = BN / 64 + 1;          // of the workgroup and four steps: columns, then the wavefronts' rows
     static constexpr int kScaleShare = (kScaleLoads + kWaves - 1) / kWaves;      // (wavefronts beyond that number repeat the last)
-    static constexpr int kBuffer = (BM + BN) * kBlock;
-    static constexpr int kScales = D * kBuffer;              // where the scales start: D buffers of four steps
+    static constexpr int kBuffer = (BM + BN) * kBlock, kSteps = 2;       // of a step, and how many LDS holds
+    static constexpr int kScales = kSteps * kBuffer;         // where the scales start: as many buffers of four steps
     static constexpr int kScaleBuffer = (BN + 64) * 16;
-    static constexpr int kLds = kScales + D * kScaleBuffer, kTops = WM * BN * 4;     // (8-bit outputs: the largest of each column, of each wavefront)
+    static constexpr int kLds = kScales + kSteps * kScaleBuffer, kTops = WM * BN * 4;     // (8-bit outputs: the largest of each column, of each wavefront)
     static_assert(TI % (2 * R) == 0 && TI > 0 && TJ > 0 && 128 % kRun == 0, "");
     static_assert(BM % (8 * kWaves) == 0 && BN % (8 * kWaves) == 0 && kRun % 8 == 0 && BN % 64 == 0 && 2 * WM <= 64, "");
-    static_assert((D == 2 || D == 4) && BM / 16 % kWaves == 0, "");
+    static_assert(BM / 16 % kWaves == 0, "");
     // Loads of a wavefront that may be on their way, at the least those asked for after the next step's early part, or after this one's second halves.  (Those of scales
     // not counted: there may be one or two more.)
-    static constexpr int kInFlight = (D - 1) * kLoads;
+    static constexpr int kInFlight = (kSteps - 1) * kLoads;
     static_assert(kInFlight + kLate < 64, "");             // (the count that a wait names)
 };
 
@@ -193,11 +193,11 @@ __device__ __forceinline__ void store_tile(const ProductArgs &a, int split, int 
     }
 }
 
-template <int BM, int BN, int WM, int WN, int D, class T, bool GATED, bool WIDE>
+template <int BM, int BN, int WM, int WN, class T, bool GATED, bool WIDE>
 __global__ __launch_bounds__(WM * WN * 64, 2) void f8_tile_kernel(ProductArgs a, int row_tiles)
 {
-    using C = Tile<BM, BN, WM, WN, D>;
-    constexpr int TI = C::TI, TJ = C::TJ, R = C::R;
+    using C = Tile<BM, BN, WM, WN>;
+    constexpr int TI = C::TI, TJ = C::TJ, R = C::R, kSteps = C::kSteps;
     extern __shared__ __align__(128) uint8_t lds[];
     typedef __attribute__((address_space(3))) void *lds_ptr;
     typedef const __attribute__((address_space(1))) void *global_ptr;
@@ -295,7 +295,7 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void f8_tile_kernel(ProductArgs a,
     // What is asked for: step `ask` of the tile that was taken, and the scales of four into their buffers in turn.  (Behind the last step of the last tile that one again, so
     // that a wait always counts the same; nothing uses what it brings.)
     int ask = 0, scales_asked = 0;
-    auto scales = [&](int n) { return lds + C::kScales + n % D * C::kScaleBuffer; };
+    auto scales = [&](int n) { return lds + C::kScales + n % kSteps * C::kScaleBuffer; };
     auto ask_scales = [&](uint8_t *__restrict__ to) __attribute__((always_inline)) {
         if (ask % 4) return;
 #pragma unroll
@@ -364,7 +364,7 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void f8_tile_kernel(ProductArgs a,
     const int nth0 = nth;
     take(nth);
 #pragma unroll
-    for (int t = 0; t < D; ++t) {
+    for (int t = 0; t < kSteps; ++t) {
         ask_scales(scales(scales_asked));
 #pragma unroll
         for (int k = 0; k < C::kLoads; ++k) request(ask, lds + t * C::kBuffer, k);
@@ -387,7 +387,7 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void f8_tile_kernel(ProductArgs a,
         for (int j = 0; j < TJ; ++j) p[j] = f32x4{0, 0, 0, 0}, by[j] = 0.0f;
         for (int t = 0; t < steps; ++t) {
             uint8_t *now = lds + buffer * C::kBuffer;
-            buffer = (buffer + 1) % D;
+            buffer = (buffer + 1) % kSteps;
             const int in = t % 4, in_next = t + 1 < steps ? (t + 1) % 4 : 0;
             const uint8_t *scales_now = scales(fours) + in * 4;
             fours += in_next == 0;
