@@ -661,7 +661,8 @@ int32_t cl_eight_dequantize(const void *d_values, const float *d_scales, int64_t
                          void *stream);
 
 /* Y = h / sqrt(mean over a row of h^2 + eps) * gain, in fp32, with h = X, or X + residual rounded to X's type, which is also what is stored as the sum.
- * Squares are added in fp32: rows with magnitudes above 2^63 / sqrt(K) may come to an infinite mean, and rows that are zeros with eps 0 are NaN.
+ * Squares are added in fp32: rows with magnitudes above 2^63 / sqrt(K) may come to an infinite mean, rows that are zeros with eps 0 are NaN, and with an eps that
+ * small rows of magnitudes below 2^-63, whose squares leave fp32's normal numbers, lose accuracy and may come to Inf.
  *  rows, K         of all matrices                  strides  elements from row to row, at least K
  *  d_residual      NULL, or of X's type: then d_sum is written (which may be d_X or d_residual itself)
  *  d_gain          K numbers of gain_type, CL_F32 or X's type, or NULL
@@ -688,7 +689,8 @@ int32_t cl_rms_norm(const cl_norm_call *call, void *stream);
  *            a pair are not neighbours here as they are for 4-bit matrices: a block of 128 of them has one scale).  For CL_F32 and CL_F8 within 9 2^-24 of that;
  *            where g is below -87, zero
  *  d_Y       batch rows of W->rows (CL_ACT_GATED: half as many) of y_type, overwritten, apart from X; CL_F8: values, and scales at d_y_scales,
- *            as cl_eight_quantize makes them of the fp32 result
+ *            as cl_eight_quantize makes them of the call's own fp32 sums (a call with CL_F32 outputs may take another form, which adds in another order: then a
+ *            scale can differ in its last bits and a value next to the middle of two steps by one)
  *  d_workspace  at least cl_eight_fc_workspace_bytes(), 256-byte aligned; NULL will do where that is 0.  What is asked for a batch is enough for
  *            every smaller one: a call whose workspace has no room for what its fastest form needs takes another that does with it (slower, and
  *            with another order of the sums)
