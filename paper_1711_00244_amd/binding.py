@@ -1100,7 +1100,8 @@ def f8_fc_resolved_form(W: F8Tensor, batch: int, dtype=None, act="none", out_dty
 def f8_fc_forward(W: F8Tensor, X, bias=None, act=None, dtype=None, out=None, workspace=None):
     """act(X W^T + bias) with W (M, K) in 8 bits with a scale to 128 x 128 and X (B, K) - float32, bfloat16 or float16, quantised on the way, or an F8Tensor.
     act: "none", "relu" or "gated" (output i from rows i and M / 2 + i of W, gate and value; W as f8_gated makes it).  The output is of dtype, X's own
-    unless given (float32 for an F8Tensor); float8_e4m3fn makes an F8Tensor."""
+    unless given (float32 for an F8Tensor); float8_e4m3fn makes an F8Tensor.  For float32 and float8_e4m3fn sums within a block are in fp32 on the bf16 instructions, which
+    a large batch takes twice as long for as for bfloat16 and float16."""
     import torch
     L = _start()
     values, K = W.values, W.K

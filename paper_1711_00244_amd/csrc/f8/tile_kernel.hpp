@@ -14,8 +14,9 @@
 // second halves at its end; and either part is waited for when it is to be read, one and a half steps (of two) later.  At both points the wavefronts wait for each
 // other.  (4096 x 4096 x 25088, 256 x 256: without loads 222 us; all of a buffer asked for at once behind the step 343, in four bunches 336; 2.5 PFLOP/s, where
 // the library's product with one scale to a matrix comes to 2.76, and the card's power holds its clock at 1.9 GHz.)
-// WIDE, 256 x 128 (the columns in bf16, and a 256 x 256 tile's sums beside them, do not fit the registers): 4096 x 2 x 9216 x 4096 gated with 8-bit outputs 540 us, 1.14 PFLOP/s,
-// matrix units busy 45 % of the time and vector units, which take operands to bf16 and multiply by scales, 38 %; without loads 523, without the former 500.
+// WIDE, 256 x 128 (the columns in bf16, and a 256 x 256 tile's sums beside them, do not fit the registers): 4096 x 2 x 9216 x 4096 gated with 8-bit outputs 531-550 us, 1.12-1.16
+// PFLOP/s, matrix units busy 48 % of the time and vector units, which take operands to bf16, multiply by scales and make the gates, 45 % (at 2.4 GHz); when it took 540, without loads 523,
+// without taking operands to bf16 500.  4096 x 4096 x 9216, fp32 outputs: 278 us, 1.11 PFLOP/s, 46 % and 39 %.
 //
 // In LDS a row's eight units of 16 bytes are 128 consecutive bytes, unit c of row r in place c ^ (r % 8).  A read of 16 bytes a lane is served sixteen lanes at a time,
 // of which eight are from one half of a half-wave and eight from the other's; those have units of either parity, and touch each of the 64 banks once.
