@@ -89,14 +89,14 @@ __device__ __forceinline__ f32x4 bias_of(const ProductArgs &a, int at, int o)
 
 // g / (1 + exp(-g)), by the hardware's exponential and reciprocal, each off by one unit in the last place.  The exponential's argument is off by |g| 2^-24, which an
 // output in 16 bits does not show (at its worst 2^-17 of it).  EXACT, for fp32 and 8 bits: what rounding leaves of -g log2(e), and log2(e) itself, goes in as a
-// factor (the minimum: an infinite gate leaves NaN); the whole is then within 9 2^-24 (62 without).  Of 4096 rows of 2 x 9216 with 8-bit outputs that takes 4 us of 542
-// (K 4096), 9 of 169 (K 1024); for 128 outputs a lane, the library's exponential and a division take 4 of a tile's 40 us.  Gates below -87, whose output is
+// factor (the minimum, of floats as whole numbers, which keeps negative ones: an infinite gate leaves NaN); the whole is then within 9 2^-24 (62 without).  Of 4096 rows of 2 x 9216 with 8-bit outputs that takes 3 us of 538
+// (K 4096), 7 of 166 (K 1024), with fp32 outputs none; for 128 outputs a lane, the library's exponential and a division take 4 of a tile's 40 us.  Gates below -87, whose output is
 // below 2^-119 of the value, come out as zeros.
 template <bool EXACT> __device__ __forceinline__ float silu(float g)
 {
     const float log2e = 1.44269504f, rest = 1.92596299e-8f, ln2 = 0.693147181f;
     if (!EXACT) return g * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-log2e * g));
-    const float c = fminf(g, 100.0f), t = -log2e * c, left = fmaf(-rest, c, fmaf(-log2e, c, -t));
+    const float c = __int_as_float(min(__float_as_int(g), __float_as_int(100.0f))), t = -log2e * c, left = fmaf(-rest, c, fmaf(-log2e, c, -t));
     return g * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(t) * fmaf(left, ln2, 1.0f));
 }
 
